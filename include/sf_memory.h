@@ -1,0 +1,76 @@
+/*
+ * sf_memory -- the operators of a memory block on one MI355X (gfx950): a recurrent core with a matrix for a
+ * state, and what stands around it in a residual block.  Next to sf_policy.h: same library, same conventions
+ * (int status, sf_last_error(), device pointers, asynchronous on the caller's stream, nothing allocated, no
+ * synchronisation, no pointer kept past the stream's work).  All functions run on the current HIP device.
+ * Workspaces belong to the caller, 256-byte aligned; their contents do not matter before or after a call, but calls
+ * that may run at the same time need one each.  Repeated calls give the same bits.
+ *
+ * Element types: SF_DTYPE_FP32 or SF_DTYPE_BF16 of the arrays marked "io"; states, decays, norm weights and
+ * their gradients are fp32 always.  Sums and states are held in fp32; what a result of a bf16 call is rounded from is
+ * said at each function.  Sizes of 0 in T, N, B or M are accepted and leave only what does not depend on them
+ * (final states, gradients of weights).
+ */
+#ifndef SF_MEMORY_H
+#define SF_MEMORY_H
+
+#include "sf_policy.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- linear attention with a decay for each head ---------------------------------
+ * For row (trajectory) n and head h, with g = exp(log_decay[h]):
+ *   S_t = g (done[t][n] ? 0 : S_{t-1}) + k_t v_t^T      S_{-1} = state0,   S is [dk][dv]
+ *   o_t = scale * S_t^T q_t                             state = S_{T-1}
+ * done = 1 at the first step of an episode, as in sf_policy_unroll; what lies before it does not reach past
+ * it, NaN and infinities included, and no step reaches an earlier one.  Key and value heads may be shared: head h
+ * reads key/value head h / (H / Hk).
+ * The passes over trajectories compute this in chunks of 32 or 64 steps (two matrix products inside a chunk, the
+ * state between chunks), and where rows x heads are few, T is cut into pieces whose states are joined.
+ *
+ * Arrays are time-major: q [T][N][H][dk], k [T][N][Hk][dk], v [T][N][Hk][dv], o and its gradient [T][N][H][dv], io;
+ * element (t, n, h, i) of q is q[t * q_stride[0] + n * q_stride[1] + h * q_stride[2] + i], strides in elements, so
+ * that all three may lie in one projection's output (any strides; 16-byte aligned rows of full 16-byte pieces are
+ * read in such pieces, others element by element).  Gradients dq, dk, dv are dense.
+ *   log_decay  dev [H] fp32, <= 0 (-infinity: the state is only the last step's)
+ *   done       dev [T][N] bytes or NULL (no episode begins)
+ *   state0     dev [N][H][dk][dv] fp32 or NULL (zero); state, dstate, dstate0 alike (NULL: not wanted / zero)
+ * Errors: SF_ERR_ARG (null or misaligned pointer, struct_size, dtype), SF_ERR_SHAPE (T, N < 0; H, Hk < 1;
+ * H % Hk != 0; dk or dv outside 1..128; T * N or N * H beyond 2^31 - 1; scale not finite), SF_ERR_DEVICE. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(sf_linattn_config) */
+  int32_t dtype;        /* SF_DTYPE_* of q, k, v, o and their gradients */
+  int32_t T, N, H, Hk, dk, dv;
+  float scale;
+  int64_t q_stride[3], k_stride[3], v_stride[3]; /* step, row, head */
+  int64_t o_stride[3];                           /* of o, and of do in the backward pass */
+} sf_linattn_config;
+
+/* Bytes of the workspace of sf_linattn (backward = 0) or sf_linattn_backward (1); 0: none is needed, NULL may be
+ * passed; -1 on a bad configuration. */
+int64_t sf_linattn_workspace_bytes(const sf_linattn_config* cfg, int backward);
+/* state may be state0 (the states are then updated in place). */
+int sf_linattn(const sf_linattn_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+               const uint8_t* done, const float* state0, void* o, float* state, void* workspace, void* hip_stream);
+/* Gradients with respect to q, k, v and state0, given those of o (do) and of the final state (dstate or NULL).
+ * log_decay is a constant.  Nothing of the forward pass is needed but its inputs.  dstate0 must overlap neither
+ * dstate nor state0 (SF_ERR_ALIAS). */
+int sf_linattn_backward(const sf_linattn_config* cfg, const void* q, const void* k, const void* v,
+                        const float* log_decay, const void* d_o, const uint8_t* done, const float* state0,
+                        const float* dstate, void* dq, void* dk, void* dv, float* dstate0, void* workspace,
+                        void* hip_stream);
+/* One step for B = cfg->N rows (cfg->T must be 1, stride[0] is not used): the policy worker's side.  Row b stands for
+ * environment e = env_ids[b] (b itself if env_ids is NULL), whose state is row e of
+ *   state_table  dev [n_env][H][dk][dv] fp32, 16-byte aligned, read and overwritten;
+ * ids must be distinct; a row whose id is outside [0, n_env) is computed from a zero state and its new state is
+ * dropped.  done [B] bytes or NULL. */
+int sf_linattn_step(const sf_linattn_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+                    float* state_table, int32_t n_env, const int32_t* env_ids, const uint8_t* done, void* o,
+                    void* hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

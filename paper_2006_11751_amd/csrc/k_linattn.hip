@@ -1,0 +1,1006 @@
+// Linear attention with a decay for each head (include/sf_memory.h), in chunks of C steps:
+//   inside a chunk  o_i += sum over j <= i, same episode: g^(i-j) (q_i . k_j) v_j
+//   from before     o_i += g^(i+1) S q_i          where no episode begins up to i
+//   the state       S <- g^n S + sum_j g^(n-1-j) k_j v_j^T   (terms from before the chunk's last episode begin: none)
+// Every gradient is the same sum with other arrays in the three places and, for two of them, time reversed:
+//   dq: (do, v, k) forwards with S transposed;  dk: (v, do, q) and dv: (k, q, do) backwards with the state
+//   R_t = scale q_t do_t^T + g R_{t+1}.
+// So there is one kernel, told by LinOp what stands where; a launch of the backward pass runs all three.
+//
+// A workgroup of four waves walks the chunks of one (row, head), or of one piece of T.  Wave w owns a quarter of
+// v's columns: its part of the state stays in registers as the accumulator of the update.  The products are arranged
+// so that accumulators feed the next product without a shuffle: a 16x16 accumulator holds rows 4g .. 4g+3 of one
+// column per lane (g = lane / 16), two of them are the eight K-slots of an operand of 16x16x32, and the other operand
+// follows the same numbering of the K axis.
+//   P^T = K Q^T   [j][i]   masked and decayed in registers, shared by the waves through LDS in operand order
+//   O^T = V^T P^T + S^T Q^T [dv][i]    the second product scaled per lane (a lane is a step i)
+//   S  += K^T V~  [dk][dv]   V~: v times its step's weight
+// K^T and V^T are read from row-major LDS with the transposing read (fp32: element by element).
+//
+// Roundings.  bf16 arrays enter the products as they are.  What is computed in fp32 and enters a product goes in as
+// a sum of bf16 numbers: P and S for the output in two terms (2^-16 of them is left out at most, the output is
+// rounded to 2^-8), V~ for the state, which is fp32, in three (nothing is left out).  fp32 arrays run on the fp32 matrix
+// instruction throughout.
+//
+// Masked entries are selected, but a product still multiplies their zeros with the other operand's rows, and 0 x NaN
+// is NaN.  So the chunk's k and v are tested as they are staged; a chunk with a NaN or an infinity in them is walked
+// step by step, which keeps it from earlier steps and from later episodes.
+#include <math.h>
+
+#include "sf_internal.h"
+#include "sf_memory.h"
+#include "sf_split.h"
+
+namespace sf {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+
+struct Strided {
+  const void* p;
+  int64_t st, sn, sh;  // step, row, head (elements)
+  int div;             // heads that share one
+  int d;               // columns
+  int vec;             // rows are read in 16-byte pieces
+};
+
+struct LinOp {
+  Strided q, k, v;
+  void* o;
+  int64_t ot, on, oh;
+  int o_f32, o_vec;     // the output is fp32 whatever the arrays are (partial sums of shared heads); 16-byte pieces
+  const float* s_in;    // state before the first step, or null; [N][H] matrices of d(k) x d(v), element (a, b) at
+  float* s_out;         //   a * s_a + b * s_b; state behind the last one, or null
+  int64_t s_a, s_b;
+  float w_scale, alpha; // of the terms k v^T (in state and output), of the output
+  int reverse;          // time runs backwards: an episode boundary lies behind its step, the state
+                        //   enters the first step undecayed and leaves decayed
+};
+struct LinArgs {
+  LinOp op[3];
+  const float* log_decay;
+  const uint8_t* done;  // or null
+  int T, N, H;
+  int n_seg, seg_len;   // pieces of T (seg_len a multiple of every C)
+  float* seg_state;     // n_seg > 1: [op][N * H][n_seg][dk * dv], first the pieces' own states, then what enters them
+  float* seg_keep;      // [op][N * H][n_seg] g^length, 0 if an episode begins in the piece
+};
+
+__device__ inline unsigned pack_bf16(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
+}
+__device__ inline float lo_of(unsigned w) { return __builtin_bit_cast(float, w << 16); }
+__device__ inline float hi_of(unsigned w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
+// two terms of two numbers
+__device__ inline void split2(float a, float b, unsigned& t0, unsigned& t1) {
+  t0 = pack_bf16(a, b);
+  t1 = pack_bf16(a - lo_of(t0), b - hi_of(t0));
+}
+
+// The arithmetic of one element type.  An operand is eight K-slots per lane.
+template <int DTYPE>
+struct Num;
+
+template <>
+struct Num<SF_DTYPE_BF16> {
+  static constexpr int kBytes = 2, kPad = 8, kPieceWords = 4;
+  typedef u32x4 Raw;                                   // exact values
+  struct Out { u32x4 t[2]; };                          // for the output: two terms
+  struct Sum { u32x4 t[3]; };                          // for the state: three terms
+  __device__ static Raw row(const unsigned char* p) { return *(const u32x4*)p; }  // eight neighbours of a row
+  // four K-slots down column col(lane % 16) of rows at .. at + 3: `p` is this lane's share (its row, its four columns)
+  __device__ static u32x2 column4(const unsigned char* p) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+  }
+  __device__ static void values(const Raw& r, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = lo_of(r[i]);
+      x[2 * i + 1] = hi_of(r[i]);
+    }
+  }
+  __device__ static Out out_terms(const float* x) {
+    Out o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      unsigned a, b;
+      split2(x[2 * i], x[2 * i + 1], a, b);
+      o.t[0][i] = a;
+      o.t[1][i] = b;
+    }
+    return o;
+  }
+  __device__ static Sum sum_terms(const float* x) {
+    Sum o;
+    float left = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      unsigned a, b, c;
+      split_pair(x[2 * i], x[2 * i + 1], a, b, c, left);
+      o.t[0][i] = a;
+      o.t[1][i] = b;
+      o.t[2][i] = c;
+    }
+    return o;
+  }
+  __device__ static f32x4 mma1(const u32x4& a, const u32x4& b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  __device__ static f32x4 mma(const Raw& a, const Raw& b, f32x4 c) { return mma1(a, b, c); }
+  __device__ static f32x4 mma(const Raw& a, const Out& b, f32x4 c) { return mma1(a, b.t[0], mma1(a, b.t[1], c)); }
+  __device__ static f32x4 mma(const Out& a, const Raw& b, f32x4 c) { return mma1(a.t[0], b, mma1(a.t[1], b, c)); }
+  __device__ static f32x4 mma(const Raw& a, const Sum& b, f32x4 c) { return mma1(a, b.t[0], mma1(a, b.t[1], mma1(a, b.t[2], c))); }
+  // P in LDS: the terms of four slots of half `h`
+  __device__ static void put4(unsigned char* frag, int term_pitch, int lane, int h, f32x4 x) {
+    unsigned a0, a1, b0, b1;
+    split2(x[0], x[1], a0, a1);
+    split2(x[2], x[3], b0, b1);
+    *(u32x2*)(frag + lane * 16 + h * 8) = u32x2{a0, b0};
+    *(u32x2*)(frag + term_pitch + lane * 16 + h * 8) = u32x2{a1, b1};
+  }
+  __device__ static Out get(const unsigned char* frag, int term_pitch, int lane) {
+    Out o;
+    o.t[0] = *(const u32x4*)(frag + lane * 16);
+    o.t[1] = *(const u32x4*)(frag + term_pitch + lane * 16);
+    return o;
+  }
+  __device__ static float element(const unsigned char* p) { return __builtin_bit_cast(float, (unsigned)*(const uint16_t*)p << 16); }
+  __device__ static void store(void* p, float x) { *(uint16_t*)p = (uint16_t)pack_bf16(x, 0.0f); }
+};
+
+template <>
+struct Num<SF_DTYPE_FP32> {
+  static constexpr int kBytes = 4, kPad = 4, kPieceWords = 8;
+  struct Raw { float x[8]; };
+  typedef Raw Out;
+  typedef Raw Sum;
+  __device__ static Raw row(const unsigned char* p) {
+    Raw r;
+    *(f32x4*)&r.x[0] = *(const f32x4*)p;
+    *(f32x4*)&r.x[4] = *(const f32x4*)(p + 16);
+    return r;
+  }
+  __device__ static void values(const Raw& r, float* x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = r.x[i];
+  }
+  __device__ static Raw out_terms(const float* x) {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.x[i] = x[i];
+    return r;
+  }
+  __device__ static Raw sum_terms(const float* x) { return out_terms(x); }
+  __device__ static f32x4 mma(const Raw& a, const Raw& b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i], b.x[i], c, 0, 0, 0);
+    return c;
+  }
+  __device__ static void put4(unsigned char* frag, int term_pitch, int lane, int h, f32x4 x) {
+    *(f32x4*)(frag + h * term_pitch + lane * 16) = x;
+  }
+  __device__ static Raw get(const unsigned char* frag, int term_pitch, int lane) {
+    Raw r;
+    *(f32x4*)&r.x[0] = *(const f32x4*)(frag + lane * 16);
+    *(f32x4*)&r.x[4] = *(const f32x4*)(frag + term_pitch + lane * 16);
+    return r;
+  }
+  __device__ static float element(const unsigned char* p) { return *(const float*)p; }
+  __device__ static void store(void* p, float x) { *(float*)p = x; }
+};
+
+// Eight columns of a row, zero past the array's end (col may lie past it altogether).
+template <int DTYPE>
+__device__ inline void load_piece(unsigned* w, const Strided& a, const unsigned char* row, int col, bool live) {
+  typedef Num<DTYPE> M;
+  constexpr int W = M::kPieceWords;
+  if (live && a.vec && col < a.d) {  // (d is a multiple of 8 then)
+#pragma unroll
+    for (int i = 0; i < W; i += 4) *(u32x4*)(w + i) = *(const u32x4*)(row + (size_t)col * M::kBytes + 4 * i);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[i] = 0;
+  if (!live || a.vec) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (col + i >= a.d) continue;
+    if constexpr (DTYPE == SF_DTYPE_BF16)
+      w[i / 2] |= (unsigned)*(const uint16_t*)(row + (size_t)(col + i) * 2) << (16 * (i & 1));
+    else
+      w[i] = *(const unsigned*)(row + (size_t)(col + i) * 4);
+  }
+}
+
+// NaN if any of the numbers is NaN or infinite
+template <int DTYPE>
+__device__ inline float finite_test(const unsigned* w, float acc) {
+#pragma unroll
+  for (int i = 0; i < Num<DTYPE>::kPieceWords; ++i) {
+    if constexpr (DTYPE == SF_DTYPE_BF16) {
+      acc = fmaf(lo_of(w[i]), 0.0f, acc);
+      acc = fmaf(hi_of(w[i]), 0.0f, acc);
+    } else {
+      acc = fmaf(__builtin_bit_cast(float, w[i]), 0.0f, acc);
+    }
+  }
+  return acc;
+}
+
+template <int DTYPE, int D, int C>
+struct Lds {
+  typedef Num<DTYPE> M;
+  static constexpr int kPitch = (D + M::kPad) * M::kBytes;  // of a row: 16 bytes more than its numbers, for the banks
+  static constexpr int kTile = C * kPitch;
+  static constexpr int kFrags = (C / 16) * (C / 32);
+  static constexpr int kTermPitch = kFrags * 1024;
+  static constexpr int kP = 3 * kTile;                      // two terms (or halves) of kFrags x 64 lanes x 16 bytes
+  static constexpr int kEp = kP + 2 * kTermPitch;           // int [C]: episode of the step, counted in the chunk
+  static constexpr int kW = kEp + C * 4;                    // float [C]: weight of the step's term in the state
+  static constexpr int kFlag = kW + C * 4;                  // int [2]: the chunk holds something not finite
+  static constexpr int kBytes = kFlag + 16;
+};
+
+// STATE: only the piece's own state (from zero) and whether an episode begins in it.
+template <int DTYPE, int D, int C, bool STATE>
+__global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
+  typedef Num<DTYPE> M;
+  typedef Lds<DTYPE, D, C> L;
+  constexpr int W = M::kPieceWords, NP = C * D / 8 / kThreads;  // pieces of a tile per thread
+  constexpr int NV = D / 64, ND = D / 16, NC = C / 32;          // a wave's tiles of v; tiles of k; K-steps over C
+  static_assert(NP >= 1 && (C == 32 || C == 64), "whole pieces");
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const LinOp& op = g.op[blockIdx.z];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int li = lane & 15, lg = lane >> 4;
+  const int bh = blockIdx.x, n = bh / g.H, h = bh % g.H, seg = blockIdx.y;
+  const int t_begin = seg * g.seg_len, t_end = min(g.T, t_begin + g.seg_len);  // in the op's own direction
+  const int dk = op.k.d, dv = op.v.d;
+  const float l2 = fmaxf(g.log_decay[h] * 1.44269504f, -1e30f);  // (no -infinity: times zero it would be NaN)
+  const bool scan = g.n_seg > 1;
+  const size_t seg_at = ((size_t)blockIdx.z * g.N * g.H + bh) * g.n_seg + seg;
+
+  const unsigned char* qrow = (const unsigned char*)op.q.p + (n * op.q.sn + h / op.q.div * op.q.sh) * M::kBytes;
+  const unsigned char* krow = (const unsigned char*)op.k.p + (n * op.k.sn + h / op.k.div * op.k.sh) * M::kBytes;
+  const unsigned char* vrow = (const unsigned char*)op.v.p + (n * op.v.sn + h / op.v.div * op.v.sh) * M::kBytes;
+
+  // column of v of this wave's tile t, operand row (or accumulator column) m
+  auto col_v = [&](int t, int m) { return NV == 2 ? 32 * wave + 8 * (m >> 2) + 4 * t + (m & 3) : 16 * wave + m; };
+  // column of k of tile t (two tiles are 32 columns: eight neighbours per lane group)
+  auto col_k = [&](int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); };
+
+  f32x4 S[ND][NV];
+  {
+    const float* s = nullptr;
+    int64_t sa = op.s_a, sb = op.s_b;
+    if constexpr (!STATE) {
+      if (scan) {
+        s = g.seg_state + seg_at * ((size_t)dk * dv);
+        sa = dv;
+        sb = 1;
+      } else if (op.s_in) {
+        s = op.s_in + (size_t)bh * dk * dv;
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < ND; ++a)
+#pragma unroll
+      for (int b = 0; b < NV; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int x = col_k(a, 4 * lg + r), y = col_v(b, li);
+          S[a][b][r] = s && x < dk && y < dv ? s[x * sa + y * sb] : 0.0f;
+        }
+  }
+
+  // the chunk that is on its way: its rows and its episode marks
+  unsigned nq[NP][W], nk[NP][W], nv[NP][W];
+  int n_done = 0;
+  auto step_of = [&](int i) { return op.reverse ? g.T - 1 - i : i; };
+  auto request = [&](int c0) {
+    const int valid = t_end - c0;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int piece = tid + p * kThreads, r = piece / (D / 8), col = piece % (D / 8) * 8;
+      const bool live = r < valid;
+      const int64_t t = step_of(live ? c0 + r : t_end - 1);
+      if constexpr (!STATE) load_piece<DTYPE>(nq[p], op.q, qrow + t * op.q.st * M::kBytes, col, live);
+      load_piece<DTYPE>(nk[p], op.k, krow + t * op.k.st * M::kBytes, col, live);
+      load_piece<DTYPE>(nv[p], op.v, vrow + t * op.v.st * M::kBytes, col, live);
+    }
+    n_done = 0;
+    if (g.done && lane < C && lane < valid) {
+      const int i = c0 + lane;  // backwards the boundary before step i is the mark of the step after it in time
+      if (!op.reverse) n_done = g.done[(size_t)i * g.N + n];
+      else if (i > 0) n_done = g.done[(size_t)(g.T - i) * g.N + n];
+    }
+  };
+  unsigned char* const tq = lds;
+  unsigned char* const tk = lds + L::kTile;
+  unsigned char* const tv = lds + 2 * L::kTile;
+  int* const ep = (int*)(lds + L::kEp);
+  float* const wgt = (float*)(lds + L::kW);
+  int* const flag = (int*)(lds + L::kFlag);
+  if (tid < 2) flag[tid] = 0;
+
+  bool any_done = false;
+  request(t_begin);
+  for (int c0 = t_begin, turn = 0; c0 < t_end; c0 += C, turn ^= 1) {
+    const int valid = min(C, t_end - c0);
+    const int late = c0 == 0 && op.reverse ? 1 : 0;  // the state enters undecayed
+    const unsigned long long marks = __ballot(n_done != 0);
+    __syncthreads();  // the chunk before has been read
+    float test = 0.0f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int piece = tid + p * kThreads, at = piece / (D / 8) * L::kPitch + piece % (D / 8) * 8 * M::kBytes;
+#pragma unroll
+      for (int i = 0; i < W; i += 4) {
+        if constexpr (!STATE) *(u32x4*)(tq + at + 4 * i) = *(u32x4*)(nq[p] + i);
+        *(u32x4*)(tk + at + 4 * i) = *(u32x4*)(nk[p] + i);
+        *(u32x4*)(tv + at + 4 * i) = *(u32x4*)(nv[p] + i);
+      }
+      test = finite_test<DTYPE>(nk[p], finite_test<DTYPE>(nv[p], test));
+    }
+    if (test != 0.0f) flag[turn] = 1;
+    const int ep_end = __popcll(marks);
+    if (tid < C) {
+      const int e = __popcll(marks & ((2ull << tid) - 1));
+      ep[tid] = e;
+      wgt[tid] = e == ep_end && tid < valid ? op.w_scale * exp2f(l2 * (float)(valid - 1 - tid)) : 0.0f;
+    }
+    __syncthreads();
+    const bool walk = flag[turn] != 0;
+    if (c0 + C < t_end) request(c0 + C);
+    any_done |= marks != 0;
+
+    if (walk) {
+      // step by step
+      const float gam = exp2f(l2);
+      for (int i = 0; i < valid; ++i) {
+        const bool begin = marks >> i & 1;
+        const float keep = i == 0 && late ? 1.0f : gam;
+        float o[NV];
+#pragma unroll
+        for (int b = 0; b < NV; ++b) o[b] = 0.0f;
+#pragma unroll
+        for (int a = 0; a < ND; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int x = col_k(a, 4 * lg + r);
+            const float kx = M::element(tk + i * L::kPitch + x * M::kBytes);
+            const float qx = STATE ? 0.0f : M::element(tq + i * L::kPitch + x * M::kBytes);
+#pragma unroll
+            for (int b = 0; b < NV; ++b) {
+              const float vy = M::element(tv + i * L::kPitch + col_v(b, li) * M::kBytes);
+              // (columns past the arrays' ends stay zero: with an infinity in the row they would be NaN)
+              const bool in = x < dk && col_v(b, li) < dv;
+              S[a][b][r] = in ? op.w_scale * kx * vy + (begin ? 0.0f : keep * S[a][b][r]) : 0.0f;
+              if (in) o[b] += qx * S[a][b][r];
+            }
+          }
+        if constexpr (!STATE) {
+#pragma unroll
+          for (int b = 0; b < NV; ++b) {
+            float x = o[b];
+            x += __shfl_xor(x, 16);
+            x += __shfl_xor(x, 32);
+            const int y = col_v(b, li);
+            if (lg == 0 && y < dv) {
+              const int64_t at = n * op.on + h * op.oh + step_of(c0 + i) * op.ot + y;
+              if (op.o_f32) ((float*)op.o)[at] = op.alpha * x;
+              else M::store((unsigned char*)op.o + at * M::kBytes, op.alpha * x);
+            }
+          }
+        }
+      }
+      if (tid == 0) flag[turn ^ 1] = 0;  // (read by all before the barrier that ended the chunk before)
+      __syncthreads();                   // as many barriers as below
+      continue;
+    }
+
+    if constexpr (!STATE) {
+      // P^T: 16 x 16 tiles [j tile J][i tile I], J <= I; a pair of tiles is one operand
+      auto tile_p = [&](int I, int J) __attribute__((always_inline)) {
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (J <= I) {
+#pragma unroll
+          for (int s = 0; s < D / 32; ++s) {
+            const int at = (32 * s + 8 * lg) * M::kBytes;
+            acc = M::mma(M::row(tk + (16 * J + li) * L::kPitch + at), M::row(tq + (16 * I + li) * L::kPitch + at), acc);
+          }
+          const int i = 16 * I + li, e = ep[i];
+          const i32x4 ej = *(const i32x4*)(ep + 16 * J + 4 * lg);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int j = 16 * J + 4 * lg + r;
+            acc[r] = j <= i && ej[r] == e ? acc[r] * (op.w_scale * exp2f(l2 * (float)(i - j))) : 0.0f;
+          }
+        }
+        M::put4(lds + L::kP + (I * NC + J / 2) * 1024, L::kTermPitch, lane, J & 1, acc);
+      };
+      if constexpr (C == 64) {
+#pragma unroll
+        for (int J = 0; J < 4; ++J)
+          if (J <= (wave | 1)) tile_p(wave, J);
+      } else {
+        tile_p(wave >> 1, wave & 1);
+      }
+    }
+    if (tid == 0) flag[turn ^ 1] = 0;
+    __syncthreads();
+
+    // V^T of this wave's columns: K-slots 0..3 are steps 32 p + 4 g .., 4..7 are 16 further on
+    typename M::Raw vt[NC][NV];
+#pragma unroll
+    for (int p = 0; p < NC; ++p)
+#pragma unroll
+      for (int b = 0; b < NV; ++b) {
+        if constexpr (DTYPE == SF_DTYPE_BF16) {
+          const unsigned char* at = tv + (32 * p + 4 * lg + (li >> 2)) * L::kPitch + col_v(b, 4 * (li & 3)) * M::kBytes;
+          const u32x2 x = M::column4(at), y = M::column4(at + 16 * L::kPitch);
+          vt[p][b] = u32x4{x[0], x[1], y[0], y[1]};
+        } else {
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            vt[p][b].x[r] = M::element(tv + (32 * p + 4 * lg + (r & 3) + 16 * (r >> 2)) * L::kPitch + col_v(b, li) * M::kBytes);
+        }
+      }
+
+    if constexpr (!STATE) {
+      // two accumulator tiles of the state are one operand
+      typename M::Out st[D / 32][NV];
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+        for (int b = 0; b < NV; ++b) {
+          float x[8];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            x[r] = S[2 * s][b][r];
+            x[4 + r] = S[2 * s + 1][b][r];
+          }
+          st[s][b] = M::out_terms(x);
+        }
+#pragma unroll
+      for (int I = 0; I < C / 16; ++I) {
+        const int i = 16 * I + li;
+        f32x4 own[NV], old[NV];
+#pragma unroll
+        for (int b = 0; b < NV; ++b) own[b] = old[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int p = 0; p <= I / 2; ++p) {
+          const typename M::Out x = M::get(lds + L::kP + (I * NC + p) * 1024, L::kTermPitch, lane);
+#pragma unroll
+          for (int b = 0; b < NV; ++b) own[b] = M::mma(vt[p][b], x, own[b]);
+        }
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+          const typename M::Raw x = M::row(tq + i * L::kPitch + (32 * s + 8 * lg) * M::kBytes);
+#pragma unroll
+          for (int b = 0; b < NV; ++b) old[b] = M::mma(st[s][b], x, old[b]);
+        }
+        const bool reach = (marks & ((2ull << i) - 1)) == 0;  // no episode has begun: the state is this step's
+        const float c = exp2f(l2 * (float)(i + 1 - late));
+#pragma unroll
+        for (int b = 0; b < NV; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) own[b][r] = op.alpha * (own[b][r] + (reach ? c * old[b][r] : 0.0f));
+        if (i < valid) {
+          const int64_t at = n * op.on + h * op.oh + step_of(c0 + i) * op.ot;
+          const int y = col_v(0, 4 * lg);  // 4 * NV neighbours
+          if (op.o_vec) {
+            if (y < dv) {
+              if constexpr (DTYPE == SF_DTYPE_BF16) {
+                if (!op.o_f32) {
+                  unsigned w[2 * NV];
+#pragma unroll
+                  for (int b = 0; b < NV; ++b) {
+                    w[2 * b] = pack_bf16(own[b][0], own[b][1]);
+                    w[2 * b + 1] = pack_bf16(own[b][2], own[b][3]);
+                  }
+                  uint16_t* to = (uint16_t*)op.o + at + y;
+                  if constexpr (NV == 2) *(u32x4*)to = u32x4{w[0], w[1], w[2], w[3]};
+                  else *(u32x2*)to = u32x2{w[0], w[1]};
+                  continue;
+                }
+              }
+#pragma unroll
+              for (int b = 0; b < NV; ++b) *(f32x4*)((float*)op.o + at + y + 4 * b) = own[b];
+            }
+          } else {
+#pragma unroll
+            for (int b = 0; b < NV; ++b)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const int z = y + 4 * b + r;
+                if (z >= dv) continue;
+                if (op.o_f32) ((float*)op.o)[at + z] = own[b][r];
+                else M::store((unsigned char*)op.o + (at + z) * M::kBytes, own[b][r]);
+              }
+          }
+        }
+      }
+    }
+
+    const float keep = marks ? 0.0f : exp2f(l2 * (float)(valid - late));
+#pragma unroll
+    for (int a = 0; a < ND; ++a)
+#pragma unroll
+      for (int b = 0; b < NV; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[a][b][r] = marks ? 0.0f : keep * S[a][b][r];
+#pragma unroll
+    for (int p = 0; p < NC; ++p) {
+      typename M::Sum vw[NV];
+      const f32x4 w0 = *(const f32x4*)(wgt + 32 * p + 4 * lg), w1 = *(const f32x4*)(wgt + 32 * p + 16 + 4 * lg);
+#pragma unroll
+      for (int b = 0; b < NV; ++b) {
+        float x[8];
+        M::values(vt[p][b], x);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[r] *= w0[r];
+          x[4 + r] *= w1[r];
+        }
+        vw[b] = M::sum_terms(x);
+      }
+#pragma unroll
+      for (int a = 0; a < ND; ++a) {
+        typename M::Raw kt;
+        if constexpr (DTYPE == SF_DTYPE_BF16) {
+          const unsigned char* at = tk + (32 * p + 4 * lg + (li >> 2)) * L::kPitch + col_k(a, 4 * (li & 3)) * M::kBytes;
+          const u32x2 x = M::column4(at), y = M::column4(at + 16 * L::kPitch);
+          kt = u32x4{x[0], x[1], y[0], y[1]};
+        } else {
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            kt.x[r] = M::element(tk + (32 * p + 4 * lg + (r & 3) + 16 * (r >> 2)) * L::kPitch + col_k(a, li) * M::kBytes);
+        }
+#pragma unroll
+        for (int b = 0; b < NV; ++b) S[a][b] = M::mma(kt, vw[b], S[a][b]);
+      }
+    }
+  }
+
+  float* s = nullptr;
+  int64_t sa = op.s_a, sb = op.s_b;
+  float f = 1.0f;
+  bool zero = false;
+  if constexpr (STATE) {
+    s = g.seg_state + seg_at * ((size_t)dk * dv);
+    sa = dv;
+    sb = 1;
+    if (tid == 0)
+      g.seg_keep[seg_at] = any_done ? 0.0f : exp2f(l2 * (float)(t_end - t_begin - (seg == 0 && op.reverse ? 1 : 0)));
+  } else if (op.s_out && seg == g.n_seg - 1) {
+    s = op.s_out + (size_t)bh * dk * dv;
+    if (op.reverse) {  // one step further back: to before the first step
+      f = t_end > t_begin ? exp2f(l2) : 1.0f;
+      zero = g.done && t_end > t_begin && g.done[n] != 0;
+    }
+  }
+  if (s) {
+#pragma unroll
+    for (int a = 0; a < ND; ++a)
+#pragma unroll
+      for (int b = 0; b < NV; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int x = col_k(a, 4 * lg + r), y = col_v(b, li);
+          if (x < dk && y < dv) s[x * sa + y * sb] = zero ? 0.0f : f * S[a][b][r];
+        }
+  }
+}
+
+// What enters each piece of T, from the pieces' own states: one thread per element of a state.
+__global__ __launch_bounds__(kThreads) void linattn_join_kernel(LinArgs g) {
+  const LinOp& op = g.op[blockIdx.z];
+  const int bh = blockIdx.y, dk = op.k.d, dv = op.v.d, e = blockIdx.x * kThreads + threadIdx.x;
+  if (e >= dk * dv) return;
+  const size_t at = ((size_t)blockIdx.z * g.N * g.H + bh) * g.n_seg;
+  float* s = g.seg_state + at * ((size_t)dk * dv) + e;
+  float in = op.s_in ? op.s_in[(size_t)bh * dk * dv + e / dv * op.s_a + e % dv * op.s_b] : 0.0f;
+  for (int i = 0; i < g.n_seg; ++i) {
+    float* x = s + (size_t)i * dk * dv;
+    const float own = *x, keep = g.seg_keep[at + i];
+    *x = in;
+    in = own + (keep == 0.0f ? 0.0f : keep * in);
+  }
+}
+
+// Sums of the gradients of shared heads: in [rows][H][d] fp32, out [rows][H / share][d].
+template <int DTYPE>
+__global__ __launch_bounds__(kThreads) void linattn_share_kernel(const float* in, void* out, int64_t n_out, int d, int share) {
+  const int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (e >= n_out) return;
+  const float* x = in + e / d * share * d + e % d;
+  float sum = 0.0f;
+  for (int i = 0; i < share; ++i) sum += x[(int64_t)i * d];
+  Num<DTYPE>::store((unsigned char*)out + e * Num<DTYPE>::kBytes, sum);
+}
+
+// One step of one (row, head): the state is read, decayed, added to, written and multiplied with q.  Bound by those
+// bytes; a thread holds four neighbours of every (256 / lanes)-th row, so that all its loads are under way at once.
+template <int DTYPE, bool VEC>
+__global__ __launch_bounds__(kThreads) void linattn_step_kernel(LinOp op, const float* log_decay, const uint8_t* done, float* table,
+                                                                int n_env, const int32_t* ids, int H, int lanes_log2) {
+  typedef Num<DTYPE> M;
+  __shared__ float sq[128], sk[128];
+  __shared__ __attribute__((aligned(16))) float part[4][128];
+  const int tid = threadIdx.x, n = blockIdx.x / H, h = blockIdx.x % H, dk = op.k.d, dv = op.v.d;
+  const int id = ids ? ids[n] : n;
+  const bool known = id >= 0 && id < n_env;
+  const bool begin = !known || (done && done[n] != 0);
+  const float gam = exp2f(fmaxf(log_decay[h] * 1.44269504f, -1e30f));
+  const int rows = kThreads >> lanes_log2, row0 = tid >> lanes_log2, c0 = (tid & ((1 << lanes_log2) - 1)) * 4;
+  float* s = table + ((int64_t)(known ? id : 0) * H + h) * dk * dv;
+  constexpr int kMost = 16;  // rows of a thread: 128 / (256 / 32)
+  float x[kMost][4];
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const int r = row0 + i * rows;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[i][j] = 0.0f;
+    if (begin || r >= dk || c0 >= dv) continue;
+    if constexpr (VEC) {
+      *(f32x4*)x[i] = *(const f32x4*)(s + r * dv + c0);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c0 + j < dv) x[i][j] = s[r * dv + c0 + j];
+    }
+  }
+  if (tid < 128) {
+    if (tid < dk) sk[tid] = M::element((const unsigned char*)op.k.p + (n * op.k.sn + h / op.k.div * op.k.sh + tid) * M::kBytes);
+  } else if (tid - 128 < dk) {
+    sq[tid - 128] = M::element((const unsigned char*)op.q.p + (n * op.q.sn + h * op.q.sh + tid - 128) * M::kBytes);
+  }
+  float v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    v[j] = c0 + j < dv ? M::element((const unsigned char*)op.v.p + (n * op.v.sn + h / op.v.div * op.v.sh + c0 + j) * M::kBytes) : 0.0f;
+  __syncthreads();
+  float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const int r = row0 + i * rows;
+    if (r >= dk || c0 >= dv) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[i][j] = sk[r] * v[j] + (begin ? 0.0f : gam * x[i][j]);
+      o[j] += sq[r] * x[i][j];
+    }
+    if (!known) continue;
+    if constexpr (VEC) {
+      *(f32x4*)(s + r * dv + c0) = *(f32x4*)x[i];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c0 + j < dv) s[r * dv + c0 + j] = x[i][j];
+    }
+  }
+  // over the rows: within the wave, then over the four waves
+  for (int m = 1 << lanes_log2; m < 64; m <<= 1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], m);
+  if ((tid & 63) < 1 << lanes_log2 && c0 < 128)
+    *(f32x4*)&part[tid >> 6][c0] = f32x4{o[0], o[1], o[2], o[3]};
+  __syncthreads();
+  if (tid < dv) {
+    const float sum = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
+    M::store((unsigned char*)op.o + (n * op.on + h * op.oh + tid) * M::kBytes, op.alpha * sum);
+  }
+}
+
+// ---- host side ---------------------------------------------------------------------------------
+
+int check(const sf_linattn_config* c, const char* fn) {
+  if (!c || c->struct_size != sizeof(sf_linattn_config)) {
+    set_error("%s: null configuration or struct_size mismatch", fn);
+    return SF_ERR_ARG;
+  }
+  if (c->dtype != SF_DTYPE_FP32 && c->dtype != SF_DTYPE_BF16) {
+    set_error("%s: dtype = %d", fn, c->dtype);
+    return SF_ERR_ARG;
+  }
+  if (c->T < 0 || c->N < 0 || c->H < 1 || c->Hk < 1 || c->H % c->Hk || c->dk < 1 || c->dk > 128 || c->dv < 1 || c->dv > 128) {
+    set_error("%s: T = %d, N = %d, H = %d, Hk = %d, dk = %d, dv = %d out of range", fn, c->T, c->N, c->H, c->Hk, c->dk, c->dv);
+    return SF_ERR_SHAPE;
+  }
+  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > INT32_MAX) {
+    set_error("%s: T * N or N * H beyond 2^31 - 1", fn);
+    return SF_ERR_SHAPE;
+  }
+  if (!isfinite(c->scale)) {
+    set_error("%s: scale is not finite", fn);
+    return SF_ERR_SHAPE;
+  }
+  return SF_OK;
+}
+
+int check_ptr(const char* fn, const char* name, const void* p, size_t align, bool optional = false) {
+  if (!p && optional) return SF_OK;
+  if (!p || (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0) {
+    set_error("%s: %s is null or not %zu-byte aligned", fn, name, align);
+    return SF_ERR_ARG;
+  }
+  return SF_OK;
+}
+
+struct Split {
+  int n_seg, seg_len;
+};
+// Pieces of T: enough workgroups to fill the chip, but each with at least four chunks.
+Split split_of(const sf_linattn_config* c, int ops) {
+  const int64_t lanes = (int64_t)c->N * c->H * ops;
+  const int64_t want = lanes > 0 ? (768 + lanes - 1) / lanes : 1;
+  int64_t len = (c->T + want - 1) / want;
+  len = (len + 63) / 64 * 64;
+  if (len < 256) len = 256;
+  if (len >= c->T) return Split{1, c->T > 0 ? c->T : 1};
+  return Split{(int)((c->T + len - 1) / len), (int)len};
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+struct Workspace {
+  size_t state, keep, dk, dv, total;  // bytes of each part, in this order
+};
+Workspace workspace_of(const sf_linattn_config* c, int backward) {
+  const int ops = backward ? 3 : 1;
+  const Split s = split_of(c, ops);
+  Workspace w = {0, 0, 0, 0, 0};
+  const size_t rows = (size_t)c->T * c->N * c->H;
+  if (s.n_seg > 1) {
+    w.state = align256((size_t)ops * c->N * c->H * s.n_seg * c->dk * c->dv * 4);
+    w.keep = align256((size_t)ops * c->N * c->H * s.n_seg * 4);
+  }
+  if (backward && c->H != c->Hk) {
+    w.dk = align256(rows * c->dk * 4);
+    w.dv = align256(rows * c->dv * 4);
+  }
+  w.total = w.state + w.keep + w.dk + w.dv;
+  return w;
+}
+
+Strided strided(const sf_linattn_config* c, const void* p, const int64_t* s, int div, int d) {
+  Strided a = {p, s[0], s[1], s[2], div, d, 0};
+  const int per = 16 / (c->dtype == SF_DTYPE_BF16 ? 2 : 4);
+  // (pieces are eight columns in both types)
+  a.vec = d % 8 == 0 && (s[0] % per) == 0 && (s[1] % per) == 0 && (s[2] % per) == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+  return a;
+}
+void put_out(const sf_linattn_config* c, LinOp& op, void* p, int64_t t, int64_t n, int64_t h, int d, bool f32) {
+  op.o = p;
+  op.ot = t;
+  op.on = n;
+  op.oh = h;
+  op.o_f32 = f32 || c->dtype == SF_DTYPE_FP32;
+  const int per = op.o_f32 ? 4 : 8;
+  op.o_vec = d % 8 == 0 && t % per == 0 && n % per == 0 && h % per == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+}
+
+template <int DTYPE, int D, int C, bool STATE>
+hipError_t launch_t(const LinArgs& g, int ops, hipStream_t st) {
+  const auto kern = linattn_kernel<DTYPE, D, C, STATE>;
+  constexpr int bytes = Lds<DTYPE, D, C>::kBytes;
+  static const hipError_t attr = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (attr != hipSuccess) return attr;
+  kern<<<dim3((unsigned)(g.N * g.H), (unsigned)g.n_seg, (unsigned)ops), kThreads, bytes, st>>>(g);
+  return hipGetLastError();
+}
+template <bool STATE>
+hipError_t launch(const sf_linattn_config* c, const LinArgs& g, int ops, hipStream_t st) {
+  const bool wide = c->dk > 64 || c->dv > 64;
+  if (c->dtype == SF_DTYPE_FP32)  // (64 steps of 128 numbers would leave a CU one workgroup)
+    return wide ? launch_t<SF_DTYPE_FP32, 128, 32, STATE>(g, ops, st) : launch_t<SF_DTYPE_FP32, 64, 32, STATE>(g, ops, st);
+  if (c->T <= 32) return wide ? launch_t<SF_DTYPE_BF16, 128, 32, STATE>(g, ops, st) : launch_t<SF_DTYPE_BF16, 64, 32, STATE>(g, ops, st);
+  return wide ? launch_t<SF_DTYPE_BF16, 128, 64, STATE>(g, ops, st) : launch_t<SF_DTYPE_BF16, 64, 64, STATE>(g, ops, st);
+}
+
+int run(const char* fn, const sf_linattn_config* c, LinArgs& g, int ops, const Workspace& w, unsigned char* ws, hipStream_t st) {
+  if (c->N == 0) return SF_OK;
+  const Split s = split_of(c, ops);
+  g.T = c->T;
+  g.N = c->N;
+  g.H = c->H;
+  g.n_seg = s.n_seg;
+  g.seg_len = s.seg_len;
+  hipError_t e = hipSuccess;
+  if (s.n_seg > 1) {
+    g.seg_state = (float*)ws;
+    g.seg_keep = (float*)(ws + w.state);
+    e = launch<true>(c, g, ops, st);
+    if (e == hipSuccess) {
+      linattn_join_kernel<<<dim3((unsigned)((c->dk * c->dv + kThreads - 1) / kThreads), (unsigned)(c->N * c->H), (unsigned)ops), kThreads, 0,
+                            st>>>(g);
+      e = hipGetLastError();
+    }
+  }
+  if (e == hipSuccess) e = launch<false>(c, g, ops, st);
+  if (e != hipSuccess) {
+    set_error("%s: launch failed: %s", fn, hipGetErrorString(e));
+    return SF_ERR_DEVICE;
+  }
+  return SF_OK;
+}
+
+}  // namespace
+
+}  // namespace sf
+
+using namespace sf;
+
+extern "C" int64_t sf_linattn_workspace_bytes(const sf_linattn_config* cfg, int backward) {
+  if (check(cfg, "sf_linattn_workspace_bytes") != SF_OK) return -1;
+  return (int64_t)workspace_of(cfg, backward).total;
+}
+
+extern "C" int sf_linattn(const sf_linattn_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+                          const uint8_t* done, const float* state0, void* o, float* state, void* workspace, void* hip_stream) {
+  static const char* fn = "sf_linattn";
+  int rc = check(cfg, fn);
+  if (rc != SF_OK) return rc;
+  const size_t e = cfg->dtype == SF_DTYPE_BF16 ? 2 : 4;
+  const bool none = (int64_t)cfg->T * cfg->N == 0;
+  const Workspace w = workspace_of(cfg, 0);
+  if ((rc = check_ptr(fn, "q", q, e, none)) || (rc = check_ptr(fn, "k", k, e, none)) || (rc = check_ptr(fn, "v", v, e, none)) ||
+      (rc = check_ptr(fn, "o", o, e, none)) || (rc = check_ptr(fn, "log_decay", log_decay, 4)) ||
+      (rc = check_ptr(fn, "state0", state0, 4, true)) || (rc = check_ptr(fn, "state", state, 4, true)) ||
+      (rc = check_ptr(fn, "workspace", workspace, 256, w.total == 0)))
+    return rc;
+  LinArgs g = {};
+  g.log_decay = log_decay;
+  g.done = done;
+  LinOp& op = g.op[0];
+  const int share = cfg->H / cfg->Hk;
+  op.q = strided(cfg, q, cfg->q_stride, 1, cfg->dk);
+  op.k = strided(cfg, k, cfg->k_stride, share, cfg->dk);
+  op.v = strided(cfg, v, cfg->v_stride, share, cfg->dv);
+  put_out(cfg, op, o, cfg->o_stride[0], cfg->o_stride[1], cfg->o_stride[2], cfg->dv, false);
+  op.s_in = state0;
+  op.s_out = state;
+  op.s_a = cfg->dv;
+  op.s_b = 1;
+  op.w_scale = 1.0f;
+  op.alpha = cfg->scale;
+  return run(fn, cfg, g, 1, w, (unsigned char*)workspace, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int sf_linattn_backward(const sf_linattn_config* cfg, const void* q, const void* k, const void* v,
+                                   const float* log_decay, const void* d_o, const uint8_t* done, const float* state0,
+                                   const float* dstate, void* dq, void* dk, void* dv, float* dstate0, void* workspace,
+                                   void* hip_stream) {
+  static const char* fn = "sf_linattn_backward";
+  int rc = check(cfg, fn);
+  if (rc != SF_OK) return rc;
+  const size_t e = cfg->dtype == SF_DTYPE_BF16 ? 2 : 4;
+  const bool none = (int64_t)cfg->T * cfg->N == 0;
+  const Workspace w = workspace_of(cfg, 1);
+  if ((rc = check_ptr(fn, "q", q, e, none)) || (rc = check_ptr(fn, "k", k, e, none)) || (rc = check_ptr(fn, "v", v, e, none)) ||
+      (rc = check_ptr(fn, "do", d_o, e, none)) || (rc = check_ptr(fn, "dq", dq, e, none)) || (rc = check_ptr(fn, "dk", dk, e, none)) ||
+      (rc = check_ptr(fn, "dv", dv, e, none)) || (rc = check_ptr(fn, "log_decay", log_decay, 4)) ||
+      (rc = check_ptr(fn, "state0", state0, 4, true)) || (rc = check_ptr(fn, "dstate", dstate, 4, true)) ||
+      (rc = check_ptr(fn, "dstate0", dstate0, 4, true)) || (rc = check_ptr(fn, "workspace", workspace, 256, w.total == 0)))
+    return rc;
+  if (dstate0 && (dstate0 == dstate || dstate0 == state0)) {
+    set_error("%s: dstate0 is dstate or state0", fn);
+    return SF_ERR_ALIAS;
+  }
+  const hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  const int H = cfg->H, Hk = cfg->Hk, share = H / Hk, Dk = cfg->dk, Dv = cfg->dv;
+  unsigned char* ws = (unsigned char*)workspace;
+  float* part_k = (float*)(ws + w.state + w.keep);
+  float* part_v = (float*)(ws + w.state + w.keep + w.dk);
+  LinArgs g = {};
+  g.log_decay = log_decay;
+  g.done = done;
+  const Strided sq = strided(cfg, q, cfg->q_stride, 1, Dk), sk = strided(cfg, k, cfg->k_stride, share, Dk),
+                sv = strided(cfg, v, cfg->v_stride, share, Dv), so = strided(cfg, d_o, cfg->o_stride, 1, Dv);
+  LinOp &oq = g.op[0], &ok = g.op[1], &ov = g.op[2];
+  oq.q = so;
+  oq.k = sv;
+  oq.v = sk;
+  put_out(cfg, oq, dq, (int64_t)cfg->N * H * Dk, (int64_t)H * Dk, Dk, Dk, false);
+  oq.s_in = state0;
+  oq.s_a = 1;
+  oq.s_b = Dv;
+  oq.w_scale = 1.0f;
+  oq.alpha = cfg->scale;
+  ok.q = sv;
+  ok.k = so;
+  ok.v = sq;
+  put_out(cfg, ok, share > 1 ? part_k : dk, (int64_t)cfg->N * H * Dk, (int64_t)H * Dk, Dk, Dk, share > 1);
+  ok.s_in = dstate;
+  ok.s_a = 1;
+  ok.s_b = Dv;
+  ok.w_scale = cfg->scale;
+  ok.alpha = 1.0f;
+  ok.reverse = 1;
+  ov.q = sk;
+  ov.k = sq;
+  ov.v = so;
+  put_out(cfg, ov, share > 1 ? part_v : dv, (int64_t)cfg->N * H * Dv, (int64_t)H * Dv, Dv, Dv, share > 1);
+  ov.s_in = dstate;
+  ov.s_out = dstate0;
+  ov.s_a = Dv;
+  ov.s_b = 1;
+  ov.w_scale = cfg->scale;
+  ov.alpha = 1.0f;
+  ov.reverse = 1;
+  rc = run(fn, cfg, g, 3, w, ws, st);
+  if (rc != SF_OK || share == 1 || none) return rc;
+  const int64_t nk = (int64_t)cfg->T * cfg->N * Hk * Dk, nv = (int64_t)cfg->T * cfg->N * Hk * Dv;
+  const unsigned gk = (unsigned)((nk + kThreads - 1) / kThreads), gv = (unsigned)((nv + kThreads - 1) / kThreads);
+  if (cfg->dtype == SF_DTYPE_BF16) {
+    linattn_share_kernel<SF_DTYPE_BF16><<<gk, kThreads, 0, st>>>(part_k, dk, nk, Dk, share);
+    linattn_share_kernel<SF_DTYPE_BF16><<<gv, kThreads, 0, st>>>(part_v, dv, nv, Dv, share);
+  } else {
+    linattn_share_kernel<SF_DTYPE_FP32><<<gk, kThreads, 0, st>>>(part_k, dk, nk, Dk, share);
+    linattn_share_kernel<SF_DTYPE_FP32><<<gv, kThreads, 0, st>>>(part_v, dv, nv, Dv, share);
+  }
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) {
+    set_error("%s: launch failed: %s", fn, hipGetErrorString(err));
+    return SF_ERR_DEVICE;
+  }
+  return SF_OK;
+}
+
+extern "C" int sf_linattn_step(const sf_linattn_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+                               float* state_table, int32_t n_env, const int32_t* env_ids, const uint8_t* done, void* o,
+                               void* hip_stream) {
+  static const char* fn = "sf_linattn_step";
+  int rc = check(cfg, fn);
+  if (rc != SF_OK) return rc;
+  if (cfg->T != 1 || n_env < 1) {
+    set_error("%s: T = %d (1 is wanted), n_env = %d", fn, cfg->T, n_env);
+    return SF_ERR_SHAPE;
+  }
+  if (!env_ids && cfg->N > n_env) {
+    set_error("%s: %d rows, but %d states and no ids", fn, cfg->N, n_env);
+    return SF_ERR_SHAPE;
+  }
+  const size_t e = cfg->dtype == SF_DTYPE_BF16 ? 2 : 4;
+  const bool none = cfg->N == 0;
+  if ((rc = check_ptr(fn, "q", q, e, none)) || (rc = check_ptr(fn, "k", k, e, none)) || (rc = check_ptr(fn, "v", v, e, none)) ||
+      (rc = check_ptr(fn, "o", o, e, none)) || (rc = check_ptr(fn, "log_decay", log_decay, 4)) ||
+      (rc = check_ptr(fn, "state_table", state_table, 16)) || (rc = check_ptr(fn, "env_ids", env_ids, 4, true)))
+    return rc;
+  if (none) return SF_OK;
+  const int share = cfg->H / cfg->Hk;
+  LinOp op = {};
+  op.q = strided(cfg, q, cfg->q_stride, 1, cfg->dk);
+  op.k = strided(cfg, k, cfg->k_stride, share, cfg->dk);
+  op.v = strided(cfg, v, cfg->v_stride, share, cfg->dv);
+  put_out(cfg, op, o, 0, cfg->o_stride[1], cfg->o_stride[2], cfg->dv, false);
+  op.alpha = cfg->scale;
+  // a thread has four columns; rows of a multiple of four floats are read 16 bytes at a time
+  int lanes_log2 = 0;
+  while ((4 << lanes_log2) < cfg->dv) ++lanes_log2;
+  if (lanes_log2 < 4) lanes_log2 = 4;  // (256 threads then have 16 rows each of at most 256)
+  const unsigned grid = (unsigned)(cfg->N * cfg->H);
+  const hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  const bool vec = cfg->dv % 4 == 0;
+  const auto kern = cfg->dtype == SF_DTYPE_BF16
+                        ? (vec ? linattn_step_kernel<SF_DTYPE_BF16, true> : linattn_step_kernel<SF_DTYPE_BF16, false>)
+                        : (vec ? linattn_step_kernel<SF_DTYPE_FP32, true> : linattn_step_kernel<SF_DTYPE_FP32, false>);
+  kern<<<grid, kThreads, 0, st>>>(op, log_decay, done, state_table, n_env, env_ids, cfg->H, lanes_log2);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) {
+    set_error("%s: launch failed: %s", fn, hipGetErrorString(err));
+    return SF_ERR_DEVICE;
+  }
+  return SF_OK;
+}

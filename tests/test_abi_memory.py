@@ -1,0 +1,65 @@
+"""include/sf_memory.h: every function it declares is exported and bound, the ctypes mirrors of its structs have the
+sizes and offsets that the C compiler gives them, and bad arguments come back as errors without a GPU."""
+import ctypes
+import os
+import re
+import subprocess
+import tempfile
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def _memory():
+    from paper_2006_11751_amd import binding, memory
+    if not os.path.exists(binding.library_path()):
+        binding.build_library()
+    return memory
+
+
+def test_every_declared_symbol_is_exported_and_bound():
+    memory = _memory()
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "sf_memory.h")).read(), flags=re.S)
+    names = set(re.findall(r"\b(sf_[a-z0-9_]+)\s*\(", text))
+    assert set(memory.EXPORTS) == names
+    lib = memory.load_library()
+    for n in names:
+        assert getattr(lib, n).argtypes, n
+
+
+def test_struct_layouts_match_the_header():
+    memory = _memory()
+    structs = {v: k for k, v in memory.STRUCTS.items()}
+    src = '#include <stdio.h>\n#include <stddef.h>\n#include "sf_memory.h"\nint main(void){\n'
+    for s, name in structs.items():
+        src += 'printf("%%zu\\n", sizeof(%s));\n' % name
+        src += "".join('printf("%%zu\\n", offsetof(%s, %s));\n' % (name, f[0]) for f in s._fields_)
+    with tempfile.TemporaryDirectory() as d:
+        c, exe = os.path.join(d, "s.c"), os.path.join(d, "s")
+        open(c, "w").write(src + "return 0;}\n")
+        subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), c, "-o", exe], check=True)
+        got = [int(v) for v in subprocess.run([exe], capture_output=True, check=True).stdout.split()]
+    want = []
+    for s in structs:
+        want += [ctypes.sizeof(s)] + [getattr(s, f[0]).offset for f in s._fields_]
+    assert got == want
+
+
+def test_linattn_refuses_without_a_gpu():
+    memory = _memory()
+    lib, C = memory.load_library(), memory.SfLinattnConfig
+    err = lambda: lib.sf_last_error().decode()
+    good = dict(struct_size=ctypes.sizeof(C), dtype=0, T=8, N=2, H=4, Hk=2, dk=16, dv=16, scale=0.25)
+    make = lambda **kw: ctypes.byref(C(**dict(good, **kw)))
+    none = [None] * 10
+    assert lib.sf_linattn(None, *none) == -1
+    for kw, code, text in ((dict(struct_size=4), -1, "struct_size"), (dict(dtype=2), -1, "dtype"), (dict(Hk=3), -2, "Hk = 3"),
+                           (dict(H=0), -2, "H = 0"), (dict(T=-1), -2, "T = -1"), (dict(dk=129), -2, "dk = 129"), (dict(dv=0), -2, "dv = 0"),
+                           (dict(scale=float("inf")), -2, "scale"), (dict(T=1 << 20, N=1 << 20), -2, "2^31"), ({}, -1, "q is null")):
+        assert lib.sf_linattn(make(**kw), *none) == code and text in err(), (kw, err())
+    assert lib.sf_linattn(make(), 2, 4, 4, 4, None, None, 4, None, None, None) == -1 and "q is null or not 4-byte" in err()
+    assert lib.sf_linattn_backward(make(), *[None] * 14) == -1
+    assert lib.sf_linattn_step(make(), *[None] * 5, 1, *[None] * 4) == -2 and "T = 8" in err()
+    assert lib.sf_linattn_step(make(T=1), *[None] * 5, 1, *[None] * 4) == -2 and "no ids" in err()
+    assert lib.sf_linattn_workspace_bytes(make(), 0) == 0
+    assert lib.sf_linattn_workspace_bytes(make(Hk=3), 0) == -1
+    assert lib.sf_linattn_workspace_bytes(make(), 1) >= 8 * 2 * 4 * 32 * 4  # the shared heads' partial sums
