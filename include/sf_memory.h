@@ -70,6 +70,44 @@ int sf_linattn_step(const sf_linattn_config* cfg, const void* q, const void* k, 
                     float* state_table, int32_t n_env, const int32_t* env_ids, const uint8_t* done, void* o,
                     void* hip_stream);
 
+/* ---- the norms behind and before a block, with its gate, residual scale and residual stream ----
+ * For each of M rows of D channels, b the block's output and x the residual stream it is added to:
+ *   u = N_post(b) * post_w            over each of `groups` equal groups of channels
+ *   y = x + scale * act(gate) * u     the residual stream behind the block
+ *   n = N_pre(y) * pre_w              what the next block is given
+ *   N = SF_NORM_NONE  the row itself (post_w is not used then)
+ *       SF_NORM_RMS   r / sqrt(mean r^2 + eps)
+ *       SF_NORM_LAYER (r - mean r) / sqrt(mean (r - mean r)^2 + eps)
+ *   act = SF_GATE_NONE: 1 (gate is not used), SF_GATE_SIGMOID, SF_GATE_SILU (g sigmoid(g))
+ * groups > 1 (an attention core's norm per head) needs pre = SF_NORM_NONE.  x NULL: no residual stream, y = scale *
+ * act(gate) * u.  post_w, scale, pre_w: fp32 [D] or NULL (ones).
+ *   b, x, gate  dev [M] rows of D, io, row m at m * *_stride elements
+ *   y, n        dev [M][D] dense, io.  y may be NULL if there is an n, n is not written without N_pre.  y may be x
+ *               (dense), b or gate, n likewise if y is not it.
+ * Backward: dy [M] rows (NULL: zero, with N_pre only) and dn [M] rows (with N_pre) are the gradients of y and n; dx, db,
+ * dgate [M][D] dense io and dpost_w, dscale, dpre_w fp32 [D] are written where they are not NULL (zeros for a
+ * weight that is not used).  Nothing of the forward pass is needed but its inputs.  dx, db, dgate may each be any one of
+ * the inputs (dense).
+ * workspace: sf_resnorm_workspace_bytes(cfg), NULL if no gradient of a weight is wanted.
+ * Any D up to 8192 a group, any strides; rows of whole 16-byte pieces, 16-byte aligned, are read in such pieces.
+ * Errors: SF_ERR_ARG, SF_ERR_SHAPE (M < 0, D or groups out of range, groups > 1024, groups with N_pre, eps < 0),
+ * SF_ERR_DEVICE. */
+enum { SF_NORM_NONE = 0, SF_NORM_RMS = 1, SF_NORM_LAYER = 2 };
+enum { SF_GATE_NONE = 0, SF_GATE_SIGMOID = 1, SF_GATE_SILU = 2 };
+typedef struct {
+  uint32_t struct_size; /* sizeof(sf_resnorm_config) */
+  int32_t dtype;        /* SF_DTYPE_* of the rows */
+  int32_t M, D, groups, post, pre, gate_act;
+  float eps;
+  int64_t b_stride, x_stride, gate_stride, dy_stride, dn_stride; /* elements between rows */
+} sf_resnorm_config;
+int sf_resnorm(const sf_resnorm_config* cfg, const void* b, const void* x, const void* gate, const float* post_w,
+               const float* scale, const float* pre_w, void* y, void* n, void* hip_stream);
+int64_t sf_resnorm_workspace_bytes(const sf_resnorm_config* cfg);
+int sf_resnorm_backward(const sf_resnorm_config* cfg, const void* b, const void* x, const void* gate, const float* post_w,
+                        const float* scale, const float* pre_w, const void* dy, const void* dn, void* dx, void* db,
+                        void* dgate, float* dpost_w, float* dscale, float* dpre_w, void* workspace, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,7 +15,8 @@ from .binding import SF_OK, SfError, sf_last_error
 
 SF_DTYPE_FP32, SF_DTYPE_BF16 = 0, 1
 
-EXPORTS = ("sf_linattn_workspace_bytes", "sf_linattn", "sf_linattn_backward", "sf_linattn_step")
+EXPORTS = ("sf_linattn_workspace_bytes", "sf_linattn", "sf_linattn_backward", "sf_linattn_step", "sf_resnorm", "sf_resnorm_workspace_bytes",
+           "sf_resnorm_backward")
 
 _STRIDE = C.c_int64 * 3
 
@@ -26,7 +27,13 @@ class SfLinattnConfig(C.Structure):
                 ("q_stride", _STRIDE), ("k_stride", _STRIDE), ("v_stride", _STRIDE), ("o_stride", _STRIDE)]
 
 
-STRUCTS = {"sf_linattn_config": SfLinattnConfig}  # by their C names
+class SfResnormConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("M", C.c_int32), ("D", C.c_int32), ("groups", C.c_int32),
+                ("post", C.c_int32), ("pre", C.c_int32), ("gate_act", C.c_int32), ("eps", C.c_float), ("b_stride", C.c_int64),
+                ("x_stride", C.c_int64), ("gate_stride", C.c_int64), ("dy_stride", C.c_int64), ("dn_stride", C.c_int64)]
+
+
+STRUCTS = {"sf_linattn_config": SfLinattnConfig, "sf_resnorm_config": SfResnormConfig}  # by their C names
 
 _lib = None
 
@@ -41,7 +48,10 @@ def load_library():
                 ("sf_linattn_workspace_bytes", C.c_int64, [C.POINTER(SfLinattnConfig), C.c_int]),
                 ("sf_linattn", C.c_int, [C.POINTER(SfLinattnConfig)] + [P] * 10),
                 ("sf_linattn_backward", C.c_int, [C.POINTER(SfLinattnConfig)] + [P] * 14),
-                ("sf_linattn_step", C.c_int, [C.POINTER(SfLinattnConfig)] + [P] * 5 + [C.c_int32] + [P] * 4)):
+                ("sf_linattn_step", C.c_int, [C.POINTER(SfLinattnConfig)] + [P] * 5 + [C.c_int32] + [P] * 4),
+                ("sf_resnorm", C.c_int, [C.POINTER(SfResnormConfig)] + [P] * 9),
+                ("sf_resnorm_workspace_bytes", C.c_int64, [C.POINTER(SfResnormConfig)]),
+                ("sf_resnorm_backward", C.c_int, [C.POINTER(SfResnormConfig)] + [P] * 16)):
             f = getattr(L, name)
             f.restype, f.argtypes = restype, argtypes
         _lib = L
@@ -196,4 +206,83 @@ def linear_attention_step(q, k, v, log_decay, state_table, env_ids=None, done=No
     o = _result(out, "o", (B, H, c.dv), q.dtype, q.device)
     _check(load_library().sf_linattn_step(C.byref(c), q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
                                           state_table.data_ptr(), n_env, ids, done, o.data_ptr(), _stream(stream, q.device)))
+    return out
+
+
+_NORMS = {"none": 0, "rms": 1, "layer": 2}
+_GATES = {"none": 0, "sigmoid": 1, "silu": 2}
+
+
+def _flat(name, t, like=None):
+    """A tensor of rows [..., D] as [M, D] (no copy)."""
+    if t.dim() != 2:
+        t = t.view(-1, t.shape[-1])
+    if like is not None:
+        _same(name, t, like, tuple(like.shape), dense=False)
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        _refuse("%s: the last axis is not dense" % name)
+    return t
+
+
+def _resnorm_config(b, x, gate, post, pre, post_w, pre_w, scale, groups, gate_act, eps):
+    """The configuration, b, x and the gate as rows, and the weights' addresses."""
+    if not b.is_cuda:
+        _refuse("b is not on the GPU")
+    b = _flat("b", b)
+    for what, how, known in (("post", post, _NORMS), ("pre", pre, _NORMS), ("gate_act", gate_act, _GATES)):
+        if how not in known:
+            _refuse("%s = %r: one of %s is wanted" % (what, how, ", ".join(known)))
+    if (gate is None) != (gate_act == "none"):
+        _refuse("a gate and its activation come together")
+    M, D = b.shape
+    x = None if x is None else _flat("x", x, b)
+    gate = None if gate is None else _flat("gate", gate, b)
+    f32 = binding._torch().float32
+    w = tuple(_optional(n, t, b, (D,), f32) for n, t in (("post_w", post_w), ("scale", scale), ("pre_w", pre_w)))
+    c = SfResnormConfig(C.sizeof(SfResnormConfig), _dtype_of(b), M, D, groups, _NORMS[post], _NORMS[pre], _GATES[gate_act], eps,
+                        b.stride(0), 0 if x is None else x.stride(0), 0 if gate is None else gate.stride(0), 0, 0)
+    return c, b, x, gate, w
+
+
+def residual_norm(b, x=None, gate=None, post="rms", pre="rms", post_w=None, pre_w=None, scale=None, groups=1, gate_act="none",
+                  eps=1e-6, out=None, stream=None):
+    """y = x + scale * act(gate) * N_post(b) * post_w and n = N_pre(y) * pre_w over rows [..., D] (bf16 or fp32, last axis
+    dense; weights fp32 [D]).  post, pre: "none", "rms" or "layer"; gate_act: "none", "sigmoid" or "silu"; groups: of
+    channels that post is taken over (pre "none" then).  Results: y and, with pre, n."""
+    out = {} if out is None else out
+    shape = tuple(b.shape)
+    c, b, x, gate, w = _resnorm_config(b, x, gate, post, pre, post_w, pre_w, scale, groups, gate_act, eps)
+    y = _result(out, "y", shape, b.dtype, b.device)
+    n = _result(out, "n", shape, b.dtype, b.device) if c.pre else None
+    _check(load_library().sf_resnorm(C.byref(c), b.data_ptr(), _ptr(x), _ptr(gate), w[0], w[1], w[2], y.data_ptr(), _ptr(n),
+                                     _stream(stream, b.device)))
+    return out
+
+
+def residual_norm_backward(b, dy, dn=None, x=None, gate=None, post="rms", pre="rms", post_w=None, pre_w=None, scale=None, groups=1,
+                           gate_act="none", eps=1e-6, out=None, stream=None):
+    """Gradients of residual_norm with the same arguments, given those of y (None: zero) and, with pre, of n.  Results: db and,
+    for what was given, dx, dgate, dpost_w, dscale, dpre_w (fp32)."""
+    out = {} if out is None else out
+    shape = tuple(b.shape)
+    c, b, x, gate, w = _resnorm_config(b, x, gate, post, pre, post_w, pre_w, scale, groups, gate_act, eps)
+    if dn is None and c.pre:
+        _refuse("dn is wanted with pre = %r" % pre)
+    if dy is None and not c.pre:
+        _refuse("dy is wanted")
+    if dy is not None:
+        dy = _flat("dy", dy, b)
+        c.dy_stride = dy.stride(0)
+    if dn is not None:
+        dn = _flat("dn", dn, b)
+        c.dn_stride = dn.stride(0)
+    d, f32, D = b.device, binding._torch().float32, (b.shape[1],)
+    db = _result(out, "db", shape, b.dtype, d)
+    dx = None if x is None else _result(out, "dx", shape, b.dtype, d)
+    dgate = None if gate is None else _result(out, "dgate", shape, b.dtype, d)
+    dw = [None if t is None else _result(out, n, D, f32, d) for n, t in (("dpost_w", post_w), ("dscale", scale), ("dpre_w", pre_w))]
+    L = load_library()
+    ws = _workspace(out, L.sf_resnorm_workspace_bytes(C.byref(c)), d) if any(t is not None for t in dw) else None
+    _check(L.sf_resnorm_backward(C.byref(c), b.data_ptr(), _ptr(x), _ptr(gate), w[0], w[1], w[2], _ptr(dy), _ptr(dn), _ptr(dx),
+                                 db.data_ptr(), _ptr(dgate), _ptr(dw[0]), _ptr(dw[1]), _ptr(dw[2]), ws, _stream(stream, d)))
     return out

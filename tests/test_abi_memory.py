@@ -63,3 +63,21 @@ def test_linattn_refuses_without_a_gpu():
     assert lib.sf_linattn_workspace_bytes(make(), 0) == 0
     assert lib.sf_linattn_workspace_bytes(make(Hk=3), 0) == -1
     assert lib.sf_linattn_workspace_bytes(make(), 1) >= 8 * 2 * 4 * 32 * 4  # the shared heads' partial sums
+
+
+def test_resnorm_refuses_without_a_gpu():
+    memory = _memory()
+    lib, C = memory.load_library(), memory.SfResnormConfig
+    err = lambda: lib.sf_last_error().decode()
+    good = dict(struct_size=ctypes.sizeof(C), dtype=0, M=8, D=64, groups=1, post=1, pre=1, gate_act=0, eps=1e-6, b_stride=64)
+    make = lambda **kw: ctypes.byref(C(**dict(good, **kw)))
+    for kw, code, text in ((dict(struct_size=4), -1, "struct_size"), (dict(dtype=2), -1, "dtype"), (dict(post=3), -1, "post = 3"),
+                           (dict(pre=-1), -1, "pre = -1"), (dict(gate_act=3), -1, "gate_act"), (dict(M=-1), -2, "M = -1"), (dict(D=0), -2, "D = 0"),
+                           (dict(D=8193), -2, "8193"), (dict(groups=5), -2, "groups = 5"), (dict(groups=2), -2, "groups = 2"),
+                           (dict(eps=-1.0), -2, "eps"), (dict(eps=float("nan")), -2, "eps"), ({}, -1, "b is null")):
+        assert lib.sf_resnorm(make(**kw), *[None] * 9) == code and text in err(), (kw, err())
+    assert lib.sf_resnorm(make(gate_act=1), 16, None, None, None, None, None, 16, 16, None) == -1 and "gate" in err()
+    assert lib.sf_resnorm(make(), 16, None, None, None, None, None, 16, None, None) == -1 and "n is null" in err()
+    assert lib.sf_resnorm_backward(make(), 16, *[None] * 15) == -1 and "dn" in err()
+    assert lib.sf_resnorm_workspace_bytes(make(groups=5)) == -1
+    assert lib.sf_resnorm_workspace_bytes(make()) > 0
