@@ -108,6 +108,35 @@ int sf_resnorm_backward(const sf_resnorm_config* cfg, const void* b, const void*
                         const float* scale, const float* pre_w, const void* dy, const void* dn, void* dx, void* db,
                         void* dgate, float* dpost_w, float* dscale, float* dpre_w, void* workspace, void* hip_stream);
 
+/* ---- the gated feed-forward block --------------------------------------------------
+ *   h = act(x w_gate^T) * (x w_up^T),   y = h w_down^T
+ * x [M] rows of D, w_gate and w_up [F] rows of D, w_down [D] rows of F, all of one type, rows *_stride elements apart; y
+ * [M][D] dense, 16-byte aligned.
+ *   act = SF_ACT_SILU (g sigmoid(g)), SF_ACT_GELU (g Phi(g), by erf), SF_ACT_SIGMOID
+ * bf16: products of bf16 numbers are added in fp32, h is rounded to bf16, y is rounded once more.  fp32: operands are the
+ * exact sums of three bf16 numbers, of whose nine products six are added (2^-27 is left out); up to 64 rows run on the
+ * fp32 matrix instruction.  Infinities and NaN are only in the rows of y whose rows of x hold them; in weights they
+ * reach all (of an infinity fp32 results are NaN).
+ * Backward: dy [M] rows -> dx [M][D], dw_gate, dw_up [F][D], dw_down [D][F], dense, 16-byte aligned, of the same type.
+ * Nothing of the forward pass is needed but its inputs.  Results must not overlap inputs.
+ * Rows of a multiple of 64 numbers, 16-byte aligned, are read where they are; others are laid out in the workspace first
+ * (up to 64 rows forwards: read element by element).
+ * workspace: sf_ffn_workspace_bytes(cfg, backward), 256-byte aligned, wanted unless M is 0.
+ * Errors: SF_ERR_ARG, SF_ERR_SHAPE (M outside 0 .. 2^24, D or F outside 1 .. 2^20), SF_ERR_DEVICE. */
+enum { SF_ACT_SILU = 0, SF_ACT_GELU = 1, SF_ACT_SIGMOID = 2 };
+typedef struct {
+  uint32_t struct_size; /* sizeof(sf_ffn_config) */
+  int32_t dtype;        /* SF_DTYPE_* of all arrays */
+  int32_t M, D, F, act;
+  int64_t x_stride, w_gate_stride, w_up_stride, w_down_stride, dy_stride; /* elements between rows */
+} sf_ffn_config;
+int64_t sf_ffn_workspace_bytes(const sf_ffn_config* cfg, int backward); /* -1 on a bad configuration */
+int sf_ffn(const sf_ffn_config* cfg, const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y,
+           void* workspace, void* hip_stream);
+int sf_ffn_backward(const sf_ffn_config* cfg, const void* x, const void* w_gate, const void* w_up, const void* w_down,
+                    const void* dy, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* workspace,
+                    void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

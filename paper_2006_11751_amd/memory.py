@@ -16,7 +16,7 @@ from .binding import SF_OK, SfError, sf_last_error
 SF_DTYPE_FP32, SF_DTYPE_BF16 = 0, 1
 
 EXPORTS = ("sf_linattn_workspace_bytes", "sf_linattn", "sf_linattn_backward", "sf_linattn_step", "sf_resnorm", "sf_resnorm_workspace_bytes",
-           "sf_resnorm_backward")
+           "sf_resnorm_backward", "sf_ffn_workspace_bytes", "sf_ffn", "sf_ffn_backward")
 
 _STRIDE = C.c_int64 * 3
 
@@ -33,7 +33,14 @@ class SfResnormConfig(C.Structure):
                 ("x_stride", C.c_int64), ("gate_stride", C.c_int64), ("dy_stride", C.c_int64), ("dn_stride", C.c_int64)]
 
 
-STRUCTS = {"sf_linattn_config": SfLinattnConfig, "sf_resnorm_config": SfResnormConfig}  # by their C names
+class SfFfnConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("M", C.c_int32), ("D", C.c_int32), ("F", C.c_int32),
+                ("act", C.c_int32), ("x_stride", C.c_int64), ("w_gate_stride", C.c_int64), ("w_up_stride", C.c_int64),
+                ("w_down_stride", C.c_int64), ("dy_stride", C.c_int64)]
+
+
+# by their C names
+STRUCTS = {"sf_linattn_config": SfLinattnConfig, "sf_resnorm_config": SfResnormConfig, "sf_ffn_config": SfFfnConfig}
 
 _lib = None
 
@@ -51,7 +58,10 @@ def load_library():
                 ("sf_linattn_step", C.c_int, [C.POINTER(SfLinattnConfig)] + [P] * 5 + [C.c_int32] + [P] * 4),
                 ("sf_resnorm", C.c_int, [C.POINTER(SfResnormConfig)] + [P] * 9),
                 ("sf_resnorm_workspace_bytes", C.c_int64, [C.POINTER(SfResnormConfig)]),
-                ("sf_resnorm_backward", C.c_int, [C.POINTER(SfResnormConfig)] + [P] * 16)):
+                ("sf_resnorm_backward", C.c_int, [C.POINTER(SfResnormConfig)] + [P] * 16),
+                ("sf_ffn_workspace_bytes", C.c_int64, [C.POINTER(SfFfnConfig), C.c_int]),
+                ("sf_ffn", C.c_int, [C.POINTER(SfFfnConfig)] + [P] * 7),
+                ("sf_ffn_backward", C.c_int, [C.POINTER(SfFfnConfig)] + [P] * 11)):
             f = getattr(L, name)
             f.restype, f.argtypes = restype, argtypes
         _lib = L
@@ -285,4 +295,51 @@ def residual_norm_backward(b, dy, dn=None, x=None, gate=None, post="rms", pre="r
     ws = _workspace(out, L.sf_resnorm_workspace_bytes(C.byref(c)), d) if any(t is not None for t in dw) else None
     _check(L.sf_resnorm_backward(C.byref(c), b.data_ptr(), _ptr(x), _ptr(gate), w[0], w[1], w[2], _ptr(dy), _ptr(dn), _ptr(dx),
                                  db.data_ptr(), _ptr(dgate), _ptr(dw[0]), _ptr(dw[1]), _ptr(dw[2]), ws, _stream(stream, d)))
+    return out
+
+
+_ACTS = {"silu": 0, "gelu": 1, "sigmoid": 2}
+
+
+def _ffn_config(x, w_gate, w_up, w_down, act):
+    if not x.is_cuda:
+        _refuse("x is not on the GPU")
+    if act not in _ACTS:
+        _refuse("act = %r: one of %s is wanted" % (act, ", ".join(_ACTS)))
+    x = _flat("x", x)
+    if w_gate.dim() != 2:
+        _refuse("w_gate: %s" % (tuple(w_gate.shape),))
+    (M, D), F = x.shape, w_gate.shape[0]
+    for name, w, shape in (("w_gate", w_gate, (F, D)), ("w_up", w_up, (F, D)), ("w_down", w_down, (D, F))):
+        _same(name, w, x, shape, dense=False)
+        _rows(name, w)
+    c = SfFfnConfig(C.sizeof(SfFfnConfig), _dtype_of(x), M, D, F, _ACTS[act], x.stride(0), w_gate.stride(0), w_up.stride(0), w_down.stride(0), 0)
+    return c, x
+
+
+def gated_ffn(x, w_gate, w_up, w_down, act="silu", out=None, stream=None):
+    """y = (act(x w_gate^T) * (x w_up^T)) w_down^T: x [..., D], w_gate and w_up [F,D], w_down [D,F] (all bf16 or all fp32, last
+    axis dense); act: "silu", "gelu" or "sigmoid".  Result: y [..., D]."""
+    out = {} if out is None else out
+    shape = tuple(x.shape)
+    c, x = _ffn_config(x, w_gate, w_up, w_down, act)
+    y = _result(out, "y", shape, x.dtype, x.device)
+    L = load_library()
+    w = _workspace(out, L.sf_ffn_workspace_bytes(C.byref(c), 0), x.device)
+    _check(L.sf_ffn(C.byref(c), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y.data_ptr(), w, _stream(stream, x.device)))
+    return out
+
+
+def gated_ffn_backward(x, w_gate, w_up, w_down, dy, act="silu", out=None, stream=None):
+    """Gradients of gated_ffn with the same arguments, given that of y.  Results: dx, dw_gate, dw_up, dw_down."""
+    out = {} if out is None else out
+    shape, d = tuple(x.shape), x.device
+    c, x = _ffn_config(x, w_gate, w_up, w_down, act)
+    dy = _flat("dy", dy, x)
+    c.dy_stride = dy.stride(0)
+    got = [_result(out, n, s, x.dtype, d) for n, s in (("dx", shape), ("dw_gate", (c.F, c.D)), ("dw_up", (c.F, c.D)), ("dw_down", (c.D, c.F)))]
+    L = load_library()
+    w = _workspace(out, L.sf_ffn_workspace_bytes(C.byref(c), 1), d)
+    _check(L.sf_ffn_backward(C.byref(c), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dy.data_ptr(),
+                             *(t.data_ptr() for t in got), w, _stream(stream, d)))
     return out

@@ -81,3 +81,22 @@ def test_resnorm_refuses_without_a_gpu():
     assert lib.sf_resnorm_backward(make(), 16, *[None] * 15) == -1 and "dn" in err()
     assert lib.sf_resnorm_workspace_bytes(make(groups=5)) == -1
     assert lib.sf_resnorm_workspace_bytes(make()) > 0
+
+
+def test_ffn_refuses_without_a_gpu():
+    memory = _memory()
+    lib, C = memory.load_library(), memory.SfFfnConfig
+    err = lambda: lib.sf_last_error().decode()
+    good = dict(struct_size=ctypes.sizeof(C), dtype=1, M=8, D=64, F=128, act=0, x_stride=64, w_gate_stride=64, w_up_stride=64,
+                w_down_stride=128, dy_stride=64)
+    make = lambda **kw: ctypes.byref(C(**dict(good, **kw)))
+    for kw, code, text in ((dict(struct_size=4), -1, "struct_size"), (dict(dtype=2), -1, "dtype"), (dict(act=3), -1, "act = 3"),
+                           (dict(M=-1), -2, "M = -1"), (dict(D=0), -2, "D = 0"), (dict(F=1 << 21), -2, "F = "), ({}, -1, "x is null")):
+        assert lib.sf_ffn(make(**kw), *[None] * 7) == code and text in err(), (kw, err())
+        assert lib.sf_ffn_backward(make(**kw), *[None] * 11) == code and text in err(), (kw, err())
+    assert lib.sf_ffn(make(), 16, 16, 16, 16, 8, 256, None) == -1 and "y is" in err()
+    assert lib.sf_ffn(make(), 16, 16, 16, 16, 16, 128, None) == -1 and "workspace" in err()
+    assert lib.sf_ffn(make(), 16, 16, 17, 16, 16, 256, None) == -1 and "w_up" in err()
+    assert lib.sf_ffn_workspace_bytes(make(act=-1), 0) == -1
+    assert lib.sf_ffn_workspace_bytes(make(), 0) >= 8 * 128 * 2
+    assert lib.sf_ffn_workspace_bytes(make(M=100), 1) > lib.sf_ffn_workspace_bytes(make(M=100), 0) > 0
