@@ -174,39 +174,62 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
   const int band = tile / (4 * g.nf), in_band = tile - band * 4 * g.nf, height = min(4, g.nm - 4 * band);
   const int f0 = in_band / height * BF, m0 = (4 * band + in_band % height) * BM;
 
-  // this thread's pieces: row (tid / PR + RS * i) of the step's rows, piece tid % PR; from the tile's first row on
-  int row_at[L::kPieces];
+  // this thread's pieces: row (tid / PR + RS * i) of the step's rows, piece tid % PR; bytes from the tile's first row on
+  constexpr int NP = L::kPieces, NK = BK / 16, MF = W * TF * TM, FR = W * TF + X * TM;  // products, operands of 16 numbers of K
+  unsigned row_at[NP];
 #pragma unroll
-  for (int i = 0; i < L::kPieces; ++i) {
+  for (int i = 0; i < NP; ++i) {
     const int first = RS * i;  // of the array's tile
     const bool of_w = first < W * BF;
     const int r = (of_w ? first % BF : (first - W * BF) % BM) + tid / PR;
     const Operand& o = of_w ? g.w[first / BF] : g.x[(first - W * BF) / BM];
-    row_at[i] = min(r, (of_w ? g.F - 1 - f0 : g.M - 1 - m0)) * (int)o.pitch + (tid % PR) * 8;  // (past the end: the last row, never stored)
+    row_at[i] = (unsigned)min(r, (of_w ? g.F - 1 - f0 : g.M - 1 - m0)) * (unsigned)o.pitch * 2 + (tid % PR) * 16;  // (past the end: the last row, never stored)
   }
-  const int steps_k = g.K / BK, passes = (g.terms == 1 ? 1 : 6) * g.pairs, steps = steps_k * passes;
-  u32x4 next[L::kPieces];
-  int pass = 0, k = 0;  // of the step to be requested
-  auto request = [&]() __attribute__((always_inline)) {
+  // the step to be requested next: its pass (pair of operands, planes) and place in K
+  const int passes = (g.terms == 1 ? 1 : 6) * g.pairs, steps = g.K / BK * passes;
+  int pass = 0, k = 0;
+  const unsigned char *wb[W], *xb[X];
+  auto begin_pass = [&]() __attribute__((always_inline)) {
     const int pair = FORM == kOne && pass >= passes / g.pairs ? 1 : 0, term = g.terms == 1 ? 5 : pass - pair * 6;
 #pragma unroll
-    for (int i = 0; i < L::kPieces; ++i) {
-      const int first = RS * i;
-      const bool of_w = first < W * BF;
-      const Operand& o = of_w ? g.w[FORM == kOne ? pair : first / BF] : g.x[FORM == kOne ? pair : (first - W * BF) / BM];
-      const uint16_t* base = o.p + (of_w ? kPlaneW[term] : kPlaneX[term]) * o.plane + (int64_t)(of_w ? f0 : m0) * o.pitch + k;
-      next[i] = *(const u32x4*)(base + row_at[i]);
+    for (int a = 0; a < W; ++a) {
+      const Operand& o = g.w[FORM == kOne ? pair : a];
+      wb[a] = (const unsigned char*)(o.p + kPlaneW[term] * o.plane + (int64_t)f0 * o.pitch);
     }
-    k += BK;
-    if (k == g.K) {
-      k = 0;
-      if (++pass == passes) pass = passes - 1;  // (the last pass again, for no use)
+#pragma unroll
+    for (int a = 0; a < X; ++a) {
+      const Operand& o = g.x[FORM == kOne ? pair : a];
+      xb[a] = (const unsigned char*)(o.p + kPlaneX[term] * o.plane + (int64_t)m0 * o.pitch);
     }
   };
-  auto put = [&](int stage) __attribute__((always_inline)) {
+  auto advance = [&]() __attribute__((always_inline)) {  // (past the end: the last step again, for no use)
+    k += BK;
+    if (k == g.K) {
+      if (pass + 1 < passes) {
+        ++pass;
+        k = 0;
+        begin_pass();
+      } else {
+        k -= BK;
+      }
+    }
+  };
+  u32x4 next[NP];
+  auto request = [&](int i) __attribute__((always_inline)) {
+    const int first = RS * i;
+    const unsigned char* base = first < W * BF ? wb[first / BF] : xb[(first - W * BF) / BM];
+    next[i] = *(const u32x4*)(base + 2 * k + row_at[i]);
+  };
+  unsigned char* const put_at = lds + tid / PR * L::kPitch + (tid % PR) * 16;
+  auto put = [&](int i, int stage) __attribute__((always_inline)) { *(u32x4*)(put_at + stage + RS * i * L::kPitch) = next[i]; };
+  const unsigned char* const w_at = lds + (wf * (BF / 2) + li) * L::kPitch + lh * 16;
+  const unsigned char* const x_at = lds + (W * BF + wm * (BM / 2) + li) * L::kPitch + lh * 16;
+  bf16x8 fw[2][W * TF], fx[2][X * TM];
+  auto operands = [&](int to, int stage, int kk) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < L::kPieces; ++i)
-      *(u32x4*)(lds + stage * L::kStage + (RS * i + tid / PR) * L::kPitch + (tid % PR) * 16) = next[i];
+    for (int i = 0; i < X * TM; ++i) fx[to][i] = *(const bf16x8*)(x_at + stage + (i / TM * BM + 32 * (i % TM)) * L::kPitch + kk * 32);
+#pragma unroll
+    for (int i = 0; i < W * TF; ++i) fw[to][i] = *(const bf16x8*)(w_at + stage + (i / TF * BF + 32 * (i % TF)) * L::kPitch + kk * 32);
   };
 
   f32x16 acc[W][TF][TM];
@@ -219,44 +242,67 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[a][b][c][v] = 0.0f;
 
-  request();
-  put(0);
-  request();
+  begin_pass();
+#pragma unroll
+  for (int i = 0; i < NP; ++i) request(i);
+#pragma unroll
+  for (int i = 0; i < NP; ++i) put(i, 0);
+  advance();
+#pragma unroll
+  for (int i = 0; i < NP; ++i) request(i);
   __syncthreads();
-  const unsigned char* const w_at = lds + (wf * (BF / 2) + li) * L::kPitch + lh * 16;
-  const unsigned char* const x_at = lds + (W * BF + wm * (BM / 2) + li) * L::kPitch + lh * 16;
+  operands(0, 0, 0);
+  // One step: behind the products of 16 numbers of K the operands of the next 16 are read, and the pieces of the next step
+  // go to LDS, each followed by the request for the step after that.  All reads of a step are done before its last products,
+  // where the barrier stands: behind it the next step's first operands are read under these products.
   for (int s = 0; s < steps; ++s) {
-    const int stage = (s & 1) * L::kStage;
-    if (s + 1 < steps) {
-      put((s + 1) & 1);
-      if (s + 2 < steps) request();
-    }
+    const int stage = (s & 1) * L::kStage, other = L::kStage - stage;
+    advance();
 #pragma unroll
-    for (int kk = 0; kk < BK / 16; ++kk) {
-      bf16x8 x[X][TM];
+    for (int kk = 0; kk < NK; ++kk) {
+      const int cur = kk & 1;
+      const bool last = kk == NK - 1;
+      if (last) __syncthreads();
+      operands(cur ^ 1, last ? other : stage, last ? 0 : kk + 1);
+      const int p0 = last ? NP : NP * kk / (NK - 1), p1 = last ? NP : NP * (kk + 1) / (NK - 1);
 #pragma unroll
-      for (int j = 0; j < X; ++j)
-#pragma unroll
-        for (int c = 0; c < TM; ++c) x[j][c] = *(const bf16x8*)(x_at + stage + (j * BM + 32 * c) * L::kPitch + kk * 32);
+      for (int i = p0; i < p1; ++i) {
+        put(i, other);
+        request(i);
+      }
 #pragma unroll
       for (int a = 0; a < W; ++a)
 #pragma unroll
-        for (int b = 0; b < TF; ++b) {
-          const bf16x8 w = *(const bf16x8*)(w_at + stage + (a * BF + 32 * b) * L::kPitch + kk * 32);
+        for (int b = 0; b < TF; ++b)
 #pragma unroll
           for (int c = 0; c < TM; ++c)
-            acc[a][b][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x[FORM == kTriple && a == 2 ? 1 : 0][c], acc[a][b][c], 0, 0, 0);
+            acc[a][b][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fw[cur][a * TF + b], fx[cur][(FORM == kTriple && a == 2 ? TM : 0) + c],
+                                                                   acc[a][b][c], 0, 0, 0);
+      // the order of all that: spread evenly behind the products
+      const int extra = FR + (p1 - p0);
+#pragma unroll
+      for (int i = 0; i < MF; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+#pragma unroll
+        for (int e = extra * i / MF; e < extra * (i + 1) / MF; ++e) {
+          if (e < FR) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          } else {
+            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+          }
         }
+      }
     }
-    __syncthreads();
   }
+  __syncthreads();  // (the last step's needless reads are done: LDS is written again)
 
   // An accumulator has one column m = li per lane and, four at a time, neighbouring rows f = 8 q + 4 lh.  The wave's columns
   // go through LDS (its own part), 32 of x at a time, so that what is stored are whole pieces of neighbours.
   constexpr int FW = 32 * TF, EP = FW + 4;      // a wave's rows of w; row length there
   constexpr int LPR = FW / 8, NI = LPR / 2;     // lanes of a row m, rounds of 64 lanes over 32 rows
   float* const area = (float*)lds + wave * (W * 32 * EP);
-  const int fw = f0 + wf * FW;
+  const int fwave = f0 + wf * FW;
 #pragma unroll
   for (int c = 0; c < TM; ++c) {
     const int mw = m0 + wm * (BM / 2) + 32 * c;
@@ -272,7 +318,7 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
     wave_order();
 #pragma unroll 1
     for (int i = 0; i < NI; ++i) {
-      const int row = i * (64 / LPR) + lane / LPR, col = lane % LPR * 8, m = mw + row, f = fw + col;
+      const int row = i * (64 / LPR) + lane / LPR, col = lane % LPR * 8, m = mw + row, f = fwave + col;
       float* const at = area + row * EP + col;
       if constexpr (FORM == kOne) {
         if (m < g.M && f < g.F) store_out8(g, (int64_t)m * g.F + f, g.F - f, at);
@@ -311,7 +357,7 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
       wave_order();
 #pragma unroll 1
       for (int i = 0; i < FW / 16; ++i) {  // 16 rows f at a time, 4 lanes with 8 columns m each
-        const int row = 16 * i + lane / 4, col = lane % 4 * 8, f = fw + row, m = mw + col;
+        const int row = 16 * i + lane / 4, col = lane % 4 * 8, f = fwave + row, m = mw + col;
         if (f >= g.Fp || m >= g.Mp) continue;
 #pragma unroll
         for (int a = 0; a < 3; ++a) {
