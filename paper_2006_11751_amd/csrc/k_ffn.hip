@@ -46,21 +46,40 @@ __device__ inline unsigned pack_bf16(float a, float b) {
 }
 __device__ inline float from_bf16(unsigned h) { return __builtin_bit_cast(float, h << 16); }
 
-// act(g) and its slope.  `fine`: for fp32 results; else the native exponential (2^-20 of a result rounded to 2^-8).
-template <bool SLOPE>
-__device__ inline float activation(int act, float g, bool fine, float& slope) {
-  if (act == SF_ACT_GELU) {
+// act(g) and its slope.  FINE: for fp32 results; else the native exponential (2^-20 of a result rounded to 2^-8).
+template <int ACT, bool FINE, bool SLOPE>
+__device__ inline float activation(float g, float& slope) {
+  if constexpr (ACT == SF_ACT_GELU) {
     const float phi = 0.5f * erfcf(-g * 0.70710678f);  // (1 + erf has lost its digits in the lower tail)
     if (SLOPE) slope = phi + g * 0.39894228f * expf(-0.5f * g * g);
     return g * phi;
+  } else {
+    const float s = FINE ? 1.0f / (1.0f + expf(-g)) : __builtin_amdgcn_rcpf(1.0f + __expf(-g));
+    if constexpr (ACT == SF_ACT_SIGMOID) {
+      if (SLOPE) slope = s * (1.0f - s);
+      return s;
+    } else {
+      if (SLOPE) slope = s * (1.0f + g * (1.0f - s));
+      return g * s;
+    }
   }
-  const float s = fine ? 1.0f / (1.0f + expf(-g)) : __builtin_amdgcn_rcpf(1.0f + __expf(-g));
-  if (act == SF_ACT_SIGMOID) {
-    if (SLOPE) slope = s * (1.0f - s);
-    return s;
+}
+// f(activation's number, whether it is fine) with both known at compile time
+template <int N>
+struct Constant {
+  static constexpr int value = N;
+};
+template <class Fn>
+__device__ inline void with_activation(int act, bool fine, const Fn& f) {
+  if (fine) {
+    if (act == SF_ACT_SILU) f(Constant<SF_ACT_SILU>(), Constant<1>());
+    else if (act == SF_ACT_GELU) f(Constant<SF_ACT_GELU>(), Constant<1>());
+    else f(Constant<SF_ACT_SIGMOID>(), Constant<1>());
+  } else {
+    if (act == SF_ACT_SILU) f(Constant<SF_ACT_SILU>(), Constant<0>());
+    else if (act == SF_ACT_GELU) f(Constant<SF_ACT_GELU>(), Constant<0>());
+    else f(Constant<SF_ACT_SIGMOID>(), Constant<0>());
   }
-  if (SLOPE) slope = s * (1.0f + g * (1.0f - s));
-  return g * s;
 }
 
 struct Operand {
@@ -303,6 +322,8 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
   constexpr int LPR = FW / 8, NI = LPR / 2;     // lanes of a row m, rounds of 64 lanes over 32 rows
   float* const area = (float*)lds + wave * (W * 32 * EP);
   const int fwave = f0 + wf * FW;
+  const GemmArgs a_ = g;  // (kept in registers: behind wave_order it would be read again and again)
+  const bool fine = a_.terms == 3;
 #pragma unroll
   for (int c = 0; c < TM; ++c) {
     const int mw = m0 + wm * (BM / 2) + 32 * c;
@@ -316,56 +337,66 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
           *(f32x4*)(area + (a * 32 + li) * EP + 32 * b + 8 * q + 4 * lh) =
               f32x4{acc[a][b][c][4 * q], acc[a][b][c][4 * q + 1], acc[a][b][c][4 * q + 2], acc[a][b][c][4 * q + 3]};
     wave_order();
-#pragma unroll 1
-    for (int i = 0; i < NI; ++i) {
-      const int row = i * (64 / LPR) + lane / LPR, col = lane % LPR * 8, m = mw + row, f = fwave + col;
-      float* const at = area + row * EP + col;
-      if constexpr (FORM == kOne) {
-        if (m < g.M && f < g.F) store_out8(g, (int64_t)m * g.F + f, g.F - f, at);
-      } else {
-        float h[8], dg[8], du[8];
+    if constexpr (FORM == kOne) {
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          const float up = at[32 * EP + r];
-          float slope = 0.0f;
-          const float v = activation<FORM == kTriple>(g.act, at[r], g.terms == 3, slope);
-          const bool in = f + r < g.F && m < g.M;  // (zeros where a later product's K is padded)
-          h[r] = in ? v * up : 0.0f;
-          if constexpr (FORM == kTriple) {
-            const float dh = at[64 * EP + r];
-            dg[r] = in ? dh * up * slope : 0.0f;
-            du[r] = in ? dh * v : 0.0f;
-          }
-        }
-        if constexpr (FORM == kPair) {
-          if (m < g.M && f < g.Fp) store_terms8(g.h, g.terms, (int64_t)m * g.h.pitch + f, h);
-        } else {
-          if (m < g.M && f < g.Fp) {
-            store_terms8(g.dg, g.terms, (int64_t)m * g.dg.pitch + f, dg);
-            store_terms8(g.du, g.terms, (int64_t)m * g.du.pitch + f, du);
-          }
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {  // for the transposed ones
-            at[r] = h[r];
-            at[32 * EP + r] = dg[r];
-            at[64 * EP + r] = du[r];
-          }
-        }
+      for (int i = 0; i < NI; ++i) {
+        const int row = i * (64 / LPR) + lane / LPR, col = lane % LPR * 8, m = mw + row, f = fwave + col;
+        if (m < a_.M && f < a_.F) store_out8(a_, (int64_t)m * a_.F + f, a_.F - f, area + row * EP + col);
       }
+    } else {
+      with_activation(a_.act, fine, [&](auto act, auto exact) __attribute__((always_inline)) {
+#pragma unroll 2
+        for (int i = 0; i < NI; ++i) {
+          const int row = i * (64 / LPR) + lane / LPR, col = lane % LPR * 8, m = mw + row, f = fwave + col;
+          float* const at = area + row * EP + col;
+          float gate[8], up[8], h[8], dh[8], dg[8], du[8];
+#pragma unroll
+          for (int r = 0; r < 8; r += 4) {
+            *(f32x4*)(gate + r) = *(const f32x4*)(at + r);
+            *(f32x4*)(up + r) = *(const f32x4*)(at + 32 * EP + r);
+            if constexpr (FORM == kTriple) *(f32x4*)(dh + r) = *(const f32x4*)(at + 64 * EP + r);
+          }
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            float slope = 0.0f;
+            const float v = activation<decltype(act)::value, decltype(exact)::value, FORM == kTriple>(gate[r], slope);
+            const bool in = f + r < a_.F && m < a_.M;  // (zeros where a later product's K is padded)
+            h[r] = in ? v * up[r] : 0.0f;
+            if constexpr (FORM == kTriple) {
+              dg[r] = in ? dh[r] * up[r] * slope : 0.0f;
+              du[r] = in ? dh[r] * v : 0.0f;
+            }
+          }
+          if constexpr (FORM == kPair) {
+            if (m < a_.M && f < a_.Fp) store_terms8(a_.h, a_.terms, (int64_t)m * a_.h.pitch + f, h);
+          } else {
+            if (m < a_.M && f < a_.Fp) {
+              store_terms8(a_.dg, a_.terms, (int64_t)m * a_.dg.pitch + f, dg);
+              store_terms8(a_.du, a_.terms, (int64_t)m * a_.du.pitch + f, du);
+            }
+#pragma unroll
+            for (int r = 0; r < 8; r += 4) {  // for the transposed ones
+              *(f32x4*)(at + r) = *(f32x4*)(h + r);
+              *(f32x4*)(at + 32 * EP + r) = *(f32x4*)(dg + r);
+              *(f32x4*)(at + 64 * EP + r) = *(f32x4*)(du + r);
+            }
+          }
+        }
+      });
     }
     if constexpr (FORM == kTriple) {
       wave_order();
-#pragma unroll 1
+#pragma unroll 2
       for (int i = 0; i < FW / 16; ++i) {  // 16 rows f at a time, 4 lanes with 8 columns m each
         const int row = 16 * i + lane / 4, col = lane % 4 * 8, f = fwave + row, m = mw + col;
-        if (f >= g.Fp || m >= g.Mp) continue;
+        if (f >= a_.Fp || m >= a_.Mp) continue;
 #pragma unroll
         for (int a = 0; a < 3; ++a) {
           float v[8];
 #pragma unroll
           for (int r = 0; r < 8; ++r) v[r] = area[(a * 32 + col + r) * EP + row];
-          const Terms& t = a == 0 ? g.ht : a == 1 ? g.dgt : g.dut;
-          store_terms8(t, g.terms, (int64_t)f * t.pitch + m, v);
+          const Terms& t = a == 0 ? a_.ht : a == 1 ? a_.dgt : a_.dut;
+          store_terms8(t, a_.terms, (int64_t)f * t.pitch + m, v);
         }
       }
     }
@@ -521,14 +552,25 @@ __global__ __launch_bounds__(64 * kRowWaves) void ffn_rows_kernel(RowsArgs g) {
     }
     const int m = 16 * c + li, f = f0 + 4 * lg;
     if (m >= g.M) continue;
+    float y[4];
+    if constexpr (W == 2) {
+      with_activation(g.act, DTYPE == SF_DTYPE_FP32, [&](auto act, auto) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float slope;
+          y[r] = activation<decltype(act)::value, DTYPE == SF_DTYPE_FP32, false>(v[0][r], slope) * v[W - 1][r];
+        }
+      });
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = v[0][r];
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       if (f + r >= g.F) continue;
-      float slope;
-      const float y = W == 2 ? activation<false>(g.act, v[0][r], DTYPE == SF_DTYPE_FP32, slope) * v[W - 1][r] : v[0][r];
       const int64_t at = (int64_t)m * g.F + f + r;
-      if (DTYPE == SF_DTYPE_BF16) ((uint16_t*)g.out)[at] = (uint16_t)pack_bf16(y, 0.0f);
-      else ((float*)g.out)[at] = y;
+      if (DTYPE == SF_DTYPE_BF16) ((uint16_t*)g.out)[at] = (uint16_t)pack_bf16(y[r], 0.0f);
+      else ((float*)g.out)[at] = y[r];
     }
   }
 }
