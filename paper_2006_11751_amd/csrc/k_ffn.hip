@@ -1,8 +1,9 @@
 // The gated feed-forward block (include/sf_memory.h): h = act(x Wg^T) * (x Wu^T), y = h Wd^T, and its gradients.
 //
-// Every product is C[m][f] = sum_k X[m][k] W[f][k] with both operands dense in k (arrays that are not are laid out so
-// first, in the workspace: for the gradients the weights and, for those of the weights, the rows transposed).  One
-// kernel in three forms, all on the 16-bit matrix instruction 32x32x16 with fp32 accumulation:
+// Every product is C[m][f] = sum_k X[m][k] W[f][k].  An operand lies in memory with k along its rows or with k from row to
+// row (the gradients' products take the same arrays the other way round); the latter is transposed by the read that
+// takes it out of LDS.  Arrays that cannot be read in whole 16-byte pieces are laid out in the workspace first.  One kernel
+// in three forms, all on the 16-bit matrix instruction 32x32x16 with fp32 accumulation:
 //   kOne    C itself; two pairs of operands may follow one another in one sum (dx = dg Wg + du Wu)
 //   kPair   both projections of one x, activation and product behind them: h
 //   kTriple both projections computed again and dy Wd beside them: h, dg = dh u act'(g), du = dh act(g)
@@ -14,8 +15,10 @@
 // as passes over K (what is dropped is 2^-27 of the product); nothing else is rounded to 16 bits.
 //
 // Tile: four waves, each with up to 256 accumulators per lane, so that a 16-byte operand read feeds four products; K in
-// steps of BK through two buffers in LDS, the step after next under way in registers.  Rows in LDS are 16 bytes longer
-// than their numbers: 16 neighbouring rows then lie in different banks.
+// steps of BK through two buffers in LDS, the step after next under way in registers.  In LDS rows along k are 16 bytes
+// longer than their numbers (16 neighbours then lie in different banks), rows across k are 16 words mod 64 apart (the
+// transposing read takes 32 columns of four rows at once).  What lies past an array's end is read as zero by the
+// buffer's bounds check.  Where tiles are too few for the chip, K is cut and the parts' sums are added by a second launch.
 //
 // Few rows (serving): the weights are what is read, so each wave takes 16 rows of them straight into operands, the
 // waves of a workgroup share K, and their sums are added in LDS.
@@ -36,6 +39,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 enum Form { kOne = 0, kPair = 1, kTriple = 2 };
@@ -64,11 +68,19 @@ __device__ inline float activation(float g, float& slope) {
     }
   }
 }
-// f(activation's number, whether it is fine) with both known at compile time
 template <int N>
 struct Constant {
   static constexpr int value = N;
 };
+// f(A), f(A + 1), .. f(B - 1) with the number known at compile time
+template <int A, int B, class Fn>
+__device__ __attribute__((always_inline)) inline void each(const Fn& f) {
+  if constexpr (A < B) {
+    f(Constant<A>());
+    each<A + 1, B>(f);
+  }
+}
+// f(activation's number, whether it is fine) with both known at compile time
 template <class Fn>
 __device__ inline void with_activation(int act, bool fine, const Fn& f) {
   if (fine) {
@@ -83,8 +95,9 @@ __device__ inline void with_activation(int act, bool fine, const Fn& f) {
 }
 
 struct Operand {
-  const uint16_t* p;  // [planes][rows][pitch] bf16, k dense, zeros from the array's own K to the padded one
+  const uint16_t* p;  // [planes][rows][pitch] bf16
   int64_t pitch, plane;
+  int rows, cols;     // as it lies in memory
 };
 // Where numbers go that are operands of a later product: rows of `pitch`, one plane or three
 struct Terms {
@@ -93,21 +106,21 @@ struct Terms {
 };
 struct GemmArgs {
   Operand w[3], x[2];
-  int K;           // padded: a multiple of 64
+  int K;           // padded to 64 (operands along k: zeros there; across k: no rows there, read as zeros)
   int pairs;       // kOne: pairs of operands that follow one another
   int terms;       // planes of each operand: 1 or 3
-  int F, M;        // rows of w, of x
+  int F, M;        // of C
   int nf, nm;      // tiles
   int act;
   void* out;       // kOne: [M][F] (bf16 or, `out_f32`, fp32)
   int out_f32;
-  int Fp, Mp;      // F, M padded to 64
-  Terms h, dg, du;            // [M][Fp]: kPair h; kTriple dg, du
-  Terms ht, dgt, dut;         // kTriple: [F][Mp]
+  int splits;      // parts of K, out is then fp32 [splits][M][F]
+  int Fp;          // F padded to 64
+  Terms h, dg, du; // [M][Fp]: kPair h; kTriple all
 };
 struct GemmGroup {
   GemmArgs g[3];
-  int n, tiles[3];  // problems of one launch and their tiles
+  int n, tiles[3];  // problems of one launch and their workgroups
 };
 
 // the planes of a product of two operands in three terms, smallest first
@@ -142,40 +155,52 @@ __device__ inline void store_terms8(const Terms& t, int terms, int64_t at, const
   for (int i = 0; i < 3; ++i) *(u32x4*)(t.p + i * t.plane + at) = w[i];
 }
 // eight neighbours of a result's row (its first `left` ones)
-__device__ inline void store_out8(const GemmArgs& g, int64_t at, int left, const float* v) {
-  if ((g.F & 7) == 0) {  // (out is 16-byte aligned)
-    if (g.out_f32) {
-      *(f32x4*)((float*)g.out + at) = *(const f32x4*)v;
-      *(f32x4*)((float*)g.out + at + 4) = *(const f32x4*)(v + 4);
+__device__ inline void store_out8(void* out, int f32, int F, int64_t at, int left, const float* v) {
+  if ((F & 7) == 0) {  // (out is 16-byte aligned)
+    if (f32) {
+      *(f32x4*)((float*)out + at) = *(const f32x4*)v;
+      *(f32x4*)((float*)out + at + 4) = *(const f32x4*)(v + 4);
     } else {
-      *(u32x4*)((uint16_t*)g.out + at) = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+      *(u32x4*)((uint16_t*)out + at) = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     }
     return;
   }
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
     if (r >= left) break;
-    if (g.out_f32) ((float*)g.out)[at + r] = v[r];
-    else ((uint16_t*)g.out)[at + r] = (uint16_t)pack_bf16(v[r], 0.0f);
+    if (f32) ((float*)out)[at + r] = v[r];
+    else ((uint16_t*)out)[at + r] = (uint16_t)pack_bf16(v[r], 0.0f);
   }
 }
 
-// BF rows of each w, BM rows of each x per workgroup; a wave has half of both.
-template <int FORM, int BF, int BM, int BK>
+// LDS of B rows of an operand, BK numbers of K: along k (0) or across (1)
+constexpr int lds_pitch(int across, int B, int BK) { return !across ? BK * 2 + 16 : B == 64 ? 192 : B * 2 + 64; }
+constexpr int lds_bytes(int across, int B, int BK) { return lds_pitch(across, B, BK) * (across ? BK : B); }
+
+// BF rows of each w, BM rows of each x per workgroup; a wave has half of both.  ACROSS: bit a: w[a], bit 4: every x.
+template <int FORM, int ACROSS, int BF, int BM, int BK>
 struct Tile {
-  static constexpr int kW = FORM == kOne ? 1 : FORM == kPair ? 2 : 3, kX = FORM == kTriple ? 2 : 1;
-  static constexpr int kRows = kW * BF + kX * BM, kPitch = BK * 2 + 16, kStage = kRows * kPitch;
+  static constexpr int kW = FORM == kOne ? 1 : FORM == kPair ? 2 : 3, kX = FORM == kTriple ? 2 : 1, kN = kW + kX;
+  static constexpr int across(int n) { return n < kW ? ACROSS >> n & 1 : ACROSS >> 4 & 1; }
+  static constexpr int rows(int n) { return n < kW ? BF : BM; }
+  static constexpr int pitch(int n) { return lds_pitch(across(n), rows(n), BK); }
+  static constexpr int at(int n) { return n == 0 ? 0 : at(n - 1) + lds_bytes(across(n - 1), rows(n - 1), BK); }
+  static constexpr int kStage = at(kN);
   static constexpr int kEnd = 4 * kW * 32 * (BF / 2 + 4) * 4;  // behind the products: see there
   static constexpr int kBytes = 2 * kStage > kEnd ? 2 * kStage : kEnd;
-  static constexpr int kPieces = kRows * (BK / 8) / kThreads;  // 16-byte pieces of a step per thread
+  static constexpr int pieces(int n) { return rows(n) * BK / 8 / kThreads; }  // 16-byte pieces of a step per thread
+  static constexpr int first(int n) { return n == 0 ? 0 : first(n - 1) + pieces(n - 1); }
+  static constexpr int of(int i) {  // the array of piece i
+    int n = 0;
+    while (i >= first(n + 1)) ++n;
+    return n;
+  }
 };
 
-template <int FORM, int BF, int BM, int BK, int WAVES>
+template <int FORM, int ACROSS, int BF, int BM, int BK, int WAVES>
 __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup group) {
-  typedef Tile<FORM, BF, BM, BK> L;
-  constexpr int W = L::kW, X = L::kX, TF = BF / 64, TM = BM / 64;  // a wave's 32 x 32 tiles
-  constexpr int PR = BK / 8, RS = kThreads / PR;                   // pieces of a row; rows that all threads take at once
-  static_assert(BF % RS == 0 && BM % RS == 0, "a piece's array is known at compile time");
+  typedef Tile<FORM, ACROSS, BF, BM, BK> L;
+  constexpr int W = L::kW, X = L::kX, N = L::kN, TF = BF / 64, TM = BM / 64;  // a wave's 32 x 32 tiles
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 31, lh = lane >> 5;
@@ -190,36 +215,59 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
   int which = 0;
   while (which + 1 < group.n && tile >= group.tiles[which]) tile -= group.tiles[which++];
   const GemmArgs& g = group.g[which];
+  const int part = FORM == kOne ? tile / (g.nf * g.nm) : 0;
+  if (FORM == kOne) tile -= part * (g.nf * g.nm);
   const int band = tile / (4 * g.nf), in_band = tile - band * 4 * g.nf, height = min(4, g.nm - 4 * band);
   const int f0 = in_band / height * BF, m0 = (4 * band + in_band % height) * BM;
 
-  // this thread's pieces: row (tid / PR + RS * i) of the step's rows, piece tid % PR; bytes from the tile's first row on
-  constexpr int NP = L::kPieces, NK = BK / 16, MF = W * TF * TM, FR = W * TF + X * TM;  // products, operands of 16 numbers of K
-  unsigned row_at[NP];
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int first = RS * i;  // of the array's tile
-    const bool of_w = first < W * BF;
-    const int r = (of_w ? first % BF : (first - W * BF) % BM) + tid / PR;
-    const Operand& o = of_w ? g.w[first / BF] : g.x[(first - W * BF) / BM];
-    row_at[i] = (unsigned)min(r, (of_w ? g.F - 1 - f0 : g.M - 1 - m0)) * (unsigned)o.pitch * 2 + (tid % PR) * 16;  // (past the end: the last row, never stored)
-  }
+  // this thread's pieces of the arrays' tiles: row (of the tile, or of K) and 16 bytes of it
+  constexpr int NP = L::first(N), NK = BK / 16;
+  auto row_of = [&](auto i) __attribute__((always_inline)) {
+    constexpr int n = L::of(decltype(i)::value), per = L::across(n) ? L::rows(n) / 8 : BK / 8;
+    return tid / per + kThreads / per * (decltype(i)::value - L::first(n));
+  };
+  auto col_of = [&](auto i) __attribute__((always_inline)) {
+    constexpr int n = L::of(decltype(i)::value), per = L::across(n) ? L::rows(n) / 8 : BK / 8;
+    return tid % per * 16;
+  };
   // the step to be requested next: its pass (pair of operands, planes) and place in K
-  const int passes = (g.terms == 1 ? 1 : 6) * g.pairs, steps = g.K / BK * passes;
-  int pass = 0, k = 0;
-  const unsigned char *wb[W], *xb[X];
+  const int passes = (g.terms == 1 ? 1 : 6) * g.pairs, steps_k = g.K / BK, all = steps_k * passes;
+  const int s_begin = FORM == kOne ? (int)((int64_t)all * part / g.splits) : 0;
+  const int steps = (FORM == kOne ? (int)((int64_t)all * (part + 1) / g.splits) : all) - s_begin;
+  int pass = s_begin / steps_k, k = s_begin % steps_k * BK;
+  const unsigned char* base[N];
+  unsigned from[N], pitch[N];  // bytes to this thread's first piece of an array, between rows
   auto begin_pass = [&]() __attribute__((always_inline)) {
     const int pair = FORM == kOne && pass >= passes / g.pairs ? 1 : 0, term = g.terms == 1 ? 5 : pass - pair * 6;
-#pragma unroll
-    for (int a = 0; a < W; ++a) {
-      const Operand& o = g.w[FORM == kOne ? pair : a];
-      wb[a] = (const unsigned char*)(o.p + kPlaneW[term] * o.plane + (int64_t)f0 * o.pitch);
-    }
-#pragma unroll
-    for (int a = 0; a < X; ++a) {
-      const Operand& o = g.x[FORM == kOne ? pair : a];
-      xb[a] = (const unsigned char*)(o.p + kPlaneX[term] * o.plane + (int64_t)m0 * o.pitch);
-    }
+    each<0, N>([&](auto i) __attribute__((always_inline)) {
+      constexpr int n = decltype(i)::value;
+      const Operand& o = n < W ? g.w[FORM == kOne ? pair : n] : g.x[FORM == kOne ? pair : n - W];
+      const int64_t r0 = n < W ? f0 : m0;
+      pitch[n] = (unsigned)o.pitch * 2;
+      from[n] = row_of(Constant<L::first(n)>()) * pitch[n] + col_of(Constant<L::first(n)>());
+      base[n] = (const unsigned char*)(o.p + (n < W ? kPlaneW[term] : kPlaneX[term]) * o.plane + (L::across(n) ? r0 : r0 * o.pitch));
+    });
+  };
+  // (the bounds: bytes from the tile's (along k) or the step's (across k) first number to the array's end)
+  __amdgpu_buffer_rsrc_t source[N];
+  int rows[N], cols[N];  // of each array, from the tile on
+  each<0, N>([&](auto i) __attribute__((always_inline)) {
+    constexpr int n = decltype(i)::value;
+    const Operand& o = n < W ? g.w[n] : g.x[n - W];
+    rows[n] = o.rows;
+    cols[n] = o.cols - (n < W ? f0 : m0);
+  });
+  auto locate = [&]() __attribute__((always_inline)) {
+    each<0, N>([&](auto i) __attribute__((always_inline)) {
+      constexpr int n = decltype(i)::value;
+      if constexpr (L::across(n)) {
+        const int left = min(BK, rows[n] - k);  // (the last row ends with its numbers)
+        source[n] = __builtin_amdgcn_make_buffer_rsrc((void*)(base[n] + (int64_t)k * pitch[n]), 0,
+                                                      left > 0 ? (left - 1) * (int)pitch[n] + cols[n] * 2 : 0, 0x00027000);
+      } else {
+        source[n] = __builtin_amdgcn_make_buffer_rsrc((void*)base[n], 0, min(L::rows(n), rows[n] - (n < W ? f0 : m0)) * (int)pitch[n], 0x00027000);
+      }
+    });
   };
   auto advance = [&]() __attribute__((always_inline)) {  // (past the end: the last step again, for no use)
     k += BK;
@@ -232,24 +280,51 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
         k -= BK;
       }
     }
+    locate();
   };
   u32x4 next[NP];
-  auto request = [&](int i) __attribute__((always_inline)) {
-    const int first = RS * i;
-    const unsigned char* base = first < W * BF ? wb[first / BF] : xb[(first - W * BF) / BM];
-    next[i] = *(const u32x4*)(base + 2 * k + row_at[i]);
+  auto request = [&](auto i) __attribute__((always_inline)) {
+    constexpr int n = L::of(decltype(i)::value), per = L::across(n) ? L::rows(n) / 8 : BK / 8;
+    next[decltype(i)::value] = __builtin_amdgcn_raw_buffer_load_b128(
+        source[n], from[n] + (unsigned)(kThreads / per * (decltype(i)::value - L::first(n))) * pitch[n], L::across(n) ? 0 : 2 * k, 0);
   };
-  unsigned char* const put_at = lds + tid / PR * L::kPitch + (tid % PR) * 16;
-  auto put = [&](int i, int stage) __attribute__((always_inline)) { *(u32x4*)(put_at + stage + RS * i * L::kPitch) = next[i]; };
-  const unsigned char* const w_at = lds + (wf * (BF / 2) + li) * L::kPitch + lh * 16;
-  const unsigned char* const x_at = lds + (W * BF + wm * (BM / 2) + li) * L::kPitch + lh * 16;
-  bf16x8 fw[2][W * TF], fx[2][X * TM];
+  auto put = [&](auto i, int stage) __attribute__((always_inline)) {
+    constexpr int n = L::of(decltype(i)::value);
+    *(u32x4*)(lds + stage + L::at(n) + row_of(i) * L::pitch(n) + col_of(i)) = next[decltype(i)::value];
+  };
+  // Operands of 16 numbers of K: row li of a 32-row tile, k = 8 lh .. 8 lh + 7.  Across k two transposing reads of four k
+  // each: of 16 lanes, lane i names row i / 4 and four columns, and is given column i of the four rows.
+  bf16x8 fr[2][W * TF + X * TM];
+  auto operand = [&](auto array, int t, int stage, int kk) __attribute__((always_inline)) {
+    constexpr int n = decltype(array)::value;
+    const int half = n < W ? wf * (BF / 2) : wm * (BM / 2), r = half + 32 * t;
+    const unsigned char* at = lds + stage + L::at(n);
+    if constexpr (!L::across(n)) {
+      return *(const bf16x8*)(at + (r + li) * L::pitch(n) + lh * 16 + kk * 32);
+    } else {
+      const int grp = lane >> 4, i = lane & 15;
+      const unsigned char* p = at + (16 * kk + 8 * (grp >> 1) + (i >> 2)) * L::pitch(n) + (r + 16 * (grp & 1) + 4 * (i & 3)) * 2;
+      typedef __attribute__((address_space(3))) s16x4* Lds4;
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(p + 4 * L::pitch(n)));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  };
+  constexpr int FR = [] {  // LDS reads of them
+    int r = 0;
+    for (int n = 0; n < N; ++n) r += (n < W ? TF : TM) * (L::across(n) ? 2 : 1);
+    return r;
+  }();
   auto operands = [&](int to, int stage, int kk) __attribute__((always_inline)) {
+    each<0, X>([&](auto n) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < X * TM; ++i) fx[to][i] = *(const bf16x8*)(x_at + stage + (i / TM * BM + 32 * (i % TM)) * L::kPitch + kk * 32);
+      for (int t = 0; t < TM; ++t) fr[to][W * TF + decltype(n)::value * TM + t] = operand(Constant<W + decltype(n)::value>(), t, stage, kk);
+    });
+    each<0, W>([&](auto n) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < W * TF; ++i) fw[to][i] = *(const bf16x8*)(w_at + stage + (i / TF * BF + 32 * (i % TF)) * L::kPitch + kk * 32);
+      for (int t = 0; t < TF; ++t) fr[to][decltype(n)::value * TF + t] = operand(n, t, stage, kk);
+    });
   };
+  constexpr int MF = W * TF * TM;
 
   f32x16 acc[W][TF][TM];
 #pragma unroll
@@ -262,13 +337,11 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
         for (int v = 0; v < 16; ++v) acc[a][b][c][v] = 0.0f;
 
   begin_pass();
-#pragma unroll
-  for (int i = 0; i < NP; ++i) request(i);
-#pragma unroll
-  for (int i = 0; i < NP; ++i) put(i, 0);
+  locate();
+  each<0, NP>(request);
+  each<0, NP>([&](auto i) __attribute__((always_inline)) { put(i, 0); });
   advance();
-#pragma unroll
-  for (int i = 0; i < NP; ++i) request(i);
+  each<0, NP>(request);
   __syncthreads();
   operands(0, 0, 0);
   // One step: behind the products of 16 numbers of K the operands of the next 16 are read, and the pieces of the next step
@@ -277,28 +350,26 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
   for (int s = 0; s < steps; ++s) {
     const int stage = (s & 1) * L::kStage, other = L::kStage - stage;
     advance();
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      const int cur = kk & 1;
-      const bool last = kk == NK - 1;
-      if (last) __syncthreads();
+    each<0, NK>([&](auto step) __attribute__((always_inline)) {
+      constexpr int kk = decltype(step)::value, cur = kk & 1;
+      constexpr bool last = kk == NK - 1;
+      if constexpr (last) __syncthreads();
       operands(cur ^ 1, last ? other : stage, last ? 0 : kk + 1);
-      const int p0 = last ? NP : NP * kk / (NK - 1), p1 = last ? NP : NP * (kk + 1) / (NK - 1);
-#pragma unroll
-      for (int i = p0; i < p1; ++i) {
+      constexpr int p0 = last ? NP : NP * kk / (NK - 1), p1 = last ? NP : NP * (kk + 1) / (NK - 1);
+      each<p0, p1>([&](auto i) __attribute__((always_inline)) {
         put(i, other);
         request(i);
-      }
+      });
 #pragma unroll
       for (int a = 0; a < W; ++a)
 #pragma unroll
         for (int b = 0; b < TF; ++b)
 #pragma unroll
           for (int c = 0; c < TM; ++c)
-            acc[a][b][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fw[cur][a * TF + b], fx[cur][(FORM == kTriple && a == 2 ? TM : 0) + c],
-                                                                   acc[a][b][c], 0, 0, 0);
+            acc[a][b][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                fr[cur][a * TF + b], fr[cur][W * TF + (FORM == kTriple && a == 2 ? TM : 0) + c], acc[a][b][c], 0, 0, 0);
       // the order of all that: spread evenly behind the products
-      const int extra = FR + (p1 - p0);
+      constexpr int extra = FR + (p1 - p0);
 #pragma unroll
       for (int i = 0; i < MF; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -312,7 +383,7 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
           }
         }
       }
-    }
+    });
   }
   __syncthreads();  // (the last step's needless reads are done: LDS is written again)
 
@@ -323,7 +394,6 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
   float* const area = (float*)lds + wave * (W * 32 * EP);
   const int fwave = f0 + wf * FW;
   const GemmArgs a_ = g;  // (kept in registers: behind wave_order it would be read again and again)
-  const bool fine = a_.terms == 3;
 #pragma unroll
   for (int c = 0; c < TM; ++c) {
     const int mw = m0 + wm * (BM / 2) + 32 * c;
@@ -341,14 +411,16 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int row = i * (64 / LPR) + lane / LPR, col = lane % LPR * 8, m = mw + row, f = fwave + col;
-        if (m < a_.M && f < a_.F) store_out8(a_, (int64_t)m * a_.F + f, a_.F - f, area + row * EP + col);
+        if (m < a_.M && f < a_.F)
+          store_out8(a_.out, a_.out_f32, a_.F, ((int64_t)part * a_.M + m) * a_.F + f, a_.F - f, area + row * EP + col);
       }
     } else {
-      with_activation(a_.act, fine, [&](auto act, auto exact) __attribute__((always_inline)) {
+      // (rows of w past F and rows of x past M were read as zeros, so that h, dg and du are zeros where they are padded)
+      with_activation(a_.act, a_.terms == 3, [&](auto act, auto exact) __attribute__((always_inline)) {
 #pragma unroll 2
         for (int i = 0; i < NI; ++i) {
           const int row = i * (64 / LPR) + lane / LPR, col = lane % LPR * 8, m = mw + row, f = fwave + col;
-          float* const at = area + row * EP + col;
+          const float* const at = area + row * EP + col;
           float gate[8], up[8], h[8], dh[8], dg[8], du[8];
 #pragma unroll
           for (int r = 0; r < 8; r += 4) {
@@ -360,46 +432,42 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
           for (int r = 0; r < 8; ++r) {
             float slope = 0.0f;
             const float v = activation<decltype(act)::value, decltype(exact)::value, FORM == kTriple>(gate[r], slope);
-            const bool in = f + r < a_.F && m < a_.M;  // (zeros where a later product's K is padded)
-            h[r] = in ? v * up[r] : 0.0f;
+            h[r] = v * up[r];
             if constexpr (FORM == kTriple) {
-              dg[r] = in ? dh[r] * up[r] * slope : 0.0f;
-              du[r] = in ? dh[r] * v : 0.0f;
+              dg[r] = dh[r] * up[r] * slope;
+              du[r] = dh[r] * v;
             }
           }
-          if constexpr (FORM == kPair) {
-            if (m < a_.M && f < a_.Fp) store_terms8(a_.h, a_.terms, (int64_t)m * a_.h.pitch + f, h);
-          } else {
-            if (m < a_.M && f < a_.Fp) {
-              store_terms8(a_.dg, a_.terms, (int64_t)m * a_.dg.pitch + f, dg);
-              store_terms8(a_.du, a_.terms, (int64_t)m * a_.du.pitch + f, du);
-            }
-#pragma unroll
-            for (int r = 0; r < 8; r += 4) {  // for the transposed ones
-              *(f32x4*)(at + r) = *(f32x4*)(h + r);
-              *(f32x4*)(at + 32 * EP + r) = *(f32x4*)(dg + r);
-              *(f32x4*)(at + 64 * EP + r) = *(f32x4*)(du + r);
-            }
+          if (m >= a_.M || f >= a_.Fp) continue;
+          const int64_t to = (int64_t)m * a_.h.pitch + f;  // (all three have one shape)
+          store_terms8(a_.h, a_.terms, to, h);
+          if constexpr (FORM == kTriple) {
+            store_terms8(a_.dg, a_.terms, to, dg);
+            store_terms8(a_.du, a_.terms, to, du);
           }
         }
       });
     }
-    if constexpr (FORM == kTriple) {
-      wave_order();
-#pragma unroll 2
-      for (int i = 0; i < FW / 16; ++i) {  // 16 rows f at a time, 4 lanes with 8 columns m each
-        const int row = 16 * i + lane / 4, col = lane % 4 * 8, f = fwave + row, m = mw + col;
-        if (f >= a_.Fp || m >= a_.Mp) continue;
-#pragma unroll
-        for (int a = 0; a < 3; ++a) {
-          float v[8];
-#pragma unroll
-          for (int r = 0; r < 8; ++r) v[r] = area[(a * 32 + col + r) * EP + row];
-          const Terms& t = a == 0 ? a_.ht : a == 1 ? a_.dgt : a_.dut;
-          store_terms8(t, a_.terms, (int64_t)f * t.pitch + m, v);
-        }
-      }
-    }
+  }
+}
+
+// The sum of the parts of K.
+template <int DTYPE>
+__global__ __launch_bounds__(kThreads) void ffn_sum_kernel(const float* parts, int n, int64_t size, void* out) {
+  const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
+  if (i >= size) return;
+  if (i + 4 <= size && (size & 3) == 0) {
+    f32x4 v = *(const f32x4*)(parts + i);
+    for (int j = 1; j < n; ++j) v += *(const f32x4*)(parts + j * size + i);
+    if (DTYPE == SF_DTYPE_BF16) *(u32x2*)((uint16_t*)out + i) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    else *(f32x4*)((float*)out + i) = v;
+    return;
+  }
+  for (int r = 0; r < 4 && i + r < size; ++r) {
+    float v = parts[i + r];
+    for (int j = 1; j < n; ++j) v += parts[j * size + i + r];
+    if (DTYPE == SF_DTYPE_BF16) ((uint16_t*)out)[i + r] = (uint16_t)pack_bf16(v, 0.0f);
+    else ((float*)out)[i + r] = v;
   }
 }
 
@@ -408,10 +476,9 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
 struct Layout {
   const void* from;   // [rows][cols] of the calls' type, rows `pitch` elements apart
   int64_t pitch;
-  int rows, cols;
-  Terms to;           // [rows][pitch] or, transposed, [cols][pitch]; zeros up to the pitch
-  int transpose;
-  int tiles;          // 64 x 64 tiles
+  int rows, cols, vec;
+  Terms to;           // [rows][pitch], zeros up to the pitch
+  int64_t pieces;     // eight numbers each
 };
 struct LayoutGroup {
   Layout l[5];
@@ -420,42 +487,23 @@ struct LayoutGroup {
 
 template <int DTYPE>
 __global__ __launch_bounds__(kThreads) void ffn_layout_kernel(LayoutGroup group) {
-  __shared__ float s[64][65];
-  int tile = blockIdx.x, which = 0;
-  while (which + 1 < group.n && tile >= group.l[which].tiles) tile -= group.l[which++].tiles;
+  int64_t piece = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  int which = 0;
+  while (which < group.n && piece >= group.l[which].pieces) piece -= group.l[which++].pieces;
+  if (which == group.n) return;
   const Layout& l = group.l[which];
-  const int nc = (l.cols + 63) / 64, r0 = tile / nc * 64, c0 = tile % nc * 64;
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+  const int per = (int)(l.to.pitch / 8), c = (int)(piece % per) * 8;
+  const int64_t r = piece / per, at = r * l.pitch + c;
+  float v[8];
+  if (DTYPE == SF_DTYPE_FP32 && l.vec && c + 8 <= l.cols) {
+    *(f32x4*)v = *(const f32x4*)((const float*)l.from + at);
+    *(f32x4*)(v + 4) = *(const f32x4*)((const float*)l.from + at + 4);
+  } else {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int r = r0 + y + 4 * i, c = c0 + x;
-    float v = 0.0f;
-    if (r < l.rows && c < l.cols) {
-      const int64_t at = r * l.pitch + c;
-      v = DTYPE == SF_DTYPE_BF16 ? from_bf16(((const uint16_t*)l.from)[at]) : ((const float*)l.from)[at];
-    }
-    s[y + 4 * i][x] = v;
+    for (int i = 0; i < 8; ++i)
+      v[i] = c + i >= l.cols ? 0.0f : DTYPE == SF_DTYPE_BF16 ? from_bf16(((const uint16_t*)l.from)[at + i]) : ((const float*)l.from)[at + i];
   }
-  __syncthreads();
-  // pairs of neighbours of the result
-  const int n_out = l.transpose ? l.cols : l.rows, o0 = l.transpose ? c0 : r0, k0 = l.transpose ? r0 : c0;
-  const int k = (threadIdx.x & 31) * 2, o1 = threadIdx.x >> 5;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int o = o1 + 8 * i;
-    if (o0 + o >= n_out) continue;
-    const float a = l.transpose ? s[k][o] : s[o][k], b = l.transpose ? s[k + 1][o] : s[o][k + 1];
-    unsigned* to = (unsigned*)(l.to.p + (o0 + o) * l.to.pitch + k0 + k);
-    if (DTYPE == SF_DTYPE_BF16) {
-      *to = pack_bf16(a, b);
-    } else {
-      unsigned t[3];
-      float left = 0.0f;
-      split_pair(a, b, t[0], t[1], t[2], left);
-#pragma unroll
-      for (int j = 0; j < 3; ++j) to[j * l.to.plane / 2] = t[j];
-    }
-  }
+  store_terms8(l.to, DTYPE == SF_DTYPE_BF16 ? 1 : 3, r * l.to.pitch + c, v);
 }
 
 // ---- few rows ----------------------------------------------------------------------------------
@@ -611,45 +659,50 @@ int64_t pad64(int64_t n) { return (n + 63) / 64 * 64; }
 struct Arena {
   unsigned char* base;
   size_t at;
+  void* bytes(size_t n) {
+    void* p = base ? base + at : nullptr;
+    at += (n + 255) / 256 * 256;
+    return p;
+  }
   Terms take(int64_t rows, int64_t pitch, int terms) {
-    Terms t = {base ? (uint16_t*)(base + at) : nullptr, pitch, rows * pitch};
-    at += ((size_t)(rows * pitch * terms) * 2 + 255) / 256 * 256;
-    return t;
+    return Terms{(uint16_t*)bytes((size_t)(rows * pitch * terms) * 2), pitch, rows * pitch};
   }
 };
-Operand operand(const Terms& t) { return Operand{t.p, t.pitch, t.plane}; }
+Operand operand(const Terms& t, int rows) { return Operand{t.p, t.pitch, t.plane, rows, (int)t.pitch}; }
 
 struct Job {
   const sf_ffn_config* c;
   hipStream_t st;
   LayoutGroup lay = {};
-  int lay_tiles = 0;
+  int64_t lay_pieces = 0;
   int terms() const { return c->dtype == SF_DTYPE_BF16 ? 1 : 3; }
-  // An array as an operand, dense in its columns: itself where it can be read as it is, else laid out in the workspace.
-  Operand rows(Arena& a, const void* p, int64_t pitch, int rows, int cols) {
-    if (terms() == 1 && cols % 64 == 0 && pitch % 8 == 0 && pitch > 0 && pitch <= 1 << 22 && (reinterpret_cast<uintptr_t>(p) & 15) == 0)
-      return Operand{(const uint16_t*)p, pitch, 0};
-    return lay_out(a, p, pitch, rows, cols, 0);
-  }
-  Operand lay_out(Arena& a, const void* p, int64_t pitch, int rows, int cols, int transpose) {
-    const Terms t = a.take(transpose ? cols : rows, pad64(transpose ? rows : cols), terms());
-    lay.l[lay.n] = Layout{p, pitch, rows, cols, t, transpose, (int)(pad64(rows) / 64 * (pad64(cols) / 64))};
-    lay_tiles += lay.l[lay.n++].tiles;
-    return operand(t);
+  // An array as an operand: itself where it can be read in whole pieces (`along`: and is one along its rows, which then have
+  // to be whole steps of K), else laid out in the workspace.
+  Operand array(Arena& a, const void* p, int64_t pitch, int rows, int cols, bool along) {
+    if (terms() == 1 && cols % (along ? 64 : 8) == 0 && pitch % 8 == 0 && pitch >= cols && pitch < 1 << 22 &&
+        (reinterpret_cast<uintptr_t>(p) & 15) == 0)
+      return Operand{(const uint16_t*)p, pitch, 0, rows, cols};
+    const Terms t = a.take(rows, pad64(cols), terms());
+    Layout& l = lay.l[lay.n++];
+    l = Layout{p, pitch, rows, cols, pitch % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0, t, rows * t.pitch / 8};
+    lay_pieces += l.pieces;
+    return operand(t, rows);
   }
   hipError_t run_layout() {
     if (!lay.n) return hipSuccess;
-    if (c->dtype == SF_DTYPE_BF16) ffn_layout_kernel<SF_DTYPE_BF16><<<lay_tiles, kThreads, 0, st>>>(lay);
-    else ffn_layout_kernel<SF_DTYPE_FP32><<<lay_tiles, kThreads, 0, st>>>(lay);
-    lay.n = lay_tiles = 0;
+    const unsigned grid = (unsigned)((lay_pieces + kThreads - 1) / kThreads);
+    if (c->dtype == SF_DTYPE_BF16) ffn_layout_kernel<SF_DTYPE_BF16><<<grid, kThreads, 0, st>>>(lay);
+    else ffn_layout_kernel<SF_DTYPE_FP32><<<grid, kThreads, 0, st>>>(lay);
+    lay.n = 0;
+    lay_pieces = 0;
     return hipGetLastError();
   }
 };
 
-template <int FORM, int BF, int BM, int BK, int WAVES>
+template <int FORM, int ACROSS, int BF, int BM, int BK, int WAVES>
 hipError_t launch_t(GemmGroup& group, hipStream_t st) {
-  const auto kern = ffn_gemm_kernel<FORM, BF, BM, BK, WAVES>;
-  constexpr int bytes = Tile<FORM, BF, BM, BK>::kBytes;
+  const auto kern = ffn_gemm_kernel<FORM, ACROSS, BF, BM, BK, WAVES>;
+  constexpr int bytes = Tile<FORM, ACROSS, BF, BM, BK>::kBytes;
   static const hipError_t attr = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (attr != hipSuccess) return attr;
   int total = 0;
@@ -657,25 +710,70 @@ hipError_t launch_t(GemmGroup& group, hipStream_t st) {
     GemmArgs& g = group.g[i];
     // (padded columns of the next product's operand are this one's rows of w)
     g.nf = ((FORM == kOne ? g.F : g.Fp) + BF - 1) / BF;
-    g.nm = ((FORM == kTriple ? g.Mp : g.M) + BM - 1) / BM;
-    total += group.tiles[i] = g.nf * g.nm;
+    g.nm = (g.M + BM - 1) / BM;
+    total += group.tiles[i] = g.nf * g.nm * (FORM == kOne ? g.splits : 1);
   }
   kern<<<(total + 7) / 8 * 8, kThreads, bytes, st>>>(group);
   return hipGetLastError();
 }
-// The large tile where it leaves no CU without one, the small one otherwise.
+int64_t tiles_of(int F, int M, int BF, int BM) { return (int64_t)((F + BF - 1) / BF) * ((M + BM - 1) / BM); }
+// The large tile where it leaves few CUs without one, the small one otherwise.
+constexpr int kEnough = 192;
 template <int FORM>
 hipError_t launch(GemmGroup& group, hipStream_t st) {
-  int64_t large = 0;
-  for (int i = 0; i < group.n; ++i) {
-    const GemmArgs& g = group.g[i];
-    if (FORM == kOne) large += (int64_t)((g.F + 255) / 256) * ((g.M + 255) / 256);
-    else large += (int64_t)((g.Fp + 127) / 128) * ((g.M + (FORM == kPair ? 255 : 127)) / (FORM == kPair ? 256 : 128));
-  }
-  if constexpr (FORM == kOne) return large >= 192 ? launch_t<kOne, 256, 256, 64, 1>(group, st) : launch_t<kOne, 128, 128, 64, 2>(group, st);
-  else if constexpr (FORM == kPair) return large >= 192 ? launch_t<kPair, 128, 256, 64, 1>(group, st) : launch_t<kPair, 64, 128, 64, 2>(group, st);
-  else return large >= 192 ? launch_t<kTriple, 128, 128, 32, 1>(group, st) : launch_t<kTriple, 64, 128, 32, 2>(group, st);
+  const GemmArgs& g = group.g[0];
+  if constexpr (FORM == kPair)
+    return tiles_of(g.Fp, g.M, 128, 256) >= kEnough ? launch_t<kPair, 0, 128, 256, 64, 1>(group, st) : launch_t<kPair, 0, 64, 128, 64, 2>(group, st);
+  else
+    return tiles_of(g.Fp, g.M, 128, 128) >= kEnough ? launch_t<kTriple, 4, 128, 128, 32, 1>(group, st) : launch_t<kTriple, 4, 64, 128, 32, 2>(group, st);
 }
+
+// Products of form kOne that do not depend on one another, as one launch, and where K is cut a second one.
+struct Products {
+  GemmGroup group = {};
+  bool large = false;
+  int splits = 1;
+  // Parts of K: about 1.5 workgroups of small tiles per CU, each part 16 steps of 64 or more.
+  void plan() {
+    int64_t big = 0, small = 0;
+    int steps = 1 << 30;
+    for (int i = 0; i < group.n; ++i) {
+      const GemmArgs& g = group.g[i];
+      big += tiles_of(g.F, g.M, 256, 256);
+      small += tiles_of(g.F, g.M, 128, 128);
+      const int s = g.K / 64 * (g.terms == 1 ? 1 : 6) * g.pairs;
+      if (s < steps) steps = s;
+    }
+    large = big >= kEnough;
+    splits = large || small == 0 ? 1 : (int)(384 / small);
+    if (splits > steps / 16) splits = steps / 16;
+    if (splits > 8) splits = 8;
+    if (splits < 1) splits = 1;
+  }
+  size_t part_bytes(int i) const { return splits > 1 ? (size_t)splits * group.g[i].M * group.g[i].F * 4 : 0; }
+  template <int ACROSS>
+  hipError_t run(Arena& a, int dtype, hipStream_t st) {
+    void* out[3];
+    for (int i = 0; i < group.n; ++i) {
+      GemmArgs& g = group.g[i];
+      g.splits = splits;
+      out[i] = g.out;
+      if (splits > 1) {
+        g.out = a.bytes(part_bytes(i));
+        g.out_f32 = 1;
+      }
+    }
+    hipError_t e = large ? launch_t<kOne, ACROSS, 256, 256, 64, 1>(group, st) : launch_t<kOne, ACROSS, 128, 128, 64, 2>(group, st);
+    for (int i = 0; i < group.n && splits > 1 && e == hipSuccess; ++i) {
+      const int64_t size = (int64_t)group.g[i].M * group.g[i].F;
+      const unsigned grid = (unsigned)((size + 4 * kThreads - 1) / (4 * kThreads));
+      if (dtype == SF_DTYPE_BF16) ffn_sum_kernel<SF_DTYPE_BF16><<<grid, kThreads, 0, st>>>((const float*)group.g[i].out, splits, size, out[i]);
+      else ffn_sum_kernel<SF_DTYPE_FP32><<<grid, kThreads, 0, st>>>((const float*)group.g[i].out, splits, size, out[i]);
+      e = hipGetLastError();
+    }
+    return e;
+  }
+};
 
 template <int DTYPE, int W, bool VEC>
 hipError_t launch_rows(const RowsArgs& g, hipStream_t st) {
@@ -695,55 +793,78 @@ GemmArgs gemm(const sf_ffn_config* c, int terms, int K, int F, int M) {
   GemmArgs g = {};
   g.K = (int)pad64(K);
   g.pairs = 1;
+  g.splits = 1;
   g.terms = terms;
   g.F = F;
   g.M = M;
   g.Fp = (int)pad64(F);
-  g.Mp = (int)pad64(M);
   g.act = c->act;
   g.out_f32 = c->dtype == SF_DTYPE_FP32;
   return g;
 }
 
-struct ForwardPlan {
-  Operand x, wg, wu, wd;
-  Terms h;
+// What a call consists of, for the call itself and for the size of its workspace.
+struct Forward {
+  GemmGroup up = {};
+  Products down;
+  Forward(Job& j, Arena& a, const void* x, const void* wg, const void* wu, const void* wd, void* y) {
+    const sf_ffn_config* c = j.c;
+    up.n = 1;
+    GemmArgs& u = up.g[0] = gemm(c, j.terms(), c->D, c->F, c->M);
+    u.x[0] = j.array(a, x, c->x_stride, c->M, c->D, true);
+    u.w[0] = j.array(a, wg, c->w_gate_stride, c->F, c->D, true);
+    u.w[1] = j.array(a, wu, c->w_up_stride, c->F, c->D, true);
+    u.h = a.take(c->M, u.Fp, j.terms());
+    down.group.n = 1;
+    GemmArgs& d = down.group.g[0] = gemm(c, j.terms(), c->F, c->D, c->M);
+    d.w[0] = j.array(a, wd, c->w_down_stride, c->D, c->F, true);
+    d.x[0] = operand(u.h, c->M);
+    d.out = y;
+    down.plan();
+  }
 };
-ForwardPlan plan_forward(Job& j, Arena& a, const void* x, const void* wg, const void* wu, const void* wd) {
-  const sf_ffn_config* c = j.c;
-  ForwardPlan p;
-  p.x = j.rows(a, x, c->x_stride, c->M, c->D);
-  p.wg = j.rows(a, wg, c->w_gate_stride, c->F, c->D);
-  p.wu = j.rows(a, wu, c->w_up_stride, c->F, c->D);
-  p.wd = j.rows(a, wd, c->w_down_stride, c->D, c->F);
-  p.h = a.take(c->M, pad64(c->F), j.terms());
-  return p;
-}
-struct BackwardPlan {
-  Operand x, wg, wu, dy, wd_t, wg_t, wu_t, x_t, dy_t;
-  Terms dg, du, ht, dgt, dut;
+struct Backward {
+  GemmGroup mid = {};
+  Products in, weights;
+  Backward(Job& j, Arena& a, const void* x, const void* wg, const void* wu, const void* wd, const void* dy, void* dx, void* dwg, void* dwu,
+           void* dwd) {
+    const sf_ffn_config* c = j.c;
+    const int terms = j.terms();
+    mid.n = 1;
+    GemmArgs& t = mid.g[0] = gemm(c, terms, c->D, c->F, c->M);
+    t.x[0] = j.array(a, x, c->x_stride, c->M, c->D, true);
+    t.x[1] = j.array(a, dy, c->dy_stride, c->M, c->D, true);
+    t.w[0] = j.array(a, wg, c->w_gate_stride, c->F, c->D, true);
+    t.w[1] = j.array(a, wu, c->w_up_stride, c->F, c->D, true);
+    t.w[2] = j.array(a, wd, c->w_down_stride, c->D, c->F, false);
+    t.h = a.take(c->M, t.Fp, terms);
+    t.dg = a.take(c->M, t.Fp, terms);
+    t.du = a.take(c->M, t.Fp, terms);
+    const Operand h = operand(t.h, c->M), dg = operand(t.dg, c->M), du = operand(t.du, c->M);
+    in.group.n = 1;
+    GemmArgs& i = in.group.g[0] = gemm(c, terms, c->F, c->D, c->M);
+    i.pairs = 2;
+    i.w[0] = t.w[0];
+    i.w[1] = t.w[1];
+    i.x[0] = dg;
+    i.x[1] = du;
+    i.out = dx;
+    in.plan();
+    weights.group.n = 3;
+    GemmArgs* w = weights.group.g;
+    w[0] = w[1] = gemm(c, terms, c->M, c->D, c->F);
+    w[2] = gemm(c, terms, c->M, c->F, c->D);
+    w[0].w[0] = w[1].w[0] = t.x[0];
+    w[0].x[0] = dg;
+    w[1].x[0] = du;
+    w[2].w[0] = h;
+    w[2].x[0] = t.x[1];
+    w[0].out = dwg;
+    w[1].out = dwu;
+    w[2].out = dwd;
+    weights.plan();
+  }
 };
-// (the layouts are run in two launches: five fit one)
-BackwardPlan plan_backward(Job& j, Job& j2, Arena& a, const void* x, const void* wg, const void* wu, const void* wd, const void* dy) {
-  const sf_ffn_config* c = j.c;
-  BackwardPlan p;
-  p.x = j.rows(a, x, c->x_stride, c->M, c->D);
-  p.wg = j.rows(a, wg, c->w_gate_stride, c->F, c->D);
-  p.wu = j.rows(a, wu, c->w_up_stride, c->F, c->D);
-  p.dy = j.rows(a, dy, c->dy_stride, c->M, c->D);
-  p.wd_t = j.lay_out(a, wd, c->w_down_stride, c->D, c->F, 1);
-  p.wg_t = j2.lay_out(a, wg, c->w_gate_stride, c->F, c->D, 1);
-  p.wu_t = j2.lay_out(a, wu, c->w_up_stride, c->F, c->D, 1);
-  p.x_t = j2.lay_out(a, x, c->x_stride, c->M, c->D, 1);
-  p.dy_t = j2.lay_out(a, dy, c->dy_stride, c->M, c->D, 1);
-  const int64_t Fp = pad64(c->F), Mp = pad64(c->M);
-  p.dg = a.take(c->M, Fp, j.terms());
-  p.du = a.take(c->M, Fp, j.terms());
-  p.ht = a.take(Fp, Mp, j.terms());
-  p.dgt = a.take(Fp, Mp, j.terms());
-  p.dut = a.take(Fp, Mp, j.terms());
-  return p;
-}
 
 int device_error(const char* fn, hipError_t e) {
   set_error("%s: launch failed: %s", fn, hipGetErrorString(e));
@@ -760,11 +881,17 @@ using namespace sf;
 extern "C" int64_t sf_ffn_workspace_bytes(const sf_ffn_config* cfg, int backward) {
   if (check(cfg, "sf_ffn_workspace_bytes") != SF_OK) return -1;
   if (!backward && cfg->M <= kFewRows) return (int64_t)pad64((int64_t)cfg->M * cfg->F) * 4;
-  Job j{cfg, nullptr}, j2{cfg, nullptr};
+  Job j{cfg, nullptr};
   Arena a = {nullptr, 0};
-  const void* const odd = (const void*)2;
-  if (backward) plan_backward(j, j2, a, odd, odd, odd, odd, odd);
-  else plan_forward(j, a, odd, odd, odd, odd);
+  void* const odd = (void*)2;
+  if (backward) {
+    const Backward p(j, a, odd, odd, odd, odd, odd, odd, odd, odd, odd);
+    a.bytes(p.in.part_bytes(0));
+    for (int i = 0; i < 3; ++i) a.bytes(p.weights.part_bytes(i));
+  } else {
+    const Forward p(j, a, odd, odd, odd, odd, odd);
+    a.bytes(p.down.part_bytes(0));
+  }
   return (int64_t)a.at;
 }
 
@@ -814,24 +941,11 @@ extern "C" int sf_ffn(const sf_ffn_config* cfg, const void* x, const void* w_gat
     return err == hipSuccess ? SF_OK : device_error(fn, err);
   }
   Arena a = {(unsigned char*)workspace, 0};
-  const ForwardPlan p = plan_forward(j, a, x, w_gate, w_up, w_down);
-  if ((err = j.run_layout()) != hipSuccess) return device_error(fn, err);
-  GemmGroup up = {};
-  up.n = 1;
-  up.g[0] = gemm(cfg, j.terms(), cfg->D, cfg->F, cfg->M);
-  up.g[0].w[0] = p.wg;
-  up.g[0].w[1] = p.wu;
-  up.g[0].x[0] = p.x;
-  up.g[0].h = p.h;
-  if ((err = launch<kPair>(up, j.st)) != hipSuccess) return device_error(fn, err);
-  GemmGroup down = {};
-  down.n = 1;
-  down.g[0] = gemm(cfg, j.terms(), cfg->F, cfg->D, cfg->M);
-  down.g[0].w[0] = p.wd;
-  down.g[0].x[0] = operand(p.h);
-  down.g[0].out = y;
-  err = launch<kOne>(down, j.st);
-  return err == hipSuccess ? SF_OK : device_error(fn, err);
+  Forward p(j, a, x, w_gate, w_up, w_down, y);
+  if ((err = j.run_layout()) != hipSuccess || (err = launch<kPair>(p.up, j.st)) != hipSuccess ||
+      (err = p.down.run<0>(a, cfg->dtype, j.st)) != hipSuccess)
+    return device_error(fn, err);
+  return SF_OK;
 }
 
 extern "C" int sf_ffn_backward(const sf_ffn_config* cfg, const void* x, const void* w_gate, const void* w_up, const void* w_down,
@@ -854,47 +968,12 @@ extern "C" int sf_ffn_backward(const sf_ffn_config* cfg, const void* x, const vo
     err = hipGetLastError();
     return err == hipSuccess ? SF_OK : device_error(fn, err);
   }
-  Job j{cfg, st}, j2{cfg, st};
+  Job j{cfg, st};
   Arena a = {(unsigned char*)workspace, 0};
-  const BackwardPlan p = plan_backward(j, j2, a, x, w_gate, w_up, w_down, dy);
-  if ((err = j.run_layout()) != hipSuccess || (err = j2.run_layout()) != hipSuccess) return device_error(fn, err);
-  const int terms = j.terms();
-  GemmGroup mid = {};
-  mid.n = 1;
-  GemmArgs& t = mid.g[0];
-  t = gemm(cfg, terms, cfg->D, cfg->F, cfg->M);
-  t.w[0] = p.wg;
-  t.w[1] = p.wu;
-  t.w[2] = p.wd_t;
-  t.x[0] = p.x;
-  t.x[1] = p.dy;
-  t.dg = p.dg;
-  t.du = p.du;
-  t.ht = p.ht;
-  t.dgt = p.dgt;
-  t.dut = p.dut;
-  if ((err = launch<kTriple>(mid, st)) != hipSuccess) return device_error(fn, err);
-  GemmGroup in = {};
-  in.n = 1;
-  in.g[0] = gemm(cfg, terms, cfg->F, cfg->D, cfg->M);
-  in.g[0].pairs = 2;
-  in.g[0].w[0] = p.wg_t;
-  in.g[0].w[1] = p.wu_t;
-  in.g[0].x[0] = operand(p.dg);
-  in.g[0].x[1] = operand(p.du);
-  in.g[0].out = dx;
-  if ((err = launch<kOne>(in, st)) != hipSuccess) return device_error(fn, err);
-  GemmGroup w = {};
-  w.n = 3;
-  for (int i = 0; i < 3; ++i) w.g[i] = i < 2 ? gemm(cfg, terms, cfg->M, cfg->D, cfg->F) : gemm(cfg, terms, cfg->M, cfg->F, cfg->D);
-  w.g[0].w[0] = w.g[1].w[0] = p.x_t;
-  w.g[0].x[0] = operand(p.dgt);
-  w.g[1].x[0] = operand(p.dut);
-  w.g[2].w[0] = operand(p.ht);
-  w.g[2].x[0] = p.dy_t;
-  w.g[0].out = dw_gate;
-  w.g[1].out = dw_up;
-  w.g[2].out = dw_down;
-  err = launch<kOne>(w, st);
-  return err == hipSuccess ? SF_OK : device_error(fn, err);
+  Backward p(j, a, x, w_gate, w_up, w_down, dy, dx, dw_gate, dw_up, dw_down);
+  // (dx: w across k; the weights' gradients: both operands)
+  if ((err = j.run_layout()) != hipSuccess || (err = launch<kTriple>(p.mid, st)) != hipSuccess ||
+      (err = p.in.run<1>(a, cfg->dtype, st)) != hipSuccess || (err = p.weights.run<17>(a, cfg->dtype, st)) != hipSuccess)
+    return device_error(fn, err);
+  return SF_OK;
 }
