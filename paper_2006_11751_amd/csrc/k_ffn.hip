@@ -733,7 +733,7 @@ struct Products {
   GemmGroup group = {};
   bool large = false;
   int splits = 1;
-  // Parts of K: about 1.5 workgroups of small tiles per CU, each part 16 steps of 64 or more.
+  // Parts of K: about three workgroups of small tiles per CU, each part 16 steps of 64 or more.
   void plan() {
     int64_t big = 0, small = 0;
     int steps = 1 << 30;
@@ -745,7 +745,7 @@ struct Products {
       if (s < steps) steps = s;
     }
     large = big >= kEnough;
-    splits = large || small == 0 ? 1 : (int)(384 / small);
+    splits = large || small == 0 ? 1 : (int)(768 / small);
     if (splits > steps / 16) splits = steps / 16;
     if (splits > 8) splits = 8;
     if (splits < 1) splits = 1;
