@@ -38,7 +38,7 @@ extern "C" {
  *   done       dev [T][N] bytes or NULL (no episode begins)
  *   state0     dev [N][H][dk][dv] fp32 or NULL (zero); state, dstate, dstate0 alike (NULL: not wanted / zero)
  * Errors: SF_ERR_ARG (null or misaligned pointer, struct_size, dtype), SF_ERR_SHAPE (T, N < 0; H, Hk < 1;
- * H % Hk != 0; dk or dv outside 1..128; T * N or N * H beyond 2^31 - 1; scale not finite), SF_ERR_DEVICE. */
+ * H % Hk != 0; dk or dv outside 1..128; T * N beyond 2^31 - 1, N * H beyond 2^22; scale not finite), SF_ERR_DEVICE. */
 typedef struct {
   uint32_t struct_size; /* sizeof(sf_linattn_config) */
   int32_t dtype;        /* SF_DTYPE_* of q, k, v, o and their gradients */

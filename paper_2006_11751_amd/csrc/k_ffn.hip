@@ -24,6 +24,8 @@
 // waves of a workgroup share K, and their sums are added in LDS.
 #include <math.h>
 
+#include <algorithm>
+
 #include "sf_internal.h"
 #include "sf_memory.h"
 #include "sf_split.h"
@@ -454,9 +456,9 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
 // The sum of the parts of K.
 template <int DTYPE>
 __global__ __launch_bounds__(kThreads) void ffn_sum_kernel(const float* parts, int n, int64_t size, void* out) {
-  const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
+  const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;  // (few tiles: size is below 384 x 128 x 128)
   if (i >= size) return;
-  if (i + 4 <= size && (size & 3) == 0) {
+  if ((size & 3) == 0) {
     f32x4 v = *(const f32x4*)(parts + i);
     for (int j = 1; j < n; ++j) v += *(const f32x4*)(parts + j * size + i);
     if (DTYPE == SF_DTYPE_BF16) *(u32x2*)((uint16_t*)out + i) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
@@ -486,12 +488,7 @@ struct LayoutGroup {
 };
 
 template <int DTYPE>
-__global__ __launch_bounds__(kThreads) void ffn_layout_kernel(LayoutGroup group) {
-  int64_t piece = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  int which = 0;
-  while (which < group.n && piece >= group.l[which].pieces) piece -= group.l[which++].pieces;
-  if (which == group.n) return;
-  const Layout& l = group.l[which];
+__device__ inline void lay_piece(const Layout& l, int64_t piece) {
   const int per = (int)(l.to.pitch / 8), c = (int)(piece % per) * 8;
   const int64_t r = piece / per, at = r * l.pitch + c;
   float v[8];
@@ -504,6 +501,17 @@ __global__ __launch_bounds__(kThreads) void ffn_layout_kernel(LayoutGroup group)
       v[i] = c + i >= l.cols ? 0.0f : DTYPE == SF_DTYPE_BF16 ? from_bf16(((const uint16_t*)l.from)[at + i]) : ((const float*)l.from)[at + i];
   }
   store_terms8(l.to, DTYPE == SF_DTYPE_BF16 ? 1 : 3, r * l.to.pitch + c, v);
+}
+
+template <int DTYPE>
+__global__ __launch_bounds__(kThreads) void ffn_layout_kernel(LayoutGroup group) {
+  for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;; at += (int64_t)gridDim.x * kThreads) {
+    int64_t piece = at;
+    int which = 0;
+    while (which < group.n && piece >= group.l[which].pieces) piece -= group.l[which++].pieces;
+    if (which == group.n) return;
+    lay_piece<DTYPE>(group.l[which], piece);
+  }
 }
 
 // ---- few rows ----------------------------------------------------------------------------------
@@ -690,7 +698,7 @@ struct Job {
   }
   hipError_t run_layout() {
     if (!lay.n) return hipSuccess;
-    const unsigned grid = (unsigned)((lay_pieces + kThreads - 1) / kThreads);
+    const unsigned grid = (unsigned)std::min<int64_t>((lay_pieces + kThreads - 1) / kThreads, 1 << 20);
     if (c->dtype == SF_DTYPE_BF16) ffn_layout_kernel<SF_DTYPE_BF16><<<grid, kThreads, 0, st>>>(lay);
     else ffn_layout_kernel<SF_DTYPE_FP32><<<grid, kThreads, 0, st>>>(lay);
     lay.n = 0;

@@ -23,9 +23,11 @@
 // instruction throughout.
 //
 // Masked entries are selected, but a product still multiplies their zeros with the other operand's rows, and 0 x NaN
-// is NaN.  So the chunk's k and v are tested as they are staged; a chunk with a NaN or an infinity in them is walked
-// step by step, which keeps it from earlier steps and from later episodes.
+// is NaN.  So the chunk's k and v are tested as they are staged; a chunk with a NaN or an infinity in them is taken again as
+// chunks of one step, which keeps it from earlier steps and from later episodes.
 #include <math.h>
+
+#include <algorithm>
 
 #include "sf_internal.h"
 #include "sf_memory.h"
@@ -70,7 +72,7 @@ struct LinArgs {
   LinOp op[3];
   const float* log_decay;
   const uint8_t* done;  // or null
-  int T, N, H;
+  int T, N, H, ops;
   int n_seg, seg_len;   // pieces of T (seg_len a multiple of every C)
   float* seg_state;     // n_seg > 1: [op][N * H][n_seg][dk * dv], first the pieces' own states, then what enters them
   float* seg_keep;      // [op][N * H][n_seg] g^length, 0 if an episode begins in the piece
@@ -88,13 +90,21 @@ __device__ inline void split2(float a, float b, unsigned& t0, unsigned& t1) {
   t1 = pack_bf16(a - lo_of(t0), b - hi_of(t0));
 }
 
+// The same number, which the compiler takes for another one: comparisons with it are made where they stand and not kept in
+// registers from one use to the next.
+__device__ inline int anew(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+__device__ inline float pow2(float x) { return __builtin_amdgcn_exp2f(x); }  // (x <= 0 here; below 2^-126: 0)
+
 // The arithmetic of one element type.  An operand is eight K-slots per lane.
 template <int DTYPE>
 struct Num;
 
 template <>
 struct Num<SF_DTYPE_BF16> {
-  static constexpr int kBytes = 2, kPad = 8, kPieceWords = 4;
+  static constexpr int kBytes = 2, kPieceWords = 4;
   typedef u32x4 Raw;                                   // exact values
   struct Out { u32x4 t[2]; };                          // for the output: two terms
   struct Sum { u32x4 t[3]; };                          // for the state: three terms
@@ -161,7 +171,7 @@ struct Num<SF_DTYPE_BF16> {
 
 template <>
 struct Num<SF_DTYPE_FP32> {
-  static constexpr int kBytes = 4, kPad = 4, kPieceWords = 8;
+  static constexpr int kBytes = 4, kPieceWords = 8;
   struct Raw { float x[8]; };
   typedef Raw Out;
   typedef Raw Sum;
@@ -201,18 +211,18 @@ struct Num<SF_DTYPE_FP32> {
 };
 
 // Eight columns of a row, zero past the array's end (col may lie past it altogether).
-template <int DTYPE>
+template <int DTYPE, bool PIECES>
 __device__ inline void load_piece(unsigned* w, const Strided& a, const unsigned char* row, int col, bool live) {
   typedef Num<DTYPE> M;
   constexpr int W = M::kPieceWords;
-  if (live && a.vec && col < a.d) {  // (d is a multiple of 8 then)
+  if (live && (PIECES || a.vec) && col < a.d) {  // (d is a multiple of 8 then)
 #pragma unroll
     for (int i = 0; i < W; i += 4) *(u32x4*)(w + i) = *(const u32x4*)(row + (size_t)col * M::kBytes + 4 * i);
     return;
   }
 #pragma unroll
   for (int i = 0; i < W; ++i) w[i] = 0;
-  if (!live || a.vec) return;
+  if (PIECES || !live || a.vec) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if (col + i >= a.d) continue;
@@ -241,7 +251,9 @@ __device__ inline float finite_test(const unsigned* w, float acc) {
 template <int DTYPE, int D, int C>
 struct Lds {
   typedef Num<DTYPE> M;
-  static constexpr int kPitch = (D + M::kPad) * M::kBytes;  // of a row: 16 bytes more than its numbers, for the banks
+  // of a row: 4 times an odd number of words, so that 16 rows' pieces of 16 bytes lie in different banks; of those 36 and 12
+  // mod 64 also keep the transposing read's four rows of 32 bytes apart
+  static constexpr int kPitch = D * M::kBytes + (M::kBytes == 2 && D == 128 ? 48 : 16);
   static constexpr int kTile = C * kPitch;
   static constexpr int kFrags = (C / 16) * (C / 32);
   static constexpr int kTermPitch = kFrags * 1024;
@@ -253,30 +265,42 @@ struct Lds {
 };
 
 // STATE: only the piece's own state (from zero) and whether an episode begins in it.
-template <int DTYPE, int D, int C, bool STATE>
-__global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
+// How much of a call is known at compile time: kAny; kPieces: all rows are read and written in 16-byte pieces; kWhole: k and v
+// have D columns besides (else columns past theirs are left out, 32 of k, 16 of v at a time).
+enum Known { kAny = 0, kPieces = 1, kWhole = 2 };
+template <int DTYPE, int D, int C, bool STATE, int KNOWN>
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinArgs g) {
   typedef Num<DTYPE> M;
   typedef Lds<DTYPE, D, C> L;
   constexpr int W = M::kPieceWords, NP = C * D / 8 / kThreads;  // pieces of a tile per thread
   constexpr int NV = D / 64, ND = D / 16, NC = C / 32;          // a wave's tiles of v; tiles of k; K-steps over C
   static_assert(NP >= 1 && (C == 32 || C == 64), "whole pieces");
+  constexpr bool WHOLE = KNOWN == kWhole;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const LinOp& op = g.op[blockIdx.z];
+  // the ops of one (row, head) read the same arrays: one after another on one XCD (workgroups go to the 8 in turn)
+  const int round = blockIdx.x / (8 * g.ops), in_round = blockIdx.x % (8 * g.ops), which = in_round / 8;
+  const int bh = round * 8 + in_round % 8;
+  if (bh >= g.N * g.H) return;
+  const LinOp op = g.op[which];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
-  const int bh = blockIdx.x, n = bh / g.H, h = bh % g.H, seg = blockIdx.y;
+  const int n = bh / g.H, h = bh % g.H, seg = blockIdx.y;
   const int t_begin = seg * g.seg_len, t_end = min(g.T, t_begin + g.seg_len);  // in the op's own direction
   const int dk = op.k.d, dv = op.v.d;
   const float l2 = fmaxf(g.log_decay[h] * 1.44269504f, -1e30f);  // (no -infinity: times zero it would be NaN)
   const bool scan = g.n_seg > 1;
-  const size_t seg_at = ((size_t)blockIdx.z * g.N * g.H + bh) * g.n_seg + seg;
+  const size_t seg_at = ((size_t)which * g.N * g.H + bh) * g.n_seg + seg;
 
   const unsigned char* qrow = (const unsigned char*)op.q.p + (n * op.q.sn + h / op.q.div * op.q.sh) * M::kBytes;
   const unsigned char* krow = (const unsigned char*)op.k.p + (n * op.k.sn + h / op.k.div * op.k.sh) * M::kBytes;
   const unsigned char* vrow = (const unsigned char*)op.v.p + (n * op.v.sn + h / op.v.div * op.v.sh) * M::kBytes;
 
-  // column of v of this wave's tile t, operand row (or accumulator column) m
-  auto col_v = [&](int t, int m) { return NV == 2 ? 32 * wave + 8 * (m >> 2) + 4 * t + (m & 3) : 16 * wave + m; };
+  // column of v of this wave's tile t, operand row (or accumulator column) m: up to 64 columns one tile a wave
+  const bool two = WHOLE ? NV == 2 : NV == 2 && dv > 64;
+  const int v0 = two ? 32 * wave : 16 * wave;  // (a wave past dv has nothing to do)
+  auto col_v = [&](int t, int m) { return two ? v0 + 8 * (m >> 2) + 4 * t + (m & 3) : v0 + 64 * t + m; };
+  auto has_v = [&](int t) { return WHOLE || (v0 < dv && (t == 0 || two)); };
+  auto has_k = [&](int s) { return WHOLE || 32 * s < dk; };  // columns 32 s .. of k
   // column of k of tile t (two tiles are 32 columns: eight neighbours per lane group)
   auto col_k = [&](int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); };
 
@@ -293,31 +317,36 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
         s = op.s_in + (size_t)bh * dk * dv;
       }
     }
+    const int xk = anew(dk), yv = anew(dv);
 #pragma unroll
-    for (int a = 0; a < ND; ++a)
+    for (int a = 0; a < ND; ++a) {
 #pragma unroll
       for (int b = 0; b < NV; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int x = col_k(a, 4 * lg + r), y = col_v(b, li);
-          S[a][b][r] = s && x < dk && y < dv ? s[x * sa + y * sb] : 0.0f;
+          S[a][b][r] = s && (WHOLE || (x < xk && y < yv)) ? s[x * sa + y * sb] : 0.0f;
         }
+      __builtin_amdgcn_sched_barrier(0);  // (the addresses of all at once would fill the registers)
+    }
   }
 
   // the chunk that is on its way: its rows and its episode marks
   unsigned nq[NP][W], nk[NP][W], nv[NP][W];
   int n_done = 0;
   auto step_of = [&](int i) { return op.reverse ? g.T - 1 - i : i; };
+  int alone_to = t_begin;  // steps before this one are chunks of their own
+  auto width = [&](int c0) { return c0 < alone_to ? 1 : min(C, t_end - c0); };
   auto request = [&](int c0) {
-    const int valid = t_end - c0;
+    const int valid = width(c0);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int piece = tid + p * kThreads, r = piece / (D / 8), col = piece % (D / 8) * 8;
       const bool live = r < valid;
       const int64_t t = step_of(live ? c0 + r : t_end - 1);
-      if constexpr (!STATE) load_piece<DTYPE>(nq[p], op.q, qrow + t * op.q.st * M::kBytes, col, live);
-      load_piece<DTYPE>(nk[p], op.k, krow + t * op.k.st * M::kBytes, col, live);
-      load_piece<DTYPE>(nv[p], op.v, vrow + t * op.v.st * M::kBytes, col, live);
+      if constexpr (!STATE) load_piece<DTYPE, KNOWN != kAny>(nq[p], op.q, qrow + t * op.q.st * M::kBytes, col, live);
+      load_piece<DTYPE, KNOWN != kAny>(nk[p], op.k, krow + t * op.k.st * M::kBytes, col, live);
+      load_piece<DTYPE, KNOWN != kAny>(nv[p], op.v, vrow + t * op.v.st * M::kBytes, col, live);
     }
     n_done = 0;
     if (g.done && lane < C && lane < valid) {
@@ -336,8 +365,8 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
 
   bool any_done = false;
   request(t_begin);
-  for (int c0 = t_begin, turn = 0; c0 < t_end; c0 += C, turn ^= 1) {
-    const int valid = min(C, t_end - c0);
+  for (int c0 = t_begin, turn = 0, step; c0 < t_end; c0 += step, turn ^= 1) {
+    const int valid = width(c0);
     const int late = c0 == 0 && op.reverse ? 1 : 0;  // the state enters undecayed
     const unsigned long long marks = __ballot(n_done != 0);
     __syncthreads();  // the chunk before has been read
@@ -358,57 +387,19 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
     if (tid < C) {
       const int e = __popcll(marks & ((2ull << tid) - 1));
       ep[tid] = e;
-      wgt[tid] = e == ep_end && tid < valid ? op.w_scale * exp2f(l2 * (float)(valid - 1 - tid)) : 0.0f;
+      wgt[tid] = e == ep_end && tid < valid ? op.w_scale * pow2(l2 * (float)(valid - 1 - tid)) : 0.0f;
     }
     __syncthreads();
-    const bool walk = flag[turn] != 0;
-    if (c0 + C < t_end) request(c0 + C);
-    any_done |= marks != 0;
-
-    if (walk) {
-      // step by step
-      const float gam = exp2f(l2);
-      for (int i = 0; i < valid; ++i) {
-        const bool begin = marks >> i & 1;
-        const float keep = i == 0 && late ? 1.0f : gam;
-        float o[NV];
-#pragma unroll
-        for (int b = 0; b < NV; ++b) o[b] = 0.0f;
-#pragma unroll
-        for (int a = 0; a < ND; ++a)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int x = col_k(a, 4 * lg + r);
-            const float kx = M::element(tk + i * L::kPitch + x * M::kBytes);
-            const float qx = STATE ? 0.0f : M::element(tq + i * L::kPitch + x * M::kBytes);
-#pragma unroll
-            for (int b = 0; b < NV; ++b) {
-              const float vy = M::element(tv + i * L::kPitch + col_v(b, li) * M::kBytes);
-              // (columns past the arrays' ends stay zero: with an infinity in the row they would be NaN)
-              const bool in = x < dk && col_v(b, li) < dv;
-              S[a][b][r] = in ? op.w_scale * kx * vy + (begin ? 0.0f : keep * S[a][b][r]) : 0.0f;
-              if (in) o[b] += qx * S[a][b][r];
-            }
-          }
-        if constexpr (!STATE) {
-#pragma unroll
-          for (int b = 0; b < NV; ++b) {
-            float x = o[b];
-            x += __shfl_xor(x, 16);
-            x += __shfl_xor(x, 32);
-            const int y = col_v(b, li);
-            if (lg == 0 && y < dv) {
-              const int64_t at = n * op.on + h * op.oh + step_of(c0 + i) * op.ot + y;
-              if (op.o_f32) ((float*)op.o)[at] = op.alpha * x;
-              else M::store((unsigned char*)op.o + at * M::kBytes, op.alpha * x);
-            }
-          }
-        }
-      }
-      if (tid == 0) flag[turn ^ 1] = 0;  // (read by all before the barrier that ended the chunk before)
-      __syncthreads();                   // as many barriers as below
+    if (tid == 0) flag[turn ^ 1] = 0;  // (read by all before the barrier above)
+    if (flag[turn] != 0 && valid > 1 && c0 >= alone_to) {  // again, step by step
+      alone_to = c0 + valid;
+      request(c0);
+      step = 0;
       continue;
     }
+    step = valid;
+    if (c0 + valid < t_end) request(c0 + valid);
+    any_done |= marks != 0;
 
     if constexpr (!STATE) {
       // P^T: 16 x 16 tiles [j tile J][i tile I], J <= I; a pair of tiles is one operand
@@ -418,14 +409,14 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
 #pragma unroll
           for (int s = 0; s < D / 32; ++s) {
             const int at = (32 * s + 8 * lg) * M::kBytes;
-            acc = M::mma(M::row(tk + (16 * J + li) * L::kPitch + at), M::row(tq + (16 * I + li) * L::kPitch + at), acc);
+            if (has_k(s)) acc = M::mma(M::row(tk + (16 * J + li) * L::kPitch + at), M::row(tq + (16 * I + li) * L::kPitch + at), acc);
           }
           const int i = 16 * I + li, e = ep[i];
           const i32x4 ej = *(const i32x4*)(ep + 16 * J + 4 * lg);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int j = 16 * J + 4 * lg + r;
-            acc[r] = j <= i && ej[r] == e ? acc[r] * (op.w_scale * exp2f(l2 * (float)(i - j))) : 0.0f;
+            acc[r] = j <= i && ej[r] == e ? acc[r] * (op.w_scale * pow2(l2 * (float)(i - j))) : 0.0f;
           }
         }
         M::put4(lds + L::kP + (I * NC + J / 2) * 1024, L::kTermPitch, lane, J & 1, acc);
@@ -438,7 +429,6 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
         tile_p(wave >> 1, wave & 1);
       }
     }
-    if (tid == 0) flag[turn ^ 1] = 0;
     __syncthreads();
 
     // V^T of this wave's columns: K-slots 0..3 are steps 32 p + 4 g .., 4..7 are 16 further on
@@ -447,6 +437,7 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
     for (int p = 0; p < NC; ++p)
 #pragma unroll
       for (int b = 0; b < NV; ++b) {
+        if (!has_v(b)) continue;
         if constexpr (DTYPE == SF_DTYPE_BF16) {
           const unsigned char* at = tv + (32 * p + 4 * lg + (li >> 2)) * L::kPitch + col_v(b, 4 * (li & 3)) * M::kBytes;
           const u32x2 x = M::column4(at), y = M::column4(at + 16 * L::kPitch);
@@ -459,82 +450,82 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
       }
 
     if constexpr (!STATE) {
-      // two accumulator tiles of the state are one operand
-      typename M::Out st[D / 32][NV];
+      // what the state gives all steps (two accumulator tiles of it are one operand), scaled per step, and on top of it what
+      // the chunk's own steps give
+      f32x4 out[C / 16][NV];
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s)
+      for (int I = 0; I < C / 16; ++I)
+#pragma unroll
+        for (int b = 0; b < NV; ++b) out[I][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) {
+        if (!has_k(s)) continue;
 #pragma unroll
         for (int b = 0; b < NV; ++b) {
+          if (!has_v(b)) continue;
           float x[8];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             x[r] = S[2 * s][b][r];
             x[4 + r] = S[2 * s + 1][b][r];
           }
-          st[s][b] = M::out_terms(x);
+          const typename M::Out st = M::out_terms(x);
+#pragma unroll
+          for (int I = 0; I < C / 16; ++I)
+            out[I][b] = M::mma(st, M::row(tq + (16 * I + li) * L::kPitch + (32 * s + 8 * lg) * M::kBytes), out[I][b]);
         }
+      }
 #pragma unroll
       for (int I = 0; I < C / 16; ++I) {
         const int i = 16 * I + li;
-        f32x4 own[NV], old[NV];
+        const bool reach = (marks & ((2ull << i) - 1)) == 0;  // no episode has begun: the state is this step's
+        const float c = pow2(l2 * (float)(i + 1 - late));
+        f32x4* own = out[I];
 #pragma unroll
-        for (int b = 0; b < NV; ++b) own[b] = old[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int b = 0; b < NV; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) own[b][r] = reach ? c * own[b][r] : 0.0f;
 #pragma unroll
         for (int p = 0; p <= I / 2; ++p) {
           const typename M::Out x = M::get(lds + L::kP + (I * NC + p) * 1024, L::kTermPitch, lane);
 #pragma unroll
-          for (int b = 0; b < NV; ++b) own[b] = M::mma(vt[p][b], x, own[b]);
+          for (int b = 0; b < NV; ++b)
+            if (has_v(b)) own[b] = M::mma(vt[p][b], x, own[b]);
         }
-#pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-          const typename M::Raw x = M::row(tq + i * L::kPitch + (32 * s + 8 * lg) * M::kBytes);
-#pragma unroll
-          for (int b = 0; b < NV; ++b) old[b] = M::mma(st[s][b], x, old[b]);
-        }
-        const bool reach = (marks & ((2ull << i) - 1)) == 0;  // no episode has begun: the state is this step's
-        const float c = exp2f(l2 * (float)(i + 1 - late));
 #pragma unroll
         for (int b = 0; b < NV; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) own[b][r] = op.alpha * (own[b][r] + (reach ? c * old[b][r] : 0.0f));
+          for (int r = 0; r < 4; ++r) own[b][r] *= op.alpha;
         if (i < valid) {
           const int64_t at = n * op.on + h * op.oh + step_of(c0 + i) * op.ot;
-          const int y = col_v(0, 4 * lg);  // 4 * NV neighbours
-          if (op.o_vec) {
-            if (y < dv) {
-              if constexpr (DTYPE == SF_DTYPE_BF16) {
-                if (!op.o_f32) {
-                  unsigned w[2 * NV];
-#pragma unroll
-                  for (int b = 0; b < NV; ++b) {
-                    w[2 * b] = pack_bf16(own[b][0], own[b][1]);
-                    w[2 * b + 1] = pack_bf16(own[b][2], own[b][3]);
-                  }
-                  uint16_t* to = (uint16_t*)op.o + at + y;
-                  if constexpr (NV == 2) *(u32x4*)to = u32x4{w[0], w[1], w[2], w[3]};
-                  else *(u32x2*)to = u32x2{w[0], w[1]};
-                  continue;
-                }
-              }
-#pragma unroll
-              for (int b = 0; b < NV; ++b) *(f32x4*)((float*)op.o + at + y + 4 * b) = own[b];
-            }
+          if ((KNOWN != kAny || op.o_vec) && DTYPE == SF_DTYPE_BF16 && !op.o_f32 && two) {  // eight neighbours
+            const int y = col_v(0, 4 * lg);
+            if (NV == 2 && y < dv)
+              *(u32x4*)((uint16_t*)op.o + at + y) = u32x4{pack_bf16(own[0][0], own[0][1]), pack_bf16(own[0][2], own[0][3]),
+                                                          pack_bf16(own[NV - 1][0], own[NV - 1][1]), pack_bf16(own[NV - 1][2], own[NV - 1][3])};
           } else {
 #pragma unroll
-            for (int b = 0; b < NV; ++b)
+            for (int b = 0; b < NV; ++b) {
+              const int y = col_v(b, 4 * lg);  // four neighbours
+              if (!has_v(b) || y >= dv) continue;
+              if (KNOWN != kAny || op.o_vec) {
+                if (op.o_f32) *(f32x4*)((float*)op.o + at + y) = own[b];
+                else *(u32x2*)((uint16_t*)op.o + at + y) = u32x2{pack_bf16(own[b][0], own[b][1]), pack_bf16(own[b][2], own[b][3])};
+              } else {
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const int z = y + 4 * b + r;
-                if (z >= dv) continue;
-                if (op.o_f32) ((float*)op.o)[at + z] = own[b][r];
-                else M::store((unsigned char*)op.o + (at + z) * M::kBytes, own[b][r]);
+                for (int r = 0; r < 4; ++r) {
+                  if (y + r >= dv) continue;
+                  if (op.o_f32) ((float*)op.o)[at + y + r] = own[b][r];
+                  else M::store((unsigned char*)op.o + (at + y + r) * M::kBytes, own[b][r]);
+                }
               }
+            }
           }
         }
       }
     }
 
-    const float keep = marks ? 0.0f : exp2f(l2 * (float)(valid - late));
+    const float keep = marks ? 0.0f : pow2(l2 * (float)(valid - late));
 #pragma unroll
     for (int a = 0; a < ND; ++a)
 #pragma unroll
@@ -547,6 +538,7 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
       const f32x4 w0 = *(const f32x4*)(wgt + 32 * p + 4 * lg), w1 = *(const f32x4*)(wgt + 32 * p + 16 + 4 * lg);
 #pragma unroll
       for (int b = 0; b < NV; ++b) {
+        if (!has_v(b)) continue;
         float x[8];
         M::values(vt[p][b], x);
 #pragma unroll
@@ -558,6 +550,7 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
       }
 #pragma unroll
       for (int a = 0; a < ND; ++a) {
+        if (!has_k(a / 2)) continue;
         typename M::Raw kt;
         if constexpr (DTYPE == SF_DTYPE_BF16) {
           const unsigned char* at = tk + (32 * p + 4 * lg + (li >> 2)) * L::kPitch + col_k(a, 4 * (li & 3)) * M::kBytes;
@@ -569,7 +562,8 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
             kt.x[r] = M::element(tk + (32 * p + 4 * lg + (r & 3) + 16 * (r >> 2)) * L::kPitch + col_k(a, li) * M::kBytes);
         }
 #pragma unroll
-        for (int b = 0; b < NV; ++b) S[a][b] = M::mma(kt, vw[b], S[a][b]);
+        for (int b = 0; b < NV; ++b)
+          if (has_v(b)) S[a][b] = M::mma(kt, vw[b], S[a][b]);
       }
     }
   }
@@ -583,52 +577,65 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_kernel(LinArgs g) {
     sa = dv;
     sb = 1;
     if (tid == 0)
-      g.seg_keep[seg_at] = any_done ? 0.0f : exp2f(l2 * (float)(t_end - t_begin - (seg == 0 && op.reverse ? 1 : 0)));
+      g.seg_keep[seg_at] = any_done ? 0.0f : pow2(l2 * (float)(t_end - t_begin - (seg == 0 && op.reverse ? 1 : 0)));
   } else if (op.s_out && seg == g.n_seg - 1) {
     s = op.s_out + (size_t)bh * dk * dv;
     if (op.reverse) {  // one step further back: to before the first step
-      f = t_end > t_begin ? exp2f(l2) : 1.0f;
+      f = t_end > t_begin ? pow2(l2) : 1.0f;
       zero = g.done && t_end > t_begin && g.done[n] != 0;
     }
   }
   if (s) {
+    const int xk = anew(dk), yv = anew(dv);
 #pragma unroll
-    for (int a = 0; a < ND; ++a)
+    for (int a = 0; a < ND; ++a) {
 #pragma unroll
       for (int b = 0; b < NV; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int x = col_k(a, 4 * lg + r), y = col_v(b, li);
-          if (x < dk && y < dv) s[x * sa + y * sb] = zero ? 0.0f : f * S[a][b][r];
+          if (WHOLE || (x < xk && y < yv)) s[x * sa + y * sb] = zero ? 0.0f : f * S[a][b][r];
         }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 }
 
-// What enters each piece of T, from the pieces' own states: one thread per element of a state.
+// What enters each piece of T, from the pieces' own states: one thread per element of a state, kAhead pieces read ahead.
 __global__ __launch_bounds__(kThreads) void linattn_join_kernel(LinArgs g) {
+  constexpr int kAhead = 16;
   const LinOp& op = g.op[blockIdx.z];
   const int bh = blockIdx.y, dk = op.k.d, dv = op.v.d, e = blockIdx.x * kThreads + threadIdx.x;
   if (e >= dk * dv) return;
-  const size_t at = ((size_t)blockIdx.z * g.N * g.H + bh) * g.n_seg;
-  float* s = g.seg_state + at * ((size_t)dk * dv) + e;
+  const size_t at = ((size_t)blockIdx.z * g.N * g.H + bh) * g.n_seg, size = (size_t)dk * dv;
+  float* s = g.seg_state + at * size + e;
   float in = op.s_in ? op.s_in[(size_t)bh * dk * dv + e / dv * op.s_a + e % dv * op.s_b] : 0.0f;
-  for (int i = 0; i < g.n_seg; ++i) {
-    float* x = s + (size_t)i * dk * dv;
-    const float own = *x, keep = g.seg_keep[at + i];
-    *x = in;
-    in = own + (keep == 0.0f ? 0.0f : keep * in);
+  for (int i0 = 0; i0 < g.n_seg; i0 += kAhead) {
+    float own[kAhead], keep[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int j = min(i0 + i, g.n_seg - 1);
+      own[i] = s[j * size];
+      keep[i] = g.seg_keep[at + j];
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (i0 + i >= g.n_seg) break;
+      s[(i0 + i) * size] = in;
+      in = own[i] + (keep[i] == 0.0f ? 0.0f : keep[i] * in);
+    }
   }
 }
 
 // Sums of the gradients of shared heads: in [rows][H][d] fp32, out [rows][H / share][d].
 template <int DTYPE>
 __global__ __launch_bounds__(kThreads) void linattn_share_kernel(const float* in, void* out, int64_t n_out, int d, int share) {
-  const int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (e >= n_out) return;
-  const float* x = in + e / d * share * d + e % d;
-  float sum = 0.0f;
-  for (int i = 0; i < share; ++i) sum += x[(int64_t)i * d];
-  Num<DTYPE>::store((unsigned char*)out + e * Num<DTYPE>::kBytes, sum);
+  for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < n_out; e += (int64_t)gridDim.x * kThreads) {
+    const float* x = in + e / d * share * d + e % d;
+    float sum = 0.0f;
+    for (int i = 0; i < share; ++i) sum += x[(int64_t)i * d];
+    Num<DTYPE>::store((unsigned char*)out + e * Num<DTYPE>::kBytes, sum);
+  }
 }
 
 // One step of one (row, head): the state is read, decayed, added to, written and multiplied with q.  Bound by those
@@ -719,8 +726,8 @@ int check(const sf_linattn_config* c, const char* fn) {
     set_error("%s: T = %d, N = %d, H = %d, Hk = %d, dk = %d, dv = %d out of range", fn, c->T, c->N, c->H, c->Hk, c->dk, c->dv);
     return SF_ERR_SHAPE;
   }
-  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > INT32_MAX) {
-    set_error("%s: T * N or N * H beyond 2^31 - 1", fn);
+  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > 1 << 22) {
+    set_error("%s: T * N beyond 2^31 - 1 or N * H beyond 2^22", fn);
     return SF_ERR_SHAPE;
   }
   if (!isfinite(c->scale)) {
@@ -742,10 +749,11 @@ int check_ptr(const char* fn, const char* name, const void* p, size_t align, boo
 struct Split {
   int n_seg, seg_len;
 };
-// Pieces of T: enough workgroups to fill the chip, but each with at least four chunks.
+// Pieces of T where rows x heads leave CUs without a workgroup (the pieces' states cost a pass over k and v more): each with
+// at least four chunks.
 Split split_of(const sf_linattn_config* c, int ops) {
   const int64_t lanes = (int64_t)c->N * c->H * ops;
-  const int64_t want = lanes > 0 ? (768 + lanes - 1) / lanes : 1;
+  const int64_t want = lanes > 0 && lanes < 384 ? (768 + lanes - 1) / lanes : 1;
   int64_t len = (c->T + want - 1) / want;
   len = (len + 63) / 64 * 64;
   if (len < 256) len = 256;
@@ -791,22 +799,29 @@ void put_out(const sf_linattn_config* c, LinOp& op, void* p, int64_t t, int64_t 
   op.o_vec = d % 8 == 0 && t % per == 0 && n % per == 0 && h % per == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 }
 
-template <int DTYPE, int D, int C, bool STATE>
-hipError_t launch_t(const LinArgs& g, int ops, hipStream_t st) {
-  const auto kern = linattn_kernel<DTYPE, D, C, STATE>;
+template <int DTYPE, int D, int C, bool STATE, int KNOWN>
+hipError_t launch_k(const LinArgs& g, hipStream_t st) {
+  const auto kern = linattn_kernel<DTYPE, D, C, STATE, KNOWN>;
   constexpr int bytes = Lds<DTYPE, D, C>::kBytes;
   static const hipError_t attr = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (attr != hipSuccess) return attr;
-  kern<<<dim3((unsigned)(g.N * g.H), (unsigned)g.n_seg, (unsigned)ops), kThreads, bytes, st>>>(g);
+  kern<<<dim3((unsigned)((g.N * g.H + 7) / 8 * 8 * g.ops), (unsigned)g.n_seg), kThreads, bytes, st>>>(g);
   return hipGetLastError();
 }
+template <int DTYPE, int D, int C, bool STATE>
+hipError_t launch_t(const sf_linattn_config* c, const LinArgs& g, hipStream_t st) {
+  bool pieces = true;
+  for (int i = 0; i < g.ops; ++i) pieces = pieces && g.op[i].q.vec && g.op[i].k.vec && g.op[i].v.vec && g.op[i].o_vec;
+  if (!pieces) return launch_k<DTYPE, D, C, STATE, kAny>(g, st);
+  return c->dk == D && c->dv == D ? launch_k<DTYPE, D, C, STATE, kWhole>(g, st) : launch_k<DTYPE, D, C, STATE, kPieces>(g, st);
+}
 template <bool STATE>
-hipError_t launch(const sf_linattn_config* c, const LinArgs& g, int ops, hipStream_t st) {
+hipError_t launch(const sf_linattn_config* c, const LinArgs& g, hipStream_t st) {
   const bool wide = c->dk > 64 || c->dv > 64;
   if (c->dtype == SF_DTYPE_FP32)  // (64 steps of 128 numbers would leave a CU one workgroup)
-    return wide ? launch_t<SF_DTYPE_FP32, 128, 32, STATE>(g, ops, st) : launch_t<SF_DTYPE_FP32, 64, 32, STATE>(g, ops, st);
-  if (c->T <= 32) return wide ? launch_t<SF_DTYPE_BF16, 128, 32, STATE>(g, ops, st) : launch_t<SF_DTYPE_BF16, 64, 32, STATE>(g, ops, st);
-  return wide ? launch_t<SF_DTYPE_BF16, 128, 64, STATE>(g, ops, st) : launch_t<SF_DTYPE_BF16, 64, 64, STATE>(g, ops, st);
+    return wide ? launch_t<SF_DTYPE_FP32, 128, 32, STATE>(c, g, st) : launch_t<SF_DTYPE_FP32, 64, 32, STATE>(c, g, st);
+  if (wide) return launch_t<SF_DTYPE_BF16, 128, 32, STATE>(c, g, st);
+  return c->T <= 32 ? launch_t<SF_DTYPE_BF16, 64, 32, STATE>(c, g, st) : launch_t<SF_DTYPE_BF16, 64, 64, STATE>(c, g, st);
 }
 
 int run(const char* fn, const sf_linattn_config* c, LinArgs& g, int ops, const Workspace& w, unsigned char* ws, hipStream_t st) {
@@ -815,20 +830,21 @@ int run(const char* fn, const sf_linattn_config* c, LinArgs& g, int ops, const W
   g.T = c->T;
   g.N = c->N;
   g.H = c->H;
+  g.ops = ops;
   g.n_seg = s.n_seg;
   g.seg_len = s.seg_len;
   hipError_t e = hipSuccess;
   if (s.n_seg > 1) {
     g.seg_state = (float*)ws;
     g.seg_keep = (float*)(ws + w.state);
-    e = launch<true>(c, g, ops, st);
+    e = launch<true>(c, g, st);
     if (e == hipSuccess) {
       linattn_join_kernel<<<dim3((unsigned)((c->dk * c->dv + kThreads - 1) / kThreads), (unsigned)(c->N * c->H), (unsigned)ops), kThreads, 0,
                             st>>>(g);
       e = hipGetLastError();
     }
   }
-  if (e == hipSuccess) e = launch<false>(c, g, ops, st);
+  if (e == hipSuccess) e = launch<false>(c, g, st);
   if (e != hipSuccess) {
     set_error("%s: launch failed: %s", fn, hipGetErrorString(e));
     return SF_ERR_DEVICE;
@@ -942,7 +958,8 @@ extern "C" int sf_linattn_backward(const sf_linattn_config* cfg, const void* q, 
   rc = run(fn, cfg, g, 3, w, ws, st);
   if (rc != SF_OK || share == 1 || none) return rc;
   const int64_t nk = (int64_t)cfg->T * cfg->N * Hk * Dk, nv = (int64_t)cfg->T * cfg->N * Hk * Dv;
-  const unsigned gk = (unsigned)((nk + kThreads - 1) / kThreads), gv = (unsigned)((nv + kThreads - 1) / kThreads);
+  const auto grid = [](int64_t n) { return (unsigned)std::min<int64_t>((n + kThreads - 1) / kThreads, 1 << 20); };
+  const unsigned gk = grid(nk), gv = grid(nv);
   if (cfg->dtype == SF_DTYPE_BF16) {
     linattn_share_kernel<SF_DTYPE_BF16><<<gk, kThreads, 0, st>>>(part_k, dk, nk, Dk, share);
     linattn_share_kernel<SF_DTYPE_BF16><<<gv, kThreads, 0, st>>>(part_v, dv, nv, Dv, share);
