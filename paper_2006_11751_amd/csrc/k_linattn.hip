@@ -318,10 +318,15 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
       }
     }
     const int xk = anew(dk), yv = anew(dv);
+    const bool four = KNOWN != kAny && sa == 1 && (reinterpret_cast<uintptr_t>(s) & 15) == 0;  // neighbours of k lie side by side
 #pragma unroll
     for (int a = 0; a < ND; ++a) {
 #pragma unroll
       for (int b = 0; b < NV; ++b)
+        if (four) {  // (columns of k are a multiple of eight)
+          const int x = col_k(a, 4 * lg), y = col_v(b, li);
+          S[a][b] = s && (WHOLE || (x < xk && y < yv)) ? *(const f32x4*)(s + x + y * sb) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        } else
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int x = col_k(a, 4 * lg + r), y = col_v(b, li);
