@@ -7,6 +7,8 @@
 Argument checks and marshalling only; every operator runs in the library's HIP kernels, on `stream` or the current
 stream.  Each function puts its results into `out` (a dict) and returns it.  A program that calls one again and
 again keeps that dict: buffers that are there already are written to (they have to fit), and so is the workspace.
+Calls are short (a policy worker's step takes a few microseconds on the GPU), so what the checks of a call found is kept
+by the shapes, strides, types and devices of its arguments, and the checks are made once for each of these.
 """
 import ctypes as C
 
@@ -15,8 +17,8 @@ from .binding import SF_OK, SfError, sf_last_error
 
 SF_DTYPE_FP32, SF_DTYPE_BF16 = 0, 1
 
-EXPORTS = ("sf_linattn_workspace_bytes", "sf_linattn", "sf_linattn_backward", "sf_linattn_step", "sf_resnorm", "sf_resnorm_workspace_bytes",
-           "sf_resnorm_backward", "sf_ffn_workspace_bytes", "sf_ffn", "sf_ffn_backward")
+EXPORTS = ("sf_linattn_workspace_bytes", "sf_linattn", "sf_linattn_backward", "sf_linattn_step", "sf_resnorm",
+           "sf_resnorm_workspace_bytes", "sf_resnorm_backward", "sf_ffn_workspace_bytes", "sf_ffn", "sf_ffn_backward")
 
 _STRIDE = C.c_int64 * 3
 
@@ -50,18 +52,18 @@ def load_library():
     global _lib
     if _lib is None:
         L = binding.load_library()
-        P = C.c_void_p
+        P = C.c_void_p  # (of a configuration too: its address is taken once, when it is made)
         for name, restype, argtypes in (
-                ("sf_linattn_workspace_bytes", C.c_int64, [C.POINTER(SfLinattnConfig), C.c_int]),
-                ("sf_linattn", C.c_int, [C.POINTER(SfLinattnConfig)] + [P] * 10),
-                ("sf_linattn_backward", C.c_int, [C.POINTER(SfLinattnConfig)] + [P] * 14),
-                ("sf_linattn_step", C.c_int, [C.POINTER(SfLinattnConfig)] + [P] * 5 + [C.c_int32] + [P] * 4),
-                ("sf_resnorm", C.c_int, [C.POINTER(SfResnormConfig)] + [P] * 9),
-                ("sf_resnorm_workspace_bytes", C.c_int64, [C.POINTER(SfResnormConfig)]),
-                ("sf_resnorm_backward", C.c_int, [C.POINTER(SfResnormConfig)] + [P] * 16),
-                ("sf_ffn_workspace_bytes", C.c_int64, [C.POINTER(SfFfnConfig), C.c_int]),
-                ("sf_ffn", C.c_int, [C.POINTER(SfFfnConfig)] + [P] * 7),
-                ("sf_ffn_backward", C.c_int, [C.POINTER(SfFfnConfig)] + [P] * 11)):
+                ("sf_linattn_workspace_bytes", C.c_int64, [P, C.c_int]),
+                ("sf_linattn", C.c_int, [P] * 11),
+                ("sf_linattn_backward", C.c_int, [P] * 15),
+                ("sf_linattn_step", C.c_int, [P] * 6 + [C.c_int32] + [P] * 4),
+                ("sf_resnorm", C.c_int, [P] * 10),
+                ("sf_resnorm_workspace_bytes", C.c_int64, [P]),
+                ("sf_resnorm_backward", C.c_int, [P] * 17),
+                ("sf_ffn_workspace_bytes", C.c_int64, [P, C.c_int]),
+                ("sf_ffn", C.c_int, [P] * 8),
+                ("sf_ffn_backward", C.c_int, [P] * 12)):
             f = getattr(L, name)
             f.restype, f.argtypes = restype, argtypes
         _lib = L
@@ -103,29 +105,9 @@ def _same(name, t, like, shape, dtype=None, dense=True):
     return t
 
 
-def _result(out, name, shape, dtype, device):
-    t = out.get(name)
-    if t is None:
-        t = out[name] = binding._torch().empty(shape, dtype=dtype, device=device)
-    elif tuple(t.shape) != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        _refuse("out[%r] does not fit: %s %s on %s is wanted, contiguous" % (name, shape, dtype, device))
-    return t
-
-
-def _workspace(out, n_bytes, device):
-    if n_bytes < 0:
-        raise SfError(binding.SF_ERR_SHAPE, sf_last_error())
-    if not n_bytes:
-        return None
-    w = out.get("workspace")
-    if w is None or w.numel() < n_bytes or w.device != device:
-        torch = binding._torch()
-        w = out["workspace"] = torch.empty(n_bytes, dtype=torch.uint8, device=device)
-    return w.data_ptr()
-
-
-def _stream(stream, device):
-    return (binding._torch().cuda.current_stream(device) if stream is None else stream).cuda_stream
+def _optional(name, t, like, shape, dtype):
+    if t is not None:
+        _same(name, t, like, shape, dtype)
 
 
 def _rows(name, t):
@@ -133,6 +115,80 @@ def _rows(name, t):
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         _refuse("%s: the last axis is not dense" % name)
     return t.stride()[:-1]
+
+
+class _Plan:
+    """What the checks of a call found: the configuration, the results' shapes and types, the size of the workspace."""
+    __slots__ = ("key", "config", "address", "results", "n_bytes", "device")
+
+    def __init__(self, config, results, n_bytes, device):
+        if n_bytes < 0:
+            raise SfError(binding.SF_ERR_SHAPE, sf_last_error())
+        self.config, self.address, self.n_bytes, self.device = config, C.addressof(config), n_bytes, device
+        torch = binding._torch()
+        self.results = [(name, torch.Size(shape), dtype) for name, shape, dtype in results]
+
+
+_plans = {}  # by key: (function, arguments that are no tensors, what the tensors are)
+_last = {}   # by function: the plan it used last
+
+
+def _plan(name, rest, tensors, build, *args):
+    key = [rest]
+    for t in tensors:
+        if t is None:
+            key.append(None)
+        else:
+            key += (t.shape, t.stride(), t.dtype, t.device)
+    plan = _last.get(name)
+    if plan is not None and plan.key == key:
+        return plan
+    whole = (name,) + tuple(key)
+    plan = _plans.get(whole)
+    if plan is None:
+        load_library()
+        plan = build(*args)
+        plan.key = key
+        if len(_plans) >= 1024:
+            _plans.clear()
+        _plans[whole] = plan
+    _last[name] = plan
+    return plan
+
+
+def _results(out, plan):
+    """The results' addresses; what is not in `out` is allocated."""
+    got = []
+    for name, shape, dtype in plan.results:
+        t = out.get(name)
+        if t is None:
+            t = out[name] = binding._torch().empty(shape, dtype=dtype, device=plan.device)
+        elif t.shape != shape or t.dtype != dtype or t.device != plan.device or not t.is_contiguous():
+            _refuse("out[%r] does not fit: %s %s on %s is wanted, contiguous" % (name, tuple(shape), dtype, plan.device))
+        got.append(t.data_ptr())
+    return got
+
+
+def _workspace(out, plan):
+    if not plan.n_bytes:
+        return None
+    w = out.get("workspace")
+    if w is None or w.numel() < plan.n_bytes or w.device != plan.device:
+        torch = binding._torch()
+        w = out["workspace"] = torch.empty(plan.n_bytes, dtype=torch.uint8, device=plan.device)
+    return w.data_ptr()
+
+
+_raw_stream = None
+
+
+def _stream(stream, device):
+    global _raw_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:  # (the handle alone: a Stream object of torch costs two microseconds)
+        _raw_stream = binding._torch()._C._cuda_getCurrentRawStream
+    return _raw_stream(device.index)
 
 
 def _linattn_config(q, k, v, log_decay, scale, steps):
@@ -155,68 +211,75 @@ def _linattn_config(q, k, v, log_decay, scale, steps):
     return c
 
 
-def _optional(name, t, like, shape, dtype):
-    return None if t is None else _same(name, t, like, shape, dtype).data_ptr()
-
-
 def linear_attention(q, k, v, log_decay, done=None, state0=None, scale=None, out=None, stream=None):
     """Over N trajectories of T steps: q [T,N,H,dk], k [T,N,Hk,dk], v [T,N,Hk,dv] (bf16 or fp32, last axis dense),
     log_decay fp32 [H], done u8 [T,N], state0 fp32 [N,H,dk,dv]; scale: dk ** -0.5.  Results: o [T,N,H,dv],
     state [N,H,dk,dv]."""
-    torch = binding._torch()
     out = {} if out is None else out
+    plan = _plan("linear_attention", scale, (q, k, v, log_decay, done, state0), _linattn_plan, q, k, v, log_decay, done, state0, scale)
+    o, state = _results(out, plan)
+    _check(_lib.sf_linattn(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), _ptr(done), _ptr(state0), o, state,
+                           _workspace(out, plan), _stream(stream, plan.device)))
+    return out
+
+
+def _linattn_plan(q, k, v, log_decay, done, state0, scale):
+    torch = binding._torch()
     c = _linattn_config(q, k, v, log_decay, scale, True)
     T, N, H, dk = q.shape
-    d, s = q.device, (N, H, dk, c.dv)
-    done = _optional("done", done, q, (T, N), torch.uint8)
-    s0 = _optional("state0", state0, q, s, torch.float32)
-    o = _result(out, "o", (T, N, H, c.dv), q.dtype, d)
-    state = _result(out, "state", s, torch.float32, d)
-    L = load_library()
-    w = _workspace(out, L.sf_linattn_workspace_bytes(C.byref(c), 0), d)
-    _check(L.sf_linattn(C.byref(c), q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), done, s0, o.data_ptr(),
-                        state.data_ptr(), w, _stream(stream, d)))
-    return out
+    s = (N, H, dk, c.dv)
+    _optional("done", done, q, (T, N), torch.uint8)
+    _optional("state0", state0, q, s, torch.float32)
+    return _Plan(c, (("o", (T, N, H, c.dv), q.dtype), ("state", s, torch.float32)),
+                 _lib.sf_linattn_workspace_bytes(C.addressof(c), 0), q.device)
 
 
 def linear_attention_backward(q, k, v, log_decay, do, done=None, state0=None, dstate=None, scale=None, out=None, stream=None):
     """Gradients of linear_attention with the same arguments, given those of o (do) and of the final state (dstate, or
     None).  Results: dq, dk, dv, dstate0."""
-    torch = binding._torch()
     out = {} if out is None else out
+    plan = _plan("linear_attention_backward", scale, (q, k, v, log_decay, do, done, state0, dstate), _linattn_back_plan, q, k, v, log_decay, do,
+                 done, state0, dstate, scale)
+    dq, dk, dv, ds0 = _results(out, plan)
+    _check(_lib.sf_linattn_backward(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), do.data_ptr(), _ptr(done),
+                                    _ptr(state0), _ptr(dstate), dq, dk, dv, ds0, _workspace(out, plan), _stream(stream, plan.device)))
+    return out
+
+
+def _linattn_back_plan(q, k, v, log_decay, do, done, state0, dstate, scale):
+    torch = binding._torch()
     c = _linattn_config(q, k, v, log_decay, scale, True)
     T, N, H, dk = q.shape
-    d, s, f32 = q.device, (N, H, dk, c.dv), torch.float32
+    s, f32 = (N, H, dk, c.dv), torch.float32
     _same("do", do, q, (T, N, H, c.dv), dense=False)
     c.o_stride[0], c.o_stride[1], c.o_stride[2] = _rows("do", do)
-    done = _optional("done", done, q, (T, N), torch.uint8)
-    s0, ds = _optional("state0", state0, q, s, f32), _optional("dstate", dstate, q, s, f32)
-    dq = _result(out, "dq", (T, N, H, dk), q.dtype, d)
-    gk = _result(out, "dk", (T, N, c.Hk, dk), q.dtype, d)
-    gv = _result(out, "dv", (T, N, c.Hk, c.dv), q.dtype, d)
-    ds0 = _result(out, "dstate0", s, f32, d)
-    L = load_library()
-    w = _workspace(out, L.sf_linattn_workspace_bytes(C.byref(c), 1), d)
-    _check(L.sf_linattn_backward(C.byref(c), q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), do.data_ptr(), done,
-                                 s0, ds, dq.data_ptr(), gk.data_ptr(), gv.data_ptr(), ds0.data_ptr(), w, _stream(stream, d)))
-    return out
+    _optional("done", done, q, (T, N), torch.uint8)
+    _optional("state0", state0, q, s, f32)
+    _optional("dstate", dstate, q, s, f32)
+    return _Plan(c, (("dq", (T, N, H, dk), q.dtype), ("dk", (T, N, c.Hk, dk), q.dtype), ("dv", (T, N, c.Hk, c.dv), q.dtype), ("dstate0", s, f32)),
+                 _lib.sf_linattn_workspace_bytes(C.addressof(c), 1), q.device)
 
 
 def linear_attention_step(q, k, v, log_decay, state_table, env_ids=None, done=None, scale=None, out=None, stream=None):
     """One step of B environments: q [B,H,dk], k [B,Hk,dk], v [B,Hk,dv], done u8 [B]; state_table fp32 [n_env,H,dk,dv] is
     read and overwritten at the rows env_ids (i32 [B], distinct; None: rows 0 .. B-1).  Result: o [B,H,dv]."""
-    torch = binding._torch()
     out = {} if out is None else out
+    plan = _plan("linear_attention_step", scale, (q, k, v, log_decay, state_table, env_ids, done), _linattn_step_plan, q, k, v, log_decay,
+                 state_table, env_ids, done, scale)
+    o, = _results(out, plan)
+    _check(_lib.sf_linattn_step(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state_table.data_ptr(),
+                                state_table.shape[0], _ptr(env_ids), _ptr(done), o, _stream(stream, plan.device)))
+    return out
+
+
+def _linattn_step_plan(q, k, v, log_decay, state_table, env_ids, done, scale):
+    torch = binding._torch()
     c = _linattn_config(q, k, v, log_decay, scale, False)
     B, H, dk = q.shape
-    n_env = state_table.shape[0]
-    _same("state_table", state_table, q, (n_env, H, dk, c.dv), torch.float32)
-    ids = _optional("env_ids", env_ids, q, (B,), torch.int32)
-    done = _optional("done", done, q, (B,), torch.uint8)
-    o = _result(out, "o", (B, H, c.dv), q.dtype, q.device)
-    _check(load_library().sf_linattn_step(C.byref(c), q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
-                                          state_table.data_ptr(), n_env, ids, done, o.data_ptr(), _stream(stream, q.device)))
-    return out
+    _same("state_table", state_table, q, (state_table.shape[0], H, dk, c.dv), torch.float32)
+    _optional("env_ids", env_ids, q, (B,), torch.int32)
+    _optional("done", done, q, (B,), torch.uint8)
+    return _Plan(c, (("o", (B, H, c.dv), q.dtype),), 0, q.device)
 
 
 _NORMS = {"none": 0, "rms": 1, "layer": 2}
@@ -235,7 +298,7 @@ def _flat(name, t, like=None):
 
 
 def _resnorm_config(b, x, gate, post, pre, post_w, pre_w, scale, groups, gate_act, eps):
-    """The configuration, b, x and the gate as rows, and the weights' addresses."""
+    """The configuration, and b as rows."""
     if not b.is_cuda:
         _refuse("b is not on the GPU")
     b = _flat("b", b)
@@ -248,10 +311,11 @@ def _resnorm_config(b, x, gate, post, pre, post_w, pre_w, scale, groups, gate_ac
     x = None if x is None else _flat("x", x, b)
     gate = None if gate is None else _flat("gate", gate, b)
     f32 = binding._torch().float32
-    w = tuple(_optional(n, t, b, (D,), f32) for n, t in (("post_w", post_w), ("scale", scale), ("pre_w", pre_w)))
+    for n, t in (("post_w", post_w), ("scale", scale), ("pre_w", pre_w)):
+        _optional(n, t, b, (D,), f32)
     c = SfResnormConfig(C.sizeof(SfResnormConfig), _dtype_of(b), M, D, groups, _NORMS[post], _NORMS[pre], _GATES[gate_act], eps,
                         b.stride(0), 0 if x is None else x.stride(0), 0 if gate is None else gate.stride(0), 0, 0)
-    return c, b, x, gate, w
+    return c, b
 
 
 def residual_norm(b, x=None, gate=None, post="rms", pre="rms", post_w=None, pre_w=None, scale=None, groups=1, gate_act="none",
@@ -260,13 +324,17 @@ def residual_norm(b, x=None, gate=None, post="rms", pre="rms", post_w=None, pre_
     dense; weights fp32 [D]).  post, pre: "none", "rms" or "layer"; gate_act: "none", "sigmoid" or "silu"; groups: of
     channels that post is taken over (pre "none" then).  Results: y and, with pre, n."""
     out = {} if out is None else out
-    shape = tuple(b.shape)
-    c, b, x, gate, w = _resnorm_config(b, x, gate, post, pre, post_w, pre_w, scale, groups, gate_act, eps)
-    y = _result(out, "y", shape, b.dtype, b.device)
-    n = _result(out, "n", shape, b.dtype, b.device) if c.pre else None
-    _check(load_library().sf_resnorm(C.byref(c), b.data_ptr(), _ptr(x), _ptr(gate), w[0], w[1], w[2], y.data_ptr(), _ptr(n),
-                                     _stream(stream, b.device)))
+    how = (post, pre, groups, gate_act, eps)
+    plan = _plan("residual_norm", how, (b, x, gate, post_w, pre_w, scale), _resnorm_plan, b, x, gate, post_w, pre_w, scale, how)
+    got = _results(out, plan)
+    _check(_lib.sf_resnorm(plan.address, b.data_ptr(), _ptr(x), _ptr(gate), _ptr(post_w), _ptr(scale), _ptr(pre_w), got[0],
+                           got[1] if len(got) > 1 else None, _stream(stream, plan.device)))
     return out
+
+
+def _resnorm_plan(b, x, gate, post_w, pre_w, scale, how):
+    c, _ = _resnorm_config(b, x, gate, *how[:2], post_w, pre_w, scale, *how[2:])
+    return _Plan(c, [(n, b.shape, b.dtype) for n in (("y", "n") if c.pre else ("y",))], 0, b.device)
 
 
 def residual_norm_backward(b, dy, dn=None, x=None, gate=None, post="rms", pre="rms", post_w=None, pre_w=None, scale=None, groups=1,
@@ -274,34 +342,44 @@ def residual_norm_backward(b, dy, dn=None, x=None, gate=None, post="rms", pre="r
     """Gradients of residual_norm with the same arguments, given those of y (None: zero) and, with pre, of n.  Results: db and,
     for what was given, dx, dgate, dpost_w, dscale, dpre_w (fp32)."""
     out = {} if out is None else out
-    shape = tuple(b.shape)
-    c, b, x, gate, w = _resnorm_config(b, x, gate, post, pre, post_w, pre_w, scale, groups, gate_act, eps)
+    how = (post, pre, groups, gate_act, eps)
+    given = (b, x, gate, post_w, scale, pre_w)
+    plan = _plan("residual_norm_backward", how, (dy, dn) + given, _resnorm_back_plan, dy, dn, given, how)
+    got = _results(out, plan)
+    db, dx, dgate, dpost_w, dscale, dpre_w = got if len(got) == 6 else _spread(got, given)
+    _check(_lib.sf_resnorm_backward(plan.address, b.data_ptr(), _ptr(x), _ptr(gate), _ptr(post_w), _ptr(scale), _ptr(pre_w), _ptr(dy), _ptr(dn),
+                                    dx, db, dgate, dpost_w, dscale, dpre_w, _workspace(out, plan), _stream(stream, plan.device)))
+    return out
+
+
+def _spread(got, given):
+    """The results' addresses at the places of what was given."""
+    got = iter(got)
+    return [None if t is None else next(got) for t in given]
+
+
+def _resnorm_back_plan(dy, dn, given, how):
+    b, x, gate, post_w, scale, pre_w = given
+    c, rows = _resnorm_config(b, x, gate, *how[:2], post_w, pre_w, scale, *how[2:])
     if dn is None and c.pre:
-        _refuse("dn is wanted with pre = %r" % pre)
+        _refuse("dn is wanted with pre = %r" % how[1])
     if dy is None and not c.pre:
         _refuse("dy is wanted")
     if dy is not None:
-        dy = _flat("dy", dy, b)
-        c.dy_stride = dy.stride(0)
+        c.dy_stride = _flat("dy", dy, rows).stride(0)
     if dn is not None:
-        dn = _flat("dn", dn, b)
-        c.dn_stride = dn.stride(0)
-    d, f32, D = b.device, binding._torch().float32, (b.shape[1],)
-    db = _result(out, "db", shape, b.dtype, d)
-    dx = None if x is None else _result(out, "dx", shape, b.dtype, d)
-    dgate = None if gate is None else _result(out, "dgate", shape, b.dtype, d)
-    dw = [None if t is None else _result(out, n, D, f32, d) for n, t in (("dpost_w", post_w), ("dscale", scale), ("dpre_w", pre_w))]
-    L = load_library()
-    ws = _workspace(out, L.sf_resnorm_workspace_bytes(C.byref(c)), d) if any(t is not None for t in dw) else None
-    _check(L.sf_resnorm_backward(C.byref(c), b.data_ptr(), _ptr(x), _ptr(gate), w[0], w[1], w[2], _ptr(dy), _ptr(dn), _ptr(dx),
-                                 db.data_ptr(), _ptr(dgate), _ptr(dw[0]), _ptr(dw[1]), _ptr(dw[2]), ws, _stream(stream, d)))
-    return out
+        c.dn_stride = _flat("dn", dn, rows).stride(0)
+    f32, names = binding._torch().float32, ("db", "dx", "dgate", "dpost_w", "dscale", "dpre_w")
+    results = [(n, b.shape if i < 3 else (c.D,), b.dtype if i < 3 else f32) for i, (n, t) in enumerate(zip(names, given)) if t is not None]
+    n_bytes = _lib.sf_resnorm_workspace_bytes(C.addressof(c))
+    return _Plan(c, results, n_bytes if n_bytes < 0 or any(t is not None for t in given[3:]) else 0, b.device)
 
 
 _ACTS = {"silu": 0, "gelu": 1, "sigmoid": 2}
 
 
 def _ffn_config(x, w_gate, w_up, w_down, act):
+    """The configuration, and x as rows."""
     if not x.is_cuda:
         _refuse("x is not on the GPU")
     if act not in _ACTS:
@@ -321,25 +399,30 @@ def gated_ffn(x, w_gate, w_up, w_down, act="silu", out=None, stream=None):
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T: x [..., D], w_gate and w_up [F,D], w_down [D,F] (all bf16 or all fp32, last
     axis dense); act: "silu", "gelu" or "sigmoid".  Result: y [..., D]."""
     out = {} if out is None else out
-    shape = tuple(x.shape)
-    c, x = _ffn_config(x, w_gate, w_up, w_down, act)
-    y = _result(out, "y", shape, x.dtype, x.device)
-    L = load_library()
-    w = _workspace(out, L.sf_ffn_workspace_bytes(C.byref(c), 0), x.device)
-    _check(L.sf_ffn(C.byref(c), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y.data_ptr(), w, _stream(stream, x.device)))
+    plan = _plan("gated_ffn", act, (x, w_gate, w_up, w_down), _ffn_plan, x, w_gate, w_up, w_down, act)
+    y, = _results(out, plan)
+    _check(_lib.sf_ffn(plan.address, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y, _workspace(out, plan),
+                       _stream(stream, plan.device)))
     return out
+
+
+def _ffn_plan(x, w_gate, w_up, w_down, act):
+    c, _ = _ffn_config(x, w_gate, w_up, w_down, act)
+    return _Plan(c, (("y", x.shape, x.dtype),), _lib.sf_ffn_workspace_bytes(C.addressof(c), 0), x.device)
 
 
 def gated_ffn_backward(x, w_gate, w_up, w_down, dy, act="silu", out=None, stream=None):
     """Gradients of gated_ffn with the same arguments, given that of y.  Results: dx, dw_gate, dw_up, dw_down."""
     out = {} if out is None else out
-    shape, d = tuple(x.shape), x.device
-    c, x = _ffn_config(x, w_gate, w_up, w_down, act)
-    dy = _flat("dy", dy, x)
-    c.dy_stride = dy.stride(0)
-    got = [_result(out, n, s, x.dtype, d) for n, s in (("dx", shape), ("dw_gate", (c.F, c.D)), ("dw_up", (c.F, c.D)), ("dw_down", (c.D, c.F)))]
-    L = load_library()
-    w = _workspace(out, L.sf_ffn_workspace_bytes(C.byref(c), 1), d)
-    _check(L.sf_ffn_backward(C.byref(c), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dy.data_ptr(),
-                             *(t.data_ptr() for t in got), w, _stream(stream, d)))
+    plan = _plan("gated_ffn_backward", act, (x, w_gate, w_up, w_down, dy), _ffn_back_plan, x, w_gate, w_up, w_down, dy, act)
+    dx, dwg, dwu, dwd = _results(out, plan)
+    _check(_lib.sf_ffn_backward(plan.address, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dy.data_ptr(), dx, dwg, dwu, dwd,
+                                _workspace(out, plan), _stream(stream, plan.device)))
     return out
+
+
+def _ffn_back_plan(x, w_gate, w_up, w_down, dy, act):
+    c, rows = _ffn_config(x, w_gate, w_up, w_down, act)
+    c.dy_stride = _flat("dy", dy, rows).stride(0)
+    return _Plan(c, [(n, s, x.dtype) for n, s in (("dx", x.shape), ("dw_gate", (c.F, c.D)), ("dw_up", (c.F, c.D)), ("dw_down", (c.D, c.F)))],
+                 _lib.sf_ffn_workspace_bytes(C.addressof(c), 1), x.device)
