@@ -33,7 +33,7 @@ struct NormArgs {
   void *y, *n, *dx, *db, *dgate;       // dense rows; null where not wanted
   const float *post_w, *pre_w, *scale; // [D] or null
   float* part;                         // backwards: [slots / groups][3][D], see the second kernel
-  int64_t rows;                        // M * groups
+  int64_t rows;                        // M
   int D, Dg, groups;                   // columns, columns of a group
   int post, pre, act;
   float eps;
@@ -132,8 +132,15 @@ struct Row {
     }
   }
   __device__ static void weights(float (*x)[8], const float* w, int lane, int Dg) {
+    const bool whole = VEC && (reinterpret_cast<uintptr_t>(w) & 15) == 0;
 #pragma unroll
     for (int v = 0; v < V; ++v)
+      if (whole) {
+        const int c = col(v, 0, lane);
+#pragma unroll
+        for (int j = 0; j < 8; j += 4)
+          *(f32x4*)&x[v][j] = c >= Dg ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : w ? *(const f32x4*)(w + c + j) : f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+      } else
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int c = col(v, j, lane);
@@ -142,17 +149,30 @@ struct Row {
   }
 };
 
+// x plus what another lane of its 16 has: quad_perm, mirrored halves of 8, mirrored 16 (no trip through LDS)
+template <int CONTROL>
+__device__ inline float plus_lane(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xF, 0xF, false));
+}
 // Sums over the lanes of a row, of two numbers at once; with 256 lanes over LDS (two areas in turn: one barrier a sum).
 template <int LPR>
 struct Sum {
   float (*area)[8];
   int turn;
   __device__ void operator()(float& a, float& b) {
-    constexpr int W = LPR < 64 ? LPR : 64;
-#pragma unroll
-    for (int m = W / 2; m >= 1; m >>= 1) {
-      a += __shfl_xor(a, m);
-      b += __shfl_xor(b, m);
+    a = plus_lane<0x141>(plus_lane<0x4E>(plus_lane<0xB1>(a)));  // lanes 1, 2 apart, then the other four of eight
+    b = plus_lane<0x141>(plus_lane<0x4E>(plus_lane<0xB1>(b)));
+    if constexpr (LPR > 8) {
+      a = plus_lane<0x140>(a);
+      b = plus_lane<0x140>(b);
+    }
+    if constexpr (LPR > 16) {
+      a += __shfl_xor(a, 16);
+      b += __shfl_xor(b, 16);
+    }
+    if constexpr (LPR > 32) {
+      a += __shfl_xor(a, 32);
+      b += __shfl_xor(b, 32);
     }
     if constexpr (LPR == 256) {
       float* s = area[turn];
@@ -192,7 +212,7 @@ __device__ inline float normalise(float (*x)[8], int how, int Dg, float eps, int
 #pragma unroll
     for (int j = 0; j < 8; ++j) a += x[v][j] * x[v][j];
   sum(a, b);
-  const float r = 1.0f / sqrtf(a * inv + eps);
+  const float r = __builtin_amdgcn_rsqf(a * inv + eps);  // (its result is off by one unit in the last place at most)
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -212,16 +232,20 @@ __device__ inline void normalise_back(float (*d)[8], float (*unit)[8], float r, 
       b += d[v][j];
     }
   sum(a, b);
-  a /= (float)Dg;
-  b = how == SF_NORM_LAYER ? b / (float)Dg : 0.0f;
+  const float inv = 1.0f / (float)Dg;
+  a *= inv * r;
+  b *= inv;
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) d[v][j] = Row::col(v, j, lane) < Dg ? r * (d[v][j] - b - unit[v][j] * a) : 0.0f;
+    for (int j = 0; j < 8; ++j) {  // (past Dg both are zero)
+      if (how == SF_NORM_LAYER) d[v][j] = Row::col(v, j, lane) < Dg ? d[v][j] - b : 0.0f;
+      d[v][j] = r * d[v][j] - unit[v][j] * a;
+    }
 }
 
 template <int DTYPE, int LPR, int V, bool VEC, bool BACK>
-__global__ __launch_bounds__(kThreads) void resnorm_kernel(NormArgs g) {
+__global__ __launch_bounds__(kThreads, BACK && V == 1 ? 2 : 1) void resnorm_kernel(NormArgs g) {
   typedef Row<DTYPE, LPR, V, VEC> R;
   typedef Io<DTYPE> I;
   constexpr int RPW = kThreads / LPR;  // rows of a workgroup at a time
@@ -229,9 +253,23 @@ __global__ __launch_bounds__(kThreads) void resnorm_kernel(NormArgs g) {
   extern __shared__ float columns[];   // backwards: [4 waves][3][Dg], where several groups of lanes are added
   const int lane = threadIdx.x % LPR;
   const int64_t slot = (int64_t)blockIdx.x * RPW + threadIdx.x / LPR, slots = (int64_t)gridDim.x * RPW;
-  const int group = (int)(slot % g.groups), Dg = g.Dg, c0 = group * Dg;  // (slots is a multiple of groups: a slot's rows are of one)
+  // (slots is a multiple of groups: a slot's rows are of one group, and `next` apart)
+  const int group = (int)(slot % g.groups), Dg = g.Dg, c0 = group * Dg;
+  const int64_t first = slot / g.groups, next = slots / g.groups;
   Sum<LPR> sum = {area, 0};
 
+  R rb, rx, rg, rdy, rdn;
+  auto request = [&](int64_t m) {
+    rb.load(g.b, m * g.b_s + c0, lane, Dg);
+    if (g.x) rx.load(g.x, m * g.x_s + c0, lane, Dg);
+    if (g.gate) rg.load(g.gate, m * g.gate_s + c0, lane, Dg);
+    if constexpr (BACK) {
+      if (g.dy) rdy.load(g.dy, m * g.dy_s + c0, lane, Dg);
+      if (g.dn) rdn.load(g.dn, m * g.dn_s + c0, lane, Dg);
+    }
+  };
+  // (with 256 lanes a row is the workgroup's, so that all of it leaves the loop together)
+  if (first < g.rows) request(first);
   float wpost[V][8], wpre[V][8], ws[V][8];
   R::weights(wpost, g.post_w ? g.post_w + c0 : nullptr, lane, Dg);
   R::weights(wpre, g.pre_w ? g.pre_w + c0 : nullptr, lane, Dg);
@@ -242,20 +280,7 @@ __global__ __launch_bounds__(kThreads) void resnorm_kernel(NormArgs g) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) spost[v][j] = spre[v][j] = ss[v][j] = 0.0f;
 
-  R rb, rx, rg, rdy, rdn;
-  auto request = [&](int64_t row) {
-    const int64_t m = row / g.groups;
-    rb.load(g.b, m * g.b_s + c0, lane, Dg);
-    if (g.x) rx.load(g.x, m * g.x_s + c0, lane, Dg);
-    if (g.gate) rg.load(g.gate, m * g.gate_s + c0, lane, Dg);
-    if constexpr (BACK) {
-      if (g.dy) rdy.load(g.dy, m * g.dy_s + c0, lane, Dg);
-      if (g.dn) rdn.load(g.dn, m * g.dn_s + c0, lane, Dg);
-    }
-  };
-  // (with 256 lanes a row is the workgroup's, so that all of it leaves the loop together)
-  if (slot < g.rows) request(slot);
-  for (int64_t row = slot; row < g.rows; row += slots) {
+  for (int64_t m = first; m < g.rows; m += next) {
     float u[V][8], y[V][8], gt[V][8], d[V][8], e[V][8];
     rb.values(u);
     if (g.x) rx.values(y);
@@ -264,8 +289,8 @@ __global__ __launch_bounds__(kThreads) void resnorm_kernel(NormArgs g) {
       if (g.dy) rdy.values(d);
       if (g.dn) rdn.values(e);
     }
-    if (row + slots < g.rows) request(row + slots);
-    const int64_t to = row / g.groups * g.D + c0;
+    if (m + next < g.rows) request(m + next);
+    const int64_t to = m * g.D + c0;
 
     const float r = normalise<V, R>(u, g.post, Dg, g.eps, lane, sum);
     float a[V][8];  // scale times the gate's activation
@@ -363,19 +388,30 @@ __global__ __launch_bounds__(kThreads) void resnorm_kernel(NormArgs g) {
   }
 }
 
-// Sums of the workgroups' partial sums: 64 columns by 16 lanes per workgroup.
+// Sums of the workgroups' partial sums: 32 columns by 32 lanes per workgroup, eight loads of a lane under way.
 __global__ __launch_bounds__(1024) void resnorm_sum_kernel(const float* part, int parts, int D, float* post, float* scale, float* pre) {
-  __shared__ float s[16][64];
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6, c = blockIdx.x * 64 + x;
+  __shared__ float s[32][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
   float a = 0.0f;
-  if (c < 3 * D)
-    for (int i = y; i < parts; i += 16) a += part[(size_t)i * 3 * D + c];
+  if (c < 3 * D) {
+    const float* p = part + c;
+    const size_t pitch = (size_t)3 * D;
+    int i = y;
+    for (; i + 224 < parts; i += 256) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = p[(i + 32 * j) * pitch];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a += v[j];
+    }
+    for (; i < parts; i += 32) a += p[i * pitch];
+  }
   s[y][x] = a;
   __syncthreads();
   if (y != 0 || c >= 3 * D) return;
   a = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) a += s[i][x];
+  for (int i = 0; i < 32; ++i) a += s[i][x];
   float* const to = c < D ? post : c < 2 * D ? scale : pre;
   if (to) to[c % D] = a;
 }
@@ -428,8 +464,8 @@ bool fits(const void* p, size_t align, bool optional) {
   return p ? (reinterpret_cast<uintptr_t>(p) & (align - 1)) == 0 : optional;
 }
 
-// Workgroups: every lane group a row, but backwards no more than leave few partial sums (512: two for each CU; the next
-// row's loads are under way besides), and a multiple of the groups.
+// Workgroups: every lane group a row, but backwards no more than leave few partial sums (512: two for each CU; the
+// next row's loads are under way besides), and a multiple of the groups.
 int grid_of(const sf_resnorm_config* c, bool back) {
   const int rpw = kThreads / shape_of(c->D / c->groups).lpr;
   int64_t n = ((int64_t)c->M * c->groups + rpw - 1) / rpw;
@@ -490,7 +526,7 @@ NormArgs common(const sf_resnorm_config* c, const void* b, const void* x, const 
   g.post_w = c->post == SF_NORM_NONE ? nullptr : post_w;
   g.scale = scale;
   g.pre_w = pre_w;
-  g.rows = (int64_t)c->M * c->groups;
+  g.rows = c->M;
   g.D = c->D;
   g.groups = c->groups;
   g.Dg = c->D / c->groups;
@@ -571,7 +607,7 @@ extern "C" int sf_resnorm_backward(const sf_resnorm_config* cfg, const void* b, 
   const hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   rc = run<true>(fn, cfg, g, st);  // (no rows: the partial sums are zeros)
   if (rc != SF_OK || !sums) return rc;
-  resnorm_sum_kernel<<<(3 * cfg->D + 63) / 64, 1024, 0, st>>>(g.part, parts_of(cfg), cfg->D, dpost_w, dscale, dpre_w);
+  resnorm_sum_kernel<<<(3 * cfg->D + 31) / 32, 1024, 0, st>>>(g.part, parts_of(cfg), cfg->D, dpost_w, dscale, dpre_w);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) {
     set_error("%s: launch failed: %s", fn, hipGetErrorString(err));
