@@ -27,7 +27,7 @@ extern "C" {
  * done = 1 at the first step of an episode, as in sf_policy_unroll; what lies before it does not reach past
  * it, NaN and infinities included, and no step reaches an earlier one.  Key and value heads may be shared: head h
  * reads key/value head h / (H / Hk).
- * The passes over trajectories compute this in chunks of 32 or 64 steps (two matrix products inside a chunk, the
+ * The passes over trajectories compute this in chunks of 32 steps (two matrix products inside a chunk, the
  * state between chunks), and where rows x heads are few, T is cut into pieces whose states are joined.
  *
  * Arrays are time-major: q [T][N][H][dk], k [T][N][Hk][dk], v [T][N][Hk][dv], o and its gradient [T][N][H][dv], io;
@@ -38,7 +38,7 @@ extern "C" {
  *   done       dev [T][N] bytes or NULL (no episode begins)
  *   state0     dev [N][H][dk][dv] fp32 or NULL (zero); state, dstate, dstate0 alike (NULL: not wanted / zero)
  * Errors: SF_ERR_ARG (null or misaligned pointer, struct_size, dtype), SF_ERR_SHAPE (T, N < 0; H, Hk < 1;
- * H % Hk != 0; dk or dv outside 1..128; T * N beyond 2^31 - 1, N * H beyond 2^22; scale not finite), SF_ERR_DEVICE. */
+ * H % Hk != 0; dk or dv outside 1..128; T * N beyond 2^31 - 1, N * H beyond 2^21; scale not finite), SF_ERR_DEVICE. */
 typedef struct {
   uint32_t struct_size; /* sizeof(sf_linattn_config) */
   int32_t dtype;        /* SF_DTYPE_* of q, k, v, o and their gradients */

@@ -1,4 +1,4 @@
-// Linear attention with a decay for each head (include/sf_memory.h), in chunks of C steps:
+// Linear attention with a decay for each head (include/sf_memory.h), in chunks of C = 32 steps:
 //   inside a chunk  o_i += sum over j <= i, same episode: g^(i-j) (q_i . k_j) v_j
 //   from before     o_i += g^(i+1) S q_i          where no episode begins up to i
 //   the state       S <- g^n S + sum_j g^(n-1-j) k_j v_j^T   (terms from before the chunk's last episode begin: none)
@@ -7,8 +7,8 @@
 //   R_t = scale q_t do_t^T + g R_{t+1}.
 // So there is one kernel, told by LinOp what stands where; a launch of the backward pass runs all three.
 //
-// A workgroup of four waves walks the chunks of one (row, head), or of one piece of T.  Wave w owns a quarter of
-// v's columns: its part of the state stays in registers as the accumulator of the update.  The products are arranged
+// A workgroup of four waves walks the chunks of one (row, head), or of one piece of T, for 64 columns of v.  A wave owns 16
+// of them: its part of the state stays in registers as the accumulator of the update.  The products are arranged
 // so that accumulators feed the next product without a shuffle: a 16x16 accumulator holds rows 4g .. 4g+3 of one
 // column per lane (g = lane / 16), two of them are the eight K-slots of an operand of 16x16x32, and the other operand
 // follows the same numbering of the K axis.
@@ -73,6 +73,7 @@ struct LinArgs {
   const float* log_decay;
   const uint8_t* done;  // or null
   int T, N, H, ops;
+  int blocks_v;         // of 64 columns of the widest v
   int n_seg, seg_len;   // pieces of T (seg_len a multiple of every C)
   float* seg_state;     // n_seg > 1: [op][N * H][n_seg][dk * dv], first the pieces' own states, then what enters them
   float* seg_keep;      // [op][N * H][n_seg] g^length, 0 if an episode begins in the piece
@@ -248,16 +249,20 @@ __device__ inline float finite_test(const unsigned* w, float acc) {
   return acc;
 }
 
-template <int DTYPE, int D, int C>
+constexpr int C = 32;   // steps of a chunk
+constexpr int DV = 64;  // columns of v of a workgroup: 16 a wave
+
+template <int DTYPE, int D>
 struct Lds {
   typedef Num<DTYPE> M;
   // of a row: 4 times an odd number of words, so that 16 rows' pieces of 16 bytes lie in different banks; of those 36 and 12
   // mod 64 also keep the transposing read's four rows of 32 bytes apart
-  static constexpr int kPitch = D * M::kBytes + (M::kBytes == 2 && D == 128 ? 48 : 16);
-  static constexpr int kTile = C * kPitch;
-  static constexpr int kFrags = (C / 16) * (C / 32);
+  static constexpr int pitch(int columns) { return columns * M::kBytes + (M::kBytes == 2 && columns == 128 ? 48 : 16); }
+  static constexpr int kPitch = pitch(D), kPitchV = pitch(DV);
+  static constexpr int kK = C * kPitch, kV = 2 * C * kPitch;
+  static constexpr int kFrags = C / 16;                     // operands of P: 32 steps j, 16 steps i
   static constexpr int kTermPitch = kFrags * 1024;
-  static constexpr int kP = 3 * kTile;                      // two terms (or halves) of kFrags x 64 lanes x 16 bytes
+  static constexpr int kP = kV + C * kPitchV;               // two terms (or halves) of kFrags x 64 lanes x 16 bytes
   static constexpr int kEp = kP + 2 * kTermPitch;           // int [C]: episode of the step, counted in the chunk
   static constexpr int kW = kEp + C * 4;                    // float [C]: weight of the step's term in the state
   static constexpr int kFlag = kW + C * 4;                  // int [2]: the chunk holds something not finite
@@ -266,22 +271,23 @@ struct Lds {
 
 // STATE: only the piece's own state (from zero) and whether an episode begins in it.
 // How much of a call is known at compile time: kAny; kPieces: all rows are read and written in 16-byte pieces; kWhole: k and v
-// have D columns besides (else columns past theirs are left out, 32 of k, 16 of v at a time).
+// have whole tiles besides, D and a multiple of 64 columns (else columns past theirs are left out, 32 of k, 16 of v at a time).
 enum Known { kAny = 0, kPieces = 1, kWhole = 2 };
-template <int DTYPE, int D, int C, bool STATE, int KNOWN>
-__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinArgs g) {
+template <int DTYPE, int D, bool STATE, int KNOWN>
+__global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void linattn_kernel(LinArgs g) {
   typedef Num<DTYPE> M;
-  typedef Lds<DTYPE, D, C> L;
-  constexpr int W = M::kPieceWords, NP = C * D / 8 / kThreads;  // pieces of a tile per thread
-  constexpr int NV = D / 64, ND = D / 16, NC = C / 32;          // a wave's tiles of v; tiles of k; K-steps over C
-  static_assert(NP >= 1 && (C == 32 || C == 64), "whole pieces");
+  typedef Lds<DTYPE, D> L;
+  constexpr int W = M::kPieceWords, NP = C * D / 8 / kThreads;  // pieces of a tile of q or k per thread; one of v's
+  constexpr int ND = D / 16;                                    // tiles of k
+  static_assert(C * DV / 8 == kThreads && C == 32, "a piece of v per thread, one operand for the chunk's steps");
   constexpr bool WHOLE = KNOWN == kWhole;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   // the ops of one (row, head) read the same arrays: one after another on one XCD (workgroups go to the 8 in turn)
-  const int round = blockIdx.x / (8 * g.ops), in_round = blockIdx.x % (8 * g.ops), which = in_round / 8;
+  const int per = 8 * g.ops * g.blocks_v, round = blockIdx.x / per, in_round = blockIdx.x % per;
+  const int which = in_round / 8 % g.ops, v_block = in_round / (8 * g.ops) * DV;
   const int bh = round * 8 + in_round % 8;
-  if (bh >= g.N * g.H) return;
   const LinOp op = g.op[which];
+  if (bh >= g.N * g.H || v_block >= op.v.d) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
   const int n = bh / g.H, h = bh % g.H, seg = blockIdx.y;
@@ -295,16 +301,13 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
   const unsigned char* krow = (const unsigned char*)op.k.p + (n * op.k.sn + h / op.k.div * op.k.sh) * M::kBytes;
   const unsigned char* vrow = (const unsigned char*)op.v.p + (n * op.v.sn + h / op.v.div * op.v.sh) * M::kBytes;
 
-  // column of v of this wave's tile t, operand row (or accumulator column) m: up to 64 columns one tile a wave
-  const bool two = WHOLE ? NV == 2 : NV == 2 && dv > 64;
-  const int v0 = two ? 32 * wave : 16 * wave;  // (a wave past dv has nothing to do)
-  auto col_v = [&](int t, int m) { return two ? v0 + 8 * (m >> 2) + 4 * t + (m & 3) : v0 + 64 * t + m; };
-  auto has_v = [&](int t) { return WHOLE || (v0 < dv && (t == 0 || two)); };
+  const int v0 = v_block + 16 * wave;  // this wave's columns of v (past dv: nothing to do)
+  const bool has_v = WHOLE || v0 < dv;
   auto has_k = [&](int s) { return WHOLE || 32 * s < dk; };  // columns 32 s .. of k
   // column of k of tile t (two tiles are 32 columns: eight neighbours per lane group)
   auto col_k = [&](int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); };
 
-  f32x4 S[ND][NV];
+  f32x4 S[ND];
   {
     const float* s = nullptr;
     int64_t sa = op.s_a, sb = op.s_b;
@@ -319,25 +322,22 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
     }
     const int xk = anew(dk), yv = anew(dv);
     const bool four = KNOWN != kAny && sa == 1 && (reinterpret_cast<uintptr_t>(s) & 15) == 0;  // neighbours of k lie side by side
+    const int y = v0 + li;
 #pragma unroll
     for (int a = 0; a < ND; ++a) {
+      const int x = col_k(a, 4 * lg);
+      if (four) {  // (columns of k are a multiple of eight)
+        S[a] = s && (WHOLE || (x < xk && y < yv)) ? *(const f32x4*)(s + x + y * sb) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      } else {
 #pragma unroll
-      for (int b = 0; b < NV; ++b)
-        if (four) {  // (columns of k are a multiple of eight)
-          const int x = col_k(a, 4 * lg), y = col_v(b, li);
-          S[a][b] = s && (WHOLE || (x < xk && y < yv)) ? *(const f32x4*)(s + x + y * sb) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        } else
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int x = col_k(a, 4 * lg + r), y = col_v(b, li);
-          S[a][b][r] = s && (WHOLE || (x < xk && y < yv)) ? s[x * sa + y * sb] : 0.0f;
-        }
+        for (int r = 0; r < 4; ++r) S[a][r] = s && (WHOLE || (x + r < xk && y < yv)) ? s[(x + r) * sa + y * sb] : 0.0f;
+      }
       __builtin_amdgcn_sched_barrier(0);  // (the addresses of all at once would fill the registers)
     }
   }
 
   // the chunk that is on its way: its rows and its episode marks
-  unsigned nq[NP][W], nk[NP][W], nv[NP][W];
+  unsigned nq[NP][W], nk[NP][W], nv[W];
   int n_done = 0;
   auto step_of = [&](int i) { return op.reverse ? g.T - 1 - i : i; };
   int alone_to = t_begin;  // steps before this one are chunks of their own
@@ -351,7 +351,12 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
       const int64_t t = step_of(live ? c0 + r : t_end - 1);
       if constexpr (!STATE) load_piece<DTYPE, KNOWN != kAny>(nq[p], op.q, qrow + t * op.q.st * M::kBytes, col, live);
       load_piece<DTYPE, KNOWN != kAny>(nk[p], op.k, krow + t * op.k.st * M::kBytes, col, live);
-      load_piece<DTYPE, KNOWN != kAny>(nv[p], op.v, vrow + t * op.v.st * M::kBytes, col, live);
+    }
+    {
+      const int r = tid / (DV / 8);
+      const bool live = r < valid;
+      const int64_t t = step_of(live ? c0 + r : t_end - 1);
+      load_piece<DTYPE, KNOWN != kAny>(nv, op.v, vrow + t * op.v.st * M::kBytes, v_block + tid % (DV / 8) * 8, live);
     }
     n_done = 0;
     if (g.done && lane < C && lane < valid) {
@@ -361,8 +366,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
     }
   };
   unsigned char* const tq = lds;
-  unsigned char* const tk = lds + L::kTile;
-  unsigned char* const tv = lds + 2 * L::kTile;
+  unsigned char* const tk = lds + L::kK;
+  unsigned char* const tv = lds + L::kV;
   int* const ep = (int*)(lds + L::kEp);
   float* const wgt = (float*)(lds + L::kW);
   int* const flag = (int*)(lds + L::kFlag);
@@ -373,7 +378,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
   for (int c0 = t_begin, turn = 0, step; c0 < t_end; c0 += step, turn ^= 1) {
     const int valid = width(c0);
     const int late = c0 == 0 && op.reverse ? 1 : 0;  // the state enters undecayed
-    const unsigned long long marks = __ballot(n_done != 0);
+    const unsigned marks = (unsigned)__ballot(n_done != 0);  // (lanes below C)
     __syncthreads();  // the chunk before has been read
     float test = 0.0f;
 #pragma unroll
@@ -383,14 +388,19 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
       for (int i = 0; i < W; i += 4) {
         if constexpr (!STATE) *(u32x4*)(tq + at + 4 * i) = *(u32x4*)(nq[p] + i);
         *(u32x4*)(tk + at + 4 * i) = *(u32x4*)(nk[p] + i);
-        *(u32x4*)(tv + at + 4 * i) = *(u32x4*)(nv[p] + i);
       }
-      test = finite_test<DTYPE>(nk[p], finite_test<DTYPE>(nv[p], test));
+      test = finite_test<DTYPE>(nk[p], test);
+    }
+    {
+      const int at = tid / (DV / 8) * L::kPitchV + tid % (DV / 8) * 8 * M::kBytes;
+#pragma unroll
+      for (int i = 0; i < W; i += 4) *(u32x4*)(tv + at + 4 * i) = *(u32x4*)(nv + i);
+      test = finite_test<DTYPE>(nv, test);
     }
     if (test != 0.0f) flag[turn] = 1;
-    const int ep_end = __popcll(marks);
+    const int ep_end = __popc(marks);
     if (tid < C) {
-      const int e = __popcll(marks & ((2ull << tid) - 1));
+      const int e = __popc(marks & ((2u << tid) - 1));
       ep[tid] = e;
       wgt[tid] = e == ep_end && tid < valid ? op.w_scale * pow2(l2 * (float)(valid - 1 - tid)) : 0.0f;
     }
@@ -424,151 +434,103 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
             acc[r] = j <= i && ej[r] == e ? acc[r] * (op.w_scale * pow2(l2 * (float)(i - j))) : 0.0f;
           }
         }
-        M::put4(lds + L::kP + (I * NC + J / 2) * 1024, L::kTermPitch, lane, J & 1, acc);
+        M::put4(lds + L::kP + I * 1024, L::kTermPitch, lane, J, acc);
       };
-      if constexpr (C == 64) {
-#pragma unroll
-        for (int J = 0; J < 4; ++J)
-          if (J <= (wave | 1)) tile_p(wave, J);
-      } else {
-        tile_p(wave >> 1, wave & 1);
-      }
+      tile_p(wave >> 1, wave & 1);
     }
     __syncthreads();
 
-    // V^T of this wave's columns: K-slots 0..3 are steps 32 p + 4 g .., 4..7 are 16 further on
-    typename M::Raw vt[NC][NV];
+    // V^T of this wave's columns: K-slots 0..3 are steps 4 g .., 4..7 are 16 further on
+    typename M::Raw vt;
+    if (has_v) {
+      if constexpr (DTYPE == SF_DTYPE_BF16) {
+        const unsigned char* at = tv + (4 * lg + (li >> 2)) * L::kPitchV + (16 * wave + 4 * (li & 3)) * M::kBytes;
+        const u32x2 x = M::column4(at), y = M::column4(at + 16 * L::kPitchV);
+        vt = u32x4{x[0], x[1], y[0], y[1]};
+      } else {
 #pragma unroll
-    for (int p = 0; p < NC; ++p)
-#pragma unroll
-      for (int b = 0; b < NV; ++b) {
-        if (!has_v(b)) continue;
-        if constexpr (DTYPE == SF_DTYPE_BF16) {
-          const unsigned char* at = tv + (32 * p + 4 * lg + (li >> 2)) * L::kPitch + col_v(b, 4 * (li & 3)) * M::kBytes;
-          const u32x2 x = M::column4(at), y = M::column4(at + 16 * L::kPitch);
-          vt[p][b] = u32x4{x[0], x[1], y[0], y[1]};
-        } else {
-#pragma unroll
-          for (int r = 0; r < 8; ++r)
-            vt[p][b].x[r] = M::element(tv + (32 * p + 4 * lg + (r & 3) + 16 * (r >> 2)) * L::kPitch + col_v(b, li) * M::kBytes);
-        }
+        for (int r = 0; r < 8; ++r)
+          vt.x[r] = M::element(tv + (4 * lg + (r & 3) + 16 * (r >> 2)) * L::kPitchV + (16 * wave + li) * M::kBytes);
       }
+    }
 
-    if constexpr (!STATE) {
+    if (!STATE && has_v) {
       // what the state gives all steps (two accumulator tiles of it are one operand), scaled per step, and on top of it what
       // the chunk's own steps give
-      f32x4 out[C / 16][NV];
+      f32x4 out[C / 16];
 #pragma unroll
-      for (int I = 0; I < C / 16; ++I)
-#pragma unroll
-        for (int b = 0; b < NV; ++b) out[I][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int I = 0; I < C / 16; ++I) out[I] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) {
         if (!has_k(s)) continue;
+        float x[8];
 #pragma unroll
-        for (int b = 0; b < NV; ++b) {
-          if (!has_v(b)) continue;
-          float x[8];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            x[r] = S[2 * s][b][r];
-            x[4 + r] = S[2 * s + 1][b][r];
-          }
-          const typename M::Out st = M::out_terms(x);
-#pragma unroll
-          for (int I = 0; I < C / 16; ++I)
-            out[I][b] = M::mma(st, M::row(tq + (16 * I + li) * L::kPitch + (32 * s + 8 * lg) * M::kBytes), out[I][b]);
+        for (int r = 0; r < 4; ++r) {
+          x[r] = S[2 * s][r];
+          x[4 + r] = S[2 * s + 1][r];
         }
+        const typename M::Out st = M::out_terms(x);
+#pragma unroll
+        for (int I = 0; I < C / 16; ++I)
+          out[I] = M::mma(st, M::row(tq + (16 * I + li) * L::kPitch + (32 * s + 8 * lg) * M::kBytes), out[I]);
       }
 #pragma unroll
       for (int I = 0; I < C / 16; ++I) {
         const int i = 16 * I + li;
-        const bool reach = (marks & ((2ull << i) - 1)) == 0;  // no episode has begun: the state is this step's
+        const bool reach = (marks & ((2u << i) - 1)) == 0;  // no episode has begun: the state is this step's
         const float c = pow2(l2 * (float)(i + 1 - late));
-        f32x4* own = out[I];
+        f32x4 own = out[I];
 #pragma unroll
-        for (int b = 0; b < NV; ++b)
+        for (int r = 0; r < 4; ++r) own[r] = reach ? c * own[r] : 0.0f;
+        own = M::mma(vt, M::get(lds + L::kP + I * 1024, L::kTermPitch, lane), own);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) own[b][r] = reach ? c * own[b][r] : 0.0f;
+        for (int r = 0; r < 4; ++r) own[r] *= op.alpha;
+        const int y = v0 + 4 * lg;  // four neighbours
+        if (i >= valid || y >= dv) continue;
+        const int64_t at = n * op.on + h * op.oh + step_of(c0 + i) * op.ot + y;
+        if (KNOWN != kAny || op.o_vec) {
+          if (op.o_f32) *(f32x4*)((float*)op.o + at) = own;
+          else *(u32x2*)((uint16_t*)op.o + at) = u32x2{pack_bf16(own[0], own[1]), pack_bf16(own[2], own[3])};
+        } else {
 #pragma unroll
-        for (int p = 0; p <= I / 2; ++p) {
-          const typename M::Out x = M::get(lds + L::kP + (I * NC + p) * 1024, L::kTermPitch, lane);
-#pragma unroll
-          for (int b = 0; b < NV; ++b)
-            if (has_v(b)) own[b] = M::mma(vt[p][b], x, own[b]);
-        }
-#pragma unroll
-        for (int b = 0; b < NV; ++b)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) own[b][r] *= op.alpha;
-        if (i < valid) {
-          const int64_t at = n * op.on + h * op.oh + step_of(c0 + i) * op.ot;
-          if ((KNOWN != kAny || op.o_vec) && DTYPE == SF_DTYPE_BF16 && !op.o_f32 && two) {  // eight neighbours
-            const int y = col_v(0, 4 * lg);
-            if (NV == 2 && y < dv)
-              *(u32x4*)((uint16_t*)op.o + at + y) = u32x4{pack_bf16(own[0][0], own[0][1]), pack_bf16(own[0][2], own[0][3]),
-                                                          pack_bf16(own[NV - 1][0], own[NV - 1][1]), pack_bf16(own[NV - 1][2], own[NV - 1][3])};
-          } else {
-#pragma unroll
-            for (int b = 0; b < NV; ++b) {
-              const int y = col_v(b, 4 * lg);  // four neighbours
-              if (!has_v(b) || y >= dv) continue;
-              if (KNOWN != kAny || op.o_vec) {
-                if (op.o_f32) *(f32x4*)((float*)op.o + at + y) = own[b];
-                else *(u32x2*)((uint16_t*)op.o + at + y) = u32x2{pack_bf16(own[b][0], own[b][1]), pack_bf16(own[b][2], own[b][3])};
-              } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                  if (y + r >= dv) continue;
-                  if (op.o_f32) ((float*)op.o)[at + y + r] = own[b][r];
-                  else M::store((unsigned char*)op.o + (at + y + r) * M::kBytes, own[b][r]);
-                }
-              }
-            }
+          for (int r = 0; r < 4; ++r) {
+            if (y + r >= dv) continue;
+            if (op.o_f32) ((float*)op.o)[at + r] = own[r];
+            else M::store((unsigned char*)op.o + (at + r) * M::kBytes, own[r]);
           }
         }
       }
     }
 
-    const float keep = marks ? 0.0f : pow2(l2 * (float)(valid - late));
+    const float keep = pow2(l2 * (float)(valid - late));
 #pragma unroll
     for (int a = 0; a < ND; ++a)
 #pragma unroll
-      for (int b = 0; b < NV; ++b)
+      for (int r = 0; r < 4; ++r) S[a][r] = marks ? 0.0f : keep * S[a][r];
+    if (has_v) {
+      const f32x4 w0 = *(const f32x4*)(wgt + 4 * lg), w1 = *(const f32x4*)(wgt + 16 + 4 * lg);
+      float x[8];
+      M::values(vt, x);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[a][b][r] = marks ? 0.0f : keep * S[a][b][r];
-#pragma unroll
-    for (int p = 0; p < NC; ++p) {
-      typename M::Sum vw[NV];
-      const f32x4 w0 = *(const f32x4*)(wgt + 32 * p + 4 * lg), w1 = *(const f32x4*)(wgt + 32 * p + 16 + 4 * lg);
-#pragma unroll
-      for (int b = 0; b < NV; ++b) {
-        if (!has_v(b)) continue;
-        float x[8];
-        M::values(vt[p][b], x);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[r] *= w0[r];
-          x[4 + r] *= w1[r];
-        }
-        vw[b] = M::sum_terms(x);
+      for (int r = 0; r < 4; ++r) {
+        x[r] *= w0[r];
+        x[4 + r] *= w1[r];
       }
+      const typename M::Sum vw = M::sum_terms(x);
 #pragma unroll
       for (int a = 0; a < ND; ++a) {
         if (!has_k(a / 2)) continue;
         typename M::Raw kt;
         if constexpr (DTYPE == SF_DTYPE_BF16) {
-          const unsigned char* at = tk + (32 * p + 4 * lg + (li >> 2)) * L::kPitch + col_k(a, 4 * (li & 3)) * M::kBytes;
-          const u32x2 x = M::column4(at), y = M::column4(at + 16 * L::kPitch);
-          kt = u32x4{x[0], x[1], y[0], y[1]};
+          const unsigned char* at = tk + (4 * lg + (li >> 2)) * L::kPitch + col_k(a, 4 * (li & 3)) * M::kBytes;
+          const u32x2 y = M::column4(at), z = M::column4(at + 16 * L::kPitch);
+          kt = u32x4{y[0], y[1], z[0], z[1]};
         } else {
 #pragma unroll
           for (int r = 0; r < 8; ++r)
-            kt.x[r] = M::element(tk + (32 * p + 4 * lg + (r & 3) + 16 * (r >> 2)) * L::kPitch + col_k(a, li) * M::kBytes);
+            kt.x[r] = M::element(tk + (4 * lg + (r & 3) + 16 * (r >> 2)) * L::kPitch + col_k(a, li) * M::kBytes);
         }
-#pragma unroll
-        for (int b = 0; b < NV; ++b)
-          if (has_v(b)) S[a][b] = M::mma(kt, vw[b], S[a][b]);
+        S[a] = M::mma(kt, vw, S[a]);
       }
     }
   }
@@ -581,7 +543,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
     s = g.seg_state + seg_at * ((size_t)dk * dv);
     sa = dv;
     sb = 1;
-    if (tid == 0)
+    if (tid == 0 && v_block == 0)
       g.seg_keep[seg_at] = any_done ? 0.0f : pow2(l2 * (float)(t_end - t_begin - (seg == 0 && op.reverse ? 1 : 0)));
   } else if (op.s_out && seg == g.n_seg - 1) {
     s = op.s_out + (size_t)bh * dk * dv;
@@ -591,16 +553,14 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void linattn_kernel(LinA
     }
   }
   if (s) {
-    const int xk = anew(dk), yv = anew(dv);
+    const int xk = anew(dk), yv = anew(dv), y = v0 + li;
 #pragma unroll
     for (int a = 0; a < ND; ++a) {
 #pragma unroll
-      for (int b = 0; b < NV; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int x = col_k(a, 4 * lg + r), y = col_v(b, li);
-          if (WHOLE || (x < xk && y < yv)) s[x * sa + y * sb] = zero ? 0.0f : f * S[a][b][r];
-        }
+      for (int r = 0; r < 4; ++r) {
+        const int x = col_k(a, 4 * lg + r);
+        if (WHOLE || (x < xk && y < yv)) s[x * sa + y * sb] = zero ? 0.0f : f * S[a][r];
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -731,8 +691,8 @@ int check(const sf_linattn_config* c, const char* fn) {
     set_error("%s: T = %d, N = %d, H = %d, Hk = %d, dk = %d, dv = %d out of range", fn, c->T, c->N, c->H, c->Hk, c->dk, c->dv);
     return SF_ERR_SHAPE;
   }
-  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > 1 << 22) {
-    set_error("%s: T * N beyond 2^31 - 1 or N * H beyond 2^22", fn);
+  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > 1 << 21) {
+    set_error("%s: T * N beyond 2^31 - 1 or N * H beyond 2^21", fn);
     return SF_ERR_SHAPE;
   }
   if (!isfinite(c->scale)) {
@@ -804,29 +764,35 @@ void put_out(const sf_linattn_config* c, LinOp& op, void* p, int64_t t, int64_t 
   op.o_vec = d % 8 == 0 && t % per == 0 && n % per == 0 && h % per == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 }
 
-template <int DTYPE, int D, int C, bool STATE, int KNOWN>
+template <int DTYPE, int D, bool STATE, int KNOWN>
 hipError_t launch_k(const LinArgs& g, hipStream_t st) {
-  const auto kern = linattn_kernel<DTYPE, D, C, STATE, KNOWN>;
-  constexpr int bytes = Lds<DTYPE, D, C>::kBytes;
-  static const hipError_t attr = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (attr != hipSuccess) return attr;
-  kern<<<dim3((unsigned)((g.N * g.H + 7) / 8 * 8 * g.ops), (unsigned)g.n_seg), kThreads, bytes, st>>>(g);
+  const auto kern = linattn_kernel<DTYPE, D, STATE, KNOWN>;
+  constexpr int bytes = Lds<DTYPE, D>::kBytes;
+  static_assert(bytes <= 64 * 1024, "no attribute needed");
+  kern<<<dim3((unsigned)((g.N * g.H + 7) / 8 * 8 * g.ops * g.blocks_v), (unsigned)g.n_seg), kThreads, bytes, st>>>(g);
   return hipGetLastError();
 }
-template <int DTYPE, int D, int C, bool STATE>
-hipError_t launch_t(const sf_linattn_config* c, const LinArgs& g, hipStream_t st) {
-  bool pieces = true;
-  for (int i = 0; i < g.ops; ++i) pieces = pieces && g.op[i].q.vec && g.op[i].k.vec && g.op[i].v.vec && g.op[i].o_vec;
-  if (!pieces) return launch_k<DTYPE, D, C, STATE, kAny>(g, st);
-  return c->dk == D && c->dv == D ? launch_k<DTYPE, D, C, STATE, kWhole>(g, st) : launch_k<DTYPE, D, C, STATE, kPieces>(g, st);
+template <int DTYPE, int D, bool STATE>
+hipError_t launch_t(const LinArgs& g, hipStream_t st) {
+  bool pieces = true, whole = true;
+  for (int i = 0; i < g.ops; ++i) {
+    const LinOp& o = g.op[i];
+    pieces = pieces && o.q.vec && o.k.vec && o.v.vec && o.o_vec;
+    whole = whole && o.k.d == D && o.v.d % DV == 0;
+  }
+  if (!pieces) return launch_k<DTYPE, D, STATE, kAny>(g, st);
+  return whole ? launch_k<DTYPE, D, STATE, kWhole>(g, st) : launch_k<DTYPE, D, STATE, kPieces>(g, st);
 }
 template <bool STATE>
-hipError_t launch(const sf_linattn_config* c, const LinArgs& g, hipStream_t st) {
-  const bool wide = c->dk > 64 || c->dv > 64;
-  if (c->dtype == SF_DTYPE_FP32)  // (64 steps of 128 numbers would leave a CU one workgroup)
-    return wide ? launch_t<SF_DTYPE_FP32, 128, 32, STATE>(c, g, st) : launch_t<SF_DTYPE_FP32, 64, 32, STATE>(c, g, st);
-  if (wide) return launch_t<SF_DTYPE_BF16, 128, 32, STATE>(c, g, st);
-  return c->T <= 32 ? launch_t<SF_DTYPE_BF16, 64, 32, STATE>(c, g, st) : launch_t<SF_DTYPE_BF16, 64, 64, STATE>(c, g, st);
+hipError_t launch(const sf_linattn_config* c, LinArgs& g, hipStream_t st) {
+  bool wide = false;
+  g.blocks_v = 1;
+  for (int i = 0; i < g.ops; ++i) {
+    wide = wide || g.op[i].k.d > 64;
+    if (g.op[i].v.d > DV) g.blocks_v = 2;
+  }
+  if (c->dtype == SF_DTYPE_FP32) return wide ? launch_t<SF_DTYPE_FP32, 128, STATE>(g, st) : launch_t<SF_DTYPE_FP32, 64, STATE>(g, st);
+  return wide ? launch_t<SF_DTYPE_BF16, 128, STATE>(g, st) : launch_t<SF_DTYPE_BF16, 64, STATE>(g, st);
 }
 
 int run(const char* fn, const sf_linattn_config* c, LinArgs& g, int ops, const Workspace& w, unsigned char* ws, hipStream_t st) {
