@@ -48,10 +48,21 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 
+// n / d for 0 <= n < 2^31, without a division on the device
+struct Divisor {
+  unsigned mul, shift;
+  __device__ unsigned of(unsigned n) const { return (__umulhi(mul, n) + n) >> shift; }
+};
+Divisor divisor(unsigned d) {
+  unsigned shift = 0;
+  while ((1u << shift) < d) ++shift;
+  return Divisor{(unsigned)(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
+}
+
 struct Strided {
   const void* p;
   int64_t st, sn, sh;  // step, row, head (elements)
-  int div;             // heads that share one
+  int shared;          // by the heads of a group
   int d;               // columns
   int vec;             // rows are read in 16-byte pieces
 };
@@ -74,6 +85,7 @@ struct LinArgs {
   const uint8_t* done;  // or null
   int T, N, H, ops;
   int blocks_v;         // of 64 columns of the widest v
+  Divisor round, heads, share;  // 8 ops blocks_v, H, heads that share one of k and v
   int n_seg, seg_len;   // pieces of T (seg_len a multiple of every C)
   float* seg_state;     // n_seg > 1: [op][N * H][n_seg][dk * dv], first the pieces' own states, then what enters them
   float* seg_keep;      // [op][N * H][n_seg] g^length, 0 if an episode begins in the piece
@@ -91,12 +103,6 @@ __device__ inline void split2(float a, float b, unsigned& t0, unsigned& t1) {
   t1 = pack_bf16(a - lo_of(t0), b - hi_of(t0));
 }
 
-// The same number, which the compiler takes for another one: comparisons with it are made where they stand and not kept in
-// registers from one use to the next.
-__device__ inline int anew(int x) {
-  asm volatile("" : "+s"(x));
-  return x;
-}
 __device__ inline float pow2(float x) { return __builtin_amdgcn_exp2f(x); }  // (x <= 0 here; below 2^-126: 0)
 
 // The arithmetic of one element type.  An operand is eight K-slots per lane.
@@ -212,18 +218,18 @@ struct Num<SF_DTYPE_FP32> {
 };
 
 // Eight columns of a row, zero past the array's end (col may lie past it altogether).
-template <int DTYPE, bool PIECES>
+template <int DTYPE>
 __device__ inline void load_piece(unsigned* w, const Strided& a, const unsigned char* row, int col, bool live) {
   typedef Num<DTYPE> M;
   constexpr int W = M::kPieceWords;
-  if (live && (PIECES || a.vec) && col < a.d) {  // (d is a multiple of 8 then)
+  if (live && a.vec && col < a.d) {  // (d is a multiple of 8 then)
 #pragma unroll
     for (int i = 0; i < W; i += 4) *(u32x4*)(w + i) = *(const u32x4*)(row + (size_t)col * M::kBytes + 4 * i);
     return;
   }
 #pragma unroll
   for (int i = 0; i < W; ++i) w[i] = 0;
-  if (PIECES || !live || a.vec) return;
+  if (!live || a.vec) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if (col + i >= a.d) continue;
@@ -240,8 +246,7 @@ __device__ inline float finite_test(const unsigned* w, float acc) {
 #pragma unroll
   for (int i = 0; i < Num<DTYPE>::kPieceWords; ++i) {
     if constexpr (DTYPE == SF_DTYPE_BF16) {
-      acc = fmaf(lo_of(w[i]), 0.0f, acc);
-      acc = fmaf(hi_of(w[i]), 0.0f, acc);
+      acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), __builtin_bit_cast(bf16x2, 0u), acc, false);
     } else {
       acc = fmaf(__builtin_bit_cast(float, w[i]), 0.0f, acc);
     }
@@ -283,23 +288,22 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
   constexpr bool WHOLE = KNOWN == kWhole;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   // the ops of one (row, head) read the same arrays: one after another on one XCD (workgroups go to the 8 in turn)
-  const int per = 8 * g.ops * g.blocks_v, round = blockIdx.x / per, in_round = blockIdx.x % per;
-  const int which = in_round / 8 % g.ops, v_block = in_round / (8 * g.ops) * DV;
-  const int bh = round * 8 + in_round % 8;
+  const unsigned round = g.round.of(blockIdx.x), in_round = blockIdx.x - round * (8 * g.ops * g.blocks_v), turn8 = in_round >> 3;
+  const int v_block = (int)turn8 >= g.ops ? DV : 0, which = (int)turn8 - (v_block ? g.ops : 0);
+  const int bh = (int)(round * 8 + (in_round & 7));
   const LinOp op = g.op[which];
   if (bh >= g.N * g.H || v_block >= op.v.d) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
-  const int n = bh / g.H, h = bh % g.H, seg = blockIdx.y;
+  const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h), seg = blockIdx.y;
   const int t_begin = seg * g.seg_len, t_end = min(g.T, t_begin + g.seg_len);  // in the op's own direction
   const int dk = op.k.d, dv = op.v.d;
   const float l2 = fmaxf(g.log_decay[h] * 1.44269504f, -1e30f);  // (no -infinity: times zero it would be NaN)
   const bool scan = g.n_seg > 1;
   const size_t seg_at = ((size_t)which * g.N * g.H + bh) * g.n_seg + seg;
 
-  const unsigned char* qrow = (const unsigned char*)op.q.p + (n * op.q.sn + h / op.q.div * op.q.sh) * M::kBytes;
-  const unsigned char* krow = (const unsigned char*)op.k.p + (n * op.k.sn + h / op.k.div * op.k.sh) * M::kBytes;
-  const unsigned char* vrow = (const unsigned char*)op.v.p + (n * op.v.sn + h / op.v.div * op.v.sh) * M::kBytes;
+  auto row_of = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
+  const unsigned char *const qrow = row_of(op.q), *const krow = row_of(op.k), *const vrow = row_of(op.v);
 
   const int v0 = v_block + 16 * wave;  // this wave's columns of v (past dv: nothing to do)
   const bool has_v = WHOLE || v0 < dv;
@@ -307,10 +311,14 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
   // column of k of tile t (two tiles are 32 columns: eight neighbours per lane group)
   auto col_k = [&](int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); };
 
+  // Memory is read and written through buffers that begin at a uniform address: what differs from lane to lane is an offset
+  // that stays the same from chunk to chunk, what is not there has an offset past the end (it is read as zero, not written).
+  constexpr unsigned kOutside = 0x80000000u;
+  auto buffer = [&](const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000); };
   f32x4 S[ND];
   {
     const float* s = nullptr;
-    int64_t sa = op.s_a, sb = op.s_b;
+    int sa = (int)op.s_a, sb = (int)op.s_b;
     if constexpr (!STATE) {
       if (scan) {
         s = g.seg_state + seg_at * ((size_t)dk * dv);
@@ -320,19 +328,24 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
         s = op.s_in + (size_t)bh * dk * dv;
       }
     }
-    const int xk = anew(dk), yv = anew(dv);
-    const bool four = KNOWN != kAny && sa == 1 && (reinterpret_cast<uintptr_t>(s) & 15) == 0;  // neighbours of k lie side by side
+    const auto from = buffer(s, s ? dk * dv * 4 : 0);
     const int y = v0 + li;
+    if (KNOWN != kAny && sa == 1) {  // neighbours of k lie side by side (their columns are a multiple of eight)
 #pragma unroll
-    for (int a = 0; a < ND; ++a) {
-      const int x = col_k(a, 4 * lg);
-      if (four) {  // (columns of k are a multiple of eight)
-        S[a] = s && (WHOLE || (x < xk && y < yv)) ? *(const f32x4*)(s + x + y * sb) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[a][r] = s && (WHOLE || (x + r < xk && y < yv)) ? s[(x + r) * sa + y * sb] : 0.0f;
+      for (int a = 0; a < ND; ++a) {
+        const int x = col_k(a, 4 * lg);
+        const unsigned at = WHOLE || (x < dk && y < dv) ? (unsigned)(y * sb + x) * 4 : kOutside;
+        S[a] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, 0));
       }
-      __builtin_amdgcn_sched_barrier(0);  // (the addresses of all at once would fill the registers)
+    } else {
+#pragma unroll
+      for (int a = 0; a < ND; ++a)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int x = col_k(a, 4 * lg + r);
+          const unsigned at = WHOLE || (x < dk && y < dv) ? (unsigned)(8 * lg * sa + y * sb) * 4 : kOutside;
+          S[a][r] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, at, (32 * (a >> 1) + 4 * (a & 1) + r) * sa * 4, 0));
+        }
     }
   }
 
@@ -342,21 +355,53 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
   auto step_of = [&](int i) { return op.reverse ? g.T - 1 - i : i; };
   int alone_to = t_begin;  // steps before this one are chunks of their own
   auto width = [&](int c0) { return c0 < alone_to ? 1 : min(C, t_end - c0); };
-  auto request = [&](int c0) {
-    const int valid = width(c0);
+  // row r of a chunk, in its order in memory
+  auto place = [&](int r) { return op.reverse ? C - 1 - r : r; };
+  auto first_of = [&](int c0) { return (int64_t)(op.reverse ? g.T - C - c0 : c0); };  // (may lie outside: its row is not there then)
+  constexpr int kPieceRow = D / 8, kPieceRowV = DV / 8;  // pieces of a row
+  unsigned at_q[NP], at_k[NP], at_v = kOutside;
+  if constexpr (KNOWN != kAny) {
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const int piece = tid + p * kThreads, r = piece / (D / 8), col = piece % (D / 8) * 8;
-      const bool live = r < valid;
-      const int64_t t = step_of(live ? c0 + r : t_end - 1);
-      if constexpr (!STATE) load_piece<DTYPE, KNOWN != kAny>(nq[p], op.q, qrow + t * op.q.st * M::kBytes, col, live);
-      load_piece<DTYPE, KNOWN != kAny>(nk[p], op.k, krow + t * op.k.st * M::kBytes, col, live);
+      const int piece = tid + p * kThreads, r = piece / kPieceRow, col = piece % kPieceRow * 8;
+      const bool in = WHOLE || col < dk;
+      at_q[p] = in ? (unsigned)(place(r) * (int)op.q.st + col) * M::kBytes : kOutside;
+      at_k[p] = in ? (unsigned)(place(r) * (int)op.k.st + col) * M::kBytes : kOutside;
     }
-    {
-      const int r = tid / (DV / 8);
+    const int col = v_block + tid % kPieceRowV * 8;
+    if (WHOLE || col < dv) at_v = (unsigned)(place(tid / kPieceRowV) * (int)op.v.st + col) * M::kBytes;
+  }
+  auto fetch = [&](unsigned* w, __amdgpu_buffer_rsrc_t from, unsigned at) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) *(u32x4*)(w + i) = __builtin_amdgcn_raw_buffer_load_b128(from, at + 4 * i, 0, 0);
+  };
+  auto request = [&](int c0) {
+    const int valid = width(c0);
+    if constexpr (KNOWN != kAny) {
+      const int64_t t = first_of(c0);
+      const auto bq = buffer(qrow + t * op.q.st * M::kBytes, 0x7FFFFFFF), bk = buffer(krow + t * op.k.st * M::kBytes, 0x7FFFFFFF),
+                 bv = buffer(vrow + t * op.v.st * M::kBytes, 0x7FFFFFFF);
+      const bool all = valid == C;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const bool live = all || (tid + p * kThreads) / kPieceRow < valid;
+        if constexpr (!STATE) fetch(nq[p], bq, live ? at_q[p] : kOutside);
+        fetch(nk[p], bk, live ? at_k[p] : kOutside);
+      }
+      fetch(nv, bv, all || tid / kPieceRowV < valid ? at_v : kOutside);
+    } else {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int piece = tid + p * kThreads, r = piece / kPieceRow, col = piece % kPieceRow * 8;
+        const bool live = r < valid;
+        const int64_t t = step_of(live ? c0 + r : t_end - 1);
+        if constexpr (!STATE) load_piece<DTYPE>(nq[p], op.q, qrow + t * op.q.st * M::kBytes, col, live);
+        load_piece<DTYPE>(nk[p], op.k, krow + t * op.k.st * M::kBytes, col, live);
+      }
+      const int r = tid / kPieceRowV;
       const bool live = r < valid;
       const int64_t t = step_of(live ? c0 + r : t_end - 1);
-      load_piece<DTYPE, KNOWN != kAny>(nv, op.v, vrow + t * op.v.st * M::kBytes, v_block + tid % (DV / 8) * 8, live);
+      load_piece<DTYPE>(nv, op.v, vrow + t * op.v.st * M::kBytes, v_block + tid % kPieceRowV * 8, live);
     }
     n_done = 0;
     if (g.done && lane < C && lane < valid) {
@@ -365,6 +410,13 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
       else if (i > 0) n_done = g.done[(size_t)(g.T - i) * g.N + n];
     }
   };
+  unsigned at_o[C / 16];  // of four neighbours of an output row
+#pragma unroll
+  for (int I = 0; I < C / 16; ++I) {
+    const int y = v0 + 4 * lg;
+    at_o[I] = y < dv ? (unsigned)(place(16 * I + li) * (int)op.ot + y) * (op.o_f32 ? 4 : M::kBytes) : kOutside;
+  }
+  unsigned char* const orow = (unsigned char*)op.o + (n * op.on + h * op.oh) * (op.o_f32 ? 4 : M::kBytes);
   unsigned char* const tq = lds;
   unsigned char* const tk = lds + L::kK;
   unsigned char* const tv = lds + L::kV;
@@ -383,7 +435,7 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
     float test = 0.0f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const int piece = tid + p * kThreads, at = piece / (D / 8) * L::kPitch + piece % (D / 8) * 8 * M::kBytes;
+      const int piece = tid + p * kThreads, at = piece / kPieceRow * L::kPitch + piece % kPieceRow * 8 * M::kBytes;
 #pragma unroll
       for (int i = 0; i < W; i += 4) {
         if constexpr (!STATE) *(u32x4*)(tq + at + 4 * i) = *(u32x4*)(nq[p] + i);
@@ -392,17 +444,16 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
       test = finite_test<DTYPE>(nk[p], test);
     }
     {
-      const int at = tid / (DV / 8) * L::kPitchV + tid % (DV / 8) * 8 * M::kBytes;
+      const int at = tid / kPieceRowV * L::kPitchV + tid % kPieceRowV * 8 * M::kBytes;
 #pragma unroll
       for (int i = 0; i < W; i += 4) *(u32x4*)(tv + at + 4 * i) = *(u32x4*)(nv + i);
       test = finite_test<DTYPE>(nv, test);
     }
     if (test != 0.0f) flag[turn] = 1;
-    const int ep_end = __popc(marks);
     if (tid < C) {
       const int e = __popc(marks & ((2u << tid) - 1));
       ep[tid] = e;
-      wgt[tid] = e == ep_end && tid < valid ? op.w_scale * pow2(l2 * (float)(valid - 1 - tid)) : 0.0f;
+      wgt[tid] = e == __popc(marks) && tid < valid ? op.w_scale * pow2(l2 * (float)(valid - 1 - tid)) : 0.0f;
     }
     __syncthreads();
     if (tid == 0) flag[turn ^ 1] = 0;  // (read by all before the barrier above)
@@ -426,12 +477,15 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
             const int at = (32 * s + 8 * lg) * M::kBytes;
             if (has_k(s)) acc = M::mma(M::row(tk + (16 * J + li) * L::kPitch + at), M::row(tq + (16 * I + li) * L::kPitch + at), acc);
           }
-          const int i = 16 * I + li, e = ep[i];
-          const i32x4 ej = *(const i32x4*)(ep + 16 * J + 4 * lg);
+          const int lag = 16 * (I - J) + li - 4 * lg;  // i - j of r = 0
+          const float p_scale = op.w_scale * op.alpha;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int j = 16 * J + 4 * lg + r;
-            acc[r] = j <= i && ej[r] == e ? acc[r] * (op.w_scale * pow2(l2 * (float)(i - j))) : 0.0f;
+          for (int r = 0; r < 4; ++r) acc[r] = I > J || lag >= r ? acc[r] * (p_scale * pow2(l2 * (float)(lag - r))) : 0.0f;
+          if (marks) {
+            const int e = ep[16 * I + li];
+            const i32x4 ej = *(const i32x4*)(ep + 16 * J + 4 * lg);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[r] = ej[r] == e ? acc[r] : 0.0f;
           }
         }
         M::put4(lds + L::kP + I * 1024, L::kTermPitch, lane, J, acc);
@@ -477,24 +531,27 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
 #pragma unroll
       for (int I = 0; I < C / 16; ++I) {
         const int i = 16 * I + li;
-        const bool reach = (marks & ((2u << i) - 1)) == 0;  // no episode has begun: the state is this step's
-        const float c = pow2(l2 * (float)(i + 1 - late));
+        const float c = op.alpha * pow2(l2 * (float)(i + 1 - late));
         f32x4 own = out[I];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) own[r] = reach ? c * own[r] : 0.0f;
-        own = M::mma(vt, M::get(lds + L::kP + I * 1024, L::kTermPitch, lane), own);
+        for (int r = 0; r < 4; ++r) own[r] *= c;
+        if (marks) {
+          const bool reach = (marks & ((2u << i) - 1)) == 0;  // no episode has begun: the state is this step's
 #pragma unroll
-        for (int r = 0; r < 4; ++r) own[r] *= op.alpha;
-        const int y = v0 + 4 * lg;  // four neighbours
-        if (i >= valid || y >= dv) continue;
-        const int64_t at = n * op.on + h * op.oh + step_of(c0 + i) * op.ot + y;
-        if (KNOWN != kAny || op.o_vec) {
-          if (op.o_f32) *(f32x4*)((float*)op.o + at) = own;
-          else *(u32x2*)((uint16_t*)op.o + at) = u32x2{pack_bf16(own[0], own[1]), pack_bf16(own[2], own[3])};
+          for (int r = 0; r < 4; ++r) own[r] = reach ? own[r] : 0.0f;
+        }
+        own = M::mma(vt, M::get(lds + L::kP + I * 1024, L::kTermPitch, lane), own);
+        if constexpr (KNOWN != kAny) {
+          const unsigned at = i < valid ? at_o[I] : kOutside;
+          const auto to = buffer(orow + first_of(c0) * op.ot * (op.o_f32 ? 4 : M::kBytes), 0x7FFFFFFF);
+          if (op.o_f32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, own), to, at, 0, 0);
+          else __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(own[0], own[1]), pack_bf16(own[2], own[3])}, to, at, 0, 0);
         } else {
+          const int y = v0 + 4 * lg;
+          const int64_t at = n * op.on + h * op.oh + step_of(c0 + i) * op.ot + y;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            if (y + r >= dv) continue;
+            if (i >= valid || y + r >= dv) continue;
             if (op.o_f32) ((float*)op.o)[at + r] = own[r];
             else M::store((unsigned char*)op.o + (at + r) * M::kBytes, own[r]);
           }
@@ -503,10 +560,15 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
     }
 
     const float keep = pow2(l2 * (float)(valid - late));
+    if (marks) {
 #pragma unroll
-    for (int a = 0; a < ND; ++a)
+      for (int a = 0; a < ND; ++a) S[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    } else {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) S[a][r] = marks ? 0.0f : keep * S[a][r];
+      for (int a = 0; a < ND; ++a)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[a][r] *= keep;
+    }
     if (has_v) {
       const f32x4 w0 = *(const f32x4*)(wgt + 4 * lg), w1 = *(const f32x4*)(wgt + 16 + 4 * lg);
       float x[8];
@@ -535,14 +597,12 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
     }
   }
 
+  // (a state that is written lies [dk][dv])
   float* s = nullptr;
-  int64_t sa = op.s_a, sb = op.s_b;
   float f = 1.0f;
   bool zero = false;
   if constexpr (STATE) {
     s = g.seg_state + seg_at * ((size_t)dk * dv);
-    sa = dv;
-    sb = 1;
     if (tid == 0 && v_block == 0)
       g.seg_keep[seg_at] = any_done ? 0.0f : pow2(l2 * (float)(t_end - t_begin - (seg == 0 && op.reverse ? 1 : 0)));
   } else if (op.s_out && seg == g.n_seg - 1) {
@@ -552,18 +612,16 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void
       zero = g.done && t_end > t_begin && g.done[n] != 0;
     }
   }
-  if (s) {
-    const int xk = anew(dk), yv = anew(dv), y = v0 + li;
+  if (!s) return;
+  const auto to = buffer(s, dk * dv * 4);
+  const int y = v0 + li;
 #pragma unroll
-    for (int a = 0; a < ND; ++a) {
+  for (int a = 0; a < ND; ++a)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int x = col_k(a, 4 * lg + r);
-        if (WHOLE || (x < xk && y < yv)) s[x * sa + y * sb] = zero ? 0.0f : f * S[a][r];
-      }
-      __builtin_amdgcn_sched_barrier(0);
+    for (int r = 0; r < 4; ++r) {  // (rows past dk lie past the end)
+      const unsigned at = WHOLE || y < dv ? (unsigned)(8 * lg * dv + y) * 4 : kOutside;
+      __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, zero ? 0.0f : f * S[a][r]), to, at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4, 0);
     }
-  }
 }
 
 // What enters each piece of T, from the pieces' own states: one thread per element of a state, kAhead pieces read ahead.
@@ -607,7 +665,7 @@ __global__ __launch_bounds__(kThreads) void linattn_share_kernel(const float* in
 // bytes; a thread holds four neighbours of every (256 / lanes)-th row, so that all its loads are under way at once.
 template <int DTYPE, bool VEC>
 __global__ __launch_bounds__(kThreads) void linattn_step_kernel(LinOp op, const float* log_decay, const uint8_t* done, float* table,
-                                                                int n_env, const int32_t* ids, int H, int lanes_log2) {
+                                                                int n_env, const int32_t* ids, int H, int share, int lanes_log2) {
   typedef Num<DTYPE> M;
   __shared__ float sq[128], sk[128];
   __shared__ __attribute__((aligned(16))) float part[4][128];
@@ -635,14 +693,14 @@ __global__ __launch_bounds__(kThreads) void linattn_step_kernel(LinOp op, const 
     }
   }
   if (tid < 128) {
-    if (tid < dk) sk[tid] = M::element((const unsigned char*)op.k.p + (n * op.k.sn + h / op.k.div * op.k.sh + tid) * M::kBytes);
+    if (tid < dk) sk[tid] = M::element((const unsigned char*)op.k.p + (n * op.k.sn + h / share * op.k.sh + tid) * M::kBytes);
   } else if (tid - 128 < dk) {
     sq[tid - 128] = M::element((const unsigned char*)op.q.p + (n * op.q.sn + h * op.q.sh + tid - 128) * M::kBytes);
   }
   float v[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    v[j] = c0 + j < dv ? M::element((const unsigned char*)op.v.p + (n * op.v.sn + h / op.v.div * op.v.sh + c0 + j) * M::kBytes) : 0.0f;
+    v[j] = c0 + j < dv ? M::element((const unsigned char*)op.v.p + (n * op.v.sn + h / share * op.v.sh + c0 + j) * M::kBytes) : 0.0f;
   __syncthreads();
   float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -747,21 +805,23 @@ Workspace workspace_of(const sf_linattn_config* c, int backward) {
   return w;
 }
 
-Strided strided(const sf_linattn_config* c, const void* p, const int64_t* s, int div, int d) {
-  Strided a = {p, s[0], s[1], s[2], div, d, 0};
+// (a chunk's rows lie within 2^31 bytes then, and one behind the other)
+bool near(int64_t st, int d) { return st >= d && st <= 1 << 23; }
+Strided strided(const sf_linattn_config* c, const void* p, const int64_t* s, bool shared, int d) {
+  Strided a = {p, c->T == 1 ? 0 : s[0], s[1], s[2], shared, d, 0};  // (one step: any stride)
   const int per = 16 / (c->dtype == SF_DTYPE_BF16 ? 2 : 4);
   // (pieces are eight columns in both types)
-  a.vec = d % 8 == 0 && (s[0] % per) == 0 && (s[1] % per) == 0 && (s[2] % per) == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+  a.vec = d % 8 == 0 && (c->T == 1 || near(s[0], d)) && (a.st % per) == 0 && (s[1] % per) == 0 && (s[2] % per) == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
   return a;
 }
 void put_out(const sf_linattn_config* c, LinOp& op, void* p, int64_t t, int64_t n, int64_t h, int d, bool f32) {
   op.o = p;
-  op.ot = t;
+  op.ot = c->T == 1 ? 0 : t;
   op.on = n;
   op.oh = h;
   op.o_f32 = f32 || c->dtype == SF_DTYPE_FP32;
   const int per = op.o_f32 ? 4 : 8;
-  op.o_vec = d % 8 == 0 && t % per == 0 && n % per == 0 && h % per == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+  op.o_vec = d % 8 == 0 && (c->T == 1 || near(t, d)) && op.ot % per == 0 && n % per == 0 && h % per == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 }
 
 template <int DTYPE, int D, bool STATE, int KNOWN>
@@ -791,6 +851,9 @@ hipError_t launch(const sf_linattn_config* c, LinArgs& g, hipStream_t st) {
     wide = wide || g.op[i].k.d > 64;
     if (g.op[i].v.d > DV) g.blocks_v = 2;
   }
+  g.round = divisor(8 * g.ops * g.blocks_v);
+  g.heads = divisor(g.H);
+  g.share = divisor(c->H / c->Hk);
   if (c->dtype == SF_DTYPE_FP32) return wide ? launch_t<SF_DTYPE_FP32, 128, STATE>(g, st) : launch_t<SF_DTYPE_FP32, 64, STATE>(g, st);
   return wide ? launch_t<SF_DTYPE_BF16, 128, STATE>(g, st) : launch_t<SF_DTYPE_BF16, 64, STATE>(g, st);
 }
@@ -852,9 +915,9 @@ extern "C" int sf_linattn(const sf_linattn_config* cfg, const void* q, const voi
   g.done = done;
   LinOp& op = g.op[0];
   const int share = cfg->H / cfg->Hk;
-  op.q = strided(cfg, q, cfg->q_stride, 1, cfg->dk);
-  op.k = strided(cfg, k, cfg->k_stride, share, cfg->dk);
-  op.v = strided(cfg, v, cfg->v_stride, share, cfg->dv);
+  op.q = strided(cfg, q, cfg->q_stride, false, cfg->dk);
+  op.k = strided(cfg, k, cfg->k_stride, share > 1, cfg->dk);
+  op.v = strided(cfg, v, cfg->v_stride, share > 1, cfg->dv);
   put_out(cfg, op, o, cfg->o_stride[0], cfg->o_stride[1], cfg->o_stride[2], cfg->dv, false);
   op.s_in = state0;
   op.s_out = state;
@@ -893,8 +956,8 @@ extern "C" int sf_linattn_backward(const sf_linattn_config* cfg, const void* q, 
   LinArgs g = {};
   g.log_decay = log_decay;
   g.done = done;
-  const Strided sq = strided(cfg, q, cfg->q_stride, 1, Dk), sk = strided(cfg, k, cfg->k_stride, share, Dk),
-                sv = strided(cfg, v, cfg->v_stride, share, Dv), so = strided(cfg, d_o, cfg->o_stride, 1, Dv);
+  const Strided sq = strided(cfg, q, cfg->q_stride, false, Dk), sk = strided(cfg, k, cfg->k_stride, share > 1, Dk),
+                sv = strided(cfg, v, cfg->v_stride, share > 1, Dv), so = strided(cfg, d_o, cfg->o_stride, false, Dv);
   LinOp &oq = g.op[0], &ok = g.op[1], &ov = g.op[2];
   oq.q = so;
   oq.k = sv;
@@ -969,9 +1032,9 @@ extern "C" int sf_linattn_step(const sf_linattn_config* cfg, const void* q, cons
   if (none) return SF_OK;
   const int share = cfg->H / cfg->Hk;
   LinOp op = {};
-  op.q = strided(cfg, q, cfg->q_stride, 1, cfg->dk);
-  op.k = strided(cfg, k, cfg->k_stride, share, cfg->dk);
-  op.v = strided(cfg, v, cfg->v_stride, share, cfg->dv);
+  op.q = strided(cfg, q, cfg->q_stride, false, cfg->dk);
+  op.k = strided(cfg, k, cfg->k_stride, share > 1, cfg->dk);
+  op.v = strided(cfg, v, cfg->v_stride, share > 1, cfg->dv);
   put_out(cfg, op, o, 0, cfg->o_stride[1], cfg->o_stride[2], cfg->dv, false);
   op.alpha = cfg->scale;
   // a thread has four columns; rows of a multiple of four floats are read 16 bytes at a time
@@ -984,7 +1047,7 @@ extern "C" int sf_linattn_step(const sf_linattn_config* cfg, const void* q, cons
   const auto kern = cfg->dtype == SF_DTYPE_BF16
                         ? (vec ? linattn_step_kernel<SF_DTYPE_BF16, true> : linattn_step_kernel<SF_DTYPE_BF16, false>)
                         : (vec ? linattn_step_kernel<SF_DTYPE_FP32, true> : linattn_step_kernel<SF_DTYPE_FP32, false>);
-  kern<<<grid, kThreads, 0, st>>>(op, log_decay, done, state_table, n_env, env_ids, cfg->H, lanes_log2);
+  kern<<<grid, kThreads, 0, st>>>(op, log_decay, done, state_table, n_env, env_ids, cfg->H, share, lanes_log2);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) {
     set_error("%s: launch failed: %s", fn, hipGetErrorString(err));
