@@ -279,7 +279,7 @@ struct Lds {
 // have whole tiles besides, D and a multiple of 64 columns (else columns past theirs are left out, 32 of k, 16 of v at a time).
 enum Known { kAny = 0, kPieces = 1, kWhole = 2 };
 template <int DTYPE, int D, bool STATE, int KNOWN>
-__global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 ? 4 : 3) void linattn_kernel(LinArgs g) {
+__global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 || DTYPE == SF_DTYPE_BF16 ? 4 : 3) void linattn_kernel(LinArgs g) {
   typedef Num<DTYPE> M;
   typedef Lds<DTYPE, D> L;
   constexpr int W = M::kPieceWords, NP = C * D / 8 / kThreads;  // pieces of a tile of q or k per thread; one of v's
