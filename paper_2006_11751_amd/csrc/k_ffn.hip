@@ -135,13 +135,11 @@ __device__ inline void wave_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// eight neighbours, or their terms, at offset `at` (a multiple of 8)
-__device__ inline void store_terms8(const Terms& t, int terms, int64_t at, const float* v) {
-  u32x4 w[3];
-  if (terms == 1) {
+// eight neighbours rounded, or (exact) as three terms
+__device__ inline void terms8(const float* v, u32x4* w, bool exact) {
+  if (!exact) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[0][i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-    *(u32x4*)(t.p + at) = w[0];
     return;
   }
   float left = 0.0f;
@@ -153,8 +151,14 @@ __device__ inline void store_terms8(const Terms& t, int terms, int64_t at, const
     w[1][i] = b;
     w[2][i] = c;
   }
+}
+// the same at offset `at` (a multiple of 8)
+__device__ inline void store_terms8(const Terms& t, bool exact, int64_t at, const float* v) {
+  u32x4 w[3];
+  terms8(v, w, exact);
 #pragma unroll
-  for (int i = 0; i < 3; ++i) *(u32x4*)(t.p + i * t.plane + at) = w[i];
+  for (int i = 0; i < 3; ++i)
+    if (i == 0 || exact) *(u32x4*)(t.p + i * t.plane + at) = w[i];
 }
 // eight neighbours of a result's row (its first `left` ones)
 __device__ inline void store_out8(void* out, int f32, int F, int64_t at, int left, const float* v) {
@@ -418,10 +422,16 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
       }
     } else {
       // (rows of w past F and rows of x past M were read as zeros, so that h, dg and du are zeros where they are padded)
+      // (a piece that is not there has an offset past the end, so that no branch parts the rounds of the loop)
+      const int64_t corner = (int64_t)mw * a_.h.pitch + fwave;  // (all three arrays have one shape)
+      auto buffer = [&](const Terms& t, int plane) __attribute__((always_inline)) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)(t.p + plane * t.plane + corner), 0, 0x7FFFFFFF, 0x00027000);
+      };
       with_activation(a_.act, a_.terms == 3, [&](auto act, auto exact) __attribute__((always_inline)) {
-#pragma unroll 2
+        constexpr bool kShort = decltype(act)::value != SF_ACT_GELU && !decltype(exact)::value;
+#pragma unroll kShort ? NI : 1
         for (int i = 0; i < NI; ++i) {
-          const int row = i * (64 / LPR) + lane / LPR, col = lane % LPR * 8, m = mw + row, f = fwave + col;
+          const int row = i * (64 / LPR) + lane / LPR, col = lane % LPR * 8;
           const float* const at = area + row * EP + col;
           float gate[8], up[8], h[8], dh[8], dg[8], du[8];
 #pragma unroll
@@ -440,12 +450,20 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
               du[r] = dh[r] * v;
             }
           }
-          if (m >= a_.M || f >= a_.Fp) continue;
-          const int64_t to = (int64_t)m * a_.h.pitch + f;  // (all three have one shape)
-          store_terms8(a_.h, a_.terms, to, h);
+          const unsigned to = mw + row < a_.M && fwave + col < a_.Fp ? (unsigned)(row * (int)a_.h.pitch + col) * 2 : 0x80000000u;
+          auto store = [&](const Terms& t, const float* v) __attribute__((always_inline)) {
+            u32x4 w[3];
+            terms8(v, w, decltype(exact)::value);
+            __builtin_amdgcn_raw_buffer_store_b128(w[0], buffer(t, 0), to, 0, 0);
+            if constexpr (decltype(exact)::value) {
+              __builtin_amdgcn_raw_buffer_store_b128(w[1], buffer(t, 1), to, 0, 0);
+              __builtin_amdgcn_raw_buffer_store_b128(w[2], buffer(t, 2), to, 0, 0);
+            }
+          };
+          store(a_.h, h);
           if constexpr (FORM == kTriple) {
-            store_terms8(a_.dg, a_.terms, to, dg);
-            store_terms8(a_.du, a_.terms, to, du);
+            store(a_.dg, dg);
+            store(a_.du, du);
           }
         }
       });
@@ -453,21 +471,33 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
   }
 }
 
-// The sum of the parts of K.
+// The sums of the parts of K, four neighbours a thread.
+struct SumGroup {
+  const float* parts[3];
+  void* out[3];
+  int64_t size[3], threads[3];
+  int n, splits;
+};
 template <int DTYPE>
-__global__ __launch_bounds__(kThreads) void ffn_sum_kernel(const float* parts, int n, int64_t size, void* out) {
-  const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;  // (few tiles: size is below 384 x 128 x 128)
+__global__ __launch_bounds__(kThreads) void ffn_sum_kernel(SumGroup g) {
+  int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  int which = 0;
+  while (which + 1 < g.n && i >= g.threads[which]) i -= g.threads[which++];
+  const float* const parts = g.parts[which];
+  void* const out = g.out[which];
+  const int64_t size = g.size[which];
+  i *= 4;
   if (i >= size) return;
   if ((size & 3) == 0) {
     f32x4 v = *(const f32x4*)(parts + i);
-    for (int j = 1; j < n; ++j) v += *(const f32x4*)(parts + j * size + i);
+    for (int j = 1; j < g.splits; ++j) v += *(const f32x4*)(parts + j * size + i);
     if (DTYPE == SF_DTYPE_BF16) *(u32x2*)((uint16_t*)out + i) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
     else *(f32x4*)((float*)out + i) = v;
     return;
   }
   for (int r = 0; r < 4 && i + r < size; ++r) {
     float v = parts[i + r];
-    for (int j = 1; j < n; ++j) v += parts[j * size + i + r];
+    for (int j = 1; j < g.splits; ++j) v += parts[j * size + i + r];
     if (DTYPE == SF_DTYPE_BF16) ((uint16_t*)out)[i + r] = (uint16_t)pack_bf16(v, 0.0f);
     else ((float*)out)[i + r] = v;
   }
@@ -500,7 +530,7 @@ __device__ inline void lay_piece(const Layout& l, int64_t piece) {
     for (int i = 0; i < 8; ++i)
       v[i] = c + i >= l.cols ? 0.0f : DTYPE == SF_DTYPE_BF16 ? from_bf16(((const uint16_t*)l.from)[at + i]) : ((const float*)l.from)[at + i];
   }
-  store_terms8(l.to, DTYPE == SF_DTYPE_BF16 ? 1 : 3, r * l.to.pitch + c, v);
+  store_terms8(l.to, DTYPE == SF_DTYPE_FP32, r * l.to.pitch + c, v);
 }
 
 template <int DTYPE>
@@ -726,7 +756,7 @@ hipError_t launch_t(GemmGroup& group, hipStream_t st) {
 }
 int64_t tiles_of(int F, int M, int BF, int BM) { return (int64_t)((F + BF - 1) / BF) * ((M + BM - 1) / BM); }
 // The large tile where it leaves few CUs without one, the small one otherwise.
-constexpr int kEnough = 192;
+constexpr int kEnough = 160;
 template <int FORM>
 hipError_t launch(GemmGroup& group, hipStream_t st) {
   const GemmArgs& g = group.g[0];
@@ -741,7 +771,7 @@ struct Products {
   GemmGroup group = {};
   bool large = false;
   int splits = 1;
-  // Parts of K: about three workgroups of small tiles per CU, each part 16 steps of 64 or more.
+  // Parts of K: as many workgroups of small tiles as run at once, each part 16 steps of 64 or more.
   void plan() {
     int64_t big = 0, small = 0;
     int steps = 1 << 30;
@@ -753,7 +783,7 @@ struct Products {
       if (s < steps) steps = s;
     }
     large = big >= kEnough;
-    splits = large || small == 0 ? 1 : (int)(768 / small);
+    splits = large || small == 0 ? 1 : (int)(512 / small);
     if (splits > steps / 16) splits = steps / 16;
     if (splits > 8) splits = 8;
     if (splits < 1) splits = 1;
@@ -772,11 +802,20 @@ struct Products {
       }
     }
     hipError_t e = large ? launch_t<kOne, ACROSS, 256, 256, 64, 1>(group, st) : launch_t<kOne, ACROSS, 128, 128, 64, 2>(group, st);
-    for (int i = 0; i < group.n && splits > 1 && e == hipSuccess; ++i) {
-      const int64_t size = (int64_t)group.g[i].M * group.g[i].F;
-      const unsigned grid = (unsigned)((size + 4 * kThreads - 1) / (4 * kThreads));
-      if (dtype == SF_DTYPE_BF16) ffn_sum_kernel<SF_DTYPE_BF16><<<grid, kThreads, 0, st>>>((const float*)group.g[i].out, splits, size, out[i]);
-      else ffn_sum_kernel<SF_DTYPE_FP32><<<grid, kThreads, 0, st>>>((const float*)group.g[i].out, splits, size, out[i]);
+    if (splits > 1 && e == hipSuccess) {
+      SumGroup sums = {};
+      int64_t threads = 0;
+      sums.n = group.n;
+      sums.splits = splits;
+      for (int i = 0; i < group.n; ++i) {
+        sums.parts[i] = (const float*)group.g[i].out;
+        sums.out[i] = out[i];
+        sums.size[i] = (int64_t)group.g[i].M * group.g[i].F;
+        threads += sums.threads[i] = (sums.size[i] + 3) / 4;
+      }
+      const unsigned grid = (unsigned)((threads + kThreads - 1) / kThreads);  // (few tiles: below 256 x 128 x 128 numbers)
+      if (dtype == SF_DTYPE_BF16) ffn_sum_kernel<SF_DTYPE_BF16><<<grid, kThreads, 0, st>>>(sums);
+      else ffn_sum_kernel<SF_DTYPE_FP32><<<grid, kThreads, 0, st>>>(sums);
       e = hipGetLastError();
     }
     return e;
