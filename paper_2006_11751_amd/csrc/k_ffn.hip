@@ -595,7 +595,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void ffn_rows_kernel(RowsArgs g) {
   for (int a = 0; a < W; ++a)
 #pragma unroll
     for (int c = 0; c < MT; ++c) acc[a][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  constexpr int U = VEC ? 2 : 1;  // steps whose loads are under way together
+  constexpr int U = VEC ? 2 : 1;  // steps whose loads are under way together (up to 8: no shorter)
   for (int k0 = wave * 32; k0 < g.K; k0 += U * kRowWaves * 32) {
     u32x4 rw[U][W], rx[U][MT];
     float vw[U][W][8], vx[U][MT][8];
@@ -667,7 +667,10 @@ __global__ __launch_bounds__(kThreads) void ffn_zero_kernel(uint16_t* p, int64_t
 
 // ---- host side ---------------------------------------------------------------------------------
 
-constexpr int kFewRows = 64;
+// Rows up to which the path for few takes a call: there the time grows with the rows of x that each wave reads beside its
+// weights (bf16, us: 512 x 2048 1 row 7.5, 16 9.3, 32 11.8, 64 16.8, 65 by tiles 20; 2048 x 8192 23, 30, 40, 62, 36; fp32 13, 16,
+// 21, 33, 58 and 58, 65, 87, 135, 283).
+int few_rows(int dtype) { return dtype == SF_DTYPE_BF16 ? 32 : 64; }
 
 int check(const sf_ffn_config* c, const char* fn) {
   if (!c || c->struct_size != sizeof(sf_ffn_config)) {
@@ -826,8 +829,8 @@ template <int DTYPE, int W, bool VEC>
 hipError_t launch_rows(const RowsArgs& g, hipStream_t st) {
   const unsigned grid = (unsigned)((g.F + 15) / 16);
   if (g.M <= 16) ffn_rows_kernel<DTYPE, W, 1, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
-  else if (g.M <= 32) ffn_rows_kernel<DTYPE, W, 2, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
-  else ffn_rows_kernel<DTYPE, W, 4, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
+  else if (DTYPE == SF_DTYPE_BF16 || g.M <= 32) ffn_rows_kernel<DTYPE, W, 2, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
+  else if constexpr (DTYPE == SF_DTYPE_FP32) ffn_rows_kernel<DTYPE, W, 4, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
   return hipGetLastError();
 }
 template <int W>
@@ -927,7 +930,7 @@ using namespace sf;
 // (Whether an array is read as it is depends on its address, which is not known here: the larger need is given.)
 extern "C" int64_t sf_ffn_workspace_bytes(const sf_ffn_config* cfg, int backward) {
   if (check(cfg, "sf_ffn_workspace_bytes") != SF_OK) return -1;
-  if (!backward && cfg->M <= kFewRows) return (int64_t)pad64((int64_t)cfg->M * cfg->F) * 4;
+  if (!backward && cfg->M <= few_rows(cfg->dtype)) return (int64_t)pad64((int64_t)cfg->M * cfg->F) * 4;
   Job j{cfg, nullptr};
   Arena a = {nullptr, 0};
   void* const odd = (void*)2;
@@ -955,7 +958,7 @@ extern "C" int sf_ffn(const sf_ffn_config* cfg, const void* x, const void* w_gat
   if (none) return SF_OK;
   Job j{cfg, reinterpret_cast<hipStream_t>(hip_stream)};
   hipError_t err;
-  if (cfg->M <= kFewRows) {
+  if (cfg->M <= few_rows(cfg->dtype)) {
     const auto whole = [&](const void* p, int64_t pitch, int cols) {
       return cols % 8 == 0 && pitch % (16 / (int64_t)e) == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
     };
