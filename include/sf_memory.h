@@ -114,13 +114,13 @@ int sf_resnorm_backward(const sf_resnorm_config* cfg, const void* b, const void*
  * [M][D] dense, 16-byte aligned.
  *   act = SF_ACT_SILU (g sigmoid(g)), SF_ACT_GELU (g Phi(g), by erf), SF_ACT_SIGMOID
  * bf16: products of bf16 numbers are added in fp32, h is rounded to bf16, y is rounded once more.  fp32: operands are the
- * exact sums of three bf16 numbers, of whose nine products six are added (2^-27 is left out); up to 64 rows forwards run
+ * exact sums of three bf16 numbers, of whose nine products six are added (2^-27 is left out); up to 128 rows forwards run
  * on the fp32 matrix instruction.  Infinities and NaN are only in the rows of y whose rows of x hold them; in weights they
  * reach all (of an infinity fp32 results are NaN).
  * Backward: dy [M] rows -> dx [M][D], dw_gate, dw_up [F][D], dw_down [D][F], dense, 16-byte aligned, of the same type.
  * Nothing of the forward pass is needed but its inputs.  Results must not overlap inputs.
  * Rows of a multiple of 64 numbers, 16-byte aligned, are read where they are; others are laid out in the workspace first
- * (up to 64 rows forwards, 32 in bf16: read element by element).
+ * (few rows forwards: read element by element).
  * workspace: sf_ffn_workspace_bytes(cfg, backward), 256-byte aligned, wanted unless M is 0.
  * Errors: SF_ERR_ARG, SF_ERR_SHAPE (M outside 0 .. 2^24, D or F outside 1 .. 2^20), SF_ERR_DEVICE. */
 enum { SF_ACT_SILU = 0, SF_ACT_GELU = 1, SF_ACT_SIGMOID = 2 };

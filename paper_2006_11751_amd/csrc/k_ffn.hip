@@ -546,7 +546,7 @@ __global__ __launch_bounds__(kThreads) void ffn_layout_kernel(LayoutGroup group)
 
 // ---- few rows ----------------------------------------------------------------------------------
 
-// C[m][f] for M <= 16 MT rows: 16 rows of each w per workgroup, its waves share K.
+// C[m][f] for 16 MT rows m: 16 rows of each w per workgroup, its waves share K.
 struct RowsArgs {
   const void *w[2], *x;
   int64_t w_pitch[2], x_pitch;
@@ -588,7 +588,7 @@ template <int DTYPE, int W, int MT, bool VEC>
 __global__ __launch_bounds__(64 * kRowWaves) void ffn_rows_kernel(RowsArgs g) {
   __shared__ __attribute__((aligned(16))) f32x4 part[kRowWaves][W][MT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, lg = lane >> 4;
-  const int f0 = blockIdx.x * 16;
+  const int f0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * MT);
   const int f_row = min(f0 + li, g.F - 1);
   f32x4 acc[W][MT];
 #pragma unroll
@@ -605,7 +605,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void ffn_rows_kernel(RowsArgs g) {
 #pragma unroll
       for (int a = 0; a < W; ++a) load8<DTYPE, VEC>(vw[u][a], rw[u][a], g.w[a], f_row * g.w_pitch[a], k, g.K);
 #pragma unroll
-      for (int c = 0; c < MT; ++c) load8<DTYPE, VEC>(vx[u][c], rx[u][c], g.x, min(16 * c + li, g.M - 1) * g.x_pitch, k, g.K);
+      for (int c = 0; c < MT; ++c) load8<DTYPE, VEC>(vx[u][c], rx[u][c], g.x, min(m0 + 16 * c + li, g.M - 1) * g.x_pitch, k, g.K);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -636,7 +636,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void ffn_rows_kernel(RowsArgs g) {
 #pragma unroll
       for (int i = 1; i < kRowWaves; ++i) v[a] += part[i][a][c][lane];
     }
-    const int m = 16 * c + li, f = f0 + 4 * lg;
+    const int m = m0 + 16 * c + li, f = f0 + 4 * lg;
     if (m >= g.M) continue;
     float y[4];
     if constexpr (W == 2) {
@@ -667,10 +667,16 @@ __global__ __launch_bounds__(kThreads) void ffn_zero_kernel(uint16_t* p, int64_t
 
 // ---- host side ---------------------------------------------------------------------------------
 
-// Rows up to which the path for few takes a call: there the time grows with the rows of x that each wave reads beside its
-// weights (bf16, us: 512 x 2048 1 row 7.5, 16 9.3, 32 11.8, 64 16.8, 65 by tiles 20; 2048 x 8192 23, 30, 40, 62, 36; fp32 13, 16,
-// 21, 33, 58 and 58, 65, 87, 135, 283).
-int few_rows(int dtype) { return dtype == SF_DTYPE_BF16 ? 32 : 64; }
+// Whether the path for few rows takes a call: there the time grows with the rows of x that each wave reads beside its weights,
+// the tiles fill few CUs where the weights are small, and in fp32 the weights' terms have to be laid out for them first.
+// us, rows (by 64) and tiles:      bf16 512 x 2048      bf16 2048 x 8192     fp32 512 x 2048      fp32 2048 x 8192
+//     1 row                         7.5                  23                   13                   58
+//    16                             9.3                  30                   16                   65
+//    32                            11.8                  40   50              21                   87
+//    64                            16.8   25             62   50              33   73             135  358
+bool few_rows(const sf_ffn_config* c) {
+  return c->M <= 32 || (c->M <= 128 && (c->dtype == SF_DTYPE_FP32 || (int64_t)c->D * c->F <= 1 << 21));
+}
 
 int check(const sf_ffn_config* c, const char* fn) {
   if (!c || c->struct_size != sizeof(sf_ffn_config)) {
@@ -827,10 +833,10 @@ struct Products {
 
 template <int DTYPE, int W, bool VEC>
 hipError_t launch_rows(const RowsArgs& g, hipStream_t st) {
-  const unsigned grid = (unsigned)((g.F + 15) / 16);
+  const dim3 grid((unsigned)((g.F + 15) / 16), (unsigned)((g.M + 63) / 64));
   if (g.M <= 16) ffn_rows_kernel<DTYPE, W, 1, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
-  else if (DTYPE == SF_DTYPE_BF16 || g.M <= 32) ffn_rows_kernel<DTYPE, W, 2, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
-  else if constexpr (DTYPE == SF_DTYPE_FP32) ffn_rows_kernel<DTYPE, W, 4, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
+  else if (g.M <= 32) ffn_rows_kernel<DTYPE, W, 2, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
+  else ffn_rows_kernel<DTYPE, W, 4, VEC><<<grid, 64 * kRowWaves, 0, st>>>(g);
   return hipGetLastError();
 }
 template <int W>
@@ -930,7 +936,7 @@ using namespace sf;
 // (Whether an array is read as it is depends on its address, which is not known here: the larger need is given.)
 extern "C" int64_t sf_ffn_workspace_bytes(const sf_ffn_config* cfg, int backward) {
   if (check(cfg, "sf_ffn_workspace_bytes") != SF_OK) return -1;
-  if (!backward && cfg->M <= few_rows(cfg->dtype)) return (int64_t)pad64((int64_t)cfg->M * cfg->F) * 4;
+  if (!backward && few_rows(cfg)) return (int64_t)pad64((int64_t)cfg->M * cfg->F) * 4;
   Job j{cfg, nullptr};
   Arena a = {nullptr, 0};
   void* const odd = (void*)2;
@@ -958,7 +964,7 @@ extern "C" int sf_ffn(const sf_ffn_config* cfg, const void* x, const void* w_gat
   if (none) return SF_OK;
   Job j{cfg, reinterpret_cast<hipStream_t>(hip_stream)};
   hipError_t err;
-  if (cfg->M <= few_rows(cfg->dtype)) {
+  if (few_rows(cfg)) {
     const auto whole = [&](const void* p, int64_t pitch, int cols) {
       return cols % 8 == 0 && pitch % (16 / (int64_t)e) == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
     };
