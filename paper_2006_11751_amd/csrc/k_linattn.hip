@@ -157,6 +157,7 @@ struct Num<SF_DTYPE_BF16> {
   __device__ static f32x4 mma(const Raw& a, const Raw& b, f32x4 c) { return mma1(a, b, c); }
   __device__ static f32x4 mma(const Raw& a, const Out& b, f32x4 c) { return mma1(a, b.t[0], mma1(a, b.t[1], c)); }
   __device__ static f32x4 mma(const Out& a, const Raw& b, f32x4 c) { return mma1(a.t[0], b, mma1(a.t[1], b, c)); }
+  __device__ static f32x4 mma(const Sum& a, const Raw& b, f32x4 c) { return mma1(a.t[0], b, mma1(a.t[1], b, mma1(a.t[2], b, c))); }
   __device__ static f32x4 mma(const Raw& a, const Sum& b, f32x4 c) { return mma1(a, b.t[0], mma1(a, b.t[1], mma1(a, b.t[2], c))); }
   // P in LDS: the terms of four slots of half `h`
   __device__ static void put4(unsigned char* frag, int term_pitch, int lane, int h, f32x4 x) {
@@ -650,6 +651,331 @@ __global__ __launch_bounds__(kThreads) void linattn_join_kernel(LinArgs g) {
   }
 }
 
+// The whole backward pass of a trajectory of at most C steps and heads of at most 64 columns, one workgroup for each (row,
+// head): a learner's rollouts (32 steps) fit.  Nothing has to be carried, so both directions of time are made from one copy
+// of the arrays in LDS, where the three sweeps above read each array two or three times:
+//   A = do v^T, P = q k^T, masked and decayed, A in both orders
+//   dq^T = k^T A^T + state0 do^T,  dk^T = q^T A + dstate v^T,  dv^T = do^T P + dstate^T k^T,  dstate0 = q~^T do + g^T dstate
+// (q~: q times what a step's term has decayed to before the first).  Roundings as above: what comes from fp32 enters a product
+// in two terms, for dstate0 in three.  Bound by memory; 2048 rows x 8 heads of 64, 32 steps, bf16, both states: 1.28 GB in
+// 265 us, 4.8 TB/s (three sweeps: 355; a row stride of 2 MB costs a tenth: 2000 rows reach 5.3).  What it took: results
+// through LDS and out by whole rows (the accumulators' own 32 bytes a row: 331 us), states read 64 bytes of a row at a time
+// (32, in two halves: 375), 16 neighbours to an XCD (one: 341).
+struct ShortArgs {
+  Strided q, k, v, d_o;
+  void *dq, *dk, *dv;              // [T][N] rows of H heads
+  const float *state0, *dstate;    // or null
+  float* dstate0;                  // or null
+  const float* log_decay;
+  const uint8_t* done;             // or null
+  int T, N, H, f32;                // f32: dk and dv are fp32 whatever the arrays are (partial sums of shared heads)
+  float scale;
+  Divisor heads, share;
+};
+
+template <int DTYPE>
+struct ShortLds {
+  static constexpr int kPitch = Lds<DTYPE, 64>::kPitch, kTile = C * kPitch;
+  static constexpr int kM = 4 * kTile, kMatrix = 4096;  // three matrices of two operands in two terms (or halves)
+  static constexpr int kEp = kM + 3 * kMatrix;          // int [C]
+  static constexpr int kFirst = kEp + C * 4;            // float [C]: the decay from before the first step to this one; 0 past an episode begin
+  static constexpr int kLast = kFirst + C * 4;          // float [C]: from this step to the last one; 0 if an episode begins between
+  static constexpr int kFlag = kLast + C * 4;
+  // at the end: dstate0 and the gradients, to go out by whole rows
+  static constexpr int kStatePitch = 68 * 4, kOut = 64 * kStatePitch, kOutBytes = kOut + 3 * kTile;
+  static constexpr int kBytes = kFlag + 16 > kOutBytes ? kFlag + 16 : kOutBytes;
+};
+
+template <int DTYPE>
+__global__ __launch_bounds__(kThreads, DTYPE == SF_DTYPE_BF16 ? 4 : 3) void linattn_short_kernel(ShortArgs g) {
+  typedef Num<DTYPE> M;
+  typedef ShortLds<DTYPE> L;
+  constexpr int W = M::kPieceWords;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int li = lane & 15, lg = lane >> 4;
+  // (workgroups go round the XCDs: 16 neighbours, whose rows of a step are neighbours too, for each)
+  const int bh = (blockIdx.x & ~127) + (blockIdx.x & 7) * 16 + ((blockIdx.x >> 3) & 15);
+  if (bh >= g.N * g.H) return;
+  const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h);
+  const int T = g.T, dk = g.q.d, dv = g.v.d;
+  const float l2 = fmaxf(g.log_decay[h] * 1.44269504f, -1e30f);
+  constexpr unsigned kOutside = 0x80000000u;
+  auto buffer = [&](const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000); };
+
+  // the arrays: one piece of each a thread
+  unsigned w[4][W];
+  const int row = tid >> 3, col = (tid & 7) * 8;
+  auto fetch = [&](unsigned* to, const Strided& a) {
+    const auto from = buffer((const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes, 0x7FFFFFFF);
+    const unsigned at = row < T && col < a.d ? (unsigned)(row * (int)a.st + col) * M::kBytes : kOutside;
+#pragma unroll
+    for (int i = 0; i < W; i += 4) *(u32x4*)(to + i) = __builtin_amdgcn_raw_buffer_load_b128(from, at + 4 * i, 0, 0);
+  };
+  fetch(w[0], g.q);
+  fetch(w[1], g.k);
+  fetch(w[2], g.v);
+  fetch(w[3], g.d_o);
+  const bool begin = g.done && lane < T && g.done[(size_t)lane * g.N + n] != 0;
+  const unsigned marks = (unsigned)__ballot(begin);
+  // the states as operands: rows 16 wave + li, eight K-slots 32 s + 16 (j / 4) + 4 lg + j % 4, so that four lanes read 64
+  // bytes of a row together and the columns' slots are the rows of an accumulator too
+  const size_t state_at = (size_t)bh * dk * dv;
+  const int state_bytes = dk * dv * 4, mine = 16 * wave + li;
+  const auto s0 = buffer(g.state0 + (g.state0 ? state_at : 0), g.state0 ? state_bytes : 0);
+  const auto ds = buffer(g.dstate + (g.dstate ? state_at : 0), g.dstate ? state_bytes : 0);
+  float in[2][8], end[2][8], end_t[2][8];  // state0 and dstate by rows of k, dstate by rows of v
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const int x = 16 * s + 4 * lg;
+    const unsigned at = x < dv ? (unsigned)(mine * dv + x) * 4 : kOutside;  // (rows past dk lie past the end)
+    *(f32x4*)(in[s >> 1] + 4 * (s & 1)) = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(s0, at, 0, 0));
+    *(f32x4*)(end[s >> 1] + 4 * (s & 1)) = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ds, at, 0, 0));
+  }
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const unsigned at = mine < dv ? (unsigned)((16 * s + 4 * lg) * dv + mine) * 4 : kOutside;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) end_t[s >> 1][4 * (s & 1) + j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(ds, at, j * dv * 4, 0));
+  }
+
+  unsigned char *const tq = lds, *const tk = lds + L::kTile, *const tv = lds + 2 * L::kTile, *const to = lds + 3 * L::kTile;
+  int* const ep = (int*)(lds + L::kEp);
+  float *const first = (float*)(lds + L::kFirst), *const last = (float*)(lds + L::kLast);
+  int* const flag = (int*)(lds + L::kFlag);
+  if (tid == 0) *flag = 0;
+  if (tid < C) {
+    const int e = __popc(marks & ((2u << tid) - 1));
+    ep[tid] = e;
+    first[tid] = e == 0 ? pow2(l2 * (float)(tid + 1)) : 0.0f;
+    last[tid] = tid < T && e == __popc(marks) ? pow2(l2 * (float)(T - 1 - tid)) : 0.0f;
+  }
+  __syncthreads();
+  float test = 0.0f;
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) *(u32x4*)(lds + a * L::kTile + row * L::kPitch + col * M::kBytes + 4 * i) = *(u32x4*)(w[a] + i);
+    test = finite_test<DTYPE>(w[a], test);
+  }
+  if (test != 0.0f) *flag = 1;
+  __syncthreads();
+
+  const int64_t head_k = ((int64_t)n * g.H + h) * dk, head_v = ((int64_t)n * g.H + h) * dv, step_k = (int64_t)g.N * g.H * dk,
+                step_v = (int64_t)g.N * g.H * dv;
+  if (*flag) {
+    // Element by element, so that nothing that is not finite meets a masked zero.
+    float *const A = (float*)(lds + L::kM), *const P = A + C * C;
+    auto at = [&](const unsigned char* tile, int r, int c) { return M::element(tile + r * L::kPitch + c * M::kBytes); };
+    for (int e = tid; e < C * C; e += kThreads) {
+      const int i = e / C, j = e % C;
+      float a = 0.0f, p = 0.0f;
+      if (j <= i && ep[i] == ep[j]) {
+        for (int y = 0; y < dv; ++y) a += at(to, i, y) * at(tv, j, y);
+        for (int x = 0; x < dk; ++x) p += at(tq, i, x) * at(tk, j, x);
+        const float c = g.scale * pow2(l2 * (float)(i - j));
+        a *= c;
+        p *= c;
+      }
+      A[e] = a;
+      P[e] = p;
+    }
+    __syncthreads();
+    auto put = [&](void* out, bool f32, int64_t i, float v) {
+      if (f32) ((float*)out)[i] = v;
+      else M::store((unsigned char*)out + i * M::kBytes, v);
+    };
+    for (int e = tid; e < T * dk; e += kThreads) {
+      const int t = e / dk, x = e % dk;
+      float q = 0.0f, k = 0.0f, v = 0.0f;
+      for (int j = 0; j <= t; ++j)
+        if (ep[j] == ep[t]) q += A[t * C + j] * at(tk, j, x);
+      for (int i = t; i < T; ++i)
+        if (ep[i] == ep[t]) k += A[i * C + t] * at(tq, i, x);
+      if (g.state0 && ep[t] == 0) {
+        for (int y = 0; y < dv; ++y) v += g.state0[state_at + x * dv + y] * at(to, t, y);
+        q += g.scale * first[t] * v;
+      }
+      if (g.dstate && ep[t] == ep[T - 1]) {
+        v = 0.0f;
+        for (int y = 0; y < dv; ++y) v += g.dstate[state_at + x * dv + y] * at(tv, t, y);
+        k += last[t] * v;
+      }
+      put(g.dq, DTYPE == SF_DTYPE_FP32, t * step_k + head_k + x, q);
+      put(g.dk, g.f32, t * step_k + head_k + x, k);
+    }
+    for (int e = tid; e < T * dv; e += kThreads) {
+      const int t = e / dv, y = e % dv;
+      float v = 0.0f, k = 0.0f;
+      for (int i = t; i < T; ++i)
+        if (ep[i] == ep[t]) v += P[i * C + t] * at(to, i, y);
+      if (g.dstate && ep[t] == ep[T - 1]) {
+        for (int x = 0; x < dk; ++x) k += g.dstate[state_at + x * dv + y] * at(tk, t, x);
+        v += last[t] * k;
+      }
+      put(g.dv, g.f32, t * step_v + head_v + y, v);
+    }
+    if (g.dstate0)
+      for (int e = tid; e < dk * dv; e += kThreads) {
+        float v = 0.0f;
+        for (int i = 0; i < T; ++i)
+          if (ep[i] == 0) v += g.scale * first[i] * at(tq, i, e / dv) * at(to, i, e % dv);
+        if (g.dstate && marks == 0) v += pow2(l2 * (float)T) * g.dstate[state_at + e];
+        g.dstate0[state_at + e] = v;
+      }
+    return;
+  }
+
+  // the matrices: wave (I, J) makes its tile of each, i in tile I, j in tile J
+  {
+    const int I = wave >> 1, J = wave & 1;
+    f32x4 m1 = {0.0f, 0.0f, 0.0f, 0.0f}, m2 = m1, m3 = m1;
+    if (J <= I) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int at_i = (16 * I + li) * L::kPitch + (32 * s + 8 * lg) * M::kBytes, at_j = (16 * J + li) * L::kPitch + (32 * s + 8 * lg) * M::kBytes;
+        if (32 * s < dv) {
+          const auto o = M::row(to + at_i), v = M::row(tv + at_j);
+          m1 = M::mma(v, o, m1);  // [j][i]
+          m2 = M::mma(o, v, m2);  // [i][j]
+        }
+        if (32 * s < dk) m3 = M::mma(M::row(tq + at_i), M::row(tk + at_j), m3);
+      }
+      const int ahead = 16 * (I - J);
+      const int ei = ep[16 * I + li], ej = ep[16 * J + li];
+      const i32x4 eis = *(const i32x4*)(ep + 16 * I + 4 * lg), ejs = *(const i32x4*)(ep + 16 * J + 4 * lg);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int lag1 = ahead + li - 4 * lg - r, lag2 = ahead + 4 * lg + r - li;
+        m1[r] = lag1 >= 0 && ejs[r] == ei ? m1[r] * (g.scale * pow2(l2 * (float)lag1)) : 0.0f;
+        const float c = g.scale * pow2(l2 * (float)lag2);
+        const bool in2 = lag2 >= 0 && eis[r] == ej;
+        m2[r] = in2 ? m2[r] * c : 0.0f;
+        m3[r] = in2 ? m3[r] * c : 0.0f;
+      }
+    }
+    unsigned char* const m = lds + L::kM;
+    M::put4(m + I * 1024, 2048, lane, J, m1);
+    M::put4(m + L::kMatrix + J * 1024, 2048, lane, I, m2);
+    M::put4(m + 2 * L::kMatrix + J * 1024, 2048, lane, I, m3);
+  }
+  __syncthreads();
+
+  // columns 16 wave .. (or, c0, others) of an array, K-slots its steps
+  auto columns = [&](const unsigned char* tile, int c0) {
+    typename M::Raw r;
+    if constexpr (DTYPE == SF_DTYPE_BF16) {
+      const unsigned char* at = tile + (4 * lg + (li >> 2)) * L::kPitch + (c0 + 4 * (li & 3)) * M::kBytes;
+      const u32x2 x = M::column4(at), y = M::column4(at + 16 * L::kPitch);
+      r = u32x4{x[0], x[1], y[0], y[1]};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r.x[j] = M::element(tile + (4 * lg + (j & 3) + 16 * (j >> 2)) * L::kPitch + (c0 + li) * M::kBytes);
+    }
+    return r;
+  };
+  constexpr bool kF32 = DTYPE == SF_DTYPE_FP32;
+  f32x4 kept[3][2] = {}, kept0[4] = {};
+  // the K-slots of the states, of a row
+  auto slots = [&](const unsigned char* at) {
+    typename M::Raw r;
+    if constexpr (DTYPE == SF_DTYPE_BF16) {
+      const u32x2 x = *(const u32x2*)at, y = *(const u32x2*)(at + 32);
+      r = u32x4{x[0], x[1], y[0], y[1]};
+    } else {
+      *(f32x4*)&r.x[0] = *(const f32x4*)at;
+      *(f32x4*)&r.x[4] = *(const f32x4*)(at + 64);
+    }
+    return r;
+  };
+  // one gradient: what the state gives (its rows by the other array's rows), scaled per step, and on top what the steps give
+  auto gradient = [&](const float (*state)[8], bool has_state, const unsigned char* rows, int d_rows, const float* weight, float scale,
+                      const typename M::Raw& by_step, int matrix, void* out, bool f32, int64_t step, int64_t head, int d) {
+    if (16 * wave >= d) return;
+#pragma unroll
+    for (int I = 0; I < 2; ++I) {
+      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      const int t = 16 * I + li;
+      if (has_state) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          if (32 * s < d_rows) acc = M::mma(M::out_terms(state[s]), slots(rows + t * L::kPitch + (32 * s + 4 * lg) * M::kBytes), acc);
+        const float c = scale * weight[t];
+        const bool reach = weight == first ? ep[t] == 0 : ep[t] == __popc(marks);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[r] = reach ? acc[r] * c : 0.0f;
+      }
+      acc = M::mma(by_step, M::get(lds + L::kM + matrix * L::kMatrix + I * 1024, 2048, lane), acc);
+      const int y = 16 * wave + 4 * lg;
+      kept[matrix][I] = acc;
+      if (f32 && !kF32 && t < T && y < d) *(f32x4*)((float*)out + t * step + head + y) = acc;
+    }
+  };
+  gradient(in, g.state0 != nullptr, to, dv, first, g.scale, columns(tk, 16 * wave), 0, g.dq, kF32, step_k, head_k, dk);
+  gradient(end, g.dstate != nullptr, tv, dv, last, 1.0f, columns(tq, 16 * wave), 1, g.dk, kF32 || g.f32, step_k, head_k, dk);
+  const typename M::Raw o = columns(to, 16 * wave);
+  gradient(end_t, g.dstate != nullptr, tk, dk, last, 1.0f, o, 2, g.dv, kF32 || g.f32, step_v, head_v, dv);
+
+  if (g.dstate0 && 16 * wave < dv) {
+    f32x4 w0 = *(const f32x4*)(first + 4 * lg), w1 = *(const f32x4*)(first + 16 + 4 * lg);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      w0[r] *= g.scale;
+      w1[r] *= g.scale;
+    }
+    const float keep = pow2(l2 * (float)T);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (16 * s >= dk) break;
+      float x[8];
+      M::values(columns(tq, 16 * s), x);
+      f32x4 acc;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[r] *= w0[r];
+        x[4 + r] *= w1[r];
+        acc[r] = marks ? 0.0f : keep * end_t[s >> 1][4 * (s & 1) + r];
+      }
+      kept0[s] = M::mma(M::sum_terms(x), o, acc);
+    }
+  }
+
+  __syncthreads();
+#pragma unroll
+  for (int m = 0; m < 3; ++m)
+#pragma unroll
+    for (int I = 0; I < 2; ++I) {
+      unsigned char* const at = lds + L::kOut + m * L::kTile + (16 * I + li) * L::kPitch + (16 * wave + 4 * lg) * M::kBytes;
+      if constexpr (kF32) *(f32x4*)at = kept[m][I];
+      else *(u32x2*)at = u32x2{pack_bf16(kept[m][I][0], kept[m][I][1]), pack_bf16(kept[m][I][2], kept[m][I][3])};
+    }
+  if (g.dstate0) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) *(float*)(lds + (16 * s + 4 * lg + r) * L::kStatePitch + mine * 4) = kept0[s][r];
+  }
+  __syncthreads();
+  auto store = [&](void* out, int m, int64_t at, int d) {
+    if (row >= T || col >= d) return;
+#pragma unroll
+    for (int i = 0; i < W; i += 4)
+      *(u32x4*)((unsigned char*)out + at * M::kBytes + 4 * i) = *(const u32x4*)(lds + L::kOut + m * L::kTile + row * L::kPitch + col * M::kBytes + 4 * i);
+  };
+  store(g.dq, 0, row * step_k + head_k + col, dk);
+  if (kF32 || !g.f32) {
+    store(g.dk, 1, row * step_k + head_k + col, dk);
+    store(g.dv, 2, row * step_v + head_v + col, dv);
+  }
+  if (!g.dstate0) return;
+  const auto put = buffer(g.dstate0 + state_at, state_bytes);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int x = 16 * i + (tid >> 4), y = 4 * (tid & 15);
+    __builtin_amdgcn_raw_buffer_store_b128(*(const u32x4*)(lds + x * L::kStatePitch + y * 4), put, y < dv ? (unsigned)(x * dv + y) * 4 : kOutside, 0, 0);
+  }
+}
+
 // Sums of the gradients of shared heads: in [rows][H][d] fp32, out [rows][H / share][d].
 template <int DTYPE>
 __global__ __launch_bounds__(kThreads) void linattn_share_kernel(const float* in, void* out, int64_t n_out, int d, int share) {
@@ -886,6 +1212,24 @@ int run(const char* fn, const sf_linattn_config* c, LinArgs& g, int ops, const W
   return SF_OK;
 }
 
+// The sums over the heads that share one of k and v.
+int add_shared(const char* fn, const sf_linattn_config* c, const float* part_k, const float* part_v, void* dk, void* dv, hipStream_t st) {
+  const int share = c->H / c->Hk;
+  const int64_t nk = (int64_t)c->T * c->N * c->Hk * c->dk, nv = (int64_t)c->T * c->N * c->Hk * c->dv;
+  const auto grid = [](int64_t n) { return (unsigned)std::min<int64_t>((n + kThreads - 1) / kThreads, 1 << 20); };
+  if (c->dtype == SF_DTYPE_BF16) {
+    linattn_share_kernel<SF_DTYPE_BF16><<<grid(nk), kThreads, 0, st>>>(part_k, dk, nk, c->dk, share);
+    linattn_share_kernel<SF_DTYPE_BF16><<<grid(nv), kThreads, 0, st>>>(part_v, dv, nv, c->dv, share);
+  } else {
+    linattn_share_kernel<SF_DTYPE_FP32><<<grid(nk), kThreads, 0, st>>>(part_k, dk, nk, c->dk, share);
+    linattn_share_kernel<SF_DTYPE_FP32><<<grid(nv), kThreads, 0, st>>>(part_v, dv, nv, c->dv, share);
+  }
+  const hipError_t err = hipGetLastError();
+  if (err == hipSuccess) return SF_OK;
+  set_error("%s: launch failed: %s", fn, hipGetErrorString(err));
+  return SF_ERR_DEVICE;
+}
+
 }  // namespace
 
 }  // namespace sf
@@ -953,11 +1297,44 @@ extern "C" int sf_linattn_backward(const sf_linattn_config* cfg, const void* q, 
   unsigned char* ws = (unsigned char*)workspace;
   float* part_k = (float*)(ws + w.state + w.keep);
   float* part_v = (float*)(ws + w.state + w.keep + w.dk);
+  const Strided sq = strided(cfg, q, cfg->q_stride, false, Dk), sk = strided(cfg, k, cfg->k_stride, share > 1, Dk),
+                sv = strided(cfg, v, cfg->v_stride, share > 1, Dv), so = strided(cfg, d_o, cfg->o_stride, false, Dv);
+  const auto sixteen = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+  if (cfg->T >= 1 && cfg->T <= C && Dk <= 64 && Dv <= 64 && sq.vec && sk.vec && sv.vec && so.vec && sixteen(dq) && sixteen(dk) && sixteen(dv)) {
+    ShortArgs a = {};
+    a.q = sq;
+    a.k = sk;
+    a.v = sv;
+    a.d_o = so;
+    a.dq = dq;
+    a.dk = share > 1 ? part_k : dk;
+    a.dv = share > 1 ? part_v : dv;
+    a.state0 = state0;
+    a.dstate = dstate;
+    a.dstate0 = dstate0;
+    a.log_decay = log_decay;
+    a.done = done;
+    a.T = cfg->T;
+    a.N = cfg->N;
+    a.H = H;
+    a.f32 = share > 1 || cfg->dtype == SF_DTYPE_FP32;
+    a.scale = cfg->scale;
+    a.heads = divisor(H);
+    a.share = divisor(share);
+    if (!none) {
+      if (cfg->dtype == SF_DTYPE_BF16) linattn_short_kernel<SF_DTYPE_BF16><<<(cfg->N * H + 127) / 128 * 128, kThreads, ShortLds<SF_DTYPE_BF16>::kBytes, st>>>(a);
+      else linattn_short_kernel<SF_DTYPE_FP32><<<(cfg->N * H + 127) / 128 * 128, kThreads, ShortLds<SF_DTYPE_FP32>::kBytes, st>>>(a);
+    }
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) {
+      set_error("%s: launch failed: %s", fn, hipGetErrorString(err));
+      return SF_ERR_DEVICE;
+    }
+    return share == 1 || none ? SF_OK : add_shared(fn, cfg, part_k, part_v, dk, dv, st);
+  }
   LinArgs g = {};
   g.log_decay = log_decay;
   g.done = done;
-  const Strided sq = strided(cfg, q, cfg->q_stride, false, Dk), sk = strided(cfg, k, cfg->k_stride, share > 1, Dk),
-                sv = strided(cfg, v, cfg->v_stride, share > 1, Dv), so = strided(cfg, d_o, cfg->o_stride, false, Dv);
   LinOp &oq = g.op[0], &ok = g.op[1], &ov = g.op[2];
   oq.q = so;
   oq.k = sv;
@@ -990,23 +1367,7 @@ extern "C" int sf_linattn_backward(const sf_linattn_config* cfg, const void* q, 
   ov.alpha = 1.0f;
   ov.reverse = 1;
   rc = run(fn, cfg, g, 3, w, ws, st);
-  if (rc != SF_OK || share == 1 || none) return rc;
-  const int64_t nk = (int64_t)cfg->T * cfg->N * Hk * Dk, nv = (int64_t)cfg->T * cfg->N * Hk * Dv;
-  const auto grid = [](int64_t n) { return (unsigned)std::min<int64_t>((n + kThreads - 1) / kThreads, 1 << 20); };
-  const unsigned gk = grid(nk), gv = grid(nv);
-  if (cfg->dtype == SF_DTYPE_BF16) {
-    linattn_share_kernel<SF_DTYPE_BF16><<<gk, kThreads, 0, st>>>(part_k, dk, nk, Dk, share);
-    linattn_share_kernel<SF_DTYPE_BF16><<<gv, kThreads, 0, st>>>(part_v, dv, nv, Dv, share);
-  } else {
-    linattn_share_kernel<SF_DTYPE_FP32><<<gk, kThreads, 0, st>>>(part_k, dk, nk, Dk, share);
-    linattn_share_kernel<SF_DTYPE_FP32><<<gv, kThreads, 0, st>>>(part_v, dv, nv, Dv, share);
-  }
-  const hipError_t err = hipGetLastError();
-  if (err != hipSuccess) {
-    set_error("%s: launch failed: %s", fn, hipGetErrorString(err));
-    return SF_ERR_DEVICE;
-  }
-  return SF_OK;
+  return rc != SF_OK || share == 1 || none ? rc : add_shared(fn, cfg, part_k, part_v, dk, dv, st);
 }
 
 extern "C" int sf_linattn_step(const sf_linattn_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,

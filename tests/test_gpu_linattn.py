@@ -346,3 +346,54 @@ def test_refusals(torch_cuda):
     with pytest.raises(SfError) as e:
         memory.linear_attention_backward(q, k, v, ld, do, dstate=ds, out=dict(dstate0=ds))
     assert e.value.code == -4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,N,H,Hk,dk,dv", [(1, 1, 1, 1, 8, 8), (7, 5, 4, 1, 24, 64), (16, 50, 6, 2, 64, 40), (17, 3, 4, 2, 48, 32),
+                                            (31, 130, 2, 2, 56, 8), (32, 7, 3, 3, 64, 64), (32, 2, 8, 4, 16, 64)])
+def test_short_trajectories(torch_cuda, T, N, H, Hk, dk, dv, dtype):
+    """At most 32 steps: the backward pass has a kernel of its own for them."""
+    torch = torch_cuda
+    from paper_2006_11751_amd import memory
+    x, do, ds = make(torch, T, N, H, Hk, dk, dv, dtype, seed=T + dk)
+    _, a = both(torch, x, do, ds, dtype, scale=-0.7)
+    # the same bits in another order in memory
+    y = [x[n].transpose(0, 1).contiguous().transpose(0, 1) for n in "qkv"]
+    b = memory.linear_attention_backward(*y, x["log_decay"], do.transpose(0, 2).contiguous().transpose(0, 2), dstate=ds, done=x["done"],
+                                         state0=x["state0"], scale=-0.7)
+    for n in ("dq", "dk", "dv", "dstate0"):
+        assert torch.equal(a[n], b[n]), n
+    # no states, no episode ends
+    args = (x["q"], x["k"], x["v"], x["log_decay"])
+    c = memory.linear_attention_backward(*args, do)
+    absargs = tuple(t.abs() for t in args[:3]) + (x["log_decay"],)
+    check(c, oracle(*args, None, None, dk ** -0.5, do), oracle(*absargs, None, None, dk ** -0.5, do.abs()), (dk + 160 + T / 16) * (H // Hk), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_short_trajectories_with_values_that_are_not_finite(torch_cuda, dtype):
+    torch = torch_cuda
+    from paper_2006_11751_amd import memory
+    T, inf, nan = 24, float("inf"), float("nan")
+    x, do, ds = make(torch, T, 2, 2, 2, 64, 64, dtype, seed=5, p_done=0.0)
+    x["done"][8], x["done"][17] = 1, 1
+    x["k"][11, 0, 0, 7], x["v"][12, 0, 1, 2], x["q"][11, 1], do[12, 0, 1, 4] = nan, inf, nan, -inf
+    x["state0"][0, 0, 3, 5], ds[1, 0, 2, 2] = inf, -inf
+    args = (x["q"], x["k"], x["v"], x["log_decay"])
+    back = memory.linear_attention_backward(*args, do, dstate=ds, done=x["done"], state0=x["state0"])
+    clean = lambda a: torch.nan_to_num(a, nan=0.0, posinf=0.0, neginf=0.0)
+    cargs = tuple(clean(a) for a in args[:3]) + (x["log_decay"],)
+    want = oracle(*cargs, x["done"], clean(x["state0"]), 0.125, clean(do), clean(ds))
+    size = oracle(*(a.abs() for a in cargs[:3]), x["log_decay"], x["done"], clean(x["state0"]).abs(), 0.125, clean(do).abs(), clean(ds).abs())
+    within = torch.arange(T, device="cuda")[:, None, None]
+    row, head = torch.arange(2, device="cuda")[:, None], torch.arange(2, device="cuda")
+    first = (within < 8) & ~((row == 0) & (head == 0))           # state0 is not finite there
+    last = (within >= 17) & ~((row == 1) & (head == 0))          # dstate is not finite there
+    inside = (within >= 8) & (within < 17)
+    for n, fine in (("dq", first | (inside & (within < 11)) | (within >= 17)), ("dk", (within < 8) | (inside & (within > 12)) | last),
+                    ("dv", (within < 8) | (inside & (within > 12)) | last)):
+        pick = lambda a: {n: torch.where(fine[..., None], a[n], torch.zeros((), dtype=a[n].dtype, device="cuda"))}
+        check(pick(back), pick(want), pick(size), 64 + 160 + T / 16, dtype)
+    check(back, {"dstate0": want["dstate0"]}, size, 64 + 160 + T / 16, dtype)
+    assert not torch.isfinite(back["dq"][3, 0, 0]).all() and not torch.isfinite(back["dk"][20, 1, 0]).all()
+    assert not torch.isfinite(back["dq"][14, 0]).all() and not torch.isfinite(back["dk"][9, 1]).all()
