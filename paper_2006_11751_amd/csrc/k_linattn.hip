@@ -1098,11 +1098,15 @@ int check_ptr(const char* fn, const char* name, const void* p, size_t align, boo
 struct Split {
   int n_seg, seg_len;
 };
-// Pieces of T where rows x heads leave CUs without a workgroup (the pieces' states cost a pass over k and v more): each with
-// at least four chunks.
+// Pieces of T where rows x heads leave CUs without a workgroup, each with at least 256 steps.  The pieces' states cost a pass
+// over k and v more, two launches and their own bytes, so T has to be longer the more heads and the larger states there are.
+// bf16, us whole and cut: 8 heads of 64, 512 steps 28 and 30, 768: 41 and 31, 4096: 200 and 32; 96 heads, 512: 29 and 37, 768: 46 and
+// 42, 2048: 115 and 54; 240 heads, 512: 35 and 53, 1024: 62 and 68; of 128: 8 heads, 512: 39 and 39, 4096: 293 and 45; 32, 512:
+// 41 and 48, 768: 61 and 50; 96, 768: 66 and 83, 1024: 85 and 87, 2048: 162 and 134; 240, 1024: 110 and 189.
 Split split_of(const sf_linattn_config* c, int ops) {
   const int64_t lanes = (int64_t)c->N * c->H * ops;
-  const int64_t want = lanes > 0 && lanes < 384 ? (768 + lanes - 1) / lanes : 1;
+  const bool cut = lanes > 0 && lanes < 384 && c->T > 512 + lanes * std::max(c->dk, c->dv) / 24;
+  const int64_t want = cut ? (768 + lanes - 1) / lanes : 1;
   int64_t len = (c->T + want - 1) / want;
   len = (len + 63) / 64 * 64;
   if (len < 256) len = 256;

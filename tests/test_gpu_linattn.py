@@ -397,3 +397,11 @@ def test_short_trajectories_with_values_that_are_not_finite(torch_cuda, dtype):
     check(back, {"dstate0": want["dstate0"]}, size, 64 + 160 + T / 16, dtype)
     assert not torch.isfinite(back["dq"][3, 0, 0]).all() and not torch.isfinite(back["dk"][20, 1, 0]).all()
     assert not torch.isfinite(back["dq"][14, 0]).all() and not torch.isfinite(back["dk"][9, 1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,N,H,dk,dv", [(700, 2, 2, 128, 128), (1300, 5, 4, 64, 64), (1027, 3, 5, 24, 100), (513, 1, 1, 8, 8)])
+def test_long_trajectories_of_few_rows(torch_cuda, T, N, H, dk, dv, dtype):
+    """Lengths that are cut into pieces, whose states are made first."""
+    x, do, ds = make(torch_cuda, T, N, H, H, dk, dv, dtype, seed=T, p_done=0.003)
+    both(torch_cuda, x, do, ds, dtype)
