@@ -5,7 +5,8 @@
 // Every gradient is the same sum with other arrays in the three places and, for two of them, time reversed:
 //   dq: (do, v, k) forwards with S transposed;  dk: (v, do, q) and dv: (k, q, do) backwards with the state
 //   R_t = scale q_t do_t^T + g R_{t+1}.
-// So there is one kernel, told by LinOp what stands where; a launch of the backward pass runs all three.
+// So there is one kernel, told by LinOp what stands where; a launch of the backward pass runs all three.  (Short trajectories
+// have a kernel of their own for the gradients, a single step has one.)
 //
 // A workgroup of four waves walks the chunks of one (row, head), or of one piece of T, for 64 columns of v.  A wave owns 16
 // of them: its part of the state stays in registers as the accumulator of the update.  The products are arranged
@@ -25,6 +26,13 @@
 // Masked entries are selected, but a product still multiplies their zeros with the other operand's rows, and 0 x NaN
 // is NaN.  So the chunk's k and v are tested as they are staged; a chunk with a NaN or an infinity in them is taken again as
 // chunks of one step, which keeps it from earlier steps and from later episodes.
+//
+// Measured, bf16.  32 steps of 64 rows x 8 heads of 64 (25 MB): 8 us, of which a chunk's chain of load, two products and
+// store is most (3.2 TB/s); 2048 rows: 186 us, 4.3 TB/s; 128 steps of 256 rows: 39 us, 5.1.  16384 steps of one row, 8 heads
+// of 128, in 64 pieces: 26 us for the pieces' states, 16 to join them (70 MB written and read), 49 for the results: the
+// eight chunks of a piece in sequence, each twice.  fp32, 333 steps of 30 rows x 6 heads of 40 and 72, gradients: 92 us for
+// the sweeps, eleven chunks in sequence of 8 us each on the fp32 matrix instruction, 11 for the shared heads' sums.
+// Columns that are no multiple of 8 are read number by number (200 rows x 100 steps x 8 heads of 100: 245 us, 1.0 TB/s).
 #include <math.h>
 
 #include <algorithm>
@@ -626,6 +634,7 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 || DTYPE == S
 }
 
 // What enters each piece of T, from the pieces' own states: one thread per element of a state, kAhead pieces read ahead.
+// Bound by those bytes' latency: 8 heads of 128 x 128, 64 pieces, 34 MB read and written: 15.7 us, 4.3 TB/s.
 __global__ __launch_bounds__(kThreads) void linattn_join_kernel(LinArgs g) {
   constexpr int kAhead = 16;
   const LinOp& op = g.op[blockIdx.z];
@@ -976,7 +985,8 @@ __global__ __launch_bounds__(kThreads, DTYPE == SF_DTYPE_BF16 ? 4 : 3) void lina
   }
 }
 
-// Sums of the gradients of shared heads: in [rows][H][d] fp32, out [rows][H / share][d].
+// Sums of the gradients of shared heads: in [rows][H][d] fp32, out [rows][H / share][d].  (In a launch of their own, in one
+// order: 9990 rows, 6 heads of 40 to 2: 4.9 us.)
 template <int DTYPE>
 __global__ __launch_bounds__(kThreads) void linattn_share_kernel(const float* in, void* out, int64_t n_out, int d, int share) {
   for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < n_out; e += (int64_t)gridDim.x * kThreads) {
@@ -988,7 +998,8 @@ __global__ __launch_bounds__(kThreads) void linattn_share_kernel(const float* in
 }
 
 // One step of one (row, head): the state is read, decayed, added to, written and multiplied with q.  Bound by those
-// bytes; a thread holds four neighbours of every (256 / lanes)-th row, so that all its loads are under way at once.
+// bytes; a thread holds four neighbours of every (256 / lanes)-th row, so that all its loads are under way at once.  2048 rows
+// x 8 heads of 64 (546 MB): 112 us, 4.9 TB/s; 16 rows: 5.5 us, a launch and one trip to memory.
 template <int DTYPE, bool VEC>
 __global__ __launch_bounds__(kThreads) void linattn_step_kernel(LinOp op, const float* log_decay, const uint8_t* done, float* table,
                                                                 int n_env, const int32_t* ids, int H, int share, int lanes_log2) {

