@@ -776,13 +776,21 @@ int64_t tiles_of(int F, int M, int BF, int BM) { return (int64_t)((F + BF - 1) /
 // kPair 96 tiles 29 and 20, 128 29 and 22, 160 29.6 and 29.2, 208 32 and 37, 512 69 and 75; kTriple 128 32 and 25, 192 34 and
 // 36, 256 36 and 41, 320 60 and 56 (a second round of large ones just begun), 416 62 and 72, 1024 135 and 148.
 constexpr int kEnough = 160;
+// And a smaller one still where a round of workgroups takes all of it (256).  us, 64 x 128 and 64 x 64, forwards and backwards: fp32, D =
+// 1920, F = 576, 939 rows (135 tiles of 64 x 64): 122 and 104, 297 and 268; 2048 rows (288): 141 and 156, 390 and 436; bf16, 1024 x
+// 2048, 320 rows (160): 28 and 25, 50 and 46; 939 rows (480): 30 and 31, 67 and 70.
+constexpr int kOneRound = 256;
 template <int FORM>
 hipError_t launch(GemmGroup& group, hipStream_t st) {
   const GemmArgs& g = group.g[0];
-  if constexpr (FORM == kPair)
-    return tiles_of(g.Fp, g.M, 128, 256) >= kEnough ? launch_t<kPair, 0, 128, 256, 64, 1>(group, st) : launch_t<kPair, 0, 64, 128, 64, 2>(group, st);
-  else
-    return tiles_of(g.Fp, g.M, 128, 128) >= kEnough ? launch_t<kTriple, 4, 128, 128, 32, 1>(group, st) : launch_t<kTriple, 4, 64, 128, 32, 2>(group, st);
+  const bool one_round = tiles_of(g.Fp, g.M, 64, 64) <= kOneRound;
+  if constexpr (FORM == kPair) {
+    if (tiles_of(g.Fp, g.M, 128, 256) >= kEnough) return launch_t<kPair, 0, 128, 256, 64, 1>(group, st);
+    return one_round ? launch_t<kPair, 0, 64, 64, 64, 2>(group, st) : launch_t<kPair, 0, 64, 128, 64, 2>(group, st);
+  } else {
+    if (tiles_of(g.Fp, g.M, 128, 128) >= kEnough) return launch_t<kTriple, 4, 128, 128, 32, 1>(group, st);
+    return one_round ? launch_t<kTriple, 4, 64, 64, 32, 2>(group, st) : launch_t<kTriple, 4, 64, 128, 32, 2>(group, st);
+  }
 }
 
 // Products of form kOne that do not depend on one another, as one launch, and where K is cut a second one.

@@ -232,3 +232,10 @@ def test_refusals(torch_cuda):
         memory.gated_ffn_backward(dy=dy[:2], **base)
     with pytest.raises(ValueError):
         memory.gated_ffn_backward(dy=dy, out=dict(dw_up=wd), **base)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,D,F", [(500, 130, 1150), (1030, 120, 1000), (700, 100, 2100), (1024, 64, 1024)])
+def test_tiles_on_both_sides_of_one_round(torch_cuda, M, D, F, dtype):
+    ws, dy = make(torch_cuda, M, D, F, dtype, seed=2)
+    both(torch_cuda, ws, dy, dtype)
