@@ -259,6 +259,9 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
       const int64_t r0 = n < W ? f0 : m0;
       pitch[n] = (unsigned)o.pitch * 2;
       from[n] = row_of(Constant<L::first(n)>()) * pitch[n] + col_of(Constant<L::first(n)>());
+      // (across K the bounds end only the step's last row: behind the others lie gaps or the next row.  All of a thread's pieces of an
+      // array are of one column, the columns a multiple of eight; 63 rows of 2^23 bytes further on is still past the end.)
+      if (L::across(n) && col_of(Constant<L::first(n)>()) >= 2 * (int)(o.cols - r0)) from[n] = 0x80000000u;
       base[n] = (const unsigned char*)(o.p + (n < W ? kPlaneW[term] : kPlaneX[term]) * o.plane + (L::across(n) ? r0 : r0 * o.pitch));
     });
   };
@@ -429,7 +432,8 @@ __global__ __launch_bounds__(kThreads, WAVES) void ffn_gemm_kernel(GemmGroup gro
           store_out8(a_.out, a_.out_f32, a_.F, ((int64_t)part * a_.M + m) * a_.F + f, a_.F - f, area + row * EP + col);
       }
     } else {
-      // (rows of w past F and rows of x past M were read as zeros, so that h, dg and du are zeros where they are padded)
+      // (rows of w along K, columns of w across K past F and rows of x past M were read as zeros, so that gate, up and dh, and with them h,
+      // dg and du, are zeros where they are padded)
       // (a piece that is not there has an offset past the end, so that no branch parts the rounds of the loop)
       const int64_t corner = (int64_t)mw * a_.h.pitch + fwave;  // (all three arrays have one shape)
       auto buffer = [&](const Terms& t, int plane) __attribute__((always_inline)) {

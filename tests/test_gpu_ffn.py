@@ -239,3 +239,25 @@ def test_refusals(torch_cuda):
 def test_tiles_on_both_sides_of_one_round(torch_cuda, M, D, F, dtype):
     ws, dy = make(torch_cuda, M, D, F, dtype, seed=2)
     both(torch_cuda, ws, dy, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("name", ["silu", "gelu", "sigmoid"])
+@pytest.mark.parametrize("M,D,F", [(20, 64, 72), (150, 64, 8), (150, 64, 72), (150, 100, 200), (200, 128, 192), (2100, 128, 1288)])
+def test_what_lies_between_rows_is_not_read_as_numbers(torch_cuda, M, D, F, name, dtype):
+    """Arrays whose rows are farther apart than they are long, NaN and infinities between them: the dense call's bits."""
+    torch = torch_cuda
+    ws, dy = make(torch, M, D, F, dtype, seed=8)
+    dense = both(torch, ws, dy, dtype, name)
+
+    def gaps(a):
+        wide = torch.full((a.shape[0], (a.shape[1] + 64) // 64 * 64 + 64), float("nan"), dtype=a.dtype, device="cuda")
+        wide[1::2] = float("inf")
+        wide[:, :a.shape[1]] = a
+        return wide[:, :a.shape[1]]
+
+    for which in ((3,), (0, 1, 2, 3, 4)):  # w_down alone (F a multiple of 8 but not of 64 is read where it is), all of them
+        arrays = [gaps(a) if i in which else a for i, a in enumerate(ws + [dy])]
+        got = both(torch, arrays[:4], arrays[4], dtype, name)
+        for n in dense:
+            assert n == "workspace" or torch.equal(got[n], dense[n]), n
