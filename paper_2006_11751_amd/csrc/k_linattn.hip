@@ -97,7 +97,7 @@ struct LinArgs {
   Divisor round, heads, share;  // 8 ops blocks_v, H, heads that share one of k and v
   int n_seg, seg_len;   // pieces of T (seg_len a multiple of every C)
   float* seg_state;     // n_seg > 1: [op][N * H][n_seg][dk * dv], first the pieces' own states, then what enters them
-  float* seg_keep;      // [op][N * H][n_seg] g^length, 0 if an episode begins in the piece
+  float* seg_keep;      // [op][N * H][n_seg] g^length, -1 if an episode begins in the piece
 };
 
 __device__ inline unsigned pack_bf16(float a, float b) {
@@ -654,7 +654,7 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 || DTYPE == S
   if constexpr (STATE) {
     s = g.seg_state + seg_at * ((size_t)dk * dv);
     if (tid == 0 && v_block == 0)
-      g.seg_keep[seg_at] = any_done ? 0.0f : pow2(l2 * (float)(t_end - t_begin - (seg == 0 && op.reverse ? 1 : 0)));
+      g.seg_keep[seg_at] = any_done ? -1.0f : pow2(l2 * (float)(t_end - t_begin - (seg == 0 && op.reverse ? 1 : 0)));
   } else if (op.s_out && seg == g.n_seg - 1) {
     s = op.s_out + (size_t)bh * dk * dv;
     if (op.reverse) {  // one step further back: to before the first step
@@ -696,7 +696,7 @@ __global__ __launch_bounds__(kThreads) void linattn_join_kernel(LinArgs g) {
     for (int i = 0; i < kAhead; ++i) {
       if (i0 + i >= g.n_seg) break;
       s[(i0 + i) * size] = in;
-      in = own[i] + (keep[i] == 0.0f ? 0.0f : keep[i] * in);
+      in = own[i] + (keep[i] < 0.0f ? 0.0f : keep[i] * in);  // (a decay may be zero: times NaN or infinity it is not)
     }
   }
 }

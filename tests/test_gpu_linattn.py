@@ -405,3 +405,15 @@ def test_long_trajectories_of_few_rows(torch_cuda, T, N, H, dk, dv, dtype):
     """Lengths that are cut into pieces, whose states are made first."""
     x, do, ds = make(torch_cuda, T, N, H, H, dk, dv, dtype, seed=T, p_done=0.003)
     both(torch_cuda, x, do, ds, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,N", [(1500, 1), (40, 3), (24, 3)])
+def test_a_state_that_is_not_finite_stays_so_however_long_the_trajectory(torch_cuda, T, N, dtype):
+    """g^T is zero in 32 bits, NaN and infinity times it are not; in pieces of T (1500 steps of few rows) as without."""
+    torch = torch_cuda
+    x, do, ds = make(torch, T, N, 2, 2, 64, 64, dtype, p_done=0.0, seed=12)
+    x["log_decay"] = torch.tensor([-1.0, -0.01], device="cuda")
+    x["state0"][0, 0, 3, 5], x["state0"][N - 1, 1, 7, 2] = float("nan"), float("-inf")
+    ds[0, 0, 9, 11], ds[N - 1, 1, 1, 4] = float("inf"), float("nan")
+    both(torch, x, do, ds, dtype)
