@@ -34,7 +34,8 @@ extern "C" {
  * element (t, n, h, i) of q is q[t * q_stride[0] + n * q_stride[1] + h * q_stride[2] + i], strides in elements, so
  * that all three may lie in one projection's output (any strides; 16-byte aligned rows of full 16-byte pieces are
  * read in such pieces, others element by element).  Gradients dq, dk, dv are dense.
- *   log_decay  dev [H] fp32, <= 0 (-infinity: the state is only the last step's)
+ *   log_decay  dev [H] fp32, <= 0 (-infinity: the state is only the last step's; NaN: every result of its head is NaN
+ *              that a decay enters)
  *   done       dev [T][N] bytes or NULL (no episode begins)
  *   state0     dev [N][H][dk][dv] fp32 or NULL (zero); state, dstate, dstate0 alike (NULL: not wanted / zero)
  * Errors: SF_ERR_ARG (null or misaligned pointer, struct_size, dtype), SF_ERR_SHAPE (T, N < 0; H, Hk < 1;

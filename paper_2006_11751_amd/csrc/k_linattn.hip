@@ -113,6 +113,11 @@ __device__ inline void split2(float a, float b, unsigned& t0, unsigned& t1) {
 }
 
 __device__ inline float pow2(float x) { return __builtin_amdgcn_exp2f(x); }  // (x <= 0 here; below 2^-126: 0)
+// The decay's binary logarithm: no -infinity (times zero it would be NaN), but a NaN stays one.
+__device__ inline float log2_decay(float log_decay) {
+  const float l2 = log_decay * 1.44269504f;
+  return l2 < -1e30f ? -1e30f : l2;
+}
 
 // The arithmetic of one element type.  An operand is eight K-slots per lane.
 template <int DTYPE>
@@ -339,7 +344,7 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny ? 2 : D == 64 || DTYPE == S
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h), seg = blockIdx.y;
   const int t_begin = seg * g.seg_len, t_end = min(g.T, t_begin + g.seg_len);  // in the op's own direction
   const int dk = op.k.d, dv = op.v.d;
-  const float l2 = fmaxf(g.log_decay[h] * 1.44269504f, -1e30f);  // (no -infinity: times zero it would be NaN)
+  const float l2 = log2_decay(g.log_decay[h]);
   const bool scan = g.n_seg > 1;
   const size_t seg_at = ((size_t)which * g.N * g.H + bh) * g.n_seg + seg;
 
@@ -749,7 +754,7 @@ __global__ __launch_bounds__(kThreads, DTYPE == SF_DTYPE_BF16 ? 4 : 3) void lina
   if (bh >= g.N * g.H) return;
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h);
   const int T = g.T, dk = g.q.d, dv = g.v.d;
-  const float l2 = fmaxf(g.log_decay[h] * 1.44269504f, -1e30f);
+  const float l2 = log2_decay(g.log_decay[h]);
   constexpr unsigned kOutside = 0x80000000u;
   auto buffer = [&](const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000); };
 
@@ -1051,7 +1056,7 @@ __global__ __launch_bounds__(kThreads) void linattn_step_kernel(LinOp op, const 
   const int id = ids ? ids[n] : n;
   const bool known = id >= 0 && id < n_env;
   const bool begin = !known || (done && done[n] != 0);
-  const float gam = exp2f(fmaxf(log_decay[h] * 1.44269504f, -1e30f));
+  const float gam = exp2f(log2_decay(log_decay[h]));
   const int rows = kThreads >> lanes_log2, row0 = tid >> lanes_log2, c0 = (tid & ((1 << lanes_log2) - 1)) * 4;
   float* s = table + ((int64_t)(known ? id : 0) * H + h) * dk * dv;
   constexpr int kMost = 16;  // rows of a thread: 128 / (256 / 32)

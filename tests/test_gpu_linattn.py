@@ -417,3 +417,30 @@ def test_a_state_that_is_not_finite_stays_so_however_long_the_trajectory(torch_c
     x["state0"][0, 0, 3, 5], x["state0"][N - 1, 1, 7, 2] = float("nan"), float("-inf")
     ds[0, 0, 9, 11], ds[N - 1, 1, 1, 4] = float("inf"), float("nan")
     both(torch, x, do, ds, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [24, 70, 1500])
+def test_a_decay_that_is_nan_is_in_its_heads_results(torch_cuda, T, dtype):
+    torch = torch_cuda
+    from paper_2006_11751_amd import memory
+    x, do, ds = make(torch, T, 2, 3, 3, 64, 64, dtype, p_done=0.0, seed=13)
+    bad = x["log_decay"].clone()
+    bad[1] = float("nan")
+    pairs = []
+    for ld in (x["log_decay"], bad):
+        args, kw = (x["q"], x["k"], x["v"], ld), dict(done=x["done"], state0=x["state0"])
+        r = dict(memory.linear_attention(*args, **kw), **{"back_" + n: t for n, t in memory.linear_attention_backward(*args, do, dstate=ds, **kw).items()})
+        table = x["state0"].clone()
+        r["step"] = memory.linear_attention_step(x["q"][0], x["k"][0], x["v"][0], ld, table)["o"][None]
+        r["table"] = table
+        pairs.append(r)
+    for n in ("o", "state", "back_dq", "back_dk", "back_dv", "back_dstate0", "step", "table"):
+        at = 2 if pairs[0][n].dim() == 4 and "state" not in n and n != "table" else 1  # the head's axis
+        head = lambda a, h: a.select(at, h)
+        for h in (0, 2):
+            assert torch.equal(head(pairs[0][n], h), head(pairs[1][n], h)), n
+        got = head(pairs[1][n], 1)
+        if n in ("back_dk", "back_dv"):
+            got = got[:-1]  # (no decay enters the last step's)
+        assert torch.isnan(got).all(), n
