@@ -91,6 +91,11 @@ def _refuse(text):
     raise ValueError(text)
 
 
+def _number(x):
+    """A number as what it is now: a plan must not hold a tensor that may change in place."""
+    return x if x is None or type(x) is float else float(x)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -215,7 +220,7 @@ def linear_attention(q, k, v, log_decay, done=None, state0=None, scale=None, out
     """Over N trajectories of T steps: q [T,N,H,dk], k [T,N,Hk,dk], v [T,N,Hk,dv] (bf16 or fp32, last axis dense),
     log_decay fp32 [H], done u8 [T,N], state0 fp32 [N,H,dk,dv]; scale: dk ** -0.5.  Results: o [T,N,H,dv],
     state [N,H,dk,dv]."""
-    out = {} if out is None else out
+    out, scale = {} if out is None else out, _number(scale)
     plan = _plan("linear_attention", scale, (q, k, v, log_decay, done, state0), _linattn_plan, q, k, v, log_decay, done, state0, scale)
     o, state = _results(out, plan)
     _check(_lib.sf_linattn(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), _ptr(done), _ptr(state0), o, state,
@@ -237,7 +242,7 @@ def _linattn_plan(q, k, v, log_decay, done, state0, scale):
 def linear_attention_backward(q, k, v, log_decay, do, done=None, state0=None, dstate=None, scale=None, out=None, stream=None):
     """Gradients of linear_attention with the same arguments, given those of o (do) and of the final state (dstate, or
     None).  Results: dq, dk, dv, dstate0."""
-    out = {} if out is None else out
+    out, scale = {} if out is None else out, _number(scale)
     plan = _plan("linear_attention_backward", scale, (q, k, v, log_decay, do, done, state0, dstate), _linattn_back_plan, q, k, v, log_decay, do,
                  done, state0, dstate, scale)
     dq, dk, dv, ds0 = _results(out, plan)
@@ -263,7 +268,7 @@ def _linattn_back_plan(q, k, v, log_decay, do, done, state0, dstate, scale):
 def linear_attention_step(q, k, v, log_decay, state_table, env_ids=None, done=None, scale=None, out=None, stream=None):
     """One step of B environments: q [B,H,dk], k [B,Hk,dk], v [B,Hk,dv], done u8 [B]; state_table fp32 [n_env,H,dk,dv] is
     read and overwritten at the rows env_ids (i32 [B], distinct; None: rows 0 .. B-1).  Result: o [B,H,dv]."""
-    out = {} if out is None else out
+    out, scale = {} if out is None else out, _number(scale)
     plan = _plan("linear_attention_step", scale, (q, k, v, log_decay, state_table, env_ids, done), _linattn_step_plan, q, k, v, log_decay,
                  state_table, env_ids, done, scale)
     o, = _results(out, plan)
@@ -324,7 +329,7 @@ def residual_norm(b, x=None, gate=None, post="rms", pre="rms", post_w=None, pre_
     dense; weights fp32 [D]).  post, pre: "none", "rms" or "layer"; gate_act: "none", "sigmoid" or "silu"; groups: of
     channels that post is taken over (pre "none" then).  Results: y and, with pre, n."""
     out = {} if out is None else out
-    how = (post, pre, groups, gate_act, eps)
+    how = (post, pre, groups, gate_act, _number(eps))
     plan = _plan("residual_norm", how, (b, x, gate, post_w, pre_w, scale), _resnorm_plan, b, x, gate, post_w, pre_w, scale, how)
     got = _results(out, plan)
     _check(_lib.sf_resnorm(plan.address, b.data_ptr(), _ptr(x), _ptr(gate), _ptr(post_w), _ptr(scale), _ptr(pre_w), got[0],
@@ -342,7 +347,7 @@ def residual_norm_backward(b, dy, dn=None, x=None, gate=None, post="rms", pre="r
     """Gradients of residual_norm with the same arguments, given those of y (None: zero) and, with pre, of n.  Results: db and,
     for what was given, dx, dgate, dpost_w, dscale, dpre_w (fp32)."""
     out = {} if out is None else out
-    how = (post, pre, groups, gate_act, eps)
+    how = (post, pre, groups, gate_act, _number(eps))
     given = (b, x, gate, post_w, scale, pre_w)
     plan = _plan("residual_norm_backward", how, (dy, dn) + given, _resnorm_back_plan, dy, dn, given, how)
     got = _results(out, plan)
