@@ -4,10 +4,11 @@
   residual_norm, residual_norm_backward
   gated_ffn, gated_ffn_backward
 
-Argument checks and marshalling only; every operator runs in the library's HIP kernels, on the current stream or, with
-`stream`, as if that were current (its order to other streams' work is the caller's; tensors and results may be dropped right
-after the call).  Each function puts its results into `out` (a dict) and returns it.  A program that calls one again and
-again keeps that dict: buffers that are there already are written to (they have to fit), and so is the workspace.
+Argument checks and marshalling only; every operator runs in the library's HIP kernels, on the tensors' device, on its
+current stream or, with `stream`, as if that were current (its order to other streams' work is the caller's; tensors and
+results may be dropped right after the call).  Each function puts its results into `out` (a dict) and returns it.  A
+program that calls one again and again keeps that dict: buffers that are there already are written to (they have to fit),
+and so is the workspace.
 Calls are short (a policy worker's step takes a few microseconds on the GPU), so what the checks of a call found is kept
 by the shapes, strides, types and devices of its arguments, and the checks are made once for each of these.
 """
@@ -125,12 +126,12 @@ def _rows(name, t):
 
 class _Plan:
     """What the checks of a call found: the configuration, the results' shapes and types, the size of the workspace."""
-    __slots__ = ("key", "config", "address", "results", "n_bytes", "device")
+    __slots__ = ("key", "config", "address", "results", "n_bytes", "device", "index")
 
     def __init__(self, config, results, n_bytes, device):
         if n_bytes < 0:
             raise SfError(binding.SF_ERR_SHAPE, sf_last_error())
-        self.config, self.address, self.n_bytes, self.device = config, C.addressof(config), n_bytes, device
+        self.config, self.address, self.n_bytes, self.device, self.index = config, C.addressof(config), n_bytes, device, device.index
         torch = binding._torch()
         self.results = [(name, torch.Size(shape), dtype) for name, shape, dtype in results]
 
@@ -185,6 +186,13 @@ def _workspace(out, plan):
     return w.data_ptr()
 
 
+def _current_device():
+    """Its index (torch's function for it, from the first call on)."""
+    global _current_device
+    _current_device = binding._torch()._C._cuda_getDevice
+    return _current_device()
+
+
 _raw_stream = None
 
 
@@ -196,11 +204,14 @@ def _stream(device):
     return _raw_stream(device.index)
 
 
-def _on_stream(stream, plan, call, first, rest, out):
-    """call(*first, *rest, out=out) with `stream` as the current one, so that what it allocates is that stream's.  The allocator is told of
-    every tensor that now has work on it there, and of the stream that was current before, for which the results are: memory
-    that is let go of after the call is given out again only when both are done with it."""
+def _elsewhere(stream, plan, call, first, rest, out):
+    """call(*first, *rest, out=out) with the tensors' device and, where one is given, `stream` as the current ones, so that what it
+    allocates is that stream's.  The allocator is told of every tensor that now has work on it there, and of the stream that was current
+    before, for which the results are: memory that is let go of after the call is given out again only when both are done with it."""
     torch = binding._torch()
+    if stream is None:
+        with torch.cuda.device(plan.device):
+            return call(*first, *rest, out=out)
     if stream.device != plan.device:
         _refuse("the stream is on %s, the tensors are on %s" % (stream.device, plan.device))
     before = torch.cuda.current_stream(plan.device)
@@ -241,8 +252,8 @@ def linear_attention(q, k, v, log_decay, done=None, state0=None, scale=None, out
     state [N,H,dk,dv]."""
     out, scale = {} if out is None else out, _number(scale)
     plan = _plan("linear_attention", scale, (q, k, v, log_decay, done, state0), _linattn_plan, q, k, v, log_decay, done, state0, scale)
-    if stream is not None:
-        return _on_stream(stream, plan, linear_attention, (q, k, v, log_decay, done, state0), (scale,), out)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, linear_attention, (q, k, v, log_decay, done, state0), (scale,), out)
     o, state = _results(out, plan)
     _check(_lib.sf_linattn(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), _ptr(done), _ptr(state0), o, state,
                            _workspace(out, plan), _stream(plan.device)))
@@ -266,8 +277,8 @@ def linear_attention_backward(q, k, v, log_decay, do, done=None, state0=None, ds
     out, scale = {} if out is None else out, _number(scale)
     plan = _plan("linear_attention_backward", scale, (q, k, v, log_decay, do, done, state0, dstate), _linattn_back_plan, q, k, v, log_decay, do,
                  done, state0, dstate, scale)
-    if stream is not None:
-        return _on_stream(stream, plan, linear_attention_backward, (q, k, v, log_decay, do, done, state0, dstate), (scale,), out)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, linear_attention_backward, (q, k, v, log_decay, do, done, state0, dstate), (scale,), out)
     dq, dk, dv, ds0 = _results(out, plan)
     _check(_lib.sf_linattn_backward(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), do.data_ptr(), _ptr(done),
                                     _ptr(state0), _ptr(dstate), dq, dk, dv, ds0, _workspace(out, plan), _stream(plan.device)))
@@ -294,8 +305,8 @@ def linear_attention_step(q, k, v, log_decay, state_table, env_ids=None, done=No
     out, scale = {} if out is None else out, _number(scale)
     plan = _plan("linear_attention_step", scale, (q, k, v, log_decay, state_table, env_ids, done), _linattn_step_plan, q, k, v, log_decay,
                  state_table, env_ids, done, scale)
-    if stream is not None:
-        return _on_stream(stream, plan, linear_attention_step, (q, k, v, log_decay, state_table, env_ids, done), (scale,), out)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, linear_attention_step, (q, k, v, log_decay, state_table, env_ids, done), (scale,), out)
     o, = _results(out, plan)
     _check(_lib.sf_linattn_step(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state_table.data_ptr(),
                                 state_table.shape[0], _ptr(env_ids), _ptr(done), o, _stream(plan.device)))
@@ -356,8 +367,8 @@ def residual_norm(b, x=None, gate=None, post="rms", pre="rms", post_w=None, pre_
     out = {} if out is None else out
     how = (post, pre, groups, gate_act, _number(eps))
     plan = _plan("residual_norm", how, (b, x, gate, post_w, pre_w, scale), _resnorm_plan, b, x, gate, post_w, pre_w, scale, how)
-    if stream is not None:
-        return _on_stream(stream, plan, residual_norm, (b, x, gate), (post, pre, post_w, pre_w, scale, groups, gate_act, eps), out)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, residual_norm, (b, x, gate), (post, pre, post_w, pre_w, scale, groups, gate_act, eps), out)
     got = _results(out, plan)
     _check(_lib.sf_resnorm(plan.address, b.data_ptr(), _ptr(x), _ptr(gate), _ptr(post_w), _ptr(scale), _ptr(pre_w), got[0],
                            got[1] if len(got) > 1 else None, _stream(plan.device)))
@@ -377,8 +388,8 @@ def residual_norm_backward(b, dy, dn=None, x=None, gate=None, post="rms", pre="r
     how = (post, pre, groups, gate_act, _number(eps))
     given = (b, x, gate, post_w, scale, pre_w)
     plan = _plan("residual_norm_backward", how, (dy, dn) + given, _resnorm_back_plan, dy, dn, given, how)
-    if stream is not None:
-        return _on_stream(stream, plan, residual_norm_backward, (b, dy, dn, x, gate), (post, pre, post_w, pre_w, scale, groups, gate_act, eps), out)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, residual_norm_backward, (b, dy, dn, x, gate), (post, pre, post_w, pre_w, scale, groups, gate_act, eps), out)
     got = _results(out, plan)
     db, dx, dgate, dpost_w, dscale, dpre_w = got if len(got) == 6 else _spread(got, given)
     _check(_lib.sf_resnorm_backward(plan.address, b.data_ptr(), _ptr(x), _ptr(gate), _ptr(post_w), _ptr(scale), _ptr(pre_w), _ptr(dy), _ptr(dn),
@@ -434,8 +445,8 @@ def gated_ffn(x, w_gate, w_up, w_down, act="silu", out=None, stream=None):
     axis dense); act: "silu", "gelu" or "sigmoid".  Result: y [..., D]."""
     out = {} if out is None else out
     plan = _plan("gated_ffn", act, (x, w_gate, w_up, w_down), _ffn_plan, x, w_gate, w_up, w_down, act)
-    if stream is not None:
-        return _on_stream(stream, plan, gated_ffn, (x, w_gate, w_up, w_down), (act,), out)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, gated_ffn, (x, w_gate, w_up, w_down), (act,), out)
     y, = _results(out, plan)
     _check(_lib.sf_ffn(plan.address, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y, _workspace(out, plan),
                        _stream(plan.device)))
@@ -451,8 +462,8 @@ def gated_ffn_backward(x, w_gate, w_up, w_down, dy, act="silu", out=None, stream
     """Gradients of gated_ffn with the same arguments, given that of y.  Results: dx, dw_gate, dw_up, dw_down."""
     out = {} if out is None else out
     plan = _plan("gated_ffn_backward", act, (x, w_gate, w_up, w_down, dy), _ffn_back_plan, x, w_gate, w_up, w_down, dy, act)
-    if stream is not None:
-        return _on_stream(stream, plan, gated_ffn_backward, (x, w_gate, w_up, w_down, dy), (act,), out)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, gated_ffn_backward, (x, w_gate, w_up, w_down, dy), (act,), out)
     dx, dwg, dwu, dwd = _results(out, plan)
     _check(_lib.sf_ffn_backward(plan.address, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dy.data_ptr(), dx, dwg, dwu, dwd,
                                 _workspace(out, plan), _stream(plan.device)))

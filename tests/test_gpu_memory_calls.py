@@ -107,3 +107,39 @@ def test_a_stream_argument_gives_the_same_bits_in_a_graph(torch_cuda):
             torch.cuda.synchronize()
             for n, t in want.items():
                 assert torch.equal(out[n], t), (name, n)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_call_runs_on_its_tensors_device(torch_cuda, name, monkeypatch):
+    """With another device current (there is one here: that it is another is pretended until torch is told to change to it)."""
+    torch = torch_cuda
+    from paper_2006_11751_amd import memory
+    call, tensors = _calls(torch)[name]
+    copy = lambda: [t.clone() for t in tensors]
+    want = {n: t.clone() for n, t in call(copy()).items() if n != "workspace"}
+    real, told = torch.cuda.device, []
+
+    class device(real):
+        def __init__(self, d):
+            told.append(d)
+            super().__init__(d)
+
+    other = lambda: 0 if told else 1
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", other)
+    monkeypatch.setattr(memory, "_current_device", other, raising=False)
+    got = call(copy())
+    monkeypatch.undo()
+    assert told == [tensors[0].device]
+    for n, t in want.items():
+        assert torch.equal(got[n], t), n
+
+
+def test_a_stream_of_another_device_is_refused(torch_cuda):
+    from paper_2006_11751_amd import memory
+
+    class Other:
+        device, cuda_stream = torch_cuda.device("cuda", 1), 0
+
+    with pytest.raises(ValueError, match="cuda:1"):
+        memory.residual_norm(torch_cuda.zeros(2, 8, device="cuda"), stream=Other())
