@@ -8,7 +8,8 @@ Argument checks and marshalling only; every operator runs in the library's HIP k
 current stream or, with `stream`, as if that were current (its order to other streams' work is the caller's; tensors and
 results may be dropped right after the call).  Each function puts its results into `out` (a dict) and returns it.  A
 program that calls one again and again keeps that dict: buffers that are there already are written to (they have to fit),
-and so is the workspace.
+and so is the workspace.  One that has become too small stays in the dict, as "workspace_1" and so on, for graphs that
+were recorded with it; who has none may take it out.
 Calls are short (a policy worker's step takes a few microseconds on the GPU), so what the checks of a call found is kept
 by the shapes, strides, types and devices of its arguments, and the checks are made once for each of these.
 """
@@ -181,6 +182,8 @@ def _workspace(out, plan):
         return None
     w = out.get("workspace")
     if w is None or w.numel() < plan.n_bytes or w.device != plan.device:
+        if w is not None:  # (a graph that was recorded with it goes on writing there)
+            out["workspace_%d" % (1 + sum(name.startswith("workspace_") for name in out))] = w
         torch = binding._torch()
         w = out["workspace"] = torch.empty(plan.n_bytes, dtype=torch.uint8, device=plan.device)
     return w.data_ptr()
