@@ -186,6 +186,8 @@ def _workspace(out, plan):
             out["workspace_%d" % (1 + sum(name.startswith("workspace_") for name in out))] = w
         torch = binding._torch()
         w = out["workspace"] = torch.empty(plan.n_bytes, dtype=torch.uint8, device=plan.device)
+    elif not w.is_contiguous():
+        _refuse("out['workspace'] is not contiguous")
     return w.data_ptr()
 
 
