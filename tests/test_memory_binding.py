@@ -3,6 +3,7 @@ import types
 
 import pytest
 
+
 def _plan(n_bytes):
     import torch
     return types.SimpleNamespace(n_bytes=n_bytes, device=torch.device("cpu"))
