@@ -52,7 +52,7 @@ typedef struct {
 /* Bytes of the workspace of sf_linattn (backward = 0) or sf_linattn_backward (1); 0: none is needed, NULL may be
  * passed; -1 on a bad configuration. */
 int64_t sf_linattn_workspace_bytes(const sf_linattn_config* cfg, int backward);
-/* state may be state0 (the states are then updated in place). */
+/* state may be state0 (the states are then updated in place), but must not overlap it otherwise (SF_ERR_ALIAS). */
 int sf_linattn(const sf_linattn_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
                const uint8_t* done, const float* state0, void* o, float* state, void* workspace, void* hip_stream);
 /* Gradients with respect to q, k, v and state0, given those of o (do) and of the final state (dstate or NULL).

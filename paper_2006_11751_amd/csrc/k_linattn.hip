@@ -1152,6 +1152,12 @@ int check_ptr(const char* fn, const char* name, const void* p, size_t align, boo
   return SF_OK;
 }
 
+// Whether two arrays of states (or null) have a number in common; of no rows, whether they begin at one address.
+bool overlap(const sf_linattn_config* c, const float* a, const float* b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b), size = (uintptr_t)c->N * c->H * c->dk * c->dv * 4;
+  return a && b && (x == y || (x < y ? y - x : x - y) < size);
+}
+
 struct Split {
   int n_seg, seg_len;
 };
@@ -1315,6 +1321,10 @@ extern "C" int sf_linattn(const sf_linattn_config* cfg, const void* q, const voi
       (rc = check_ptr(fn, "state0", state0, 4, true)) || (rc = check_ptr(fn, "state", state, 4, true)) ||
       (rc = check_ptr(fn, "workspace", workspace, 256, w.total == 0)))
     return rc;
+  if (state != state0 && overlap(cfg, state, state0)) {
+    set_error("%s: state overlaps state0", fn);
+    return SF_ERR_ALIAS;
+  }
   LinArgs g = {};
   g.log_decay = log_decay;
   g.done = done;
@@ -1349,8 +1359,8 @@ extern "C" int sf_linattn_backward(const sf_linattn_config* cfg, const void* q, 
       (rc = check_ptr(fn, "state0", state0, 4, true)) || (rc = check_ptr(fn, "dstate", dstate, 4, true)) ||
       (rc = check_ptr(fn, "dstate0", dstate0, 4, true)) || (rc = check_ptr(fn, "workspace", workspace, 256, w.total == 0)))
     return rc;
-  if (dstate0 && (dstate0 == dstate || dstate0 == state0)) {
-    set_error("%s: dstate0 is dstate or state0", fn);
+  if (overlap(cfg, dstate0, dstate) || overlap(cfg, dstate0, state0)) {
+    set_error("%s: dstate0 overlaps dstate or state0", fn);
     return SF_ERR_ALIAS;
   }
   const hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);

@@ -100,3 +100,19 @@ def test_ffn_refuses_without_a_gpu():
     assert lib.sf_ffn_workspace_bytes(make(act=-1), 0) == -1
     assert lib.sf_ffn_workspace_bytes(make(), 0) >= 8 * 128 * 2
     assert lib.sf_ffn_workspace_bytes(make(M=100), 1) > lib.sf_ffn_workspace_bytes(make(M=100), 0) > 0
+
+
+def test_linattn_refuses_states_that_overlap():
+    """(Addresses that are never read: the calls come back before they launch anything.)"""
+    memory = _memory()
+    lib, C = memory.load_library(), memory.SfLinattnConfig
+    cfg = ctypes.byref(C(struct_size=ctypes.sizeof(C), dtype=0, T=8, N=2, H=4, Hk=4, dk=16, dv=16, scale=0.25))
+    size = 2 * 4 * 16 * 16 * 4
+    a, states = 1 << 20, 1 << 24
+    for off in (4 - size, -size // 2, 4, size - 4):
+        assert lib.sf_linattn(cfg, a, a, a, a, None, states, a, states + off, None, None) == -4, off
+        assert "state overlaps state0" in lib.sf_last_error().decode()
+    for off in (4 - size, -size // 2, 0, 4, size - 4):
+        for where in ((states, states + (1 << 20)), (states + (1 << 20), states)):  # state0, dstate
+            assert lib.sf_linattn_backward(cfg, a, a, a, a, a, None, *where, a, a, a, states + off, None, None) == -4, off
+            assert "dstate0 overlaps" in lib.sf_last_error().decode()
