@@ -87,7 +87,7 @@ int sf_linattn_step(const sf_linattn_config* cfg, const void* q, const void* k, 
  *               (dense), b or gate, n likewise if y is not it.
  * Backward: dy [M] rows (NULL: zero, with N_pre only) and dn [M] rows (with N_pre) are the gradients of y and n; dx, db,
  * dgate [M][D] dense io and dpost_w, dscale, dpre_w fp32 [D] are written where they are not NULL (zeros for a
- * weight that is not used).  Nothing of the forward pass is needed but its inputs.  dx, db, dgate may each be any one of
+ * weight that is not used; dgate only with a gate, SF_ERR_ARG).  Nothing of the forward pass is needed but its inputs.  dx, db, dgate may each be any one of
  * the inputs (dense).
  * workspace: sf_resnorm_workspace_bytes(cfg), NULL if no gradient of a weight is wanted.
  * Any D up to 8192 a group, any strides; rows of whole 16-byte pieces, 16-byte aligned, are read in such pieces.

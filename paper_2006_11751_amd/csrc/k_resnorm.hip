@@ -593,6 +593,10 @@ extern "C" int sf_resnorm_backward(const sf_resnorm_config* cfg, const void* b, 
   if (!fits(dx, e, true)) return bad_ptr(fn, "dx");
   if (!fits(db, e, true)) return bad_ptr(fn, "db");
   if (!fits(dgate, e, true)) return bad_ptr(fn, "dgate");
+  if (dgate && cfg->gate_act == SF_GATE_NONE) {
+    set_error("%s: dgate without a gate", fn);
+    return SF_ERR_ARG;
+  }
   if (!fits(dpost_w, 4, true)) return bad_ptr(fn, "dpost_w");
   if (!fits(dscale, 4, true)) return bad_ptr(fn, "dscale");
   if (!fits(dpre_w, 4, true)) return bad_ptr(fn, "dpre_w");

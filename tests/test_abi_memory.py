@@ -116,3 +116,13 @@ def test_linattn_refuses_states_that_overlap():
         for where in ((states, states + (1 << 20)), (states + (1 << 20), states)):  # state0, dstate
             assert lib.sf_linattn_backward(cfg, a, a, a, a, a, None, *where, a, a, a, states + off, None, None) == -4, off
             assert "dstate0 overlaps" in lib.sf_last_error().decode()
+
+
+def test_resnorm_refuses_the_gradient_of_a_gate_that_is_not_there():
+    """(Nothing would be written to it.)"""
+    memory = _memory()
+    lib, C = memory.load_library(), memory.SfResnormConfig
+    cfg = ctypes.byref(C(struct_size=ctypes.sizeof(C), dtype=0, M=8, D=64, groups=1, post=1, pre=0, gate_act=0, eps=1e-6, b_stride=64, dy_stride=64))
+    a = 1 << 20
+    assert lib.sf_resnorm_backward(cfg, a, None, a, None, None, None, a, None, None, a, a, None, None, None, None, None) == -1
+    assert "dgate" in lib.sf_last_error().decode()
