@@ -1161,14 +1161,22 @@ bool overlap(const sf_linattn_config* c, const float* a, const float* b) {
 struct Split {
   int n_seg, seg_len;
 };
-// Pieces of T where rows x heads leave CUs without a workgroup, each with at least 256 steps.  The pieces' states cost a pass
-// over k and v more, two launches and their own bytes, so T has to be longer the more heads and the larger states there are.
-// bf16, us whole and cut: 8 heads of 64, 512 steps 28 and 30, 768: 41 and 31, 4096: 200 and 32; 96 heads, 512: 29 and 37, 768: 46 and
-// 42, 2048: 115 and 54; 240 heads, 512: 35 and 53, 1024: 62 and 68; of 128: 8 heads, 512: 39 and 39, 4096: 293 and 45; 32, 512:
-// 41 and 48, 768: 61 and 50; 96, 768: 66 and 83, 1024: 85 and 87, 2048: 162 and 134; 240, 1024: 110 and 189.
+// Pieces of T where the workgroups (one for each 64 columns of a head, and backwards for each of the three gradients) leave CUs
+// idle, each with at least 256 steps.  The pieces' states cost a pass over k and v more, two launches and their own bytes, so T has
+// to be longer the more heads and the larger states there are, and from 384 workgroups on no length pays.
+// us whole and cut, heads of 64 and 128 columns, H of them over all rows:
+//                     bf16 64, 1024 steps   4096       128, 1024    4096        fp32 64, 1024   4096       128, 1024    4096
+//   forwards    8     52 30                 199 32     75 40        291 46      87 42           342 45     133 62       550 74
+//              96     59 43                 225 86     85 87        361 250     98 70           440 180    144 153      616 513
+//             192     59 58                 262 178    98 153       413 444     100 98          449 347    224 292      867 944
+//             240     60 68                 264 222    108 189      419 540     104 119         455 410    226 375      871 1234
+//   backwards   8     52 31                 200 41     75 49        308 72      88 44           363 65     134 71       544 146
+//              48     58 52                 223 116    95 123       388 320     96 88           406 240    209 231      846 731
+//              96     66 78                 286 229    114 200      474 595     130 141         567 473    299 440      1185 1447
 Split split_of(const sf_linattn_config* c, int ops) {
   const int64_t lanes = (int64_t)c->N * c->H * ops;
-  const bool cut = lanes > 0 && lanes < 384 && c->T > 512 + lanes * std::max(c->dk, c->dv) / 24;
+  const int columns = std::max(c->dk, c->dv);
+  const bool cut = lanes > 0 && lanes * (columns > DV ? 2 : 1) < 384 && c->T > 512 + lanes * columns / 24;
   const int64_t want = cut ? (768 + lanes - 1) / lanes : 1;
   int64_t len = (c->T + want - 1) / want;
   len = (len + 63) / 64 * 64;

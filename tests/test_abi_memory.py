@@ -126,3 +126,14 @@ def test_resnorm_refuses_the_gradient_of_a_gate_that_is_not_there():
     a = 1 << 20
     assert lib.sf_resnorm_backward(cfg, a, None, a, None, None, None, a, None, None, a, a, None, None, None, None, None) == -1
     assert "dgate" in lib.sf_last_error().decode()
+
+
+def test_linattn_is_cut_into_pieces_only_where_workgroups_are_few():
+    """What pieces need is in the workspace; a head of more than 64 columns has two workgroups."""
+    memory = _memory()
+    lib, C = memory.load_library(), memory.SfLinattnConfig
+    size = lambda T, N, d, back: lib.sf_linattn_workspace_bytes(ctypes.byref(C(
+        struct_size=ctypes.sizeof(C), dtype=1, T=T, N=N, H=8, Hk=8, dk=d, dv=d, scale=1.0)), back)
+    for T, N, d, back, cut in ((4096, 1, 64, 0, 1), (512, 1, 64, 0, 0), (4096, 30, 64, 0, 1), (4096, 60, 64, 0, 0), (4096, 12, 64, 1, 1),
+                               (4096, 4, 128, 0, 1), (4096, 12, 128, 0, 1), (4096, 30, 128, 0, 0), (4096, 6, 128, 1, 1), (4096, 12, 128, 1, 0)):
+        assert (size(T, N, d, back) > 0) == bool(cut), (T, N, d, back)
