@@ -778,11 +778,13 @@ hipError_t launch_t(GemmGroup& group, hipStream_t st) {
 int64_t tiles_of(int F, int M, int BF, int BM) { return (int64_t)((F + BF - 1) / BF) * ((M + BM - 1) / BM); }
 // The large tile where it leaves few CUs without one, the small one otherwise.  us, large and small, by large tiles (D = 1024):
 // kPair 96 tiles 29 and 20, 128 29 and 22, 160 29.6 and 29.2, 208 32 and 37, 512 69 and 75; kTriple 128 32 and 25, 192 34 and
-// 36, 256 36 and 41, 320 60 and 56 (a second round of large ones just begun), 416 62 and 72, 1024 135 and 148.
+// 36, 256 36 and 41, 320 60 and 56 (a second round of large ones just begun), 416 62 and 72, 1024 135 and 148.  Whole backward passes in
+// fp32: 64 tiles 259 and 201, 128 336 and 327, 160 377 and 428, 256 505 and 602, 320 715 and 756, 512 970 and 1157.
 constexpr int kEnough = 160;
-// And a smaller one still where a round of workgroups takes all of it (256).  us, 64 x 128 and 64 x 64, forwards and backwards: fp32, D =
-// 1920, F = 576, 939 rows (135 tiles of 64 x 64): 122 and 104, 297 and 268; 2048 rows (288): 141 and 156, 390 and 436; bf16, 1024 x
-// 2048, 320 rows (160): 28 and 25, 50 and 46; 939 rows (480): 30 and 31, 67 and 70.
+// And a smaller one still where a round of workgroups takes all of it (256).  us of whole calls, 64 x 128 and 64 x 64, forwards and
+// backwards, by tiles of 64 x 64: fp32 1024 x 2048, 160 tiles backwards 179 and 171, 256 213 and 197, 480 301 and 314; 1920 x 576, 135 122
+// and 104, 300 and 269, 288 141 and 156, 390 and 436; bf16 1024 x 2048, 160 28 and 25, 50 and 46, 256 backwards 55 and 50, 480 30 and 31,
+// 70 and 72.
 constexpr int kOneRound = 256;
 template <int FORM>
 hipError_t launch(GemmGroup& group, hipStream_t st) {

@@ -444,3 +444,20 @@ def test_a_decay_that_is_nan_is_in_its_heads_results(torch_cuda, T, dtype):
         if n in ("back_dk", "back_dv"):
             got = got[:-1]  # (no decay enters the last step's)
         assert torch.isnan(got).all(), n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [24, 40])
+@pytest.mark.parametrize("stride", [1 << 23, (1 << 23) + 8])
+def test_steps_far_apart(torch_cuda, T, stride, dtype):
+    """Steps up to 2^23 elements apart are read through 32-bit offsets from the chunk, others through 64-bit addresses."""
+    torch = torch_cuda
+    x, do, ds = make(torch, T, 2, 2, 2, 64, 64, dtype, seed=14)
+    a, b = both(torch, x, do, ds, dtype)
+    wide = torch.full((T, stride), float("nan"), dtype=do.dtype, device="cuda")
+    parts = wide[:, :4 * 256].unflatten(1, (4, 2, 2, 64)).unbind(1)
+    for n, part, t in zip(("q", "k", "v", "do"), parts, (x["q"], x["k"], x["v"], do)):
+        part.copy_(t)
+    c, d = both(torch, dict(x, q=parts[0], k=parts[1], v=parts[2]), parts[3], ds, dtype)
+    for n in ("o", "state"):
+        assert torch.equal(a[n], c[n]), n
