@@ -191,22 +191,18 @@ def _workspace(out, plan):
     return w.data_ptr()
 
 
+# Torch's functions for the current device's index and for the handle of a device's current stream, from the first call on (the
+# handle alone: a Stream object of torch costs two microseconds).
 def _current_device():
-    """Its index (torch's function for it, from the first call on)."""
     global _current_device
     _current_device = binding._torch()._C._cuda_getDevice
     return _current_device()
 
 
-_raw_stream = None
-
-
-def _stream(device):
-    """The current stream's handle."""
-    global _raw_stream
-    if _raw_stream is None:  # (the handle alone: a Stream object of torch costs two microseconds)
-        _raw_stream = binding._torch()._C._cuda_getCurrentRawStream
-    return _raw_stream(device.index)
+def _stream(index):
+    global _stream
+    _stream = binding._torch()._C._cuda_getCurrentRawStream
+    return _stream(index)
 
 
 def _elsewhere(stream, plan, call, first, rest, out):
@@ -261,7 +257,7 @@ def linear_attention(q, k, v, log_decay, done=None, state0=None, scale=None, out
         return _elsewhere(stream, plan, linear_attention, (q, k, v, log_decay, done, state0), (scale,), out)
     o, state = _results(out, plan)
     _check(_lib.sf_linattn(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), _ptr(done), _ptr(state0), o, state,
-                           _workspace(out, plan), _stream(plan.device)))
+                           _workspace(out, plan), _stream(plan.index)))
     return out
 
 
@@ -286,7 +282,7 @@ def linear_attention_backward(q, k, v, log_decay, do, done=None, state0=None, ds
         return _elsewhere(stream, plan, linear_attention_backward, (q, k, v, log_decay, do, done, state0, dstate), (scale,), out)
     dq, dk, dv, ds0 = _results(out, plan)
     _check(_lib.sf_linattn_backward(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), do.data_ptr(), _ptr(done),
-                                    _ptr(state0), _ptr(dstate), dq, dk, dv, ds0, _workspace(out, plan), _stream(plan.device)))
+                                    _ptr(state0), _ptr(dstate), dq, dk, dv, ds0, _workspace(out, plan), _stream(plan.index)))
     return out
 
 
@@ -314,7 +310,7 @@ def linear_attention_step(q, k, v, log_decay, state_table, env_ids=None, done=No
         return _elsewhere(stream, plan, linear_attention_step, (q, k, v, log_decay, state_table, env_ids, done), (scale,), out)
     o, = _results(out, plan)
     _check(_lib.sf_linattn_step(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state_table.data_ptr(),
-                                state_table.shape[0], _ptr(env_ids), _ptr(done), o, _stream(plan.device)))
+                                state_table.shape[0], _ptr(env_ids), _ptr(done), o, _stream(plan.index)))
     return out
 
 
@@ -376,7 +372,7 @@ def residual_norm(b, x=None, gate=None, post="rms", pre="rms", post_w=None, pre_
         return _elsewhere(stream, plan, residual_norm, (b, x, gate), (post, pre, post_w, pre_w, scale, groups, gate_act, eps), out)
     got = _results(out, plan)
     _check(_lib.sf_resnorm(plan.address, b.data_ptr(), _ptr(x), _ptr(gate), _ptr(post_w), _ptr(scale), _ptr(pre_w), got[0],
-                           got[1] if len(got) > 1 else None, _stream(plan.device)))
+                           got[1] if len(got) > 1 else None, _stream(plan.index)))
     return out
 
 
@@ -398,7 +394,7 @@ def residual_norm_backward(b, dy, dn=None, x=None, gate=None, post="rms", pre="r
     got = _results(out, plan)
     db, dx, dgate, dpost_w, dscale, dpre_w = got if len(got) == 6 else _spread(got, given)
     _check(_lib.sf_resnorm_backward(plan.address, b.data_ptr(), _ptr(x), _ptr(gate), _ptr(post_w), _ptr(scale), _ptr(pre_w), _ptr(dy), _ptr(dn),
-                                    dx, db, dgate, dpost_w, dscale, dpre_w, _workspace(out, plan), _stream(plan.device)))
+                                    dx, db, dgate, dpost_w, dscale, dpre_w, _workspace(out, plan), _stream(plan.index)))
     return out
 
 
@@ -454,7 +450,7 @@ def gated_ffn(x, w_gate, w_up, w_down, act="silu", out=None, stream=None):
         return _elsewhere(stream, plan, gated_ffn, (x, w_gate, w_up, w_down), (act,), out)
     y, = _results(out, plan)
     _check(_lib.sf_ffn(plan.address, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y, _workspace(out, plan),
-                       _stream(plan.device)))
+                       _stream(plan.index)))
     return out
 
 
@@ -471,7 +467,7 @@ def gated_ffn_backward(x, w_gate, w_up, w_down, dy, act="silu", out=None, stream
         return _elsewhere(stream, plan, gated_ffn_backward, (x, w_gate, w_up, w_down, dy), (act,), out)
     dx, dwg, dwu, dwd = _results(out, plan)
     _check(_lib.sf_ffn_backward(plan.address, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dy.data_ptr(), dx, dwg, dwu, dwd,
-                                _workspace(out, plan), _stream(plan.device)))
+                                _workspace(out, plan), _stream(plan.index)))
     return out
 
 
