@@ -32,8 +32,10 @@ extern "C" {
  *
  * Arrays are time-major: q [T][N][H][dk], k [T][N][Hk][dk], v [T][N][Hk][dv], o and its gradient [T][N][H][dv], io;
  * element (t, n, h, i) of q is q[t * q_stride[0] + n * q_stride[1] + h * q_stride[2] + i], strides in elements, so
- * that all three may lie in one projection's output (any strides; 16-byte aligned rows of full 16-byte pieces are
- * read in such pieces, others element by element).  Gradients dq, dk, dv are dense.
+ * that all three may lie in one projection's output.  Any strides and any alignment of the elements; a call is fast if in all its
+ * arrays rows are of a multiple of eight elements, 16-byte aligned, and steps at least a row and at most 2^23 elements
+ * apart.  Gradients dq, dk, dv are dense.  Results must not overlap inputs, nor one another, but for state as said below.
+ * Of an infinity in an array or a state the results that it reaches are infinite or NaN.
  *   log_decay  dev [H] fp32, <= 0 (-infinity: the state is only the last step's; NaN: every result of its head is NaN
  *              that a decay enters)
  *   done       dev [T][N] bytes or NULL (no episode begins)
@@ -120,8 +122,9 @@ int sf_resnorm_backward(const sf_resnorm_config* cfg, const void* b, const void*
  * reach all (of an infinity fp32 results are NaN).
  * Backward: dy [M] rows -> dx [M][D], dw_gate, dw_up [F][D], dw_down [D][F], dense, 16-byte aligned, of the same type.
  * Nothing of the forward pass is needed but its inputs.  Results must not overlap inputs.
- * Rows of a multiple of 64 numbers, 16-byte aligned, are read where they are; others are laid out in the workspace first
- * (few rows forwards: read element by element).
+ * Rows may have anything between them.  bf16 rows of a multiple of 64 numbers (w_down backwards: of 8), 16-byte aligned and less than 2^22
+ * elements apart, are read where they are; others, and all fp32 arrays, are laid out in the workspace first.  A call of few rows forwards
+ * reads all arrays where they are, in 16-byte pieces if x, w_gate and w_up (and w_down) consist of them, else number by number.
  * workspace: sf_ffn_workspace_bytes(cfg, backward), 256-byte aligned, wanted unless M is 0.
  * Errors: SF_ERR_ARG, SF_ERR_SHAPE (M outside 0 .. 2^24, D or F outside 1 .. 2^20), SF_ERR_DEVICE. */
 enum { SF_ACT_SILU = 0, SF_ACT_GELU = 1, SF_ACT_SIGMOID = 2 };

@@ -12,6 +12,8 @@ and so is the workspace.  One that has become too small stays in the dict, as "w
 were recorded with it; who has none may take it out.
 Calls are short (a policy worker's step takes a few microseconds on the GPU), so what the checks of a call found is kept
 by the shapes, strides, types and devices of its arguments, and the checks are made once for each of these.
+They are not part of autograd's graph: results carry no history, whether or not an argument requires a gradient, and the
+gradients are what the *_backward functions return.
 """
 import ctypes as C
 
