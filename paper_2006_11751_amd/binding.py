@@ -400,6 +400,20 @@ def sf_appo_loss_static(cfg, logits, actions, logp_mu, values, rewards, dones, v
         raise SfError(rc, sf_last_error())
 
 
+def _made_on(torch, stream, make):
+    """make()'s dict of tensors, as memory of the stream that work is enqueued on (None: the current one): what the current stream has
+    let go of may still be in use there.  They are kept for both streams when they are dropped."""
+    if stream is None:
+        return make()
+    before = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        made = make()
+    for t in made.values():
+        if t is not None:
+            t.record_stream(before)
+    return made
+
+
 def appo_loss(hp, tr, want_grads=True, stream=None, out=None):
     """tr: dict of contiguous CUDA tensors (logits, actions, logp_mu, values, rewards, dones),
     time-major.  Returns dict(vs, adv, loss[4], dlogits, dvalues) of CUDA tensors."""
@@ -420,11 +434,11 @@ def appo_loss(hp, tr, want_grads=True, stream=None, out=None):
     assert dones.dtype == torch.uint8 and dones.is_contiguous() and dones.is_cuda, "dones"
     assert T == hp["T"] and N == hp["N"] and sumA == sum(hp["heads"]) and values.shape == (T + 1, N)
     if out is None:
-        out = dict(vs=torch.empty((T, N), device=d), adv=torch.empty((T, N), device=d),
-                   loss=torch.empty(4, device=d),
-                   dlogits=torch.empty((T, N, sumA), device=d) if want_grads else None,
-                   dvalues=torch.empty((T, N), device=d) if want_grads else None,
-                   workspace=torch.empty(sf_appo_loss_workspace_bytes(cfg), dtype=torch.uint8, device=d))
+        out = _made_on(torch, stream, lambda: dict(
+            vs=torch.empty((T, N), device=d), adv=torch.empty((T, N), device=d), loss=torch.empty(4, device=d),
+            dlogits=torch.empty((T, N, sumA), device=d) if want_grads else None,
+            dvalues=torch.empty((T, N), device=d) if want_grads else None,
+            workspace=torch.empty(sf_appo_loss_workspace_bytes(cfg), dtype=torch.uint8, device=d)))
     s = stream if stream is not None else torch.cuda.current_stream(d)
     # (a buffer that is None is the library's to refuse, or to leave out)
     vs, adv, loss, dlogits, dvalues, workspace = (out["vs"], out["adv"], out["loss"], out["dlogits"], out["dvalues"],
@@ -540,7 +554,7 @@ class Policy:
         assert tuple(obs.shape[1:]) == tuple(self.net["obs"]) and tuple(h_in.shape) == (B, self.H)
         assert done.shape == (B,)
         if out is None:
-            out = self.alloc_outputs(B)
+            out = _made_on(t, stream, lambda: self.alloc_outputs(B))
         s = stream if stream is not None else t.cuda.current_stream(self.device)
         sf_policy_step(self.handle, B, obs.data_ptr(), self._meas_ptr(meas, B), h_in.data_ptr(),
                        done.data_ptr(), seed, step,
@@ -561,7 +575,7 @@ class Policy:
         assert env_ids.is_contiguous() and h_table.shape[1] == self.H
         assert tuple(obs.shape[1:]) == tuple(self.net["obs"])
         if out is None:
-            out = self.alloc_outputs(B)
+            out = _made_on(t, stream, lambda: self.alloc_outputs(B))
             del out["h_out"]
         s = stream if stream is not None else t.cuda.current_stream(self.device)
         sf_policy_step_indexed(self.handle, B, obs.data_ptr(), self._meas_ptr(meas, B),
@@ -585,8 +599,8 @@ class Policy:
         assert tuple(h0.shape) == (N, self.H)
         if out is None:
             f32 = dict(dtype=t.float32, device=self.device)
-            out = {"logits": t.empty((T, N, sum(self.net["heads"])), **f32), "value": t.empty((T, N), **f32),
-                   "h_seq": t.empty((T, N, self.H), **f32)}
+            out = _made_on(t, stream, lambda: {"logits": t.empty((T, N, sum(self.net["heads"])), **f32), "value": t.empty((T, N), **f32),
+                                               "h_seq": t.empty((T, N, self.H), **f32)})
         meas_ptr = None
         if self.meas_dim:
             assert meas is not None and meas.dtype == t.float32 and meas.is_contiguous()
