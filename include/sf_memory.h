@@ -141,6 +141,26 @@ int sf_ffn_backward(const sf_ffn_config* cfg, const void* x, const void* w_gate,
                     const void* dy, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* workspace,
                     void* hip_stream);
 
+/* ---- the global norm of a list of gradients, and their clipping ---------------------
+ *   norm = sqrt(sum of g^2 over all numbers of all tensors),   out = min(1, max_norm / (norm + eps)) g
+ * n tensors of sizes[i] numbers (dense, in any order of their axes) of type dtypes[i] (SF_DTYPE_*; a list may mix them) at
+ * the device addresses grads[i], aligned to their type.  Results of the same type at out[i], which may be grads[i] (clipped in
+ * place: nothing is written then where the factor is 1), but overlap no other tensor (SF_ERR_ALIAS).  The four arrays are host
+ * memory and not used after the call; a tensor of no numbers is left out, its addresses do not matter.
+ *   norm       dev [1] fp32: the norm before clipping.  Squares are added in 64 bits.  With a NaN or infinity in the list the norm
+ *              is one too; the factor is then NaN, or 0 (an infinity in the list becomes NaN, all else 0).
+ *   workspace  sf_gradclip_workspace_bytes(n, sizes), 256-byte aligned
+ * Errors: SF_ERR_ARG, SF_ERR_SHAPE (n outside 0 .. 2^20, a size outside 0 .. 2^40, max_norm negative or NaN, eps not positive and
+ * finite), SF_ERR_ALIAS, SF_ERR_OOM, SF_ERR_DEVICE. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(sf_gradclip_config) */
+  int32_t n;            /* tensors */
+  float max_norm, eps;
+} sf_gradclip_config;
+int64_t sf_gradclip_workspace_bytes(int32_t n, const int64_t* sizes); /* -1 on bad sizes */
+int sf_gradclip(const sf_gradclip_config* cfg, const void* const* grads, const int64_t* sizes, const int32_t* dtypes,
+                void* const* out, float* norm, void* workspace, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

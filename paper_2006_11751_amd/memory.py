@@ -3,6 +3,7 @@
   linear_attention, linear_attention_backward, linear_attention_step
   residual_norm, residual_norm_backward
   gated_ffn, gated_ffn_backward
+  clip_gradients
 
 Argument checks and marshalling only; every operator runs in the library's HIP kernels, on the tensors' device, on its
 current stream or, with `stream`, as if that were current (its order to other streams' work is the caller's; tensors and
@@ -16,6 +17,7 @@ They are not part of autograd's graph: results carry no history, whether or not 
 gradients are what the *_backward functions return.
 """
 import ctypes as C
+import operator
 
 from . import binding
 from .binding import SF_OK, SfError, sf_last_error
@@ -23,7 +25,8 @@ from .binding import SF_OK, SfError, sf_last_error
 SF_DTYPE_FP32, SF_DTYPE_BF16 = 0, 1
 
 EXPORTS = ("sf_linattn_workspace_bytes", "sf_linattn", "sf_linattn_backward", "sf_linattn_step", "sf_resnorm",
-           "sf_resnorm_workspace_bytes", "sf_resnorm_backward", "sf_ffn_workspace_bytes", "sf_ffn", "sf_ffn_backward")
+           "sf_resnorm_workspace_bytes", "sf_resnorm_backward", "sf_ffn_workspace_bytes", "sf_ffn", "sf_ffn_backward",
+           "sf_gradclip_workspace_bytes", "sf_gradclip")
 
 _STRIDE = C.c_int64 * 3
 
@@ -46,8 +49,13 @@ class SfFfnConfig(C.Structure):
                 ("w_down_stride", C.c_int64), ("dy_stride", C.c_int64)]
 
 
+class SfGradclipConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n", C.c_int32), ("max_norm", C.c_float), ("eps", C.c_float)]
+
+
 # by their C names
-STRUCTS = {"sf_linattn_config": SfLinattnConfig, "sf_resnorm_config": SfResnormConfig, "sf_ffn_config": SfFfnConfig}
+STRUCTS = {"sf_linattn_config": SfLinattnConfig, "sf_resnorm_config": SfResnormConfig, "sf_ffn_config": SfFfnConfig,
+           "sf_gradclip_config": SfGradclipConfig}
 
 _lib = None
 
@@ -68,7 +76,9 @@ def load_library():
                 ("sf_resnorm_backward", C.c_int, [P] * 17),
                 ("sf_ffn_workspace_bytes", C.c_int64, [P, C.c_int]),
                 ("sf_ffn", C.c_int, [P] * 8),
-                ("sf_ffn_backward", C.c_int, [P] * 12)):
+                ("sf_ffn_backward", C.c_int, [P] * 12),
+                ("sf_gradclip_workspace_bytes", C.c_int64, [C.c_int32, P]),
+                ("sf_gradclip", C.c_int, [P] * 8)):
             f = getattr(L, name)
             f.restype, f.argtypes = restype, argtypes
         _lib = L
@@ -224,9 +234,10 @@ def _elsewhere(stream, plan, call, first, rest, out):
         finally:
             if stream != before:
                 for t in (*first, *rest, *out.values()):
-                    if isinstance(t, torch.Tensor) and t.is_cuda:
-                        t.record_stream(stream)
-                        t.record_stream(before)
+                    for t in t if isinstance(t, (list, tuple)) else (t,):
+                        if isinstance(t, torch.Tensor) and t.is_cuda:
+                            t.record_stream(stream)
+                            t.record_stream(before)
 
 
 def _linattn_config(q, k, v, log_decay, scale, steps):
@@ -478,3 +489,82 @@ def _ffn_back_plan(x, w_gate, w_up, w_down, dy, act):
     c.dy_stride = _flat("dy", dy, rows).stride(0)
     return _Plan(c, [(n, s, x.dtype) for n, s in (("dx", x.shape), ("dw_gate", (c.F, c.D)), ("dw_up", (c.F, c.D)), ("dw_down", (c.D, c.F)))],
                  _lib.sf_ffn_workspace_bytes(C.addressof(c), 1), x.device)
+
+
+def _dense(t):
+    """Whether a tensor's elements fill its memory, in whatever order of its axes."""
+    size = 1
+    for stride, n in sorted((stride, n) for stride, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != size:
+            return False
+        size *= n
+    return True
+
+
+_tensor_facts = None  # of a list's tensors, by functions that map() calls (a list may have hundreds)
+
+
+def _list_key(name, tensors):
+    """What a list of gradients is: the device's index, sizes and types; their strides where a tensor is not contiguous."""
+    global _tensor_facts
+    if _tensor_facts is None:
+        T = binding._torch().Tensor
+        _tensor_facts = T.get_device, T.numel, operator.attrgetter("dtype"), T.is_contiguous
+    device, numel, dtype, contiguous = _tensor_facts
+    try:
+        where = set(map(device, tensors))
+        sizes, types = list(map(numel, tensors)), list(map(dtype, tensors))
+        strides = None if all(map(contiguous, tensors)) else [(t.shape, t.stride()) for t in tensors]
+    except TypeError:
+        _refuse("%s: a list of tensors is wanted" % name)
+    if len(where) != 1 or min(where) < 0:
+        _refuse("%s: %s, tensors on one GPU are wanted" % (name, "an empty list" if not where else "on %s" % ", ".join(
+            "the CPU" if i < 0 else "cuda:%d" % i for i in sorted(where))))
+    return [where, sizes, types, strides]
+
+
+class _ListPlan(_Plan):
+    __slots__ = ("sizes", "types", "kinds")
+
+
+def clip_gradients(grads, max_norm, eps=1e-6, in_place=True, out=None, stream=None):
+    """The global norm of a list of gradients (bf16 or fp32 or both, dense in any order of their axes), and the gradients times
+    min(1, max_norm / (norm + eps)): in place, or in_place=False as results.  Results: norm, fp32 [1], before clipping, and unless
+    in place grads, a list of tensors like the ones given."""
+    out, max_norm, eps = {} if out is None else out, _number(max_norm), _number(eps)
+    grads = grads if type(grads) is list else list(grads)
+    key = _list_key("grads", grads)
+    plan = _last.get("clip_gradients")
+    if plan is None or plan.key != key:
+        plan = _last["clip_gradients"] = _clip_plan(grads, key)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, clip_gradients, (grads,), (max_norm, eps, in_place), out)
+    torch = binding._torch()
+    data_ptr = torch.Tensor.data_ptr
+    norm, = _results(out, plan)
+    pointers = plan.kinds(*map(data_ptr, grads))
+    results = pointers
+    if not in_place:
+        to = out.get("grads")
+        if to is None:
+            to = out["grads"] = [torch.empty_like(g) for g in grads]
+        elif len(to) != len(grads) or _list_key("out['grads']", to) != key:
+            _refuse("out['grads'] does not fit: %d tensors of the same sizes, types and strides as the gradients are wanted" % len(grads))
+        results = plan.kinds(*map(data_ptr, to))
+    config = SfGradclipConfig(C.sizeof(SfGradclipConfig), len(grads), max_norm, eps)
+    _check(_lib.sf_gradclip(C.addressof(config), pointers, plan.sizes, plan.types, results, norm, _workspace(out, plan), _stream(plan.index)))
+    return out
+
+
+def _clip_plan(grads, key):
+    load_library()
+    types = [_dtype_of(g) for g in grads]
+    if key[3] is not None:
+        for i, g in enumerate(grads):
+            if not _dense(g):
+                _refuse("grads[%d] is not dense: %s, strides %s" % (i, tuple(g.shape), g.stride()))
+    n = len(grads)
+    sizes = (C.c_int64 * n)(*key[1])
+    plan = _ListPlan(SfGradclipConfig(), (("norm", (1,), binding._torch().float32),), _lib.sf_gradclip_workspace_bytes(n, sizes), grads[0].device)
+    plan.key, plan.sizes, plan.types, plan.kinds = key, sizes, (C.c_int32 * n)(*types), C.c_void_p * n
+    return plan
