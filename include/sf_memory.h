@@ -73,6 +73,56 @@ int sf_linattn_step(const sf_linattn_config* cfg, const void* q, const void* k, 
                     float* state_table, int32_t n_env, const int32_t* env_ids, const uint8_t* done, void* o,
                     void* hip_stream);
 
+/* ---- the gated delta rule --------------------------------------------------------------
+ * A matrix memory that each step decays, corrects at its key and reads.  For row (trajectory) n and head h, with a decay and a
+ * writing strength for each step:
+ *   S'  = exp(log_decay_t) (done[t][n] ? 0 : S_{t-1})     S_{-1} = state0,   S is [dk][dv]
+ *   S_t = S' + beta_t k_t (v_t - S'^T k_t)^T              state = S_{T-1}
+ *   o_t = scale * S_t^T q_t
+ * done as in sf_linattn; what lies before an episode's begin does not reach past it, NaN and infinities included, and no step
+ * reaches an earlier one.  A decay below 2^-126 (-infinity too) begins the memory anew, as done does.  Query and key heads may be
+ * shared: head h reads query and key head h / (H / Hk); values, decays and strengths are each head's own.  The correction grows
+ * without bound unless beta |k|^2 is at most 2: keys are meant to be of unit length (sf_resnorm over the heads as groups with
+ * scale dk^-0.5 makes them so) and strengths between 0 and 1; neither is tested.
+ * The passes over trajectories compute this in chunks of 32 steps, whose corrections are solved for by substitution.
+ *
+ * Arrays are time-major: q, k [T][N][Hk][dk], v [T][N][H][dv] and do, io, with strides as in sf_linattn_config, of any
+ * alignment of the elements; a call is fast if rows are of a multiple of eight elements and 16-byte aligned.  o, dq, dk, dv are dense.
+ *   log_decay, beta  dev [T][N][H] fp32 dense, their gradients alike.  log_decay is meant to be <= 0.  The gradient of a log_decay that no
+ *                    decay was made with (done, or below 2^-126) is 0.
+ *   done             dev [T][N] bytes or NULL
+ *   state0, state, dstate, dstate0  dev [N][H][dk][dv] fp32 or NULL (zero, not wanted)
+ * fp32 results, the states and the gradients of log_decay and beta come from fp32 sums of unrounded products; bf16 results are
+ * rounded from such, with 2^-16 of what enters the last products left out.  Of numbers whose products leave the range of fp32
+ * nothing is promised, but that they stay in their row, head and chunk of 32 steps or go on by the state.
+ * Results must not overlap inputs, nor one another, but for state as said below.
+ * Errors: SF_ERR_ARG, SF_ERR_SHAPE (as sf_linattn; N * H * T / 32 beyond 2^31 - 1), SF_ERR_ALIAS, SF_ERR_DEVICE. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(sf_deltarule_config) */
+  int32_t dtype;        /* SF_DTYPE_* of q, k, v, o and their gradients */
+  int32_t T, N, H, Hk, dk, dv;
+  float scale;
+  int64_t q_stride[3], k_stride[3], v_stride[3], do_stride[3]; /* step, row, head */
+} sf_deltarule_config;
+/* Bytes of the workspace of sf_deltarule (backward = 0) or sf_deltarule_backward (1); 0: none is needed, NULL may be
+ * passed; -1 on a bad configuration. */
+int64_t sf_deltarule_workspace_bytes(const sf_deltarule_config* cfg, int backward);
+/* state may be state0 (the states are then updated in place), but must not overlap it otherwise (SF_ERR_ALIAS). */
+int sf_deltarule(const sf_deltarule_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+                 const float* beta, const uint8_t* done, const float* state0, void* o, float* state, void* workspace,
+                 void* hip_stream);
+/* Gradients with respect to q, k, v, log_decay, beta and state0, given those of o (do) and of the final state (dstate or
+ * NULL).  Nothing of the forward pass is needed but its inputs.  dstate0 (or NULL) must overlap neither dstate nor state0
+ * (SF_ERR_ALIAS). */
+int sf_deltarule_backward(const sf_deltarule_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+                          const float* beta, const void* d_o, const uint8_t* done, const float* state0, const float* dstate,
+                          void* dq, void* dk, void* dv, float* dlog_decay, float* dbeta, float* dstate0, void* workspace,
+                          void* hip_stream);
+/* One step for B = cfg->N rows (cfg->T must be 1, stride[0] is not used), its states in a table, as sf_linattn_step. */
+int sf_deltarule_step(const sf_deltarule_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+                      const float* beta, float* state_table, int32_t n_env, const int32_t* env_ids, const uint8_t* done,
+                      void* o, void* hip_stream);
+
 /* ---- the norms behind and before a block, with its gate, residual scale and residual stream ----
  * For each of M rows of D channels, b the block's output and x the residual stream it is added to:
  *   u = N_post(b) * post_w            over each of `groups` equal groups of channels

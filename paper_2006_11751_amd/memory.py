@@ -1,6 +1,7 @@
 """The operators of a memory block on torch tensors: binding of include/sf_memory.h.
 
   linear_attention, linear_attention_backward, linear_attention_step
+  delta_rule, delta_rule_backward, delta_rule_step
   residual_norm, residual_norm_backward
   gated_ffn, gated_ffn_backward
   clip_gradients
@@ -24,7 +25,8 @@ from .binding import SF_OK, SfError, sf_last_error
 
 SF_DTYPE_FP32, SF_DTYPE_BF16 = 0, 1
 
-EXPORTS = ("sf_linattn_workspace_bytes", "sf_linattn", "sf_linattn_backward", "sf_linattn_step", "sf_resnorm",
+EXPORTS = ("sf_linattn_workspace_bytes", "sf_linattn", "sf_linattn_backward", "sf_linattn_step",
+           "sf_deltarule_workspace_bytes", "sf_deltarule", "sf_deltarule_backward", "sf_deltarule_step", "sf_resnorm",
            "sf_resnorm_workspace_bytes", "sf_resnorm_backward", "sf_ffn_workspace_bytes", "sf_ffn", "sf_ffn_backward",
            "sf_gradclip_workspace_bytes", "sf_gradclip")
 
@@ -35,6 +37,12 @@ class SfLinattnConfig(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("T", C.c_int32), ("N", C.c_int32), ("H", C.c_int32),
                 ("Hk", C.c_int32), ("dk", C.c_int32), ("dv", C.c_int32), ("scale", C.c_float),
                 ("q_stride", _STRIDE), ("k_stride", _STRIDE), ("v_stride", _STRIDE), ("o_stride", _STRIDE)]
+
+
+class SfDeltaruleConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("T", C.c_int32), ("N", C.c_int32), ("H", C.c_int32),
+                ("Hk", C.c_int32), ("dk", C.c_int32), ("dv", C.c_int32), ("scale", C.c_float),
+                ("q_stride", _STRIDE), ("k_stride", _STRIDE), ("v_stride", _STRIDE), ("do_stride", _STRIDE)]
 
 
 class SfResnormConfig(C.Structure):
@@ -54,7 +62,7 @@ class SfGradclipConfig(C.Structure):
 
 
 # by their C names
-STRUCTS = {"sf_linattn_config": SfLinattnConfig, "sf_resnorm_config": SfResnormConfig, "sf_ffn_config": SfFfnConfig,
+STRUCTS = {"sf_linattn_config": SfLinattnConfig, "sf_deltarule_config": SfDeltaruleConfig, "sf_resnorm_config": SfResnormConfig, "sf_ffn_config": SfFfnConfig,
            "sf_gradclip_config": SfGradclipConfig}
 
 _lib = None
@@ -71,6 +79,10 @@ def load_library():
                 ("sf_linattn", C.c_int, [P] * 11),
                 ("sf_linattn_backward", C.c_int, [P] * 15),
                 ("sf_linattn_step", C.c_int, [P] * 6 + [C.c_int32] + [P] * 4),
+                ("sf_deltarule_workspace_bytes", C.c_int64, [P, C.c_int]),
+                ("sf_deltarule", C.c_int, [P] * 12),
+                ("sf_deltarule_backward", C.c_int, [P] * 18),
+                ("sf_deltarule_step", C.c_int, [P] * 7 + [C.c_int32] + [P] * 4),
                 ("sf_resnorm", C.c_int, [P] * 10),
                 ("sf_resnorm_workspace_bytes", C.c_int64, [P]),
                 ("sf_resnorm_backward", C.c_int, [P] * 17),
@@ -335,6 +347,102 @@ def _linattn_step_plan(q, k, v, log_decay, state_table, env_ids, done, scale):
     _optional("env_ids", env_ids, q, (B,), torch.int32)
     _optional("done", done, q, (B,), torch.uint8)
     return _Plan(c, (("o", (B, H, c.dv), q.dtype),), 0, q.device)
+
+
+def _delta_config(q, k, v, log_decay, beta, scale, steps):
+    """steps: the arrays have a time axis in front."""
+    if not q.is_cuda:
+        _refuse("q is not on the GPU")
+    if q.dim() != (4 if steps else 3) or k.dim() != q.dim() or v.dim() != q.dim():
+        _refuse("q, k, v: %s, %s, %s" % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
+    lead, (Hk, dk) = tuple(q.shape[:-2]), q.shape[-2:]
+    H, dv = v.shape[-2:]
+    _same("k", k, q, lead + (Hk, dk), dense=False)
+    _same("v", v, q, lead + (H, dv), dense=False)
+    for name, t in (("log_decay", log_decay), ("beta", beta)):
+        _same(name, t, q, lead + (H,), dtype=binding._torch().float32)
+    c = SfDeltaruleConfig(C.sizeof(SfDeltaruleConfig), _dtype_of(q), lead[0] if steps else 1, lead[-1], H, Hk, dk, dv,
+                          dk ** -0.5 if scale is None else scale)
+    for field, name, t in ((c.q_stride, "q", q), (c.k_stride, "k", k), (c.v_stride, "v", v)):
+        s = _rows(name, t)
+        field[0], field[1], field[2] = s if steps else (0,) + s
+    return c
+
+
+def delta_rule(q, k, v, log_decay, beta, done=None, state0=None, scale=None, out=None, stream=None):
+    """The gated delta rule over N trajectories of T steps: q, k [T,N,Hk,dk], v [T,N,H,dv] (bf16 or fp32, last axis dense; keys
+    of unit length), log_decay and beta fp32 [T,N,H], done u8 [T,N], state0 fp32 [N,H,dk,dv]; scale: dk ** -0.5.  Results:
+    o [T,N,H,dv], state [N,H,dk,dv]."""
+    out, scale = {} if out is None else out, _number(scale)
+    given = (q, k, v, log_decay, beta, done, state0)
+    plan = _plan("delta_rule", scale, given, _delta_plan, *given, scale)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, delta_rule, given, (scale,), out)
+    o, state = _results(out, plan)
+    _check(_lib.sf_deltarule(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), beta.data_ptr(), _ptr(done),
+                             _ptr(state0), o, state, _workspace(out, plan), _stream(plan.index)))
+    return out
+
+
+def _delta_plan(q, k, v, log_decay, beta, done, state0, scale):
+    torch = binding._torch()
+    c = _delta_config(q, k, v, log_decay, beta, scale, True)
+    s = (c.N, c.H, c.dk, c.dv)
+    _optional("done", done, q, (c.T, c.N), torch.uint8)
+    _optional("state0", state0, q, s, torch.float32)
+    return _Plan(c, (("o", (c.T, c.N, c.H, c.dv), q.dtype), ("state", s, torch.float32)),
+                 _lib.sf_deltarule_workspace_bytes(C.addressof(c), 0), q.device)
+
+
+def delta_rule_backward(q, k, v, log_decay, beta, do, done=None, state0=None, dstate=None, scale=None, out=None, stream=None):
+    """Gradients of delta_rule with the same arguments, given those of o (do) and of the final state (dstate, or None).  Results:
+    dq, dk, dv, dlog_decay, dbeta, dstate0."""
+    out, scale = {} if out is None else out, _number(scale)
+    given = (q, k, v, log_decay, beta, do, done, state0, dstate)
+    plan = _plan("delta_rule_backward", scale, given, _delta_back_plan, *given, scale)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, delta_rule_backward, given, (scale,), out)
+    dq, dk, dv, dld, dbeta, ds0 = _results(out, plan)
+    _check(_lib.sf_deltarule_backward(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), beta.data_ptr(), do.data_ptr(),
+                                      _ptr(done), _ptr(state0), _ptr(dstate), dq, dk, dv, dld, dbeta, ds0, _workspace(out, plan),
+                                      _stream(plan.index)))
+    return out
+
+
+def _delta_back_plan(q, k, v, log_decay, beta, do, done, state0, dstate, scale):
+    torch = binding._torch()
+    c = _delta_config(q, k, v, log_decay, beta, scale, True)
+    s, f32 = (c.N, c.H, c.dk, c.dv), torch.float32
+    _same("do", do, q, (c.T, c.N, c.H, c.dv), dense=False)
+    c.do_stride[0], c.do_stride[1], c.do_stride[2] = _rows("do", do)
+    _optional("done", done, q, (c.T, c.N), torch.uint8)
+    _optional("state0", state0, q, s, f32)
+    _optional("dstate", dstate, q, s, f32)
+    return _Plan(c, (("dq", q.shape, q.dtype), ("dk", q.shape, q.dtype), ("dv", v.shape, q.dtype), ("dlog_decay", log_decay.shape, f32),
+                     ("dbeta", beta.shape, f32), ("dstate0", s, f32)), _lib.sf_deltarule_workspace_bytes(C.addressof(c), 1), q.device)
+
+
+def delta_rule_step(q, k, v, log_decay, beta, state_table, env_ids=None, done=None, scale=None, out=None, stream=None):
+    """One step of B environments: q, k [B,Hk,dk], v [B,H,dv], log_decay and beta fp32 [B,H], done u8 [B]; state_table fp32
+    [n_env,H,dk,dv] is read and overwritten at the rows env_ids (i32 [B], distinct; None: rows 0 .. B-1).  Result: o [B,H,dv]."""
+    out, scale = {} if out is None else out, _number(scale)
+    given = (q, k, v, log_decay, beta, state_table, env_ids, done)
+    plan = _plan("delta_rule_step", scale, given, _delta_step_plan, *given, scale)
+    if stream is not None or plan.index != _current_device():
+        return _elsewhere(stream, plan, delta_rule_step, given, (scale,), out)
+    o, = _results(out, plan)
+    _check(_lib.sf_deltarule_step(plan.address, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), beta.data_ptr(),
+                                  state_table.data_ptr(), state_table.shape[0], _ptr(env_ids), _ptr(done), o, _stream(plan.index)))
+    return out
+
+
+def _delta_step_plan(q, k, v, log_decay, beta, state_table, env_ids, done, scale):
+    torch = binding._torch()
+    c = _delta_config(q, k, v, log_decay, beta, scale, False)
+    _same("state_table", state_table, q, (state_table.shape[0], c.H, c.dk, c.dv), torch.float32)
+    _optional("env_ids", env_ids, q, (c.N,), torch.int32)
+    _optional("done", done, q, (c.N,), torch.uint8)
+    return _Plan(c, (("o", (c.N, c.H, c.dv), q.dtype),), 0, q.device)
 
 
 _NORMS = {"none": 0, "rms": 1, "layer": 2}
