@@ -26,6 +26,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "sf_chunk.h"
 #include "sf_internal.h"
@@ -56,9 +57,16 @@ struct DeltaArgs {
   float *dlog_decay, *dbeta;
   float* dstate0;                 // of one chunk, or null
   int f32;                        // dq and dk are fp32 whatever the arrays are (partial sums of shared heads)
-  int T, N, H, chunks, blocks_v;
+  float* made;                    // [N * H][chunks] what the chunks' steps make of each other (made_words() each), or null
+  // pieces of T, of whole chunks
+  int n_seg, seg_len, piece;      // piece: the pieces' own states are what is made
+  float* seg_state;               // [N * H][n_seg][dk * dv] first the pieces' own states, then what enters them
+  float* seg_through;             // [N * H][n_seg][dk * dk] what a piece makes of the state that enters it
+  int* seg_begin;                 // [N * H][n_seg] an episode begins in the piece
+  int T, N, H, chunks, back;
+  int blocks_v, blocks;           // workgroups of 64 columns of v; and of the identity besides
   float scale;
-  Divisor heads, share, per;      // H, heads that share one of q and k; chunks
+  Divisor heads, share, rows, round;  // H, heads that share one of q and k, N * H, 8 blocks
 };
 
 typedef Num<SF_DTYPE_FP32> F32;
@@ -97,15 +105,18 @@ __device__ inline float wave_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// What the chunk's steps have of their own, in LDS.
+// What the chunk's steps have of their own.
 struct Steps {
   float gh[C], gl[C];  // G in binary logarithms, as two numbers
   float enter[C];      // E
   float leave[C];      // W
   float beta[C];
   int ep[C];           // episode of the step, counted in the chunk; steps that are not there have their own, which is nobody else's
-  int flag[4];
 };
+constexpr int kStepWords = sizeof(Steps) / 4;
+// A chunk's matrices [32][32] and Steps, where a launch leaves them for others: T, P (backwards P^T and A^T), Steps.
+constexpr int kDense = C * C;
+__host__ __device__ constexpr int made_words(bool back) { return (back ? 3 : 2) * kDense + kStepWords; }
 
 struct StepIn {
   float ld, beta;
@@ -123,22 +134,34 @@ __device__ inline StepIn read_step(const DeltaArgs& g, int n, int h, int t0, int
   return s;
 }
 __device__ inline bool begins(const StepIn& s) { return s.done || s.ld * 1.44269504f < (float)kLeastLog2; }
-// NaN if something of the step is not finite that should be
-__device__ inline float finite_step(const StepIn& s) { return fmaf(s.beta, 0.0f, begins(s) ? 0.0f : s.ld * 0.0f); }
 
-// One wave: the arrays of Steps from the lanes' steps (all lanes call it).
+// A lane's number from the lane n before it in its row of 16 (0 where there is none).
+template <int N>
+__device__ inline double row_shift(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, 0x110 + N, 0xF, 0xF, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), 0x110 + N, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)(unsigned)hi << 32 | (unsigned)lo);
+}
+
+// One wave: the arrays of Steps from the lanes' steps (all lanes call it; those from 32 on do as those before).
 __device__ inline void put_steps(Steps& s, const StepIn& in, unsigned marks, int valid, int lane) {
   const int i = lane & (C - 1);
-  const int e = __popc(marks & ((2u << i) - 1));
-  // the sum since the episode's begin in the chunk
-  double G = begins(in) || i >= valid ? 0.0 : (double)in.ld * 1.4426950408889634;
-#pragma unroll
-  for (int d = 1; d < C; d <<= 1) {
-    const double before = __shfl_up(G, d, C);
-    // (the steps from i - d + 1 on are in G; the ones before belong to it if none of these begins an episode)
-    if (i >= d && (marks & (((2u << i) - 1) & ~((1u << (i - d + 1)) - 1))) == 0) G += before;
-  }
-  const double last = __shfl(G, valid - 1, C);
+  const unsigned upto = (2u << i) - 1;
+  const int e = __popc(marks & upto);
+  // the sum since the episode's begin in the chunk: a lane adds what the one d before it has, if no episode begins behind that one
+  double G = lane >= C || begins(in) || i >= valid ? 0.0 : (double)in.ld * 1.4426950408889634;
+  const int reach = i - (31 - __clz((int)((marks & upto) | 1u)));  // steps since the last begin, or the chunk's
+  double b = row_shift<1>(G);
+  G += reach >= 1 ? b : 0.0;
+  b = row_shift<2>(G);
+  G += reach >= 2 ? b : 0.0;
+  b = row_shift<4>(G);
+  G += reach >= 4 ? b : 0.0;
+  b = row_shift<8>(G);
+  G += reach >= 8 ? b : 0.0;
+  b = __shfl(G, 15);
+  G += i >= 16 && reach >= i - 15 ? b : 0.0;
+  const double last = __shfl(G, valid - 1);
   const int e_last = __popc(marks);
   if (lane < C) {
     const float hi = (float)G;
@@ -160,46 +183,129 @@ struct Slots {
 __device__ inline Slots slots_of(const float* m, int row, int lg) {
   return Slots{*(const f32x4*)(m + row * kMat + 4 * lg), *(const f32x4*)(m + row * kMat + 16 + 4 * lg)};
 }
-
-// One wave: T = (1 + A beta)^-1 from A^T [j][i] into `by_row` [i][j] and `by_column` [j][i].  The block above the diagonal is not written.
-__device__ inline void invert(const float* at, const float* beta, float* by_row, float* by_column, int lane) {
-  const int li = lane & 15, lg = lane >> 4;
-  if (lane < 32) {
-    const int b0 = lane & 16;
-    float t[16];
+// The same of a column.
+__device__ inline Slots slots_down(const float* m, int column, int lg) {
+  Slots s;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t[i] = i == li ? 1.0f : 0.0f;
-#pragma unroll
-    for (int l = 0; l < 15; ++l) {
-      const float x = beta[b0 + l] * t[l];
-#pragma unroll
-      for (int i4 = (l + 1) & ~3; i4 < 16; i4 += 4) {
-        const f32x4 a = *(const f32x4*)(at + (b0 + l) * kMat + b0 + i4);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (i4 + r > l) t[i4 + r] = fmaf(-a[r], x, t[i4 + r]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) by_row[(b0 + i) * kMat + b0 + li] = t[i];
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) *(f32x4*)(by_column + (b0 + li) * kMat + b0 + i) = f32x4{t[i], t[i + 1], t[i + 2], t[i + 3]};
+  for (int r = 0; r < 4; ++r) {
+    s.a[r] = m[(4 * lg + r) * kMat + column];
+    s.b[r] = m[(16 + 4 * lg + r) * kMat + column];
   }
+  return s;
+}
+// Between what lanes of a wave write to LDS and what others of it read.
+__device__ inline void wave_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
+}
+
+// One wave: T = (1 + A beta)^-1 [i][j] from A^T [j][i].  The block above the diagonal is not written.
+// A row of 16 lanes has a block of 16, a lane one column of A (times its beta) and one of T; what all lanes need of A comes from its
+// lane by a broadcast within the row, so that nothing is read in between.
+__device__ inline void invert(const float* at, const float* beta, float* T, int lane) {
+  const int li = lane & 15, lg = lane >> 4, b0 = lane & 16;  // (rows 2 and 3 of the wave do as 0 and 1)
+  float a[16], t[16];
+  {
+    const float b = -beta[b0 + li];
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const f32x4 x = *(const f32x4*)(at + (b0 + li) * kMat + b0 + i);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) a[i + r] = b * x[r];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) t[i] = i == li ? 1.0f : 0.0f;
+  auto step = [&](auto at_l) {
+    constexpr int l = decltype(at_l)::value;
+#pragma unroll
+    for (int i = l + 1; i < 16; ++i)
+      t[i] = fmaf(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, a[i]), 0x150 + l, 0xF, 0xF, false)), t[l], t[i]);
+  };
+#define SF_STEP(l) step(std::integral_constant<int, l>())
+  SF_STEP(0); SF_STEP(1); SF_STEP(2); SF_STEP(3); SF_STEP(4); SF_STEP(5); SF_STEP(6); SF_STEP(7);
+  SF_STEP(8); SF_STEP(9); SF_STEP(10); SF_STEP(11); SF_STEP(12); SF_STEP(13); SF_STEP(14);
+#undef SF_STEP
+  if (lane < 32) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) T[(b0 + i) * kMat + b0 + li] = t[i];
+  }
+  wave_order();
   // the lower left block: -T22 A21 beta T11
   f32x4 a21, bt, zero = {0.0f, 0.0f, 0.0f, 0.0f};
-  const f32x4 t11 = *(const f32x4*)(by_column + li * kMat + 4 * lg), be = *(const f32x4*)(beta + 4 * lg);
+  const f32x4 be = *(const f32x4*)(beta + 4 * lg);
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     a21[r] = at[(4 * lg + r) * kMat + 16 + li];
-    bt[r] = be[r] * t11[r];
+    bt[r] = be[r] * T[(4 * lg + r) * kMat + li];
   }
   const f32x4 z = mm4(a21, bt, zero);
-  const f32x4 t21 = mm4(*(const f32x4*)(by_row + (16 + li) * kMat + 16 + 4 * lg), z, zero);
+  const f32x4 t21 = mm4(*(const f32x4*)(T + (16 + li) * kMat + 16 + 4 * lg), z, zero);
 #pragma unroll
-  for (int r = 0; r < 4; ++r) by_row[(16 + 4 * lg + r) * kMat + li] = -t21[r];
-  *(f32x4*)(by_column + li * kMat + 16 + 4 * lg) = -t21;
+  for (int r = 0; r < 4; ++r) T[(16 + 4 * lg + r) * kMat + li] = -t21[r];
+}
+
+// One wave: a chunk's Steps, A^T, P (backwards P^T, without the scale) and T into LDS (pitch kMat).  Keys and queries are read as operands.
+template <int DTYPE, int D, bool BACK>
+__device__ inline void make_chunk(const DeltaArgs& g, int n, int h, int hk, int t0, int valid, int lane, Steps& steps, float* mA, float* mP, float* mT) {
+  typedef Num<DTYPE> M;
+  const int li = lane & 15, lg = lane >> 4, dk = g.k.d;
+  auto base = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
+  const unsigned char *const qb = base(g.q), *const kb = base(g.k);
+  typename M::Raw q[2][D / 32], k[2][D / 32];
+#pragma unroll
+  for (int I = 0; I < 2; ++I) {
+    const int r = 16 * I + li;
+    const int64_t t = t0 + (r < valid ? r : 0);
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      unsigned w[M::kPieceWords];
+      load_piece<DTYPE>(w, g.k, kb + t * g.k.st * M::kBytes, 32 * s + 8 * lg, r < valid);
+      __builtin_memcpy(&k[I][s], w, sizeof w);
+      load_piece<DTYPE>(w, g.q, qb + t * g.q.st * M::kBytes, 32 * s + 8 * lg, r < valid);
+      __builtin_memcpy(&q[I][s], w, sizeof w);
+    }
+  }
+  const StepIn in = read_step(g, n, h, t0, valid, lane);
+  const unsigned marks = (unsigned)__ballot(begins(in));
+  put_steps(steps, in, marks, valid, lane);
+  wave_order();
+#pragma unroll
+  for (int I = 0; I < 2; ++I)
+#pragma unroll
+    for (int J = 0; J < 2; ++J) {
+      f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, p = a;
+      if (J <= I) {
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+          if (32 * s >= dk) continue;
+          a = M::mma(k[I][s], k[J][s], a);                                           // [i][j]
+          p = BACK ? M::mma(q[I][s], k[J][s], p) : M::mma(k[J][s], q[I][s], p);  // [i][j], forwards [j][i]
+        }
+        // rows are steps 16 R + 4 lg + r of tile R, columns are steps of the other one
+        auto decayed = [&](f32x4 x, int rows, int columns, bool rows_later, bool strict, float scale) {
+          const int c = 16 * columns + li, ec = steps.ep[c];
+          const float hc = steps.gh[c], lc = steps.gl[c];
+          const f32x4 h4 = *(const f32x4*)(steps.gh + 16 * rows + 4 * lg), l4 = *(const f32x4*)(steps.gl + 16 * rows + 4 * lg);
+          const i32x4 e4 = *(const i32x4*)(steps.ep + 16 * rows + 4 * lg);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int later = rows_later ? 16 * rows + 4 * lg + r - c : c - (16 * rows + 4 * lg + r);
+            const float d = rows_later ? decay_of(h4[r], l4[r], hc, lc) : decay_of(hc, lc, h4[r], l4[r]);
+            x[r] = later >= (strict ? 1 : 0) && e4[r] == ec ? x[r] * (scale * d) : 0.0f;
+          }
+          return x;
+        };
+        a = decayed(a, I, J, true, true, 1.0f);
+        p = BACK ? decayed(p, I, J, true, false, 1.0f) : decayed(p, J, I, false, false, g.scale);
+      }
+      *(f32x4*)(mA + (16 * J + li) * kMat + 16 * I + 4 * lg) = a;                // A^T [j][i]
+      if (BACK) *(f32x4*)(mP + (16 * J + li) * kMat + 16 * I + 4 * lg) = p;      // P^T [j][i]
+      else *(f32x4*)(mP + (16 * I + li) * kMat + 16 * J + 4 * lg) = p;           // P [i][j]
+    }
+  wave_order();
+  invert(mA, steps.beta, mT, lane);
+  wave_order();
 }
 
 template <int DTYPE, int D>
@@ -243,103 +349,170 @@ __device__ inline void put_piece(unsigned char* tile, int pitch, const unsigned*
 template <int DTYPE, int D>
 struct SweepLds {
   static constexpr int kPitch = Pitch<DTYPE, D>::value, kPitchV = Pitch<DTYPE, DV>::value;
-  static constexpr int kK = C * kPitch, kV = 2 * C * kPitch, kA = kV + C * kPitchV, kP = kA + C * kMat * 4, kRow = kP + C * kMat * 4,
-                       kColumn = kRow + C * kMat * 4, kSteps = kColumn + C * kMat * 4, kBytes = kSteps + (int)sizeof(Steps);
+  static constexpr int kK = C * kPitch, kV = 2 * C * kPitch, kP = kV + C * kPitchV, kT = kP + C * kMat * 4, kSteps = kT + C * kMat * 4,
+                       kFlag = kSteps + (int)sizeof(Steps), kA = kFlag + 16, kBytes = kA, kBytesAlone = kA + C * kMat * 4;
 };
+
+// The matrices of every chunk, for the sweeps and the gradients: a wave makes one chunk's.
+template <int DTYPE, int D, bool BACK>
+__global__ __launch_bounds__(kThreads) void delta_chunks_kernel(DeltaArgs g) {
+  constexpr int kWave = 3 * C * kMat * 4 + (int)sizeof(Steps);
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned at = blockIdx.x * 4 + wave;
+  if (at >= (unsigned)g.N * g.H * g.chunks) return;
+  const int chunk = (int)g.rows.of(at), bh = (int)(at - (unsigned)chunk * (g.N * g.H));
+  const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h), t0 = chunk * C, valid = min(C, g.T - t0);
+  float *const mA = (float*)(lds + wave * kWave), *const mP = mA + C * kMat, *const mT = mP + C * kMat;
+  Steps& steps = *(Steps*)(mT + C * kMat);
+  make_chunk<DTYPE, D, BACK>(g, n, h, hk, t0, valid, lane, steps, mA, mP, mT);
+  float* const out = g.made + ((size_t)bh * g.chunks + chunk) * made_words(BACK);
+#pragma unroll
+  for (int i = 0; i < kDense / 256; ++i) {
+    const int e = (i * 64 + lane) * 4, from = e / C * kMat + e % C;
+    *(f32x4*)(out + e) = *(const f32x4*)(mT + from);
+    *(f32x4*)(out + kDense + e) = *(const f32x4*)(mP + from);
+    if (BACK) *(f32x4*)(out + 2 * kDense + e) = *(const f32x4*)(mA + from);
+  }
+  if (lane < kStepWords / 4) *(f32x4*)(out + (BACK ? 3 : 2) * kDense + 4 * lane) = *(const f32x4*)((const float*)&steps + 4 * lane);
+}
 
 enum Sweep { kResults = 0, kStates = 1, kBack = 2 };
 
-// A workgroup of four waves goes over the chunks of one (row, head) for 64 columns of v, of which a wave owns 16: its part of the state stays
-// in registers as the accumulator of the update.  The products are arranged so that accumulators feed the next product without a
-// shuffle: a 16x16 accumulator holds rows 4 lg .. 4 lg + 3 of one column per lane (lg = lane / 16), two of them are
+// A workgroup of four waves goes over the chunks of one (row, head), or of one piece of T, for 64 columns of v, of which a wave owns 16: its part of
+// the state stays in registers as the accumulator of the update.  The products are arranged so that accumulators feed the next
+// product without a shuffle: a 16x16 accumulator holds rows 4 lg .. 4 lg + 3 of one column per lane (lg = lane / 16), two of them are
 // the eight K-slots of an operand of 16x16x32, and the other operand follows the same numbering of the K axis.
-//   kResults: o and the last state;  kStates: the states that enter the chunks;  kBack: R, from the last chunk to the first
-template <int DTYPE, int D, int SWEEP>
-__global__ __launch_bounds__(kThreads, 2) void delta_sweep_kernel(DeltaArgs g) {
+//   kResults: o and the last state;  kStates: the states that enter the chunks, or the last one of a piece;  kBack: R, from the last chunk to the first
+// ALONE: of one chunk, whose matrices the first wave makes (else they are read).  VEC: arrays are read in 16-byte pieces.
+template <int DTYPE, int D, int SWEEP, bool ALONE, bool VEC>
+__global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_sweep_kernel(DeltaArgs g) {
   typedef Num<DTYPE> M;
   typedef SweepLds<DTYPE, D> L;
   constexpr int W = M::kPieceWords, NP = C * D / 8 / kThreads, ND = D / 16, kRow = D / 8, kRowV = DV / 8;
-  constexpr bool kQ = SWEEP != kStates;
+  constexpr bool kQ = SWEEP != kStates, kUp = SWEEP != kBack;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   // the blocks of one (row, head) read the same arrays: one after another on one XCD (workgroups go to the 8 in turn)
-  const unsigned round = blockIdx.x >> (g.blocks_v == 2 ? 4 : 3), in_round = blockIdx.x & (8 * g.blocks_v - 1);
-  const int v_block = in_round >> 3 ? DV : 0, bh = (int)(round * 8 + (in_round & 7));
+  const unsigned round = g.round.of(blockIdx.x), in_round = blockIdx.x - round * (8 * g.blocks), turn8 = in_round >> 3;
+  const int bh = (int)(round * 8 + (in_round & 7));
   if (bh >= g.N * g.H) return;
+  // a piece has blocks of the identity's columns besides: what a state that enters becomes
+  const bool identity = (int)turn8 >= g.blocks_v;
+  const int v_block = DV * ((int)turn8 - (identity ? g.blocks_v : 0)), seg = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h);
-  const int dk = g.k.d, dv = g.v.d;
+  const int dk = g.k.d, dv = identity ? dk : g.v.d;
+  const int t_begin = seg * g.seg_len, t_end = min(g.T, t_begin + g.seg_len);
   auto base = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
   const Strided third = SWEEP == kBack ? g.d_o : g.v;
   const unsigned char *const qb = base(g.q), *const kb = base(g.k), *const vb = base(third);
   unsigned char *const tq = lds, *const tk = lds + L::kK, *const tv = lds + L::kV;
-  float *const mA = (float*)(lds + L::kA), *const mP = (float*)(lds + L::kP), *const by_row = (float*)(lds + L::kRow),
-               *const by_column = (float*)(lds + L::kColumn);
+  float *const mP = (float*)(lds + L::kP), *const mT = (float*)(lds + L::kT);
   Steps& steps = *(Steps*)(lds + L::kSteps);
+  int* const flag = (int*)(lds + L::kFlag);
+
+  if (tid < 2) flag[tid] = 0;
+  if constexpr (ALONE) {
+    __syncthreads();
+    if (wave == 0) make_chunk<DTYPE, D, SWEEP == kBack>(g, n, h, hk, 0, g.T, lane, steps, (float*)(lds + L::kA), mP, mT);
+  }
 
   const int v0 = v_block + 16 * wave, y = v0 + li;  // this wave's columns of v, this lane's
   const bool has_v = v0 < dv;
   auto has_k = [&](int s) { return 32 * s < dk; };
   // row of tile t of the state (two tiles are 32 rows: eight neighbours per lane group)
   auto col_k = [&](int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); };
+  // Memory is read and written through buffers that begin at a uniform address; what is not there has an offset past the end
+  // (it is read as zero, not written).
+  constexpr unsigned kOutside = 0x80000000u;
+  auto buffer = [&](const void* p, unsigned bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000); };
 
   f32x4 S[ND];
   bool odd_state = false;  // it holds something not finite
+  const unsigned y_at = y < dv ? (unsigned)(8 * lg * dv + y) * 4 : kOutside;  // (rows past dk lie past the end)
   {
-    const float* const s = g.s_in ? g.s_in + (size_t)bh * dk * dv : nullptr;
+    const float* s = nullptr;
+    if (g.piece) s = nullptr;
+    else if (g.n_seg > 1) s = g.seg_state + ((size_t)bh * g.n_seg + seg) * dk * dv;
+    else if (g.s_in) s = g.s_in + (size_t)bh * dk * dv;
+    const auto from = buffer(s, s ? (unsigned)(dk * dv) * 4 : 0);
     float test = 0.0f;
 #pragma unroll
     for (int a = 0; a < ND; ++a)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int x = col_k(a, 4 * lg + r);
-        S[a][r] = s && x < dk && y < dv ? s[x * dv + y] : 0.0f;
+        S[a][r] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4, 0));
+        if (identity) S[a][r] = col_k(a, 4 * lg + r) == y ? 1.0f : 0.0f;
         test = fmaf(S[a][r], 0.0f, test);
       }
     odd_state = test != 0.0f;
   }
   auto store_state = [&](float* s) {
+    const auto to = buffer(s, (unsigned)(dk * dv) * 4);
 #pragma unroll
     for (int a = 0; a < ND; ++a)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int x = col_k(a, 4 * lg + r);
-        if (x < dk && y < dv) s[x * dv + y] = S[a][r];
-      }
+      for (int r = 0; r < 4; ++r)
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, (float)S[a][r]), to, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4, 0);
   };
 
+  // the chunk that is on its way: its rows, matrices and steps
   unsigned nq[NP][W], nk[NP][W], nv[W];
-  StepIn in;
-  auto request = [&](int t0, int valid) {
+  f32x4 n_p, n_t, n_steps;
+  unsigned at_q[NP], at_k[NP], at_v = kOutside;
+  if constexpr (VEC) {
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      if constexpr (kQ) fetch<DTYPE>(nq[p], g.q, qb, t0, valid, tid + p * kThreads, kRow, 0);
-      fetch<DTYPE>(nk[p], g.k, kb, t0, valid, tid + p * kThreads, kRow, 0);
+      const int piece = tid + p * kThreads, r = piece / kRow, col = piece % kRow * 8;
+      at_q[p] = col < dk ? (unsigned)(r * (int)g.q.st + col) * M::kBytes : kOutside;
+      at_k[p] = col < dk ? (unsigned)(r * (int)g.k.st + col) * M::kBytes : kOutside;
     }
-    fetch<DTYPE>(nv, third, vb, t0, valid, tid, kRowV, v_block);
-    in = read_step(g, n, h, t0, valid, lane);
-  };
-  // the chunk [lo, hi); of a flagged one, step by step
-  int alone = SWEEP == kBack ? g.T : 0;  // steps before this one (backwards: from it on) are chunks of their own
-  int lo, hi;
-  auto bounds = [&](int at) {  // of the chunk that begins (backwards: ends) at `at`
-    if (SWEEP == kBack) {
-      hi = at;
-      lo = at > alone ? at - 1 : (at - 1) / C * C;
-    } else {
-      lo = at;
-      hi = at < alone ? at + 1 : min(g.T, (at / C + 1) * C);
-    }
-  };
-  if (tid < 4) steps.flag[tid] = 0;
-  if (g.T > 0) {
-    bounds(SWEEP == kBack ? g.T : 0);
-    request(lo, hi - lo);
+    const int col = v_block + tid % kRowV * 8;
+    if (col < third.d && !identity) at_v = (unsigned)(tid / kRowV * (int)third.st + col) * M::kBytes;
   }
-  for (int turn = 0; g.T > 0; turn ^= 1) {
-    const int valid = hi - lo;
-    const unsigned marks = (unsigned)__ballot(begins(in));  // (lanes below C)
-    __syncthreads();  // the chunk before has been read
+  const float* const made = g.made + (size_t)bh * g.chunks * made_words(!kUp || g.back);
+  auto request = [&](int c) {
+    const int t0 = c * C, valid = min(C, g.T - t0);
+    if constexpr (VEC) {
+      auto get = [&](unsigned* w, const Strided& a, const unsigned char* row, int r, unsigned at) {
+        const auto from = buffer(row + (int64_t)t0 * a.st * M::kBytes, 0x7FFFFFFF);
+        at = r < valid ? at : kOutside;
+#pragma unroll
+        for (int i = 0; i < W; i += 4) *(u32x4*)(w + i) = __builtin_amdgcn_raw_buffer_load_b128(from, at + 4 * i, 0, 0);
+      };
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        if constexpr (kQ) get(nq[p], g.q, qb, (tid + p * kThreads) / kRow, at_q[p]);
+        get(nk[p], g.k, kb, (tid + p * kThreads) / kRow, at_k[p]);
+      }
+      get(nv, third, vb, tid / kRowV, at_v);
+    } else {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        if constexpr (kQ) fetch<DTYPE>(nq[p], g.q, qb, t0, valid, tid + p * kThreads, kRow, 0);
+        fetch<DTYPE>(nk[p], g.k, kb, t0, valid, tid + p * kThreads, kRow, 0);
+      }
+      fetch<DTYPE>(nv, third, vb, t0, identity ? 0 : valid, tid, kRowV, v_block);
+    }
+    if constexpr (!ALONE) {
+      const float* const m = made + (size_t)c * made_words(!kUp || g.back);
+      n_t = *(const f32x4*)(m + 4 * tid);
+      if constexpr (kQ) n_p = *(const f32x4*)(m + kDense + 4 * tid);
+      if (tid < kStepWords / 4) n_steps = *(const f32x4*)(m + (!kUp || g.back ? 3 : 2) * kDense + 4 * tid);
+    }
+  };
+  unsigned at_o[2];  // of four neighbours of an output row
+#pragma unroll
+  for (int I = 0; I < 2; ++I) at_o[I] = v0 + 4 * lg < dv ? (unsigned)((16 * I + li) * (g.N * g.H * dv) + v0 + 4 * lg) * M::kBytes : kOutside;
+
+  const int first = t_begin / C, last = (t_end - 1) / C;  // chunks
+  if (t_begin < t_end) request(kUp ? first : last);
+  bool any_begin = false;
+  for (int c = kUp ? first : last, turn = 0; t_begin < t_end && (kUp ? c <= last : c >= first); c += kUp ? 1 : -1, turn ^= 1) {
+    const int t0 = c * C, valid = min(C, g.T - t0);
+    if (SWEEP != kResults && g.kept && has_v) store_state(g.kept + ((size_t)bh * g.chunks + c) * ((size_t)dk * dv));
+    if constexpr (!ALONE) __syncthreads();  // the chunk before has been read
     float test = 0.0f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -350,243 +523,289 @@ __global__ __launch_bounds__(kThreads, 2) void delta_sweep_kernel(DeltaArgs g) {
     }
     put_piece<DTYPE>(tv, L::kPitchV, nv, tid, kRowV);
     test = finite_test<DTYPE>(nv, test);
-    if (wave == 0) {
-      put_steps(steps, in, marks, valid, lane);
-      test += finite_step(in);
+    if constexpr (!ALONE) {
+      const int to = tid / 8 * kMat + tid % 8 * 4;
+      *(f32x4*)(mT + to) = n_t;
+      if constexpr (kQ) *(f32x4*)(mP + to) = n_p;
+      if (tid < kStepWords / 4) *(f32x4*)((float*)&steps + 4 * tid) = n_steps;
     }
-    if (test != 0.0f || (odd_state && marks)) steps.flag[turn] = 1;
+    if (test != 0.0f) flag[turn] = 1;
     __syncthreads();
-    if (tid == 0) steps.flag[turn ^ 1] = 0;  // (read by all before the barrier above)
-    if (steps.flag[turn] != 0 && valid > 1) {  // again, step by step
-      alone = SWEEP == kBack ? lo : hi;
-      bounds(SWEEP == kBack ? hi : lo);
-      request(lo, hi - lo);
-      continue;
-    }
-    const int c0 = lo;
-    const bool more = SWEEP == kBack ? lo > 0 : hi < g.T;
-    if (SWEEP != kResults && (SWEEP == kBack ? hi == g.T || hi % C == 0 : lo % C == 0) && has_v)
-      store_state(g.kept + ((size_t)bh * g.chunks + (SWEEP == kBack ? (hi - 1) / C : lo / C)) * ((size_t)dk * dv));
-    if (more) {
-      bounds(SWEEP == kBack ? lo : hi);
-      request(lo, hi - lo);
-    }
+    if (c != (kUp ? last : first)) request(kUp ? c + 1 : c - 1);
+    // (marks of begins are where the episode's number grows)
+    const int my_ep = steps.ep[lane & (C - 1)];
+    const float my_steps = fmaf(steps.gh[lane & (C - 1)], 0.0f, steps.beta[lane & (C - 1)] * 0.0f);
+    const int e_last = __builtin_amdgcn_readlane(my_ep, valid - 1);
+    const bool marked = e_last != 0;
+    any_begin = any_begin || marked;
+    const bool one_by_one = flag[turn] != 0 || __any(my_steps != 0.0f) || (marked && __any(odd_state));
+    if (tid == 0) flag[turn ^ 1] = 0;  // (read by all before the barrier above)
 
-    // the chunk's matrices, by tiles of 16 x 16: wave (I, J) has steps i of tile I and j of tile J
-    {
-      const int I = wave >> 1, J = wave & 1;
-      f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, p = a;
-      if (J <= I) {
+    if (one_by_one && has_v) {
+      // Step by step, each wave for its columns, so that nothing that is not finite meets a masked zero.
+      auto element = [&](const unsigned char* tile, int pitch, int i, int x) { return M::element(tile + i * pitch + x * M::kBytes); };
+      for (int at = 0; at < valid; ++at) {
+        const int i = kUp ? at : valid - 1 - at;
+        const StepIn in = read_step(g, n, h, t0 + i, 1, lane & 0);
+        const bool begin = begins(in);
+        const float keep = exp2f(in.ld * 1.44269504f), v = element(tv, L::kPitchV, i, 16 * wave + li);
+        float sum = 0.0f;
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-          if (!has_k(s)) continue;
-          const int at = (32 * s + 8 * lg) * M::kBytes;
-          const auto ki = M::row(tk + (16 * I + li) * L::kPitch + at), kj = M::row(tk + (16 * J + li) * L::kPitch + at);
-          a = M::mma(ki, kj, a);  // [i][j]
-          if constexpr (SWEEP == kResults) p = M::mma(kj, M::row(tq + (16 * I + li) * L::kPitch + at), p);  // [j][i]
-          if constexpr (SWEEP == kBack) p = M::mma(M::row(tq + (16 * I + li) * L::kPitch + at), kj, p);     // [i][j]
-        }
-        const int j = 16 * J + li, ej = steps.ep[j];
-        const float hj = steps.gh[j], lj = steps.gl[j];
-        const f32x4 h4 = *(const f32x4*)(steps.gh + 16 * I + 4 * lg), l4 = *(const f32x4*)(steps.gl + 16 * I + 4 * lg);
-        const i32x4 e4 = *(const i32x4*)(steps.ep + 16 * I + 4 * lg);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int i = 16 * I + 4 * lg + r;
-          const float d = decay_of(h4[r], l4[r], hj, lj);
-          a[r] = i > j && e4[r] == ej ? a[r] * d : 0.0f;
-          if constexpr (SWEEP == kBack) p[r] = i >= j && e4[r] == ej ? p[r] * (g.scale * d) : 0.0f;
-        }
-        if constexpr (SWEEP == kResults) {
-          const int i = 16 * I + li, ei = steps.ep[i];
-          const float hi_ = steps.gh[i], lo_ = steps.gl[i];
-          const f32x4 hj4 = *(const f32x4*)(steps.gh + 16 * J + 4 * lg), lj4 = *(const f32x4*)(steps.gl + 16 * J + 4 * lg);
-          const i32x4 ej4 = *(const i32x4*)(steps.ep + 16 * J + 4 * lg);
+        for (int a = 0; a < ND; ++a)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int jj = 16 * J + 4 * lg + r;
-            p[r] = jj <= i && ej4[r] == ei ? p[r] * (g.scale * decay_of(hi_, lo_, hj4[r], lj4[r])) : 0.0f;
+            const int x = col_k(a, 4 * lg + r);
+            if (x >= dk) continue;
+            if constexpr (kUp) S[a][r] = begin ? 0.0f : keep * S[a][r];
+            else S[a][r] += g.scale * element(tq, L::kPitch, i, x) * v;
+            sum += element(tk, L::kPitch, i, x) * S[a][r];
           }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        const float u = in.beta * (kUp ? v - sum : -sum);
+        float o = 0.0f;
+#pragma unroll
+        for (int a = 0; a < ND; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int x = col_k(a, 4 * lg + r);
+            if (x >= dk) continue;
+            S[a][r] += element(tk, L::kPitch, i, x) * u;
+            if constexpr (SWEEP == kResults) o += element(tq, L::kPitch, i, x) * S[a][r];
+            if constexpr (!kUp) S[a][r] = begin ? 0.0f : keep * S[a][r];
+          }
+        if constexpr (SWEEP == kResults) {
+          o += __shfl_xor(o, 16);
+          o += __shfl_xor(o, 32);
+          if (lg == 0 && y < dv) M::store((unsigned char*)g.o + ((((int64_t)(t0 + i) * g.N + n) * g.H + h) * dv + y) * M::kBytes, g.scale * o);
         }
       }
-      *(f32x4*)(mA + (16 * J + li) * kMat + 16 * I + 4 * lg) = a;                              // A^T [j][i]
-      if constexpr (SWEEP == kResults) *(f32x4*)(mP + (16 * I + li) * kMat + 16 * J + 4 * lg) = p;  // P [i][j]
-      if constexpr (SWEEP == kBack) *(f32x4*)(mP + (16 * J + li) * kMat + 16 * I + 4 * lg) = p;     // P^T [j][i]
+      float test2 = 0.0f;
+#pragma unroll
+      for (int a = 0; a < ND; ++a)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) test2 = fmaf(S[a][r], 0.0f, test2);
+      odd_state = test2 != 0.0f;
+      continue;
     }
-    __syncthreads();
+    if (!has_v) continue;
 
-    if (wave == 0) invert(mA, steps.beta, by_row, by_column, lane);
     // what the state gives the steps: k S, and q S
     f32x4 ks[2] = {}, qs[2] = {};
-    if (has_v) {
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        if (!has_k(s)) continue;
-        float x[8];
+    for (int s = 0; s < D / 32; ++s) {
+      if (!has_k(s)) continue;
+      float x[8];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[r] = S[2 * s][r];
-          x[4 + r] = S[2 * s + 1][r];
-        }
-        const typename M::Sum st = M::sum_terms(x);
-#pragma unroll
-        for (int J = 0; J < 2; ++J) {
-          const int at = (16 * J + li) * L::kPitch + (32 * s + 8 * lg) * M::kBytes;
-          ks[J] = M::mma(M::row(tk + at), st, ks[J]);                                               // [step][y]
-          if constexpr (SWEEP == kResults) qs[J] = M::mma(leading<DTYPE>(st), M::row(tq + at), qs[J]);  // [y][step]
-        }
+      for (int r = 0; r < 4; ++r) {
+        x[r] = S[2 * s][r];
+        x[4 + r] = S[2 * s + 1][r];
       }
-    }
-    __syncthreads();
-
-    if (has_v) {
-      // columns of the third array: K-slots 0..3 are steps 4 lg .., 4..7 are 16 further on
-      const typename M::Raw vt = columns<DTYPE>(tv, L::kPitchV, 16 * wave, 4, li, lg);
-      float v[8];
-      M::values(vt, v);
-      f32x4 x[2], e4[2], w4[2], b4[2];
+      const typename M::Sum st = M::sum_terms(x);
 #pragma unroll
       for (int J = 0; J < 2; ++J) {
-        const int j = 16 * J + 4 * lg;
-        e4[J] = *(const f32x4*)(steps.enter + j);
-        w4[J] = *(const f32x4*)(steps.leave + j);
-        b4[J] = *(const f32x4*)(steps.beta + j);
+        const int at = (16 * J + li) * L::kPitch + (32 * s + 8 * lg) * M::kBytes;
+        ks[J] = M::mma(M::row(tk + at), st, ks[J]);                                               // [step][y]
+        if constexpr (SWEEP == kResults) qs[J] = M::mma(leading<DTYPE>(st), M::row(tq + at), qs[J]);  // [y][step]
       }
-      const float keep = marks ? 0.0f : steps.enter[valid - 1];
-      if constexpr (SWEEP != kBack) {
+    }
+    // columns of the third array: K-slots 0..3 are steps 4 lg .., 4..7 are 16 further on
+    const typename M::Raw vt = columns<DTYPE>(tv, L::kPitchV, 16 * wave, 4, li, lg);
+    float v[8];
+    M::values(vt, v);
+    f32x4 e4[2], w4[2], b4[2];
 #pragma unroll
-        for (int J = 0; J < 2; ++J) {
-          const i32x4 ep = *(const i32x4*)(steps.ep + 16 * J + 4 * lg);
+    for (int J = 0; J < 2; ++J) {
+      const int j = 16 * J + 4 * lg;
+      e4[J] = *(const f32x4*)(steps.enter + j);
+      w4[J] = *(const f32x4*)(steps.leave + j);
+      b4[J] = *(const f32x4*)(steps.beta + j);
+    }
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float keep = marked ? 0.0f : steps.enter[valid - 1];
+    // (a state that is not finite is here only in a chunk that it all reaches: a factor of zero leaves out a finite number)
+    if constexpr (kUp) {
+      f32x4 x[2], e[2];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[J][r] = v[4 * J + r] - (ep[r] == 0 ? e4[J][r] * ks[J][r] : 0.0f);
-        }
-        f32x4 u[2];
-        {
-          const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-          const Slots t1 = slots_of(by_row, 16 + li, lg);
-          u[0] = mm4(*(const f32x4*)(by_row + li * kMat + 4 * lg), x[0], zero);
-          u[1] = mm4(t1.b, x[1], mm4(t1.a, x[0], zero));
-        }
-        float us[8];
+      for (int J = 0; J < 2; ++J)
 #pragma unroll
-        for (int J = 0; J < 2; ++J)
+        for (int r = 0; r < 4; ++r) x[J][r] = v[4 * J + r] - e4[J][r] * ks[J][r];
+      const Slots t1 = slots_of(mT, 16 + li, lg);
+      e[0] = mm4(*(const f32x4*)(mT + li * kMat + 4 * lg), x[0], zero);
+      e[1] = mm4(t1.b, x[1], mm4(t1.a, x[0], zero));
+      float us[8];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) us[4 * J + r] = b4[J][r] * u[J][r];
-        if constexpr (SWEEP == kResults) {
-          const typename M::Out uo = M::out_terms(us);
+      for (int J = 0; J < 2; ++J)
 #pragma unroll
-          for (int I = 0; I < 2; ++I) {
-            const int i = 16 * I + li;
-            const float c = g.scale * steps.enter[i];
-            const bool reach = steps.ep[i] == 0;
-            f32x4 own;
+        for (int r = 0; r < 4; ++r) us[4 * J + r] = b4[J][r] * e[J][r];
+      if constexpr (SWEEP == kResults) {
+        const typename M::Out uo = M::out_terms(us);
+        const auto to = buffer((unsigned char*)g.o + (((int64_t)t0 * g.N + n) * g.H + h) * dv * M::kBytes, 0x7FFFFFFF);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) own[r] = reach ? c * qs[I][r] : 0.0f;
-            const Slots p = slots_of(mP, i, lg);
-            float ps[8];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              ps[r] = p.a[r];
-              ps[4 + r] = p.b[r];
-            }
-            own = mma_oo<DTYPE>(uo, M::out_terms(ps), own);  // [y][i]
-            if (i >= valid) continue;
-            const int yo = v0 + 4 * lg;
-            unsigned char* const to = (unsigned char*)g.o + ((((int64_t)(c0 + i) * g.N + n) * g.H + h) * dv + yo) * M::kBytes;
-            if (yo + 4 <= dv) {
-              if constexpr (DTYPE == SF_DTYPE_BF16) {
-                const u32x2 two = {pack_bf16(own[0], own[1]), pack_bf16(own[2], own[3])};
-                __builtin_memcpy(to, &two, 8);
-              } else {
-                __builtin_memcpy(to, &own, 16);
-              }
-            } else {
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (yo + r < dv) M::store(to + r * M::kBytes, own[r]);
-            }
-          }
-        }
-#pragma unroll
-        for (int J = 0; J < 2; ++J)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) us[4 * J + r] *= w4[J][r];
-        const typename M::Sum uw = M::sum_terms(us);
-        float test2 = 0.0f;
-#pragma unroll
-        for (int a = 0; a < ND; ++a) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) S[a][r] = marks ? 0.0f : S[a][r] * keep;
-          if (has_k(a / 2)) S[a] = M::mma(columns<DTYPE>(tk, L::kPitch, col_k(a, 0), 8, li, lg), uw, S[a]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) test2 = fmaf(S[a][r], 0.0f, test2);
-        }
-        odd_state = test2 != 0.0f;
-      } else {
-        const int e_last = steps.ep[valid - 1];
-        // f, and of it z = T^T beta f
-        f32x4 f[2], z[2];
-#pragma unroll
-        for (int J = 0; J < 2; ++J) {
-          const i32x4 ep = *(const i32x4*)(steps.ep + 16 * J + 4 * lg);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) f[J][r] = ep[r] == e_last ? w4[J][r] * ks[J][r] : 0.0f;
-          const Slots p = slots_of(mP, 16 * J + li, lg);
+        for (int I = 0; I < 2; ++I) {
+          const int i = 16 * I + li;
+          f32x4 own = (g.scale * steps.enter[i]) * qs[I];
+          const Slots p = slots_of(mP, i, lg);
           float ps[8];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             ps[r] = p.a[r];
             ps[4 + r] = p.b[r];
           }
-          f[J] = M::mma(M::sum_terms(ps), vt, f[J]);
+          own = mma_oo<DTYPE>(uo, M::out_terms(ps), own);  // [y][i]
+          if constexpr (VEC) {
+            const unsigned at = i < valid ? at_o[I] : kOutside;
+            if constexpr (DTYPE == SF_DTYPE_BF16) __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(own[0], own[1]), pack_bf16(own[2], own[3])}, to, at, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, own), to, at, 0, 0);
+          } else {
+            if (i >= valid) continue;
+            const int yo = v0 + 4 * lg;
+            unsigned char* const out = (unsigned char*)g.o + ((((int64_t)(t0 + i) * g.N + n) * g.H + h) * dv + yo) * M::kBytes;
+            if (yo + 4 <= dv) {
+              if constexpr (DTYPE == SF_DTYPE_BF16) {
+                const u32x2 two = {pack_bf16(own[0], own[1]), pack_bf16(own[2], own[3])};
+                __builtin_memcpy(out, &two, 8);
+              } else {
+                __builtin_memcpy(out, &own, 16);
+              }
+            } else {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) f[J][r] *= b4[J][r];
-        }
-        const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-        const Slots t0 = slots_of(by_column, li, lg);
-        z[0] = mm4(t0.b, f[1], mm4(t0.a, f[0], zero));
-        z[1] = mm4(*(const f32x4*)(by_column + (16 + li) * kMat + 16 + 4 * lg), f[1], zero);
-        float zs[8], os[8];
-#pragma unroll
-        for (int J = 0; J < 2; ++J) {
-          const i32x4 ep = *(const i32x4*)(steps.ep + 16 * J + 4 * lg);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            zs[4 * J + r] = ep[r] == 0 ? -e4[J][r] * z[J][r] : 0.0f;
-            os[4 * J + r] = ep[r] == 0 ? g.scale * e4[J][r] * v[4 * J + r] : 0.0f;
+              for (int r = 0; r < 4; ++r)
+                if (yo + r < dv) M::store(out + r * M::kBytes, own[r]);
+            }
           }
         }
-        const typename M::Sum zt = M::sum_terms(zs), ot = M::sum_terms(os);
-        float test2 = 0.0f;
+      }
 #pragma unroll
-        for (int a = 0; a < ND; ++a) {
+      for (int J = 0; J < 2; ++J)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[a][r] = marks ? 0.0f : S[a][r] * keep;
-          if (has_k(a / 2)) {
-            S[a] = M::mma(columns<DTYPE>(tk, L::kPitch, col_k(a, 0), 8, li, lg), zt, S[a]);
-            S[a] = M::mma(columns<DTYPE>(tq, L::kPitch, col_k(a, 0), 8, li, lg), ot, S[a]);
-          }
+        for (int r = 0; r < 4; ++r) us[4 * J + r] *= w4[J][r];
+      const typename M::Sum uw = M::sum_terms(us);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) test2 = fmaf(S[a][r], 0.0f, test2);
+      for (int a = 0; a < ND; ++a) {
+        S[a] *= keep;
+        if (has_k(a / 2)) S[a] = M::mma(columns<DTYPE>(tk, L::kPitch, col_k(a, 0), 8, li, lg), uw, S[a]);
+      }
+    } else {
+      // f, and of it z = T^T beta f
+      f32x4 f[2], z[2];
+#pragma unroll
+      for (int J = 0; J < 2; ++J) {
+        f[J] = w4[J] * ks[J];
+        const Slots p = slots_of(mP, 16 * J + li, lg);
+        float ps[8];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          ps[r] = g.scale * p.a[r];
+          ps[4 + r] = g.scale * p.b[r];
         }
-        odd_state = test2 != 0.0f;
+        f[J] = M::mma(M::sum_terms(ps), vt, f[J]);
+        f[J] *= b4[J];
+      }
+      const Slots c0 = slots_down(mT, li, lg), c1 = slots_down(mT, 16 + li, lg);
+      z[0] = mm4(c0.b, f[1], mm4(c0.a, f[0], zero));
+      z[1] = mm4(c1.b, f[1], zero);
+      float zs[8], os[8];
+#pragma unroll
+      for (int J = 0; J < 2; ++J)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          zs[4 * J + r] = -e4[J][r] * z[J][r];
+          os[4 * J + r] = g.scale * e4[J][r] * v[4 * J + r];
+        }
+      const typename M::Sum zt = M::sum_terms(zs), ot = M::sum_terms(os);
+#pragma unroll
+      for (int a = 0; a < ND; ++a) {
+        S[a] *= keep;
+        if (has_k(a / 2)) {
+          S[a] = M::mma(columns<DTYPE>(tk, L::kPitch, col_k(a, 0), 8, li, lg), zt, S[a]);
+          S[a] = M::mma(columns<DTYPE>(tq, L::kPitch, col_k(a, 0), 8, li, lg), ot, S[a]);
+        }
       }
     }
-    if (!more) break;
+    float test2 = 0.0f;
+#pragma unroll
+    for (int a = 0; a < ND; ++a)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) test2 = fmaf(S[a][r], 0.0f, test2);
+    odd_state = test2 != 0.0f;
   }
-  if (g.s_out && has_v) store_state(g.s_out + (size_t)bh * dk * dv);
+  if (!has_v) return;
+  if (g.piece) {
+    const size_t at = (size_t)bh * g.n_seg + seg;
+    if (identity) store_state(g.seg_through + at * dk * dk);
+    else store_state(g.seg_state + at * dk * dv);
+    if (!identity && v_block == 0 && tid == 0) g.seg_begin[at] = any_begin ? 1 : 0;
+  } else if (g.s_out && seg == (kUp ? g.n_seg - 1 : 0)) {
+    store_state(g.s_out + (size_t)bh * dk * dv);
+  }
+}
+
+// What enters each piece of T, from the pieces' own states and what they make of one that enters:  S <- M S + own, backwards R <- M^T R + own;
+// where an episode begins in the piece, own alone.  A workgroup has 16 columns of one (row, head), a wave 16 rows of the state; the state goes
+// round through LDS.
+template <bool BACK>
+__global__ __launch_bounds__(512) void delta_join_kernel(DeltaArgs g) {
+  constexpr int kPitch = 132;
+  __shared__ __attribute__((aligned(16))) float state[2][16 * kPitch];  // [y][row]
+  const int dk = g.k.d, dv = g.v.d, bh = blockIdx.y, y0 = blockIdx.x * 16;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, lg = lane >> 4;
+  const int x0 = 16 * wave, y = y0 + li;
+  f32x4 in = {0.0f, 0.0f, 0.0f, 0.0f};  // rows x0 + 4 lg + r
+  if (g.s_in)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (x0 + 4 * lg + r < dk && y < dv) in[r] = g.s_in[(size_t)bh * dk * dv + (x0 + 4 * lg + r) * dv + y];
+  f32x4 m[8], own;
+  bool begin;
+  auto request = [&](int seg) {
+    const size_t at = (size_t)bh * g.n_seg + seg;
+    const float* const M = g.seg_through + at * dk * dk;
+    const float* const o = g.seg_state + at * dk * dv;
+    begin = g.seg_begin[at] != 0;
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int a = x0 + li, b = 16 * s + 4 * lg + r;
+        m[s][r] = a < dk && b < dk ? (BACK ? M[b * dk + a] : M[a * dk + b]) : 0.0f;
+      }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) own[r] = x0 + 4 * lg + r < dk && y < dv ? o[(x0 + 4 * lg + r) * dv + y] : 0.0f;
+  };
+  request(BACK ? g.n_seg - 1 : 0);
+  for (int i = 0; i < g.n_seg; ++i) {
+    const int seg = BACK ? g.n_seg - 1 - i : i;
+    float* const to = g.seg_state + ((size_t)bh * g.n_seg + seg) * dk * dv;
+    // (its own state has been read, by this thread)
+    f32x4 next = own;
+    f32x4 M[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) M[s] = m[s];
+    const bool stop = begin;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (x0 + 4 * lg + r < dk && y < dv) to[(x0 + 4 * lg + r) * dv + y] = in[r];
+    *(f32x4*)(state[i & 1] + li * kPitch + x0 + 4 * lg) = in;
+    if (i + 1 < g.n_seg) request(BACK ? seg - 1 : seg + 1);
+    __syncthreads();
+    if (!stop)
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        if (16 * s < dk) next = mm4(M[s], *(const f32x4*)(state[i & 1] + li * kPitch + 16 * s + 4 * lg), next);
+    in = next;
+  }
 }
 
 template <int DTYPE, int D>
 struct GradLds {
   static constexpr int kPitch = Pitch<DTYPE, D>::value, kTile = C * kPitch, kPitchF = (D + 4) * 4, kTileF = C * kPitchF;
   static constexpr int kWaves = D / 16, kThreads = 64 * kWaves;
-  // q, k, v, do; u and z in fp32; A^T, P^T, T by rows and by columns, of which the last two make room for dP D and its like as operands
-  static constexpr int kU = 4 * kTile, kZ = kU + kTileF, kA = kZ + kTileF, kP = kA + C * kMat * 4, kRow = kP + C * kMat * 4, kColumn = kRow + C * kMat * 4,
-                       kOperand = 4096, kM = kRow;  // [3] of two terms (or halves) of 2 x 64 lanes x 16 bytes
-  static_assert(kOperand * 3 <= 2 * C * kMat * 4 + 4096, "operands");
-  static constexpr int kSteps = kRow + 3 * kOperand;
-  static constexpr int kSums = kSteps + (int)sizeof(Steps);  // float [kWaves + 4][C] of each kind
+  // q, k, v, do; u and z in fp32; A^T, P^T, and T, which makes room for dP D and its like as operands
+  static constexpr int kU = 4 * kTile, kZ = kU + kTileF, kA = kZ + kTileF, kP = kA + C * kMat * 4, kT = kP + C * kMat * 4,
+                       kOperand = 4096, kM = kT;  // [3] of two terms (or halves) of 2 x 64 lanes x 16 bytes
+  static constexpr int kSteps = kT + 3 * kOperand, kFlag = kSteps + (int)sizeof(Steps);
+  static constexpr int kSums = kFlag + 16;  // float [kWaves + 4][C] of each kind
   static constexpr int kSumRows = 2 * kWaves + 5;
   static constexpr int kBytes = kSums + kSumRows * C * 4;
 };
@@ -599,8 +818,10 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
   typedef GradLds<DTYPE, D> L;
   constexpr int W = M::kPieceWords, ND = D / 16, kRow8 = D / 8, kT = L::kThreads;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const unsigned which = blockIdx.x;
-  const int bh = (int)g.per.of(which), chunk = (int)which - bh * g.chunks;
+  // (workgroups go round the XCDs: 16 neighbours, whose rows of a step are neighbours too, for each)
+  const unsigned which = (blockIdx.x & ~127u) + (blockIdx.x & 7) * 16 + ((blockIdx.x >> 3) & 15);
+  const int chunk = (int)g.rows.of(which), bh = (int)(which - (unsigned)chunk * (g.N * g.H));
+  if (chunk >= g.chunks) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h);
@@ -608,7 +829,7 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
   auto base = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
   unsigned char *const tq = lds, *const tk = lds + L::kTile, *const tv = lds + 2 * L::kTile, *const to = lds + 3 * L::kTile;
   float *const mU = (float*)(lds + L::kU), *const mZ = (float*)(lds + L::kZ), *const mA = (float*)(lds + L::kA), *const mP = (float*)(lds + L::kP),
-               *const by_row = (float*)(lds + L::kRow), *const by_column = (float*)(lds + L::kColumn);
+               *const mT = (float*)(lds + L::kT);
   constexpr int kF = D + 4;
   Steps& steps = *(Steps*)(lds + L::kSteps);
   // by waves: sums over their columns for each step; by tiles: of dP P + dA A along its rows and columns; a number of each wave
@@ -625,8 +846,12 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
   fetch<DTYPE>(w[1], g.k, base(g.k), t0, valid, tid, kRow8, 0);
   fetch<DTYPE>(w[2], g.v, base(g.v), t0, valid, tid, kRow8, 0);
   fetch<DTYPE>(w[3], g.d_o, base(g.d_o), t0, valid, tid, kRow8, 0);
-  const StepIn in = read_step(g, n, h, t0, valid, lane);
-  const unsigned marks = (unsigned)__ballot(begins(in));
+  const float* const from_steps = g.made + ((size_t)bh * g.chunks + chunk) * made_words(true);
+  f32x4 n_m[(3 * kDense / 4 + kT - 1) / kT], n_steps;
+#pragma unroll
+  for (int i = 0; i < 3 * kDense / 4; i += kT)
+    if (i + tid < 3 * kDense / 4) n_m[i / kT] = *(const f32x4*)(from_steps + 4 * (i + tid));
+  if (tid < kStepWords / 4) n_steps = *(const f32x4*)(from_steps + 3 * kDense + 4 * tid);
 
   // the states by columns of v
   const int y0 = 16 * wave, y = y0 + li;
@@ -643,21 +868,29 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
       R[a][r] = r1 && there ? r1[x * dv + y] : 0.0f;
       test = fmaf(S[a][r], 0.0f, fmaf(R[a][r], 0.0f, test));
     }
-  if (tid < 4) steps.flag[tid] = 0;
+  int* const flag = (int*)(lds + L::kFlag);
+  if (tid == 0) *flag = 0;
   __syncthreads();
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
     put_piece<DTYPE>(lds + a * L::kTile, L::kPitch, w[a], tid, kRow8);
     test = finite_test<DTYPE>(w[a], test);
   }
-  if (wave == 0) {
-    put_steps(steps, in, marks, valid, lane);
-    test += finite_step(in);
+#pragma unroll
+  for (int i = 0; i < 3 * kDense / 4; i += kT) {
+    const int e = i + tid, m = e / (kDense / 4), in = e % (kDense / 4);
+    if (e < 3 * kDense / 4) *(f32x4*)((m == 0 ? mT : m == 1 ? mP : mA) + in / 8 * kMat + in % 8 * 4) = n_m[i / kT];
   }
-  if (test != 0.0f) steps.flag[0] = 1;
+  if (tid < kStepWords / 4) *(f32x4*)((float*)&steps + 4 * tid) = n_steps;
+  if (test != 0.0f) *flag = 1;
   __syncthreads();
-  const int e_last = steps.ep[valid - 1];
-  const float keep = marks ? 0.0f : steps.enter[valid - 1];
+  const int my_ep = steps.ep[lane & (C - 1)];
+  const float my_steps = fmaf(steps.gh[lane & (C - 1)], 0.0f, steps.beta[lane & (C - 1)] * 0.0f);
+  const int e_last = __builtin_amdgcn_readlane(my_ep, valid - 1);
+  const bool marked = e_last != 0;
+  // steps that an episode begins with: another one's episode than the step before
+  const unsigned begin = (unsigned)__ballot(lane < valid && my_ep != (lane ? __shfl_up(my_ep, 1) : 0));
+  const float keep = marked ? 0.0f : steps.enter[valid - 1];
 
   const int64_t head_k = ((int64_t)n * g.H + h) * dk, head_v = ((int64_t)n * g.H + h) * dv, step_k = (int64_t)g.N * g.H * dk,
                 step_v = (int64_t)g.N * g.H * dv;
@@ -666,11 +899,11 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
     float s = 0.0f;
     for (int l = C - 1; l >= 0; --l)
       if (l >= i && steps.ep[l] == steps.ep[i]) s += dG[l];
-    return marks >> i & 1 ? 0.0f : s;
+    return begin >> i & 1 ? 0.0f : s;
   };
   const int64_t step_at = ((int64_t)t0 * g.N + n) * g.H + h;
 
-  if (steps.flag[0] != 0) {
+  if (*flag != 0 || __any(my_steps != 0.0f)) {
     // Number by number, so that nothing that is not finite meets a masked zero.
     auto at = [&](const unsigned char* tile, int r, int c) { return M::element(tile + r * L::kPitch + c * M::kBytes); };
     auto put = [&](void* out, bool f32, int64_t i, float v) {
@@ -678,7 +911,7 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
       else M::store((unsigned char*)out + i * M::kBytes, v);
     };
     auto decay = [&](int i, int j) { return decay_of(steps.gh[i], steps.gl[i], steps.gh[j], steps.gl[j]); };
-    float *const dP = by_row, *const dA = by_row + C * C;  // [i][j], with D; (both fit where T would be)
+    float *const dP = (float*)(lds + L::kM), *const dA = dP + C * C;  // [i][j]
     for (int e = tid; e < C * C; e += kT) {
       const int i = e / C, j = e % C;
       float a = 0.0f, p = 0.0f;
@@ -752,7 +985,7 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
         sum_g[j] += -sk - (steps.ep[j] == e_last ? sw : 0.0f);
       }
     }
-    if (s0 && r1 && !marks) {
+    if (s0 && r1 && !marked) {
       float rs = 0.0f;
       for (int e = tid; e < dk * dv; e += kT) rs += r1[e] * s0[e];
       tail += keep * sum_all(rs);
@@ -820,7 +1053,7 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
     if (g.dstate0)
       for (int e = tid; e < dk * dv; e += kT) {
         const int x = e / dv, c = e % dv;
-        float s = r1 && !marks ? keep * r1[e] : 0.0f;
+        float s = r1 && !marked ? keep * r1[e] : 0.0f;
         for (int i = 0; i < valid; ++i)
           if (steps.ep[i] == 0) s += steps.enter[i] * (g.scale * at(tq, i, x) * at(to, i, c) - at(tk, i, x) * steps.beta[i] * mZ[i * kF + c]);
         g.dstate0[(size_t)bh * state + e] = s;
@@ -828,7 +1061,7 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
     return;
   }
 
-  // the chunk's matrices, [i][j] with i in tile I, j in tile J: the first four waves A, the last four P
+  // tiles of the chunk's matrices, [i][j] with i in tile I, j in tile J: the first four waves those of A, the last four those of P
   const int I = wave >> 1 & 1, J = wave & 1;
   float decays[4];  // of steps i = 16 I + 4 lg + r and j = 16 J + li
   {
@@ -838,26 +1071,6 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) decays[r] = 16 * I + 4 * lg + r >= j && e4[r] == ej ? decay_of(h4[r], l4[r], steps.gh[j], steps.gl[j]) : 0.0f;
   }
-  auto product = [&](const unsigned char* rows, float* to_matrix, bool strict, float scale) {
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (J <= I) {
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        const int at = (32 * s + 8 * lg) * M::kBytes;
-        if (32 * s < dk) acc = M::mma(M::row(rows + (16 * I + li) * L::kPitch + at), M::row(tk + (16 * J + li) * L::kPitch + at), acc);
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = 16 * I + 4 * lg + r, j = 16 * J + li;
-        acc[r] = decays[r] != 0.0f && (!strict || i > j) ? acc[r] * (scale * decays[r]) : 0.0f;
-      }
-    }
-    *(f32x4*)(to_matrix + (16 * J + li) * kMat + 16 * I + 4 * lg) = acc;  // [j][i]
-  };
-  if (wave < 4) product(tk, mA, true, 1.0f);
-  if (L::kWaves == 4 || wave >= 4) product(tq, mP, false, 1.0f);
-  __syncthreads();
-  if (wave == 0) invert(mA, steps.beta, by_row, by_column, lane);
   // what the states give the steps
   f32x4 ks[2] = {}, qs[2] = {}, kr[2] = {};
 #pragma unroll
@@ -881,7 +1094,6 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
       qs[t] = M::mma(M::row(tq + at), st, qs[t]);
     }
   }
-  __syncthreads();
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
   f32x4 z[2];
   {
@@ -903,8 +1115,8 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[t][r] = v[4 * t + r] - ks[t][r];
     }
-    const Slots t1 = slots_of(by_row, 16 + li, lg);
-    e[0] = mm4(*(const f32x4*)(by_row + li * kMat + 4 * lg), x[0], zero);
+    const Slots t1 = slots_of(mT, 16 + li, lg);
+    e[0] = mm4(*(const f32x4*)(mT + li * kMat + 4 * lg), x[0], zero);
     e[1] = mm4(t1.b, x[1], mm4(t1.a, x[0], zero));
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -918,9 +1130,9 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
       f[t] = M::mma(M::sum_terms(ps), ot, kr[t]);
       bf[t] = b4[t] * f[t];
     }
-    const Slots c0 = slots_of(by_column, li, lg);
+    const Slots c0 = slots_down(mT, li, lg), c1 = slots_down(mT, 16 + li, lg);
     z[0] = mm4(c0.b, bf[1], mm4(c0.a, bf[0], zero));
-    z[1] = mm4(*(const f32x4*)(by_column + (16 + li) * kMat + 16 + 4 * lg), bf[1], zero);
+    z[1] = mm4(c1.b, bf[1], zero);
     const Slots a0 = slots_of(mA, li, lg);
     gu[0] = f[0] - mm4(a0.b, z[1], mm4(a0.a, z[0], zero));
     gu[1] = f[1] - mm4(*(const f32x4*)(mA + (16 + li) * kMat + 16 + 4 * lg), z[1], zero);
@@ -1295,7 +1507,7 @@ int check(const sf_deltarule_config* c, const char* fn) {
     set_error("%s: T = %d, N = %d, H = %d, Hk = %d, dk = %d, dv = %d out of range", fn, c->T, c->N, c->H, c->Hk, c->dk, c->dv);
     return SF_ERR_SHAPE;
   }
-  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > 1 << 21 || (int64_t)c->N * c->H * ((c->T + (int64_t)C - 1) / C) > INT32_MAX) {
+  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > 1 << 21 || (int64_t)c->N * c->H * ((c->T + (int64_t)C - 1) / C) > INT32_MAX - 128) {
     set_error("%s: T * N or N * H * T / 32 beyond 2^31 - 1, or N * H beyond 2^21", fn);
     return SF_ERR_SHAPE;
   }
@@ -1323,24 +1535,49 @@ bool overlap(const sf_deltarule_config* c, const float* a, const float* b) {
 
 int chunks_of(const sf_deltarule_config* c) { return (c->T + C - 1) / C; }
 
+// Pieces of T where the workgroups that go over the chunks (one for each 64 columns of a head) leave CUs idle.
+struct Split {
+  int n_seg, seg_len;
+};
+Split split_of(const sf_deltarule_config* c) {
+  const int64_t lanes = (int64_t)c->N * c->H * (c->dv > DV ? 2 : 1);
+  const int chunks = chunks_of(c);
+  if (lanes == 0 || lanes > 128 || chunks < 16) return Split{1, std::max(1, chunks) * C};
+  const int want = (int)std::min<int64_t>((512 + lanes - 1) / lanes, 32);
+  const int per = std::max(8, (chunks + want - 1) / want);
+  return Split{(chunks + per - 1) / per, per * C};
+}
+
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 struct Workspace {
-  size_t states, dq, dk, total;  // bytes of each part: the states that enter the chunks and as many R's, the shared heads' gradients
+  size_t made, seg_state, seg_through, seg_begin;  // bytes of each part, in this order
+  size_t states, dq, dk, total;                    // the states that enter the chunks and as many R's; the shared heads' gradients
 };
 Workspace workspace_of(const sf_deltarule_config* c, int backward) {
-  Workspace w = {0, 0, 0, 0};
-  if (!backward) return w;
-  if (c->T > C) w.states = align256((size_t)c->N * c->H * chunks_of(c) * c->dk * c->dv * 4);
-  if (c->H != c->Hk) w.dq = w.dk = align256((size_t)c->T * c->N * c->H * c->dk * 4);
-  w.total = 2 * w.states + w.dq + w.dk;
+  Workspace w = {};
+  const size_t lanes = (size_t)c->N * c->H, chunks = chunks_of(c), state = (size_t)c->dk * c->dv * 4;
+  const Split s = split_of(c);
+  if (backward || c->T > C) w.made = align256(lanes * chunks * made_words(backward) * 4);
+  if (s.n_seg > 1) {
+    w.seg_state = align256(lanes * s.n_seg * state);
+    w.seg_through = align256(lanes * s.n_seg * c->dk * c->dk * 4);
+    w.seg_begin = align256(lanes * s.n_seg * 4);
+  }
+  if (backward) {
+    if (c->T > C) w.states = align256(lanes * chunks * state);
+    if (c->H != c->Hk) w.dq = w.dk = align256((size_t)c->T * c->N * c->H * c->dk * 4);
+  }
+  w.total = w.made + w.seg_state + w.seg_through + w.seg_begin + 2 * w.states + w.dq + w.dk;
   return w;
 }
 
+// (a chunk's rows lie within 2^31 bytes then, and one behind the other)
+bool near(int64_t st, int d) { return st >= d && st <= 1 << 23; }
 Strided strided(const sf_deltarule_config* c, const void* p, const int64_t* s, bool shared, int d) {
   Strided a = {p, c->T == 1 ? 0 : s[0], s[1], s[2], shared, d, 0};  // (one step: any stride)
   const int per = 16 / (c->dtype == SF_DTYPE_BF16 ? 2 : 4);
   // (pieces are eight columns in both types)
-  a.vec = d % 8 == 0 && a.st % per == 0 && s[1] % per == 0 && s[2] % per == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+  a.vec = d % 8 == 0 && (c->T == 1 || near(s[0], d)) && a.st % per == 0 && s[1] % per == 0 && s[2] % per == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
   return a;
 }
 
@@ -1358,25 +1595,72 @@ DeltaArgs args_of(const sf_deltarule_config* c, const void* q, const void* k, co
   g.N = c->N;
   g.H = c->H;
   g.chunks = std::max(1, chunks_of(c));
-  g.blocks_v = c->dv > DV ? 2 : 1;
+  g.blocks_v = g.blocks = c->dv > DV ? 2 : 1;
+  g.n_seg = 1;
+  g.seg_len = g.chunks * C;
   g.scale = c->scale;
   g.heads = divisor(c->H);
   g.share = divisor(share);
-  g.per = divisor(g.chunks);
+  g.rows = divisor((unsigned)std::max(1, c->N * c->H));
   return g;
 }
 
-template <int DTYPE, int SWEEP>
-void launch_sweep(const DeltaArgs& g, hipStream_t st) {
-  const unsigned grid = (unsigned)((g.N * g.H + 7) / 8 * 8 * g.blocks_v);
-  static_assert(SweepLds<DTYPE, 128>::kBytes <= 64 * 1024, "no attribute needed");
-  if (g.k.d > 64) delta_sweep_kernel<DTYPE, 128, SWEEP><<<grid, kThreads, SweepLds<DTYPE, 128>::kBytes, st>>>(g);
-  else delta_sweep_kernel<DTYPE, 64, SWEEP><<<grid, kThreads, SweepLds<DTYPE, 64>::kBytes, st>>>(g);
+// The parts of the workspace.
+void with_pieces(const sf_deltarule_config* c, DeltaArgs& g, const Workspace& w, unsigned char* ws) {
+  const Split s = split_of(c);
+  g.made = (float*)ws;
+  g.n_seg = s.n_seg;
+  g.seg_len = s.seg_len;
+  g.seg_state = (float*)(ws + w.made);
+  g.seg_through = (float*)(ws + w.made + w.seg_state);
+  g.seg_begin = (int*)(ws + w.made + w.seg_state + w.seg_through);
 }
-template <int SWEEP>
-hipError_t sweep(const sf_deltarule_config* c, const DeltaArgs& g, hipStream_t st) {
-  if (c->dtype == SF_DTYPE_BF16) launch_sweep<SF_DTYPE_BF16, SWEEP>(g, st);
-  else launch_sweep<SF_DTYPE_FP32, SWEEP>(g, st);
+
+template <int DTYPE, int D, bool BACK>
+void launch_chunks(const DeltaArgs& g, hipStream_t st) {
+  constexpr int bytes = 4 * (3 * C * kMat * 4 + (int)sizeof(Steps));
+  static_assert(bytes <= 64 * 1024, "no attribute needed");
+  delta_chunks_kernel<DTYPE, D, BACK><<<(unsigned)(((int64_t)g.N * g.H * g.chunks + 3) / 4), kThreads, bytes, st>>>(g);
+}
+template <int DTYPE>
+void launch_chunks(const DeltaArgs& g, hipStream_t st) {
+  if (g.k.d > 64) g.back ? launch_chunks<DTYPE, 128, true>(g, st) : launch_chunks<DTYPE, 128, false>(g, st);
+  else g.back ? launch_chunks<DTYPE, 64, true>(g, st) : launch_chunks<DTYPE, 64, false>(g, st);
+}
+hipError_t make_chunks(const sf_deltarule_config* c, const DeltaArgs& g, hipStream_t st) {
+  if (c->dtype == SF_DTYPE_BF16) launch_chunks<SF_DTYPE_BF16>(g, st);
+  else launch_chunks<SF_DTYPE_FP32>(g, st);
+  return hipGetLastError();
+}
+
+template <int DTYPE, int D, int SWEEP, bool ALONE>
+void launch_sweep(const DeltaArgs& g, bool vec, hipStream_t st) {
+  typedef SweepLds<DTYPE, D> L;
+  constexpr int bytes = ALONE ? L::kBytesAlone : L::kBytes;
+  static_assert(bytes <= 64 * 1024, "no attribute needed");
+  const dim3 grid((unsigned)((g.N * g.H + 7) / 8 * 8 * g.blocks), (unsigned)g.n_seg);
+  if (vec) delta_sweep_kernel<DTYPE, D, SWEEP, ALONE, true><<<grid, kThreads, bytes, st>>>(g);
+  else delta_sweep_kernel<DTYPE, D, SWEEP, ALONE, false><<<grid, kThreads, bytes, st>>>(g);
+}
+template <int SWEEP, bool ALONE = false>
+hipError_t sweep(const sf_deltarule_config* c, DeltaArgs g, hipStream_t st) {
+  if (g.piece && SWEEP == kStates) g.blocks = g.blocks_v + (c->dk > DV ? 2 : 1);
+  g.round = divisor(8 * g.blocks);
+  const Strided& third = SWEEP == kBack ? g.d_o : g.v;
+  const bool vec = g.k.vec && third.vec && (SWEEP == kStates || g.q.vec) &&
+                   (SWEEP != kResults || ((reinterpret_cast<uintptr_t>(g.o) & 15) == 0 && (int64_t)c->N * c->H * c->dv * 4 * C < (int64_t)1 << 31));
+  if (c->dtype == SF_DTYPE_BF16) {
+    if (c->dk > 64) launch_sweep<SF_DTYPE_BF16, 128, SWEEP, ALONE>(g, vec, st);
+    else launch_sweep<SF_DTYPE_BF16, 64, SWEEP, ALONE>(g, vec, st);
+  } else {
+    if (c->dk > 64) launch_sweep<SF_DTYPE_FP32, 128, SWEEP, ALONE>(g, vec, st);
+    else launch_sweep<SF_DTYPE_FP32, 64, SWEEP, ALONE>(g, vec, st);
+  }
+  return hipGetLastError();
+}
+template <bool BACK>
+hipError_t join(const sf_deltarule_config* c, const DeltaArgs& g, hipStream_t st) {
+  delta_join_kernel<BACK><<<dim3((unsigned)((c->dv + 15) / 16), (unsigned)(c->N * c->H)), 512, 0, st>>>(g);
   return hipGetLastError();
 }
 
@@ -1389,7 +1673,7 @@ hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  kern<<<(unsigned)(g.N * g.H * g.chunks), 4 * D, bytes, st>>>(g);
+  kern<<<(unsigned)(((int64_t)g.N * g.H * g.chunks + 127) / 128 * 128), 4 * D, bytes, st>>>(g);
   return hipGetLastError();
 }
 hipError_t grad(const sf_deltarule_config* c, const DeltaArgs& g, hipStream_t st) {
@@ -1435,10 +1719,21 @@ extern "C" int sf_deltarule(const sf_deltarule_config* cfg, const void* q, const
   }
   if (cfg->N == 0) return SF_OK;
   DeltaArgs g = args_of(cfg, q, k, v, log_decay, beta, done);
+  const hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   g.o = o;
   g.s_in = state0;
   g.s_out = state;
-  return launched(fn, sweep<kResults>(cfg, g, reinterpret_cast<hipStream_t>(hip_stream)));
+  if (cfg->T <= C) return launched(fn, sweep<kResults, true>(cfg, g, st));
+  with_pieces(cfg, g, w, (unsigned char*)workspace);
+  hipError_t err = make_chunks(cfg, g, st);
+  if (err == hipSuccess && g.n_seg > 1) {
+    g.piece = 1;
+    err = sweep<kStates>(cfg, g, st);
+    g.piece = 0;
+    if (err == hipSuccess) err = join<false>(cfg, g, st);
+  }
+  if (err == hipSuccess) err = sweep<kResults>(cfg, g, st);
+  return launched(fn, err);
 }
 
 extern "C" int sf_deltarule_backward(const sf_deltarule_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
@@ -1469,18 +1764,34 @@ extern "C" int sf_deltarule_backward(const sf_deltarule_config* cfg, const void*
   const int share = cfg->H / cfg->Hk;
   DeltaArgs g = args_of(cfg, q, k, v, log_decay, beta, done);
   g.d_o = strided(cfg, d_o, cfg->do_stride, false, cfg->dv);
-  hipError_t err = hipSuccess;
+  with_pieces(cfg, g, w, ws);
+  g.back = 1;
+  const size_t at = w.made + w.seg_state + w.seg_through + w.seg_begin;
+  hipError_t err = none ? hipSuccess : make_chunks(cfg, g, st);
   if (cfg->T == 0 || cfg->T > C) {
     if (cfg->T > 0) {
       g.s_in = state0;
-      g.kept = (float*)ws;
-      err = sweep<kStates>(cfg, g, st);
+      if (err == hipSuccess && g.n_seg > 1) {
+        g.piece = 1;
+        err = sweep<kStates>(cfg, g, st);
+        g.piece = 0;
+        if (err == hipSuccess) err = join<false>(cfg, g, st);
+      }
+      g.kept = (float*)(ws + at);
+      if (err == hipSuccess) err = sweep<kStates>(cfg, g, st);
+      g.kept = nullptr;
     }
     g.s_in = dstate;
+    if (err == hipSuccess && g.n_seg > 1) {
+      g.piece = 1;
+      err = sweep<kBack>(cfg, g, st);
+      g.piece = 0;
+      if (err == hipSuccess) err = join<true>(cfg, g, st);
+    }
     g.s_out = dstate0;
-    g.kept = (float*)(ws + w.states);
+    if (cfg->T > 0) g.kept = (float*)(ws + at + w.states);
     if (err == hipSuccess) err = sweep<kBack>(cfg, g, st);
-    g.kept_s = (const float*)ws;
+    g.kept_s = (const float*)(ws + at);
     g.kept_r = g.kept;
   } else {
     g.kept_s = state0;
@@ -1488,8 +1799,8 @@ extern "C" int sf_deltarule_backward(const sf_deltarule_config* cfg, const void*
     g.dstate0 = dstate0;
   }
   if (none || err != hipSuccess) return launched(fn, err);
-  float* const part_q = (float*)(ws + 2 * w.states);
-  float* const part_k = (float*)(ws + 2 * w.states + w.dq);
+  float* const part_q = (float*)(ws + at + 2 * w.states);
+  float* const part_k = (float*)(ws + at + 2 * w.states + w.dq);
   g.dq = share > 1 ? part_q : dq;
   g.dk = share > 1 ? part_k : dk;
   g.dv = dv;

@@ -116,7 +116,7 @@ def test_strided_and_unaligned_arrays(torch_cuda, T, dtype):
     b = both(torch, y, do.transpose(0, 2).contiguous().transpose(0, 2), ds, dtype)
     for one, other in zip(a, b):
         for n in one:
-            assert torch.equal(one[n], other[n]), n
+            assert n == "workspace" or torch.equal(one[n], other[n]), n
 
 
 def test_results_at_odd_addresses_and_nothing_behind_them(torch_cuda):
