@@ -71,6 +71,19 @@ struct DeltaArgs {
 
 typedef Num<SF_DTYPE_FP32> F32;
 
+// Memory is read and written through buffers that begin at a uniform address: what differs from lane to lane is an offset, what is not
+// there has an offset past the end (it is read as zero, not written).  A branch around a load would wait for the loads before it.
+constexpr unsigned kOutside = 0x80000000u, kWholeBuffer = 0x7FFFFFFFu;
+__device__ inline __amdgpu_buffer_rsrc_t buffer(const void* p, unsigned bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000); }
+template <int WORDS>
+__device__ inline void load_words(unsigned* w, __amdgpu_buffer_rsrc_t from, unsigned at) {
+#pragma unroll
+  for (int i = 0; i < WORDS; i += 4) *(u32x4*)(w + i) = __builtin_amdgcn_raw_buffer_load_b128(from, at + 4 * i, 0, 0);
+}
+__device__ inline float load_float(__amdgpu_buffer_rsrc_t from, unsigned at, int more) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, at, more, 0));
+}
+
 // Four K-slots of two fp32 operands.
 __device__ inline f32x4 mm4(const f32x4 a, const f32x4 b, f32x4 c) {
 #pragma unroll
@@ -91,7 +104,7 @@ __device__ inline typename Num<DTYPE>::Out leading(const typename Num<DTYPE>::Su
 
 // Sum over the 16 lanes of a row (each lane gets it).
 __device__ inline float row_sum(float x) {
-#define SF_ROR(n) x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + (n), 0xF, 0xF, false))
+#define SF_ROR(n) x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + (n), 0xF, 0xF, true))
   SF_ROR(8);
   SF_ROR(4);
   SF_ROR(2);
@@ -124,12 +137,21 @@ struct StepIn {
 };
 // Lane i < 32 reads step t0 + i.
 __device__ inline StepIn read_step(const DeltaArgs& g, int n, int h, int t0, int valid, int lane) {
-  StepIn s = {0.0f, 0.0f, false};
-  if (lane < valid) {
-    const int64_t row = (int64_t)(t0 + lane) * g.N + n, at = row * g.H + h;
-    s.ld = g.log_decay[at];
-    s.beta = g.beta[at];
-    s.done = g.done && g.done[row] != 0;
+  const int64_t row = (int64_t)t0 * g.N + n;
+  const int64_t last = (int64_t)(valid - 1) * g.N;  // (rows may lie far apart)
+  StepIn s;
+  if (last * g.H < (int64_t)1 << 28) {
+    const unsigned at = (unsigned)(lane * g.N);
+    const auto ld = buffer(g.log_decay + row * g.H + h, kWholeBuffer), be = buffer(g.beta + row * g.H + h, kWholeBuffer);
+    const auto dn = buffer(g.done + (g.done ? row : 0), g.done ? kWholeBuffer : 0);
+    s.ld = load_float(ld, lane < valid ? at * g.H * 4 : kOutside, 0);
+    s.beta = load_float(be, lane < valid ? at * g.H * 4 : kOutside, 0);
+    s.done = __builtin_amdgcn_raw_buffer_load_b8(dn, lane < valid ? at : kOutside, 0, 0) != 0;
+  } else {
+    const int64_t r = row + (int64_t)(lane < valid ? lane : 0) * g.N, at = r * g.H + h;
+    s.ld = lane < valid ? g.log_decay[at] : 0.0f;
+    s.beta = lane < valid ? g.beta[at] : 0.0f;
+    s.done = lane < valid && g.done && g.done[r] != 0;
   }
   return s;
 }
@@ -139,7 +161,7 @@ __device__ inline bool begins(const StepIn& s) { return s.done || s.ld * 1.44269
 template <int N>
 __device__ inline double row_shift(double x) {
   const uint64_t b = __builtin_bit_cast(uint64_t, x);
-  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, 0x110 + N, 0xF, 0xF, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), 0x110 + N, 0xF, 0xF, false);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, 0x110 + N, 0xF, 0xF, true), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), 0x110 + N, 0xF, 0xF, true);
   return __builtin_bit_cast(double, (uint64_t)(unsigned)hi << 32 | (unsigned)lo);
 }
 
@@ -220,7 +242,7 @@ __device__ inline void invert(const float* at, const float* beta, float* T, int 
     constexpr int l = decltype(at_l)::value;
 #pragma unroll
     for (int i = l + 1; i < 16; ++i)
-      t[i] = fmaf(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, a[i]), 0x150 + l, 0xF, 0xF, false)), t[l], t[i]);
+      t[i] = fmaf(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, a[i]), 0x150 + l, 0xF, 0xF, true)), t[l], t[i]);
   };
 #define SF_STEP(l) step(std::integral_constant<int, l>())
   SF_STEP(0); SF_STEP(1); SF_STEP(2); SF_STEP(3); SF_STEP(4); SF_STEP(5); SF_STEP(6); SF_STEP(7);
@@ -246,23 +268,32 @@ __device__ inline void invert(const float* at, const float* beta, float* T, int 
 }
 
 // One wave: a chunk's Steps, A^T, P (backwards P^T, without the scale) and T into LDS (pitch kMat).  Keys and queries are read as operands.
-template <int DTYPE, int D, bool BACK>
+template <int DTYPE, int D, bool BACK, bool VEC>
 __device__ inline void make_chunk(const DeltaArgs& g, int n, int h, int hk, int t0, int valid, int lane, Steps& steps, float* mA, float* mP, float* mT) {
   typedef Num<DTYPE> M;
   const int li = lane & 15, lg = lane >> 4, dk = g.k.d;
   auto base = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
   const unsigned char *const qb = base(g.q), *const kb = base(g.k);
   typename M::Raw q[2][D / 32], k[2][D / 32];
+  const auto from_q = buffer(qb + (int64_t)t0 * g.q.st * M::kBytes, kWholeBuffer), from_k = buffer(kb + (int64_t)t0 * g.k.st * M::kBytes, kWholeBuffer);
 #pragma unroll
   for (int I = 0; I < 2; ++I) {
     const int r = 16 * I + li;
-    const int64_t t = t0 + (r < valid ? r : 0);
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
+      const int col = 32 * s + 8 * lg;
       unsigned w[M::kPieceWords];
-      load_piece<DTYPE>(w, g.k, kb + t * g.k.st * M::kBytes, 32 * s + 8 * lg, r < valid);
-      __builtin_memcpy(&k[I][s], w, sizeof w);
-      load_piece<DTYPE>(w, g.q, qb + t * g.q.st * M::kBytes, 32 * s + 8 * lg, r < valid);
+      if constexpr (VEC) {
+        const bool there = r < valid && col < dk;
+        load_words<M::kPieceWords>(w, from_k, there ? (unsigned)(r * (int)g.k.st + col) * M::kBytes : kOutside);
+        __builtin_memcpy(&k[I][s], w, sizeof w);
+        load_words<M::kPieceWords>(w, from_q, there ? (unsigned)(r * (int)g.q.st + col) * M::kBytes : kOutside);
+      } else {
+        const int64_t t = t0 + (r < valid ? r : 0);
+        load_piece<DTYPE>(w, g.k, kb + t * g.k.st * M::kBytes, col, r < valid);
+        __builtin_memcpy(&k[I][s], w, sizeof w);
+        load_piece<DTYPE>(w, g.q, qb + t * g.q.st * M::kBytes, col, r < valid);
+      }
       __builtin_memcpy(&q[I][s], w, sizeof w);
     }
   }
@@ -354,7 +385,7 @@ struct SweepLds {
 };
 
 // The matrices of every chunk, for the sweeps and the gradients: a wave makes one chunk's.
-template <int DTYPE, int D, bool BACK>
+template <int DTYPE, int D, bool BACK, bool VEC>
 __global__ __launch_bounds__(kThreads) void delta_chunks_kernel(DeltaArgs g) {
   constexpr int kWave = 3 * C * kMat * 4 + (int)sizeof(Steps);
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -365,7 +396,7 @@ __global__ __launch_bounds__(kThreads) void delta_chunks_kernel(DeltaArgs g) {
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h), t0 = chunk * C, valid = min(C, g.T - t0);
   float *const mA = (float*)(lds + wave * kWave), *const mP = mA + C * kMat, *const mT = mP + C * kMat;
   Steps& steps = *(Steps*)(mT + C * kMat);
-  make_chunk<DTYPE, D, BACK>(g, n, h, hk, t0, valid, lane, steps, mA, mP, mT);
+  make_chunk<DTYPE, D, BACK, VEC>(g, n, h, hk, t0, valid, lane, steps, mA, mP, mT);
   float* const out = g.made + ((size_t)bh * g.chunks + chunk) * made_words(BACK);
 #pragma unroll
   for (int i = 0; i < kDense / 256; ++i) {
@@ -378,19 +409,22 @@ __global__ __launch_bounds__(kThreads) void delta_chunks_kernel(DeltaArgs g) {
 }
 
 enum Sweep { kResults = 0, kStates = 1, kBack = 2 };
+// How much of a call is known at compile time: kAny; kPieces: all rows are read and written in 16-byte pieces; kWhole: there are whole
+// tiles besides, D columns of k and a multiple of 64 of v (else columns past theirs are left out, 32 of k, 16 of v at a time).
+enum Known { kAny = 0, kPieces = 1, kWhole = 2 };
 
 // A workgroup of four waves goes over the chunks of one (row, head), or of one piece of T, for 64 columns of v, of which a wave owns 16: its part of
 // the state stays in registers as the accumulator of the update.  The products are arranged so that accumulators feed the next
 // product without a shuffle: a 16x16 accumulator holds rows 4 lg .. 4 lg + 3 of one column per lane (lg = lane / 16), two of them are
 // the eight K-slots of an operand of 16x16x32, and the other operand follows the same numbering of the K axis.
 //   kResults: o and the last state;  kStates: the states that enter the chunks, or the last one of a piece;  kBack: R, from the last chunk to the first
-// ALONE: of one chunk, whose matrices the first wave makes (else they are read).  VEC: arrays are read in 16-byte pieces.
-template <int DTYPE, int D, int SWEEP, bool ALONE, bool VEC>
-__global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_sweep_kernel(DeltaArgs g) {
+// ALONE: of one chunk, whose matrices the first wave makes (else they are read).
+template <int DTYPE, int D, int SWEEP, bool ALONE, int KNOWN>
+__global__ __launch_bounds__(kThreads, KNOWN != kAny ? (D == 64 ? 4 : 3) : 2) void delta_sweep_kernel(DeltaArgs g) {
   typedef Num<DTYPE> M;
   typedef SweepLds<DTYPE, D> L;
   constexpr int W = M::kPieceWords, NP = C * D / 8 / kThreads, ND = D / 16, kRow = D / 8, kRowV = DV / 8;
-  constexpr bool kQ = SWEEP != kStates, kUp = SWEEP != kBack;
+  constexpr bool kQ = SWEEP != kStates, kUp = SWEEP != kBack, VEC = KNOWN != kAny, WHOLE = KNOWN == kWhole;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   // the blocks of one (row, head) read the same arrays: one after another on one XCD (workgroups go to the 8 in turn)
   const unsigned round = g.round.of(blockIdx.x), in_round = blockIdx.x - round * (8 * g.blocks), turn8 = in_round >> 3;
@@ -402,7 +436,7 @@ __global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_s
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h);
-  const int dk = g.k.d, dv = identity ? dk : g.v.d;
+  const int dk = WHOLE ? D : g.k.d, dv = identity ? dk : g.v.d;
   const int t_begin = seg * g.seg_len, t_end = min(g.T, t_begin + g.seg_len);
   auto base = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
   const Strided third = SWEEP == kBack ? g.d_o : g.v;
@@ -415,46 +449,39 @@ __global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_s
   if (tid < 2) flag[tid] = 0;
   if constexpr (ALONE) {
     __syncthreads();
-    if (wave == 0) make_chunk<DTYPE, D, SWEEP == kBack>(g, n, h, hk, 0, g.T, lane, steps, (float*)(lds + L::kA), mP, mT);
+    if (wave == 0) make_chunk<DTYPE, D, SWEEP == kBack, VEC>(g, n, h, hk, 0, g.T, lane, steps, (float*)(lds + L::kA), mP, mT);
   }
 
   const int v0 = v_block + 16 * wave, y = v0 + li;  // this wave's columns of v, this lane's
-  const bool has_v = v0 < dv;
-  auto has_k = [&](int s) { return 32 * s < dk; };
+  const bool has_v = WHOLE || v0 < dv;
+  auto has_k = [&](int s) { return WHOLE || 32 * s < dk; };
   // row of tile t of the state (two tiles are 32 rows: eight neighbours per lane group)
   auto col_k = [&](int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); };
-  // Memory is read and written through buffers that begin at a uniform address; what is not there has an offset past the end
-  // (it is read as zero, not written).
-  constexpr unsigned kOutside = 0x80000000u;
-  auto buffer = [&](const void* p, unsigned bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000); };
-
   f32x4 S[ND];
-  bool odd_state = false;  // it holds something not finite
-  const unsigned y_at = y < dv ? (unsigned)(8 * lg * dv + y) * 4 : kOutside;  // (rows past dk lie past the end)
+  const unsigned y_at = WHOLE || y < dv ? (unsigned)(8 * lg * dv + y) * 4 : kOutside;  // (rows past dk lie past the end)
   {
     const float* s = nullptr;
     if (g.piece) s = nullptr;
     else if (g.n_seg > 1) s = g.seg_state + ((size_t)bh * g.n_seg + seg) * dk * dv;
     else if (g.s_in) s = g.s_in + (size_t)bh * dk * dv;
     const auto from = buffer(s, s ? (unsigned)(dk * dv) * 4 : 0);
-    float test = 0.0f;
 #pragma unroll
     for (int a = 0; a < ND; ++a)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        S[a][r] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4, 0));
+        S[a][r] = load_float(from, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4);
         if (identity) S[a][r] = col_k(a, 4 * lg + r) == y ? 1.0f : 0.0f;
-        test = fmaf(S[a][r], 0.0f, test);
       }
-    odd_state = test != 0.0f;
   }
   auto store_state = [&](float* s) {
+    int row = dv * 4;
+    asm volatile("" : "+s"(row));  // (else the rows' offsets are kept in registers from here to there)
     const auto to = buffer(s, (unsigned)(dk * dv) * 4);
 #pragma unroll
     for (int a = 0; a < ND; ++a)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, (float)S[a][r]), to, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, (float)S[a][r]), to, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * row, 0);
   };
 
   // the chunk that is on its way: its rows, matrices and steps
@@ -465,21 +492,19 @@ __global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_s
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int piece = tid + p * kThreads, r = piece / kRow, col = piece % kRow * 8;
-      at_q[p] = col < dk ? (unsigned)(r * (int)g.q.st + col) * M::kBytes : kOutside;
-      at_k[p] = col < dk ? (unsigned)(r * (int)g.k.st + col) * M::kBytes : kOutside;
+      at_q[p] = WHOLE || col < dk ? (unsigned)(r * (int)g.q.st + col) * M::kBytes : kOutside;
+      at_k[p] = WHOLE || col < dk ? (unsigned)(r * (int)g.k.st + col) * M::kBytes : kOutside;
     }
     const int col = v_block + tid % kRowV * 8;
-    if (col < third.d && !identity) at_v = (unsigned)(tid / kRowV * (int)third.st + col) * M::kBytes;
+    if ((WHOLE || col < third.d) && !identity) at_v = (unsigned)(tid / kRowV * (int)third.st + col) * M::kBytes;
   }
   const float* const made = g.made + (size_t)bh * g.chunks * made_words(!kUp || g.back);
   auto request = [&](int c) {
     const int t0 = c * C, valid = min(C, g.T - t0);
     if constexpr (VEC) {
       auto get = [&](unsigned* w, const Strided& a, const unsigned char* row, int r, unsigned at) {
-        const auto from = buffer(row + (int64_t)t0 * a.st * M::kBytes, 0x7FFFFFFF);
-        at = r < valid ? at : kOutside;
-#pragma unroll
-        for (int i = 0; i < W; i += 4) *(u32x4*)(w + i) = __builtin_amdgcn_raw_buffer_load_b128(from, at + 4 * i, 0, 0);
+        const auto from = buffer(row + (int64_t)t0 * a.st * M::kBytes, kWholeBuffer);
+        load_words<W>(w, from, r < valid ? at : kOutside);
       };
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
@@ -504,7 +529,7 @@ __global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_s
   };
   unsigned at_o[2];  // of four neighbours of an output row
 #pragma unroll
-  for (int I = 0; I < 2; ++I) at_o[I] = v0 + 4 * lg < dv ? (unsigned)((16 * I + li) * (g.N * g.H * dv) + v0 + 4 * lg) * M::kBytes : kOutside;
+  for (int I = 0; I < 2; ++I) at_o[I] = WHOLE || v0 + 4 * lg < dv ? (unsigned)((16 * I + li) * (g.N * g.H * dv) + v0 + 4 * lg) * M::kBytes : kOutside;
 
   const int first = t_begin / C, last = (t_end - 1) / C;  // chunks
   if (t_begin < t_end) request(kUp ? first : last);
@@ -538,56 +563,8 @@ __global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_s
     const int e_last = __builtin_amdgcn_readlane(my_ep, valid - 1);
     const bool marked = e_last != 0;
     any_begin = any_begin || marked;
-    const bool one_by_one = flag[turn] != 0 || __any(my_steps != 0.0f) || (marked && __any(odd_state));
+    const bool odd = flag[turn] != 0 || __any(my_steps != 0.0f);
     if (tid == 0) flag[turn ^ 1] = 0;  // (read by all before the barrier above)
-
-    if (one_by_one && has_v) {
-      // Step by step, each wave for its columns, so that nothing that is not finite meets a masked zero.
-      auto element = [&](const unsigned char* tile, int pitch, int i, int x) { return M::element(tile + i * pitch + x * M::kBytes); };
-      for (int at = 0; at < valid; ++at) {
-        const int i = kUp ? at : valid - 1 - at;
-        const StepIn in = read_step(g, n, h, t0 + i, 1, lane & 0);
-        const bool begin = begins(in);
-        const float keep = exp2f(in.ld * 1.44269504f), v = element(tv, L::kPitchV, i, 16 * wave + li);
-        float sum = 0.0f;
-#pragma unroll
-        for (int a = 0; a < ND; ++a)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int x = col_k(a, 4 * lg + r);
-            if (x >= dk) continue;
-            if constexpr (kUp) S[a][r] = begin ? 0.0f : keep * S[a][r];
-            else S[a][r] += g.scale * element(tq, L::kPitch, i, x) * v;
-            sum += element(tk, L::kPitch, i, x) * S[a][r];
-          }
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        const float u = in.beta * (kUp ? v - sum : -sum);
-        float o = 0.0f;
-#pragma unroll
-        for (int a = 0; a < ND; ++a)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int x = col_k(a, 4 * lg + r);
-            if (x >= dk) continue;
-            S[a][r] += element(tk, L::kPitch, i, x) * u;
-            if constexpr (SWEEP == kResults) o += element(tq, L::kPitch, i, x) * S[a][r];
-            if constexpr (!kUp) S[a][r] = begin ? 0.0f : keep * S[a][r];
-          }
-        if constexpr (SWEEP == kResults) {
-          o += __shfl_xor(o, 16);
-          o += __shfl_xor(o, 32);
-          if (lg == 0 && y < dv) M::store((unsigned char*)g.o + ((((int64_t)(t0 + i) * g.N + n) * g.H + h) * dv + y) * M::kBytes, g.scale * o);
-        }
-      }
-      float test2 = 0.0f;
-#pragma unroll
-      for (int a = 0; a < ND; ++a)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) test2 = fmaf(S[a][r], 0.0f, test2);
-      odd_state = test2 != 0.0f;
-      continue;
-    }
     if (!has_v) continue;
 
     // what the state gives the steps: k S, and q S
@@ -608,6 +585,55 @@ __global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_s
         ks[J] = M::mma(M::row(tk + at), st, ks[J]);                                               // [step][y]
         if constexpr (SWEEP == kResults) qs[J] = M::mma(leading<DTYPE>(st), M::row(tq + at), qs[J]);  // [y][step]
       }
+    }
+    // (of a state with something not finite every product is not finite: that an episode begins in the chunk does not stop it)
+    if (odd || (marked && __any(ks[0][0] * 0.0f != 0.0f))) {
+      // Step by step, each wave for its columns, so that nothing that is not finite meets a masked zero.
+      auto element = [&](const unsigned char* tile, int pitch, int i, int x) { return M::element(tile + i * pitch + x * M::kBytes); };
+      float s[ND][4];
+#pragma unroll
+      for (int a = 0; a < ND; ++a)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[a][r] = S[a][r];
+      for (int at = 0; at < valid; ++at) {
+        const int i = kUp ? at : valid - 1 - at;
+        const StepIn in = read_step(g, n, h, t0 + i, 1, lane & 0);
+        const bool begin = begins(in);
+        const float keep = exp2f(in.ld * 1.44269504f), v = element(tv, L::kPitchV, i, 16 * wave + li);
+        float sum = 0.0f;
+#pragma unroll
+        for (int a = 0; a < ND; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int x = col_k(a, 4 * lg + r);
+            if (x >= dk) continue;
+            if constexpr (kUp) s[a][r] = begin ? 0.0f : keep * s[a][r];
+            else s[a][r] += g.scale * element(tq, L::kPitch, i, x) * v;
+            sum += element(tk, L::kPitch, i, x) * s[a][r];
+          }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        const float u = in.beta * (kUp ? v - sum : -sum);
+        float o = 0.0f;
+#pragma unroll
+        for (int a = 0; a < ND; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int x = col_k(a, 4 * lg + r);
+            if (x >= dk) continue;
+            s[a][r] += element(tk, L::kPitch, i, x) * u;
+            if constexpr (SWEEP == kResults) o += element(tq, L::kPitch, i, x) * s[a][r];
+            if constexpr (!kUp) s[a][r] = begin ? 0.0f : keep * s[a][r];
+          }
+        if constexpr (SWEEP == kResults) {
+          o += __shfl_xor(o, 16);
+          o += __shfl_xor(o, 32);
+          if (lg == 0 && y < dv) M::store((unsigned char*)g.o + ((((int64_t)(t0 + i) * g.N + n) * g.H + h) * dv + y) * M::kBytes, g.scale * o);
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < ND; ++a) S[a] = f32x4{s[a][0], s[a][1], s[a][2], s[a][3]};
+      continue;
     }
     // columns of the third array: K-slots 0..3 are steps 4 lg .., 4..7 are 16 further on
     const typename M::Raw vt = columns<DTYPE>(tv, L::kPitchV, 16 * wave, 4, li, lg);
@@ -640,7 +666,7 @@ __global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_s
         for (int r = 0; r < 4; ++r) us[4 * J + r] = b4[J][r] * e[J][r];
       if constexpr (SWEEP == kResults) {
         const typename M::Out uo = M::out_terms(us);
-        const auto to = buffer((unsigned char*)g.o + (((int64_t)t0 * g.N + n) * g.H + h) * dv * M::kBytes, 0x7FFFFFFF);
+        const auto to = buffer((unsigned char*)g.o + (((int64_t)t0 * g.N + n) * g.H + h) * dv * M::kBytes, kWholeBuffer);
 #pragma unroll
         for (int I = 0; I < 2; ++I) {
           const int i = 16 * I + li;
@@ -723,12 +749,6 @@ __global__ __launch_bounds__(kThreads, VEC ? (D == 64 ? 4 : 3) : 2) void delta_s
         }
       }
     }
-    float test2 = 0.0f;
-#pragma unroll
-    for (int a = 0; a < ND; ++a)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) test2 = fmaf(S[a][r], 0.0f, test2);
-    odd_state = test2 != 0.0f;
   }
   if (!has_v) return;
   if (g.piece) {
@@ -748,44 +768,49 @@ template <bool BACK>
 __global__ __launch_bounds__(512) void delta_join_kernel(DeltaArgs g) {
   constexpr int kPitch = 132;
   __shared__ __attribute__((aligned(16))) float state[2][16 * kPitch];  // [y][row]
-  const int dk = g.k.d, dv = g.v.d, bh = blockIdx.y, y0 = blockIdx.x * 16;
+  // the workgroups of one (row, head) read the same matrices: one after another on one XCD
+  const unsigned round = g.round.of(blockIdx.x), in_round = blockIdx.x - round * (8 * g.blocks);
+  const int dk = g.k.d, dv = g.v.d, bh = (int)(round * 8 + (in_round & 7)), y0 = (int)(in_round >> 3) * 16;
+  if (bh >= g.N * g.H) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, lg = lane >> 4;
   const int x0 = 16 * wave, y = y0 + li;
-  f32x4 in = {0.0f, 0.0f, 0.0f, 0.0f};  // rows x0 + 4 lg + r
-  if (g.s_in)
+  const unsigned size = (unsigned)(dk * dv) * 4, y_at = y < dv ? (unsigned)((x0 + 4 * lg) * dv + y) * 4 : kOutside;  // (rows past dk lie past the end)
+  f32x4 in;  // rows x0 + 4 lg + r
+  const auto from_in = buffer(g.s_in ? g.s_in + (size_t)bh * dk * dv : nullptr, g.s_in ? size : 0);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (x0 + 4 * lg + r < dk && y < dv) in[r] = g.s_in[(size_t)bh * dk * dv + (x0 + 4 * lg + r) * dv + y];
+  for (int r = 0; r < 4; ++r) in[r] = load_float(from_in, y_at, r * dv * 4);
   f32x4 m[8], own;
-  bool begin;
+  int begin;
   auto request = [&](int seg) {
     const size_t at = (size_t)bh * g.n_seg + seg;
-    const float* const M = g.seg_through + at * dk * dk;
-    const float* const o = g.seg_state + at * dk * dv;
-    begin = g.seg_begin[at] != 0;
+    const auto from_m = buffer(g.seg_through + at * dk * dk, (unsigned)(dk * dk) * 4), from_o = buffer(g.seg_state + at * dk * dv, size);
+    begin = g.seg_begin[at];
 #pragma unroll
-    for (int s = 0; s < 8; ++s)
+    for (int s = 0; s < 8; ++s) {
+      // (of a matrix's row what lies behind its columns is the next row's or zero, and meets rows of the state that are zero)
+      const int a = x0 + li, b = 16 * s + 4 * lg;
+      if constexpr (BACK) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int a = x0 + li, b = 16 * s + 4 * lg + r;
-        m[s][r] = a < dk && b < dk ? (BACK ? M[b * dk + a] : M[a * dk + b]) : 0.0f;
+        for (int r = 0; r < 4; ++r) m[s][r] = load_float(from_m, a < dk ? (unsigned)(b * dk + a) * 4 : kOutside, r * dk * 4);
+      } else {
+        m[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from_m, b < dk ? (unsigned)(a * dk + b) * 4 : kOutside, 0, 0));
       }
+    }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) own[r] = x0 + 4 * lg + r < dk && y < dv ? o[(x0 + 4 * lg + r) * dv + y] : 0.0f;
+    for (int r = 0; r < 4; ++r) own[r] = load_float(from_o, y_at, r * dv * 4);
   };
   request(BACK ? g.n_seg - 1 : 0);
   for (int i = 0; i < g.n_seg; ++i) {
     const int seg = BACK ? g.n_seg - 1 - i : i;
-    float* const to = g.seg_state + ((size_t)bh * g.n_seg + seg) * dk * dv;
+    const auto to = buffer(g.seg_state + ((size_t)bh * g.n_seg + seg) * dk * dv, size);
     // (its own state has been read, by this thread)
     f32x4 next = own;
     f32x4 M[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s) M[s] = m[s];
-    const bool stop = begin;
+    const bool stop = begin != 0;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (x0 + 4 * lg + r < dk && y < dv) to[(x0 + 4 * lg + r) * dv + y] = in[r];
+    for (int r = 0; r < 4; ++r) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, (float)in[r]), to, y_at, r * dv * 4, 0);
     *(f32x4*)(state[i & 1] + li * kPitch + x0 + 4 * lg) = in;
     if (i + 1 < g.n_seg) request(BACK ? seg - 1 : seg + 1);
     __syncthreads();
@@ -812,10 +837,11 @@ struct GradLds {
 
 // All gradients of one chunk, given the states S that enters it and R behind it: one workgroup for each (row, head, chunk), a wave for 16
 // columns of v and then for 16 of k.
-template <int DTYPE, int D>
+template <int DTYPE, int D, int KNOWN>
 __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
   typedef Num<DTYPE> M;
   typedef GradLds<DTYPE, D> L;
+  constexpr bool VEC = KNOWN != kAny, WHOLE = KNOWN == kWhole;
   constexpr int W = M::kPieceWords, ND = D / 16, kRow8 = D / 8, kT = L::kThreads;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   // (workgroups go round the XCDs: 16 neighbours, whose rows of a step are neighbours too, for each)
@@ -825,7 +851,7 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h);
-  const int dk = g.k.d, dv = g.v.d, t0 = chunk * C, valid = min(C, g.T - t0);
+  const int dk = WHOLE ? D : g.k.d, dv = WHOLE ? D : g.v.d, t0 = chunk * C, valid = min(C, g.T - t0);
   auto base = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
   unsigned char *const tq = lds, *const tk = lds + L::kTile, *const tv = lds + 2 * L::kTile, *const to = lds + 3 * L::kTile;
   float *const mU = (float*)(lds + L::kU), *const mZ = (float*)(lds + L::kZ), *const mA = (float*)(lds + L::kA), *const mP = (float*)(lds + L::kP),
@@ -842,10 +868,18 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
   // the arrays: one piece of each a thread
   unsigned w[4][W];
   const int row8 = tid / kRow8, col8 = tid % kRow8 * 8;
-  fetch<DTYPE>(w[0], g.q, base(g.q), t0, valid, tid, kRow8, 0);
-  fetch<DTYPE>(w[1], g.k, base(g.k), t0, valid, tid, kRow8, 0);
-  fetch<DTYPE>(w[2], g.v, base(g.v), t0, valid, tid, kRow8, 0);
-  fetch<DTYPE>(w[3], g.d_o, base(g.d_o), t0, valid, tid, kRow8, 0);
+  auto array = [&](unsigned* to_w, const Strided& a) {
+    if constexpr (VEC) {
+      const auto from = buffer(base(a) + (int64_t)t0 * a.st * M::kBytes, kWholeBuffer);
+      load_words<W>(to_w, from, row8 < valid && col8 < a.d ? (unsigned)(row8 * (int)a.st + col8) * M::kBytes : kOutside);
+    } else {
+      fetch<DTYPE>(to_w, a, base(a), t0, valid, tid, kRow8, 0);
+    }
+  };
+  array(w[0], g.q);
+  array(w[1], g.k);
+  array(w[2], g.v);
+  array(w[3], g.d_o);
   const float* const from_steps = g.made + ((size_t)bh * g.chunks + chunk) * made_words(true);
   f32x4 n_m[(3 * kDense / 4 + kT - 1) / kT], n_steps;
 #pragma unroll
@@ -856,18 +890,21 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
   // the states by columns of v
   const int y0 = 16 * wave, y = y0 + li;
   auto col_k = [&](int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); };
+  const auto from_s = buffer(s0, s0 ? (unsigned)state * 4 : 0), from_r = buffer(r1, r1 ? (unsigned)state * 4 : 0);
+  const unsigned y_at = y < dv ? (unsigned)(8 * lg * dv + y) * 4 : kOutside;  // (rows past dk lie past the end)
   f32x4 S[ND], R[ND];
   float test = 0.0f;
 #pragma unroll
   for (int a = 0; a < ND; ++a)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int x = col_k(a, 4 * lg + r);
-      const bool there = x < dk && y < dv;
-      S[a][r] = s0 && there ? s0[x * dv + y] : 0.0f;
-      R[a][r] = r1 && there ? r1[x * dv + y] : 0.0f;
-      test = fmaf(S[a][r], 0.0f, fmaf(R[a][r], 0.0f, test));
+      S[a][r] = load_float(from_s, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4);
+      R[a][r] = load_float(from_r, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4);
     }
+#pragma unroll
+  for (int a = 0; a < ND; ++a)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) test = fmaf(S[a][r], 0.0f, fmaf(R[a][r], 0.0f, test));
   int* const flag = (int*)(lds + L::kFlag);
   if (tid == 0) *flag = 0;
   __syncthreads();
@@ -1169,7 +1206,7 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
           os[4 * t + r] = g.scale * e4[t][r] * o[4 * t + r];
         }
       const typename M::Sum zt = M::sum_terms(zs), dt = M::sum_terms(os);
-      float* const to_state = g.dstate0 + (size_t)bh * state;
+      const auto to_state = buffer(g.dstate0 + (size_t)bh * state, (unsigned)state * 4);
 #pragma unroll
       for (int a = 0; a < ND; ++a) {
         if (32 * (a >> 1) >= dk) continue;
@@ -1177,10 +1214,8 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
         acc = M::mma(columns<DTYPE>(tk, L::kPitch, col_k(a, 0), 8, li, lg), zt, acc);
         acc = M::mma(columns<DTYPE>(tq, L::kPitch, col_k(a, 0), 8, li, lg), dt, acc);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int xk = col_k(a, 4 * lg + r);
-          if (xk < dk && y < dv) to_state[xk * dv + y] = acc[r];
-        }
+        for (int r = 0; r < 4; ++r)
+          __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, (float)acc[r]), to_state, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4, 0);
       }
     }
   }
@@ -1300,14 +1335,10 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
       if (32 * s >= dv) continue;
+      // (columns past dv are the next row's numbers, or zero behind the last one: what they meet is zero)
       float a[8], b[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int c = 32 * s + 8 * lg + i;
-        const bool there = x < dk && c < dv;
-        a[i] = s0 && there ? s0[x * dv + c] : 0.0f;
-        b[i] = r1 && there ? r1[x * dv + c] : 0.0f;
-      }
+      load_words<8>((unsigned*)a, from_s, (unsigned)(x * dv + 32 * s + 8 * lg) * 4);
+      load_words<8>((unsigned*)b, from_r, (unsigned)(x * dv + 32 * s + 8 * lg) * 4);
       const typename M::Out st = M::out_terms(a), rt = M::out_terms(b);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -1618,9 +1649,11 @@ void with_pieces(const sf_deltarule_config* c, DeltaArgs& g, const Workspace& w,
 
 template <int DTYPE, int D, bool BACK>
 void launch_chunks(const DeltaArgs& g, hipStream_t st) {
+  const unsigned grid = (unsigned)(((int64_t)g.N * g.H * g.chunks + 3) / 4);
   constexpr int bytes = 4 * (3 * C * kMat * 4 + (int)sizeof(Steps));
   static_assert(bytes <= 64 * 1024, "no attribute needed");
-  delta_chunks_kernel<DTYPE, D, BACK><<<(unsigned)(((int64_t)g.N * g.H * g.chunks + 3) / 4), kThreads, bytes, st>>>(g);
+  if (g.q.vec && g.k.vec) delta_chunks_kernel<DTYPE, D, BACK, true><<<grid, kThreads, bytes, st>>>(g);
+  else delta_chunks_kernel<DTYPE, D, BACK, false><<<grid, kThreads, bytes, st>>>(g);
 }
 template <int DTYPE>
 void launch_chunks(const DeltaArgs& g, hipStream_t st) {
@@ -1639,8 +1672,9 @@ void launch_sweep(const DeltaArgs& g, bool vec, hipStream_t st) {
   constexpr int bytes = ALONE ? L::kBytesAlone : L::kBytes;
   static_assert(bytes <= 64 * 1024, "no attribute needed");
   const dim3 grid((unsigned)((g.N * g.H + 7) / 8 * 8 * g.blocks), (unsigned)g.n_seg);
-  if (vec) delta_sweep_kernel<DTYPE, D, SWEEP, ALONE, true><<<grid, kThreads, bytes, st>>>(g);
-  else delta_sweep_kernel<DTYPE, D, SWEEP, ALONE, false><<<grid, kThreads, bytes, st>>>(g);
+  if (!vec) delta_sweep_kernel<DTYPE, D, SWEEP, ALONE, kAny><<<grid, kThreads, bytes, st>>>(g);
+  else if (g.k.d == D && g.v.d % DV == 0) delta_sweep_kernel<DTYPE, D, SWEEP, ALONE, kWhole><<<grid, kThreads, bytes, st>>>(g);
+  else delta_sweep_kernel<DTYPE, D, SWEEP, ALONE, kPieces><<<grid, kThreads, bytes, st>>>(g);
 }
 template <int SWEEP, bool ALONE = false>
 hipError_t sweep(const sf_deltarule_config* c, DeltaArgs g, hipStream_t st) {
@@ -1659,14 +1693,16 @@ hipError_t sweep(const sf_deltarule_config* c, DeltaArgs g, hipStream_t st) {
   return hipGetLastError();
 }
 template <bool BACK>
-hipError_t join(const sf_deltarule_config* c, const DeltaArgs& g, hipStream_t st) {
-  delta_join_kernel<BACK><<<dim3((unsigned)((c->dv + 15) / 16), (unsigned)(c->N * c->H)), 512, 0, st>>>(g);
+hipError_t join(const sf_deltarule_config* c, DeltaArgs g, hipStream_t st) {
+  g.blocks = (c->dv + 15) / 16;
+  g.round = divisor(8 * g.blocks);
+  delta_join_kernel<BACK><<<(unsigned)((c->N * c->H + 7) / 8 * 8 * g.blocks), 512, 0, st>>>(g);
   return hipGetLastError();
 }
 
-template <int DTYPE, int D>
+template <int DTYPE, int D, int KNOWN>
 hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
-  const auto kern = delta_grad_kernel<DTYPE, D>;
+  const auto kern = delta_grad_kernel<DTYPE, D, KNOWN>;
   constexpr int bytes = GradLds<DTYPE, D>::kBytes;
   static_assert(bytes <= 160 * 1024, "LDS");
   if (bytes > 64 * 1024) {
@@ -1675,6 +1711,11 @@ hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
   }
   kern<<<(unsigned)(((int64_t)g.N * g.H * g.chunks + 127) / 128 * 128), 4 * D, bytes, st>>>(g);
   return hipGetLastError();
+}
+template <int DTYPE, int D>
+hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
+  if (!(g.q.vec && g.k.vec && g.v.vec && g.d_o.vec)) return launch_grad<DTYPE, D, kAny>(g, st);
+  return g.k.d == D && g.v.d == D ? launch_grad<DTYPE, D, kWhole>(g, st) : launch_grad<DTYPE, D, kPieces>(g, st);
 }
 hipError_t grad(const sf_deltarule_config* c, const DeltaArgs& g, hipStream_t st) {
   const bool wide = c->dk > 64 || c->dv > 64;
