@@ -102,6 +102,11 @@ __device__ inline typename Num<DTYPE>::Out leading(const typename Num<DTYPE>::Su
   else return s;
 }
 
+// A lane's number from the lane N behind it in its row of 16 (0 where there is none).
+template <int N>
+__device__ inline float row_left(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x100 + N, 0xF, 0xF, true));
+}
 // Sum over the 16 lanes of a row (each lane gets it).
 __device__ inline float row_sum(float x) {
 #define SF_ROR(n) x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + (n), 0xF, 0xF, true))
@@ -267,9 +272,9 @@ __device__ inline void invert(const float* at, const float* beta, float* T, int 
   for (int r = 0; r < 4; ++r) T[(16 + 4 * lg + r) * kMat + li] = -t21[r];
 }
 
-// One wave: a chunk's Steps, A^T, P (backwards P^T, without the scale) and T into LDS (pitch kMat).  Keys and queries are read as operands.
+// One wave: a chunk's Steps, A^T and P (backwards P^T, without the scale) into LDS (pitch kMat).  Keys and queries are read as operands.
 template <int DTYPE, int D, bool BACK, bool VEC>
-__device__ inline void make_chunk(const DeltaArgs& g, int n, int h, int hk, int t0, int valid, int lane, Steps& steps, float* mA, float* mP, float* mT) {
+__device__ inline void make_products(const DeltaArgs& g, int n, int h, int hk, int t0, int valid, int lane, Steps& steps, float* mA, float* mP) {
   typedef Num<DTYPE> M;
   const int li = lane & 15, lg = lane >> 4, dk = g.k.d;
   auto base = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
@@ -335,6 +340,11 @@ __device__ inline void make_chunk(const DeltaArgs& g, int n, int h, int hk, int 
       else *(f32x4*)(mP + (16 * I + li) * kMat + 16 * J + 4 * lg) = p;           // P [i][j]
     }
   wave_order();
+}
+// And T.
+template <int DTYPE, int D, bool BACK, bool VEC>
+__device__ inline void make_chunk(const DeltaArgs& g, int n, int h, int hk, int t0, int valid, int lane, Steps& steps, float* mA, float* mP, float* mT) {
+  make_products<DTYPE, D, BACK, VEC>(g, n, h, hk, t0, valid, lane, steps, mA, mP);
   invert(mA, steps.beta, mT, lane);
   wave_order();
 }
@@ -387,24 +397,30 @@ struct SweepLds {
 // The matrices of every chunk, for the sweeps and the gradients: a wave makes one chunk's.
 template <int DTYPE, int D, bool BACK, bool VEC>
 __global__ __launch_bounds__(kThreads) void delta_chunks_kernel(DeltaArgs g) {
-  constexpr int kWave = 3 * C * kMat * 4 + (int)sizeof(Steps);
+  constexpr int kWave = 2 * C * kMat * 4 + (int)sizeof(Steps);  // (T takes the place of P when that has left)
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned at = blockIdx.x * 4 + wave;
   if (at >= (unsigned)g.N * g.H * g.chunks) return;
   const int chunk = (int)g.rows.of(at), bh = (int)(at - (unsigned)chunk * (g.N * g.H));
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h), t0 = chunk * C, valid = min(C, g.T - t0);
-  float *const mA = (float*)(lds + wave * kWave), *const mP = mA + C * kMat, *const mT = mP + C * kMat;
-  Steps& steps = *(Steps*)(mT + C * kMat);
-  make_chunk<DTYPE, D, BACK, VEC>(g, n, h, hk, t0, valid, lane, steps, mA, mP, mT);
+  float *const mA = (float*)(lds + wave * kWave), *const mP = mA + C * kMat;
+  Steps& steps = *(Steps*)(mP + C * kMat);
   float* const out = g.made + ((size_t)bh * g.chunks + chunk) * made_words(BACK);
+  auto store = [&](float* to, const float* from) {
 #pragma unroll
-  for (int i = 0; i < kDense / 256; ++i) {
-    const int e = (i * 64 + lane) * 4, from = e / C * kMat + e % C;
-    *(f32x4*)(out + e) = *(const f32x4*)(mT + from);
-    *(f32x4*)(out + kDense + e) = *(const f32x4*)(mP + from);
-    if (BACK) *(f32x4*)(out + 2 * kDense + e) = *(const f32x4*)(mA + from);
-  }
+    for (int i = 0; i < kDense / 256; ++i) {
+      const int e = (i * 64 + lane) * 4;
+      *(f32x4*)(to + e) = *(const f32x4*)(from + e / C * kMat + e % C);
+    }
+  };
+  make_products<DTYPE, D, BACK, VEC>(g, n, h, hk, t0, valid, lane, steps, mA, mP);
+  store(out + kDense, mP);
+  wave_order();
+  invert(mA, steps.beta, mP, lane);
+  wave_order();
+  store(out, mP);
+  if (BACK) store(out + 2 * kDense, mA);
   if (lane < kStepWords / 4) *(f32x4*)(out + (BACK ? 3 : 2) * kDense + 4 * lane) = *(const f32x4*)((const float*)&steps + 4 * lane);
 }
 
@@ -779,46 +795,50 @@ __global__ __launch_bounds__(512) void delta_join_kernel(DeltaArgs g) {
   const auto from_in = buffer(g.s_in ? g.s_in + (size_t)bh * dk * dv : nullptr, g.s_in ? size : 0);
 #pragma unroll
   for (int r = 0; r < 4; ++r) in[r] = load_float(from_in, y_at, r * dv * 4);
-  f32x4 m[8], own;
-  int begin;
-  auto request = [&](int seg) {
-    const size_t at = (size_t)bh * g.n_seg + seg;
+  struct Piece {
+    f32x4 m[8], own;
+    int begin;
+  };
+  auto request = [&](Piece& p, int i) {
+    const size_t at = (size_t)bh * g.n_seg + (BACK ? g.n_seg - 1 - i : i);
     const auto from_m = buffer(g.seg_through + at * dk * dk, (unsigned)(dk * dk) * 4), from_o = buffer(g.seg_state + at * dk * dv, size);
-    begin = g.seg_begin[at];
+    p.begin = g.seg_begin[at];
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       // (of a matrix's row what lies behind its columns is the next row's or zero, and meets rows of the state that are zero)
       const int a = x0 + li, b = 16 * s + 4 * lg;
       if constexpr (BACK) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) m[s][r] = load_float(from_m, a < dk ? (unsigned)(b * dk + a) * 4 : kOutside, r * dk * 4);
+        for (int r = 0; r < 4; ++r) p.m[s][r] = load_float(from_m, a < dk ? (unsigned)(b * dk + a) * 4 : kOutside, r * dk * 4);
       } else {
-        m[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from_m, b < dk ? (unsigned)(a * dk + b) * 4 : kOutside, 0, 0));
+        p.m[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from_m, b < dk ? (unsigned)(a * dk + b) * 4 : kOutside, 0, 0));
       }
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) own[r] = load_float(from_o, y_at, r * dv * 4);
+    for (int r = 0; r < 4; ++r) p.own[r] = load_float(from_o, y_at, r * dv * 4);
   };
-  request(BACK ? g.n_seg - 1 : 0);
-  for (int i = 0; i < g.n_seg; ++i) {
-    const int seg = BACK ? g.n_seg - 1 - i : i;
-    const auto to = buffer(g.seg_state + ((size_t)bh * g.n_seg + seg) * dk * dv, size);
-    // (its own state has been read, by this thread)
-    f32x4 next = own;
-    f32x4 M[8];
-#pragma unroll
-    for (int s = 0; s < 8; ++s) M[s] = m[s];
-    const bool stop = begin != 0;
+  // what entered piece i is written to the place of its own state, which is in registers by then
+  auto turn = [&](Piece& p, int i) {
+    const auto to = buffer(g.seg_state + ((size_t)bh * g.n_seg + (BACK ? g.n_seg - 1 - i : i)) * dk * dv, size);
+    float* const round_trip = state[i & 1];
+    *(f32x4*)(round_trip + li * kPitch + x0 + 4 * lg) = in;
+    __syncthreads();
+    f32x4 next = p.own;
 #pragma unroll
     for (int r = 0; r < 4; ++r) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, (float)in[r]), to, y_at, r * dv * 4, 0);
-    *(f32x4*)(state[i & 1] + li * kPitch + x0 + 4 * lg) = in;
-    if (i + 1 < g.n_seg) request(BACK ? seg - 1 : seg + 1);
-    __syncthreads();
-    if (!stop)
+    if (p.begin == 0)
 #pragma unroll
       for (int s = 0; s < 8; ++s)
-        if (16 * s < dk) next = mm4(M[s], *(const f32x4*)(state[i & 1] + li * kPitch + 16 * s + 4 * lg), next);
+        if (16 * s < dk) next = mm4(p.m[s], *(const f32x4*)(round_trip + li * kPitch + 16 * s + 4 * lg), next);
     in = next;
+    if (i + 2 < g.n_seg) request(p, i + 2);
+  };
+  Piece even, odd;
+  request(even, 0);
+  if (g.n_seg > 1) request(odd, 1);
+  for (int i = 0; i < g.n_seg; i += 2) {
+    turn(even, i);
+    if (i + 1 < g.n_seg) turn(odd, i + 1);
   }
 }
 
@@ -826,19 +846,21 @@ template <int DTYPE, int D>
 struct GradLds {
   static constexpr int kPitch = Pitch<DTYPE, D>::value, kTile = C * kPitch, kPitchF = (D + 4) * 4, kTileF = C * kPitchF;
   static constexpr int kWaves = D / 16, kThreads = 64 * kWaves;
-  // q, k, v, do; u and z in fp32; A^T, P^T, and T, which makes room for dP D and its like as operands
+  // q, k, v, do; u and z in fp32; A^T, P^T and T, which make room for dP D and its like as operands
   static constexpr int kU = 4 * kTile, kZ = kU + kTileF, kA = kZ + kTileF, kP = kA + C * kMat * 4, kT = kP + C * kMat * 4,
-                       kOperand = 4096, kM = kT;  // [3] of two terms (or halves) of 2 x 64 lanes x 16 bytes
-  static constexpr int kSteps = kT + 3 * kOperand, kFlag = kSteps + (int)sizeof(Steps);
-  static constexpr int kSums = kFlag + 16;  // float [kWaves + 4][C] of each kind
+                       kOperand = 4096, kM = kA;  // [3] of two terms (or halves) of 2 x 64 lanes x 16 bytes
+  static_assert(3 * kOperand <= 3 * C * kMat * 4, "operands");
+  static constexpr int kSteps = kT + C * kMat * 4, kFlag = kSteps + (int)sizeof(Steps);
+  static constexpr int kSums = kFlag + 32;  // float [kWaves + 4][C] of each kind
   static constexpr int kSumRows = 2 * kWaves + 5;
   static constexpr int kBytes = kSums + kSumRows * C * 4;
 };
 
 // All gradients of one chunk, given the states S that enters it and R behind it: one workgroup for each (row, head, chunk), a wave for 16
 // columns of v and then for 16 of k.
-template <int DTYPE, int D, int KNOWN>
-__global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
+// ALONE: the only chunk, whose matrices the first wave makes (else they are read).
+template <int DTYPE, int D, bool ALONE, int KNOWN>
+__global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) void delta_grad_kernel(DeltaArgs g) {
   typedef Num<DTYPE> M;
   typedef GradLds<DTYPE, D> L;
   constexpr bool VEC = KNOWN != kAny, WHOLE = KNOWN == kWhole;
@@ -880,12 +902,14 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
   array(w[1], g.k);
   array(w[2], g.v);
   array(w[3], g.d_o);
-  const float* const from_steps = g.made + ((size_t)bh * g.chunks + chunk) * made_words(true);
   f32x4 n_m[(3 * kDense / 4 + kT - 1) / kT], n_steps;
+  if constexpr (!ALONE) {
+    const float* const from_steps = g.made + ((size_t)bh * g.chunks + chunk) * made_words(true);
 #pragma unroll
-  for (int i = 0; i < 3 * kDense / 4; i += kT)
-    if (i + tid < 3 * kDense / 4) n_m[i / kT] = *(const f32x4*)(from_steps + 4 * (i + tid));
-  if (tid < kStepWords / 4) n_steps = *(const f32x4*)(from_steps + 3 * kDense + 4 * tid);
+    for (int i = 0; i < 3 * kDense / 4; i += kT)
+      if (i + tid < 3 * kDense / 4) n_m[i / kT] = *(const f32x4*)(from_steps + 4 * (i + tid));
+    if (tid < kStepWords / 4) n_steps = *(const f32x4*)(from_steps + 3 * kDense + 4 * tid);
+  }
 
   // the states by columns of v
   const int y0 = 16 * wave, y = y0 + li;
@@ -901,25 +925,30 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
       S[a][r] = load_float(from_s, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4);
       R[a][r] = load_float(from_r, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4);
     }
+  int* const flag = (int*)(lds + L::kFlag);  // by waves
+  if constexpr (ALONE) {
+    // (while the others wait for their loads)
+    if (wave == L::kWaves - 1) make_chunk<DTYPE, D, true, VEC>(g, n, h, hk, 0, valid, lane, steps, mA, mP, mT);
+  }
 #pragma unroll
   for (int a = 0; a < ND; ++a)
 #pragma unroll
     for (int r = 0; r < 4; ++r) test = fmaf(S[a][r], 0.0f, fmaf(R[a][r], 0.0f, test));
-  int* const flag = (int*)(lds + L::kFlag);
-  if (tid == 0) *flag = 0;
-  __syncthreads();
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
     put_piece<DTYPE>(lds + a * L::kTile, L::kPitch, w[a], tid, kRow8);
     test = finite_test<DTYPE>(w[a], test);
   }
+  if constexpr (!ALONE) {
 #pragma unroll
-  for (int i = 0; i < 3 * kDense / 4; i += kT) {
-    const int e = i + tid, m = e / (kDense / 4), in = e % (kDense / 4);
-    if (e < 3 * kDense / 4) *(f32x4*)((m == 0 ? mT : m == 1 ? mP : mA) + in / 8 * kMat + in % 8 * 4) = n_m[i / kT];
+    for (int i = 0; i < 3 * kDense / 4; i += kT) {
+      const int e = i + tid, m = e / (kDense / 4), in = e % (kDense / 4);
+      if (e < 3 * kDense / 4) *(f32x4*)((m == 0 ? mT : m == 1 ? mP : mA) + in / 8 * kMat + in % 8 * 4) = n_m[i / kT];
+    }
+    if (tid < kStepWords / 4) *(f32x4*)((float*)&steps + 4 * tid) = n_steps;
   }
-  if (tid < kStepWords / 4) *(f32x4*)((float*)&steps + 4 * tid) = n_steps;
-  if (test != 0.0f) *flag = 1;
+  const bool odd = __any(test != 0.0f);
+  if (lane == 0) flag[wave] = odd;
   __syncthreads();
   const int my_ep = steps.ep[lane & (C - 1)];
   const float my_steps = fmaf(steps.gh[lane & (C - 1)], 0.0f, steps.beta[lane & (C - 1)] * 0.0f);
@@ -931,16 +960,27 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
 
   const int64_t head_k = ((int64_t)n * g.H + h) * dk, head_v = ((int64_t)n * g.H + h) * dv, step_k = (int64_t)g.N * g.H * dk,
                 step_v = (int64_t)g.N * g.H * dv;
-  // of step i: what the sums over steps behind it make of dG
-  auto decay_gradient = [&](const float* dG, int i) {
-    float s = 0.0f;
-    for (int l = C - 1; l >= 0; --l)
-      if (l >= i && steps.ep[l] == steps.ep[i]) s += dG[l];
+  // One wave: the sums of dG over each step and the ones behind it in its episode, which is what a decay's gradient is (0 where none was made).
+  auto decay_gradient = [&](float dG) {
+    const int i = lane & (C - 1);
+    const unsigned behind = (begin & ~((2u << i) - 1)) | (valid < C ? 1u << valid : 0u);
+    const int reach = (behind ? __ffs((int)behind) - 1 : C) - 1 - i;  // steps behind it
+    float s = i < valid ? dG : 0.0f;
+    float b = row_left<1>(s);
+    s += reach >= 1 ? b : 0.0f;
+    b = row_left<2>(s);
+    s += reach >= 2 ? b : 0.0f;
+    b = row_left<4>(s);
+    s += reach >= 4 ? b : 0.0f;
+    b = row_left<8>(s);
+    s += reach >= 8 ? b : 0.0f;
+    b = __shfl(s, 16);
+    s += i < 16 && reach >= 16 - i ? b : 0.0f;
     return begin >> i & 1 ? 0.0f : s;
   };
   const int64_t step_at = ((int64_t)t0 * g.N + n) * g.H + h;
 
-  if (*flag != 0 || __any(my_steps != 0.0f)) {
+  if (__any(lane < L::kWaves && flag[lane & 7] != 0) || __any(my_steps != 0.0f)) {
     // Number by number, so that nothing that is not finite meets a masked zero.
     auto at = [&](const unsigned char* tile, int r, int c) { return M::element(tile + r * L::kPitch + c * M::kBytes); };
     auto put = [&](void* out, bool f32, int64_t i, float v) {
@@ -948,7 +988,7 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
       else M::store((unsigned char*)out + i * M::kBytes, v);
     };
     auto decay = [&](int i, int j) { return decay_of(steps.gh[i], steps.gl[i], steps.gh[j], steps.gl[j]); };
-    float *const dP = (float*)(lds + L::kM), *const dA = dP + C * C;  // [i][j]
+    float *const dP = mT, *const dA = (float*)tv;  // [i][j], in the places of T and, when e is made, of v
     for (int e = tid; e < C * C; e += kT) {
       const int i = e / C, j = e % C;
       float a = 0.0f, p = 0.0f;
@@ -1054,7 +1094,10 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
       sum_b[tid] = 0.0f;
     }
     __syncthreads();
-    if (tid < valid) g.dlog_decay[step_at + (int64_t)tid * g.N * g.H] = decay_gradient(sum_b, tid);
+    if (wave == 0) {
+      const float d = decay_gradient(sum_b[lane & (C - 1)]);
+      if (lane < valid) g.dlog_decay[step_at + (int64_t)lane * g.N * g.H] = d;
+    }
     for (int e = tid; e < valid * dk; e += kT) {
       const int t = e / dk, x = e % dk;
       float q = 0.0f, k = 0.0f, s = 0.0f;
@@ -1303,27 +1346,26 @@ __global__ __launch_bounds__(4 * D) void delta_grad_kernel(DeltaArgs g) {
   if (wave < 4) M::put4(m + 2 * L::kOperand + J * 1024, 2048, lane, I, made[2]);
   __syncthreads();
 
-  if (wave == 0 && lane < C) {
-    float b = 0.0f, s = 0.0f;
-    for (int i = 0; i < L::kWaves; ++i) {
-      b += sum_b[i * C + lane];
-      s += sum_g[i * C + lane];
+  if (wave == 0) {
+    const int i = lane & (C - 1);
+    float b = 0.0f, s = 0.0f, rest = 0.0f;
+#pragma unroll
+    for (int w = 0; w < L::kWaves; ++w) {
+      b += sum_b[w * C + i];
+      s += sum_g[w * C + i];
+      rest += sum_1[w];
     }
-    auto add = [&](const float* t) { s += (t[lane] + t[C + lane]) - (t[2 * C + lane] + t[3 * C + lane]); };
+    auto add = [&](const float* t) { s += (t[i] + t[C + i]) - (t[2 * C + i] + t[3 * C + i]); };
     if (L::kWaves == 4) {
       add(tile_sums);
     } else {
       add((float*)tv);
       add((float*)tv + 4 * C);
     }
-    if (lane == valid - 1)
-      for (int i = 0; i < L::kWaves; ++i) s += sum_1[i];
-    sum_b[lane] = s;  // (of the first wave: read above)
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    const float d = decay_gradient(i == valid - 1 ? s + rest : s);
     if (lane < valid) {
       g.dbeta[step_at + (int64_t)lane * g.N * g.H] = b;
-      g.dlog_decay[step_at + (int64_t)lane * g.N * g.H] = decay_gradient(sum_b, lane);
+      g.dlog_decay[step_at + (int64_t)lane * g.N * g.H] = d;
     }
   }
 
@@ -1588,7 +1630,7 @@ Workspace workspace_of(const sf_deltarule_config* c, int backward) {
   Workspace w = {};
   const size_t lanes = (size_t)c->N * c->H, chunks = chunks_of(c), state = (size_t)c->dk * c->dv * 4;
   const Split s = split_of(c);
-  if (backward || c->T > C) w.made = align256(lanes * chunks * made_words(backward) * 4);
+  if (c->T > C) w.made = align256(lanes * chunks * made_words(backward) * 4);
   if (s.n_seg > 1) {
     w.seg_state = align256(lanes * s.n_seg * state);
     w.seg_through = align256(lanes * s.n_seg * c->dk * c->dk * 4);
@@ -1650,7 +1692,7 @@ void with_pieces(const sf_deltarule_config* c, DeltaArgs& g, const Workspace& w,
 template <int DTYPE, int D, bool BACK>
 void launch_chunks(const DeltaArgs& g, hipStream_t st) {
   const unsigned grid = (unsigned)(((int64_t)g.N * g.H * g.chunks + 3) / 4);
-  constexpr int bytes = 4 * (3 * C * kMat * 4 + (int)sizeof(Steps));
+  constexpr int bytes = 4 * (2 * C * kMat * 4 + (int)sizeof(Steps));
   static_assert(bytes <= 64 * 1024, "no attribute needed");
   if (g.q.vec && g.k.vec) delta_chunks_kernel<DTYPE, D, BACK, true><<<grid, kThreads, bytes, st>>>(g);
   else delta_chunks_kernel<DTYPE, D, BACK, false><<<grid, kThreads, bytes, st>>>(g);
@@ -1700,9 +1742,9 @@ hipError_t join(const sf_deltarule_config* c, DeltaArgs g, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int DTYPE, int D, int KNOWN>
+template <int DTYPE, int D, bool ALONE, int KNOWN>
 hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
-  const auto kern = delta_grad_kernel<DTYPE, D, KNOWN>;
+  const auto kern = delta_grad_kernel<DTYPE, D, ALONE, KNOWN>;
   constexpr int bytes = GradLds<DTYPE, D>::kBytes;
   static_assert(bytes <= 160 * 1024, "LDS");
   if (bytes > 64 * 1024) {
@@ -1712,10 +1754,14 @@ hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
   kern<<<(unsigned)(((int64_t)g.N * g.H * g.chunks + 127) / 128 * 128), 4 * D, bytes, st>>>(g);
   return hipGetLastError();
 }
+template <int DTYPE, int D, bool ALONE>
+hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
+  if (!(g.q.vec && g.k.vec && g.v.vec && g.d_o.vec)) return launch_grad<DTYPE, D, ALONE, kAny>(g, st);
+  return g.k.d == D && g.v.d == D ? launch_grad<DTYPE, D, ALONE, kWhole>(g, st) : launch_grad<DTYPE, D, ALONE, kPieces>(g, st);
+}
 template <int DTYPE, int D>
 hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
-  if (!(g.q.vec && g.k.vec && g.v.vec && g.d_o.vec)) return launch_grad<DTYPE, D, kAny>(g, st);
-  return g.k.d == D && g.v.d == D ? launch_grad<DTYPE, D, kWhole>(g, st) : launch_grad<DTYPE, D, kPieces>(g, st);
+  return g.chunks == 1 ? launch_grad<DTYPE, D, true>(g, st) : launch_grad<DTYPE, D, false>(g, st);
 }
 hipError_t grad(const sf_deltarule_config* c, const DeltaArgs& g, hipStream_t st) {
   const bool wide = c->dk > 64 || c->dv > 64;
@@ -1808,7 +1854,7 @@ extern "C" int sf_deltarule_backward(const sf_deltarule_config* cfg, const void*
   with_pieces(cfg, g, w, ws);
   g.back = 1;
   const size_t at = w.made + w.seg_state + w.seg_through + w.seg_begin;
-  hipError_t err = none ? hipSuccess : make_chunks(cfg, g, st);
+  hipError_t err = cfg->T <= C ? hipSuccess : make_chunks(cfg, g, st);
   if (cfg->T == 0 || cfg->T > C) {
     if (cfg->T > 0) {
       g.s_in = state0;

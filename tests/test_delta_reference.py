@@ -127,8 +127,8 @@ def test_workspace_bytes():
     memory = _memory()
     lib = memory.load_library()
     size = lambda back, **kw: lib.sf_deltarule_workspace_bytes(_config(memory, **kw), back)
-    assert size(0) == 0 and size(0, T=32) == 0
-    assert size(1, Hk=4) >= 2 * 4 * 3 * 32 * 32 * 4                 # three matrices for each chunk
+    assert size(0) == 0 and size(0, T=32) == 0 and size(1, Hk=4, T=32) == 0
+    assert size(0, T=33) >= 2 * 2 * 4 * 2 * 32 * 32 * 4             # two matrices for each chunk
     assert size(1) >= 2 * 8 * 2 * 4 * 16 * 4                        # the shared heads' partial sums
     assert size(1, Hk=4, T=33) >= 2 * 2 * 2 * 4 * 16 * 16 * 4  # two states for each chunk
 
