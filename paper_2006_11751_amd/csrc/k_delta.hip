@@ -879,6 +879,7 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
   float *const mU = (float*)(lds + L::kU), *const mZ = (float*)(lds + L::kZ), *const mA = (float*)(lds + L::kA), *const mP = (float*)(lds + L::kP),
                *const mT = (float*)(lds + L::kT);
   constexpr int kF = D + 4;
+  int* const flag = (int*)(lds + L::kFlag);  // by waves
   Steps& steps = *(Steps*)(lds + L::kSteps);
   // by waves: sums over their columns for each step; by tiles: of dP P + dA A along its rows and columns; a number of each wave
   float *const sum_b = (float*)(lds + L::kSums), *const sum_g = sum_b + L::kWaves * C, *const sum_m = sum_g + L::kWaves * C, *const sum_1 = sum_m + 4 * C;
@@ -911,29 +912,29 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
     if (tid < kStepWords / 4) n_steps = *(const f32x4*)(from_steps + 3 * kDense + 4 * tid);
   }
 
-  // the states by columns of v
-  const int y0 = 16 * wave, y = y0 + li;
+  StepIn in = {};
+  if constexpr (ALONE) in = read_step(g, n, h, 0, valid, lane);
+  // the states, 32 rows of both at a time: two pieces of four numbers of each a thread
+  const int y0 = 16 * wave, y = y0 + li;  // this wave's columns of v, this lane's
   auto col_k = [&](int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); };
   const auto from_s = buffer(s0, s0 ? (unsigned)state * 4 : 0), from_r = buffer(r1, r1 ? (unsigned)state * 4 : 0);
-  const unsigned y_at = y < dv ? (unsigned)(8 * lg * dv + y) * 4 : kOutside;  // (rows past dk lie past the end)
-  f32x4 S[ND], R[ND];
-  float test = 0.0f;
+  constexpr int kPer = D / 4;
+  f32x4 ns[2], nr[2];
+  auto request = [&](int s) {
 #pragma unroll
-  for (int a = 0; a < ND; ++a)
+    for (int p = 0; p < 2; ++p) {
+      const int row = 32 * s + (tid + p * kT) / kPer, c = (tid + p * kT) % kPer * 4;
+      const unsigned at = WHOLE || c < dv ? (unsigned)(row * dv + c) * 4 : kOutside;  // (rows past dk lie past the end)
+      ns[p] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from_s, at, 0, 0));
+      nr[p] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from_r, at, 0, 0));
+      if (!WHOLE && c + 4 > dv)  // (the next row's numbers)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      S[a][r] = load_float(from_s, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4);
-      R[a][r] = load_float(from_r, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4);
+        for (int i = 1; i < 4; ++i)
+          if (c + i >= dv) ns[p][i] = nr[p][i] = 0.0f;
     }
-  int* const flag = (int*)(lds + L::kFlag);  // by waves
-  if constexpr (ALONE) {
-    // (while the others wait for their loads)
-    if (wave == L::kWaves - 1) make_chunk<DTYPE, D, true, VEC>(g, n, h, hk, 0, valid, lane, steps, mA, mP, mT);
-  }
-#pragma unroll
-  for (int a = 0; a < ND; ++a)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) test = fmaf(S[a][r], 0.0f, fmaf(R[a][r], 0.0f, test));
+  };
+  request(0);
+  float test = 0.0f;
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
     put_piece<DTYPE>(lds + a * L::kTile, L::kPitch, w[a], tid, kRow8);
@@ -946,9 +947,9 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
       if (e < 3 * kDense / 4) *(f32x4*)((m == 0 ? mT : m == 1 ? mP : mA) + in / 8 * kMat + in % 8 * 4) = n_m[i / kT];
     }
     if (tid < kStepWords / 4) *(f32x4*)((float*)&steps + 4 * tid) = n_steps;
+  } else if (wave == 0) {
+    put_steps(steps, in, (unsigned)__ballot(begins(in)), valid, lane);
   }
-  const bool odd = __any(test != 0.0f);
-  if (lane == 0) flag[wave] = odd;
   __syncthreads();
   const int my_ep = steps.ep[lane & (C - 1)];
   const float my_steps = fmaf(steps.gh[lane & (C - 1)], 0.0f, steps.beta[lane & (C - 1)] * 0.0f);
@@ -957,6 +958,79 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
   // steps that an episode begins with: another one's episode than the step before
   const unsigned begin = (unsigned)__ballot(lane < valid && my_ep != (lane ? __shfl_up(my_ep, 1) : 0));
   const float keep = marked ? 0.0f : steps.enter[valid - 1];
+
+  // tiles of the chunk's matrices, [i][j] with i in tile I, j in tile J: the first four waves those of A, the last four those of P
+  const int I = wave >> 1 & 1, J = wave & 1;
+  float decays[4];  // of steps i = 16 I + 4 lg + r and j = 16 J + li
+  {
+    const int j = 16 * J + li, ej = steps.ep[j];
+    const f32x4 h4 = *(const f32x4*)(steps.gh + 16 * I + 4 * lg), l4 = *(const f32x4*)(steps.gl + 16 * I + 4 * lg);
+    const i32x4 e4 = *(const i32x4*)(steps.ep + 16 * I + 4 * lg);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) decays[r] = 16 * I + 4 * lg + r >= j && e4[r] == ej ? decay_of(h4[r], l4[r], steps.gh[j], steps.gl[j]) : 0.0f;
+  }
+  if constexpr (ALONE) {
+    auto product = [&](const unsigned char* rows, float* to_matrix, bool strict) {
+      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (J <= I) {
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+          const int at = (32 * s + 8 * lg) * M::kBytes;
+          if (32 * s < dk) acc = M::mma(M::row(rows + (16 * I + li) * L::kPitch + at), M::row(tk + (16 * J + li) * L::kPitch + at), acc);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[r] = decays[r] != 0.0f && (!strict || 16 * I + 4 * lg + r > 16 * J + li) ? acc[r] * decays[r] : 0.0f;
+      }
+      *(f32x4*)(to_matrix + (16 * J + li) * kMat + 16 * I + 4 * lg) = acc;  // [j][i]
+    };
+    if (wave < 4) product(tk, mA, true);
+    if (L::kWaves == 4 || wave >= 4) product(tq, mP, false);
+  }
+
+  // what the states give the steps; the slabs go through the places of u and z
+  f32x4 ks[2] = {}, qs[2] = {}, kr[2] = {};
+  float through = 0.0f;
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    if (32 * s >= dk) continue;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int at = (tid + p * kT) / kPer * kF + (tid + p * kT) % kPer * 4;
+      *(f32x4*)(mU + at) = ns[p];
+      *(f32x4*)(mZ + at) = nr[p];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        through = fmaf(ns[p][i], nr[p][i], through);
+        test = fmaf(ns[p][i], 0.0f, fmaf(nr[p][i], 0.0f, test));
+      }
+    }
+    __syncthreads();
+    if (32 * (s + 1) < dk) request(s + 1);
+    if constexpr (ALONE) {
+      if (s == 0 && wave == L::kWaves - 1) invert(mA, steps.beta, mT, lane);
+    }
+    float xs[8], xr[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      xs[i] = mU[(8 * lg + i) * kF + y];
+      xr[i] = mZ[(8 * lg + i) * kF + y];
+    }
+    const typename M::Sum st = M::sum_terms(xs), rt = M::sum_terms(xr);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int at = (16 * t + li) * L::kPitch + (32 * s + 8 * lg) * M::kBytes;
+      const auto kk = M::row(tk + at);
+      ks[t] = M::mma(kk, st, ks[t]);
+      kr[t] = M::mma(kk, rt, kr[t]);
+      qs[t] = M::mma(M::row(tq + at), st, qs[t]);
+    }
+    __syncthreads();
+  }
+  {
+    const bool odd = __any(test != 0.0f);
+    if (lane == 0) flag[wave] = odd;
+  }
+  __syncthreads();
 
   const int64_t head_k = ((int64_t)n * g.H + h) * dk, head_v = ((int64_t)n * g.H + h) * dv, step_k = (int64_t)g.N * g.H * dk,
                 step_v = (int64_t)g.N * g.H * dv;
@@ -1141,39 +1215,6 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
     return;
   }
 
-  // tiles of the chunk's matrices, [i][j] with i in tile I, j in tile J: the first four waves those of A, the last four those of P
-  const int I = wave >> 1 & 1, J = wave & 1;
-  float decays[4];  // of steps i = 16 I + 4 lg + r and j = 16 J + li
-  {
-    const int j = 16 * J + li, ej = steps.ep[j];
-    const f32x4 h4 = *(const f32x4*)(steps.gh + 16 * I + 4 * lg), l4 = *(const f32x4*)(steps.gl + 16 * I + 4 * lg);
-    const i32x4 e4 = *(const i32x4*)(steps.ep + 16 * I + 4 * lg);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) decays[r] = 16 * I + 4 * lg + r >= j && e4[r] == ej ? decay_of(h4[r], l4[r], steps.gh[j], steps.gl[j]) : 0.0f;
-  }
-  // what the states give the steps
-  f32x4 ks[2] = {}, qs[2] = {}, kr[2] = {};
-#pragma unroll
-  for (int s = 0; s < D / 32; ++s) {
-    if (32 * s >= dk) continue;
-    float xs[8], xr[8];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      xs[r] = S[2 * s][r];
-      xs[4 + r] = S[2 * s + 1][r];
-      xr[r] = R[2 * s][r];
-      xr[4 + r] = R[2 * s + 1][r];
-    }
-    const typename M::Sum st = M::sum_terms(xs), rt = M::sum_terms(xr);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int at = (16 * t + li) * L::kPitch + (32 * s + 8 * lg) * M::kBytes;
-      const auto kk = M::row(tk + at);
-      ks[t] = M::mma(kk, st, ks[t]);
-      kr[t] = M::mma(kk, rt, kr[t]);
-      qs[t] = M::mma(M::row(tq + at), st, qs[t]);
-    }
-  }
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
   f32x4 z[2];
   {
@@ -1232,11 +1273,6 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
         mU[j * kF + y] = u;
         mZ[j * kF + y] = z[t][r];
       }
-    float through = 0.0f;
-#pragma unroll
-    for (int a = 0; a < ND; ++a)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) through = fmaf(S[a][r], R[a][r], through);
     rest = wave_sum(fmaf(keep, through, rest));
     if (lane == 0) sum_1[wave] = rest;
     if (g.dstate0 && y0 < dv) {
@@ -1250,10 +1286,13 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
         }
       const typename M::Sum zt = M::sum_terms(zs), dt = M::sum_terms(os);
       const auto to_state = buffer(g.dstate0 + (size_t)bh * state, (unsigned)state * 4);
+      const unsigned y_at = WHOLE || y < dv ? (unsigned)(8 * lg * dv + y) * 4 : kOutside;
 #pragma unroll
       for (int a = 0; a < ND; ++a) {
         if (32 * (a >> 1) >= dk) continue;
-        f32x4 acc = keep * R[a];
+        f32x4 acc;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[r] = keep * load_float(from_r, y_at, (32 * (a >> 1) + 4 * (a & 1) + r) * dv * 4);
         acc = M::mma(columns<DTYPE>(tk, L::kPitch, col_k(a, 0), 8, li, lg), zt, acc);
         acc = M::mma(columns<DTYPE>(tq, L::kPitch, col_k(a, 0), 8, li, lg), dt, acc);
 #pragma unroll
@@ -1322,6 +1361,14 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
       made[2][r] = -(i > j ? low[r] * decays[r] : high[r] * up);
     }
   }
+  // (on their way for what follows: rows y0 + li of both states, eight numbers at 32 s + 8 lg; past dv they are the next row's, or zero
+  // behind the last one, and what they meet is zero)
+  float row_s[D / 32][8], row_r[D / 32][8];
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    load_words<8>((unsigned*)row_s[s], from_s, (unsigned)(y * dv + 32 * s + 8 * lg) * 4);
+    load_words<8>((unsigned*)row_r[s], from_r, (unsigned)(y * dv + 32 * s + 8 * lg) * 4);
+  }
   f32x4 row_sums = made[3];
   float col_sum = (made[3][0] + made[3][1]) + (made[3][2] + made[3][3]);
 #pragma unroll
@@ -1373,15 +1420,10 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
   f32x4 dq[2] = {}, dkk[2] = {};
   if (y0 < dk) {
     f32x4 zs[2] = {}, us[2] = {};
-    const int x = y0 + li;
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
       if (32 * s >= dv) continue;
-      // (columns past dv are the next row's numbers, or zero behind the last one: what they meet is zero)
-      float a[8], b[8];
-      load_words<8>((unsigned*)a, from_s, (unsigned)(x * dv + 32 * s + 8 * lg) * 4);
-      load_words<8>((unsigned*)b, from_r, (unsigned)(x * dv + 32 * s + 8 * lg) * 4);
-      const typename M::Out st = M::out_terms(a), rt = M::out_terms(b);
+      const typename M::Out st = M::out_terms(row_s[s]), rt = M::out_terms(row_r[s]);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int i = 16 * t + li;
@@ -1408,13 +1450,19 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
   for (int t = 0; t < 2; ++t) {
     const int i = 16 * t + li, c = y0 + 4 * lg;
     if (g.f32 && !kF32) {
-      if (i < valid)
+      float* const at_q = (float*)g.dq + (t0 + i) * step_k + head_k + c;
+      float* const at_k = (float*)g.dk + (t0 + i) * step_k + head_k + c;
+      if (i < valid && c + 4 <= dk) {
+        __builtin_memcpy(at_q, &dq[t], 16);
+        __builtin_memcpy(at_k, &dkk[t], 16);
+      } else if (i < valid) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (c + r < dk) {
-            ((float*)g.dq)[(t0 + i) * step_k + head_k + c + r] = dq[t][r];
-            ((float*)g.dk)[(t0 + i) * step_k + head_k + c + r] = dkk[t][r];
+            at_q[r] = dq[t][r];
+            at_k[r] = dkk[t][r];
           }
+      }
       continue;
     }
     unsigned char* const at = lds + i * L::kPitch + c * M::kBytes;
@@ -1757,7 +1805,7 @@ hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
 template <int DTYPE, int D, bool ALONE>
 hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
   if (!(g.q.vec && g.k.vec && g.v.vec && g.d_o.vec)) return launch_grad<DTYPE, D, ALONE, kAny>(g, st);
-  return g.k.d == D && g.v.d == D ? launch_grad<DTYPE, D, ALONE, kWhole>(g, st) : launch_grad<DTYPE, D, ALONE, kPieces>(g, st);
+  return launch_grad<DTYPE, D, ALONE, kPieces>(g, st);
 }
 template <int DTYPE, int D>
 hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
