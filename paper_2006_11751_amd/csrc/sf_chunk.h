@@ -10,25 +10,12 @@
 
 namespace sf {
 
-namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kThreads = 256;
-
 // n / d for 0 <= n < 2^31, without a division on the device
 struct Divisor {
   unsigned mul, shift;
   __device__ unsigned of(unsigned n) const { return (__umulhi(mul, n) + n) >> shift; }
 };
-Divisor divisor(unsigned d) {
+inline Divisor divisor(unsigned d) {
   unsigned shift = 0;
   while ((1u << shift) < d) ++shift;
   return Divisor{(unsigned)(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
@@ -41,6 +28,19 @@ struct Strided {
   int d;               // columns
   int vec;             // rows are read in 16-byte pieces
 };
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
 
 __device__ inline unsigned pack_bf16(float a, float b) {
   const f32x2 v = {a, b};
