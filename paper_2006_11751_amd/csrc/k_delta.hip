@@ -71,6 +71,11 @@ __global__ __launch_bounds__(kThreads) void delta_chunks_kernel(DeltaArgs g) {
   if (lane < kStepWords / 4) *(f32x4*)(out + (BACK ? 3 : 2) * kDense + 4 * lane) = *(const f32x4*)((const float*)&steps + 4 * lane);
 }
 
+// Where element (x, y) of what a piece makes of a state lies: tiles of 16 x 16, of which a lane of the join has four neighbours of a row.
+__host__ __device__ inline int up16(int d) { return (d + 15) & ~15; }
+__host__ __device__ inline int64_t through_size(int dk) { return (int64_t)up16(dk) * up16(dk); }
+__device__ inline int through_at(int dk, int x, int y) { return ((x >> 4) * (up16(dk) >> 4) + (y >> 4)) * 256 + ((y & 15) >> 2) * 64 + (x & 15) * 4 + (y & 3); }
+
 enum Sweep { kResults = 0, kStates = 1, kBack = 2 };
 
 // A workgroup of four waves goes over the chunks of one (row, head), or of one piece of T, for 64 NT columns of v, of which a wave owns 16 NT: its
@@ -474,8 +479,21 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : D == 64 ? 
   if (!has_v) return;
   if (g.piece) {
     const size_t at = (size_t)bh * g.n_seg + seg;
-    if (identity) store_state(g.seg_through + at * dk * dk);
-    else store_state(g.seg_state + at * dk * dv);
+    if (identity) {
+      // by tiles of 16 x 16 as the join reads them; for the gradients its transpose besides
+      float* const to = g.seg_through + at * through_size(dk) * (g.back ? 2 : 1);
+#pragma unroll
+      for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int a = 0; a < ND; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int x = col_k(a, 4 * lg + r), y = v0 + 16 * c + li;
+            if (x >= up16(dk) || y >= up16(dk)) continue;
+            to[through_at(dk, x, y)] = S[c][a][r];
+            if (g.back) to[through_size(dk) + through_at(dk, y, x)] = S[c][a][r];
+          }
+    } else store_state(g.seg_state + at * dk * dv);
     if (!identity && v_block == 0 && tid == 0) g.seg_begin[at] = any_begin ? 1 : 0;
   } else if (g.s_out && seg == (kUp ? g.n_seg - 1 : 0)) {
     store_state(g.s_out + (size_t)bh * dk * dv);
@@ -506,19 +524,14 @@ __global__ __launch_bounds__(512) void delta_join_kernel(DeltaArgs g) {
   };
   auto request = [&](Piece& p, int i) {
     const size_t at = (size_t)bh * g.n_seg + (BACK ? g.n_seg - 1 - i : i);
-    const auto from_m = buffer(g.seg_through + at * dk * dk, (unsigned)(dk * dk) * 4), from_o = buffer(g.seg_state + at * dk * dv, size);
+    const float* const through = g.seg_through + at * through_size(dk) * (g.back ? 2 : 1) + (BACK ? through_size(dk) : 0);
+    const auto from_m = buffer(through, (unsigned)through_size(dk) * 4), from_o = buffer(g.seg_state + at * dk * dv, size);
     p.begin = g.seg_begin[at];
+    const int tiles = up16(dk) >> 4;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      // (of a matrix's row what lies behind its columns is the next row's or zero, and meets rows of the state that are zero)
-      const int a = x0 + li, b = 16 * s + 4 * lg;
-      if constexpr (BACK) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) p.m[s][r] = load_float(from_m, a < dk ? (unsigned)(b * dk + a) * 4 : kOutside, r * dk * 4);
-      } else {
-        p.m[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from_m, b < dk ? (unsigned)(a * dk + b) * 4 : kOutside, 0, 0));
-      }
-    }
+    for (int s = 0; s < 8; ++s)
+      p.m[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                             from_m, wave < tiles && s < tiles ? (unsigned)((wave * tiles + s) * 256 + lane * 4) * 4 : kOutside, 0, 0));
 #pragma unroll
     for (int r = 0; r < 4; ++r) p.own[r] = load_float(from_o, y_at, r * dv * 4);
   };
@@ -692,16 +705,32 @@ bool overlap(const sf_deltarule_config* c, const float* a, const float* b) {
 
 int chunks_of(const sf_deltarule_config* c) { return (c->T + C - 1) / C; }
 
-// Pieces of T where the workgroups that go over the chunks (one for each 64 columns of a head) leave CUs idle.
+// Pieces of T where heads are few: a pass over the pieces with the identity's columns besides, and as many steps in a row to join them as there
+// are pieces, for chunks in a row that are fewer by that factor.  Both grow together least at a number of pieces near the root of
+// twice the chunks, while the workgroups (w, one for each 64 columns of a head) find CUs that are idle; from w = 128 on no number pays.
+// us with 1, 4, 8, 16, 32 pieces, bf16, forwards | backwards (H heads over all rows):
+//   H x columns, T      w
+//    8 x  64, 1024      8    67  45  36  39    -  | 146  103   83   87    -
+//    8 x  64, 16384     8   933 436 237 146  119  | 2052 1049 600  392  323
+//    8 x 128, 512      16    49  41  40   -    -  | 118  102   97    -    -
+//    8 x 128, 4096     16   323 164 102  88  104  | 769  439  302  262  298
+//    8 x 128, 16384    16  1270 586 322 221  212  | 3038 1618 1026 774  782
+//   32 x  64, 1024     32    68  48  42  50    -  | 165  126  109  124    -
+//   64 x  64, 2048     64   133  91  83  93  126  | 356  266  245  273  333
+//   32 x 128, 1024     64    90  73  74  93    -  | 267  228  237  283    -
+//   32 x 128, 4096     64   336 206 182 190  230  | 1020 747  713  733  855
+//  128 x  64, 1024    128    76  82  90 117    -  | 237  246  267  315    -
+//   64 x 128, 2048    128   182 184 190 224  335  | 694  716  731  847 1059
 struct Split {
   int n_seg, seg_len;
 };
 Split split_of(const sf_deltarule_config* c) {
-  const int64_t lanes = (int64_t)c->N * c->H * (c->dv > DV ? 2 : 1);
+  const int64_t w = (int64_t)c->N * c->H * (std::max(c->dk, c->dv) > DV ? 2 : 1);
   const int chunks = chunks_of(c);
-  if (lanes == 0 || lanes > 128 || chunks < 16) return Split{1, std::max(1, chunks) * C};
-  const int want = (int)std::min<int64_t>((512 + lanes - 1) / lanes, 32);
-  const int per = std::max(8, (chunks + want - 1) / want);
+  if (w == 0 || w > 64 || chunks < std::max<int64_t>(16, w / 2)) return Split{1, std::max(1, chunks) * C};
+  int want = 1;
+  while ((want + 1) * (want + 1) <= 2 * chunks && want + 1 <= 512 / w && want < 32) ++want;
+  const int per = (chunks + want - 1) / want;
   return Split{(chunks + per - 1) / per, per * C};
 }
 
@@ -717,7 +746,7 @@ Workspace workspace_of(const sf_deltarule_config* c, int backward) {
   if (c->T > C) w.made = align256(lanes * chunks * made_words(backward) * 4);
   if (s.n_seg > 1) {
     w.seg_state = align256(lanes * s.n_seg * state);
-    w.seg_through = align256(lanes * s.n_seg * c->dk * c->dk * 4);
+    w.seg_through = align256(lanes * s.n_seg * through_size(c->dk) * (backward ? 8 : 4));
     w.seg_begin = align256(lanes * s.n_seg * 4);
   }
   if (backward) {
@@ -807,7 +836,7 @@ template <int DTYPE, int D, int SWEEP, bool ALONE>
 void launch_sweep(DeltaArgs& g, bool vec, hipStream_t st) {
   if (!vec) return launch_sweep<DTYPE, D, 1, SWEEP, ALONE, kAny>(g, st);
   if constexpr (!ALONE)
-    if (g.v.d > DV) {
+    if (g.v.d > DV && (int64_t)g.N * g.H * g.n_seg * (g.piece && SWEEP == kStates ? 4 : 2) >= 1024) {
       const bool whole = g.k.d == D && g.v.d == 2 * DV && !(g.piece && SWEEP == kStates && D == 64);  // (the identity has D columns)
       return whole ? launch_sweep<DTYPE, D, 2, SWEEP, ALONE, kWhole>(g, st) : launch_sweep<DTYPE, D, 2, SWEEP, ALONE, kPieces>(g, st);
     }

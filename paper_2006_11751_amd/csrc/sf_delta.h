@@ -28,7 +28,7 @@ struct DeltaArgs {
   // pieces of T, of whole chunks
   int n_seg, seg_len, piece;      // piece: the pieces' own states are what is made
   float* seg_state;               // [N * H][n_seg][dk * dv] first the pieces' own states, then what enters them
-  float* seg_through;             // [N * H][n_seg][dk * dk] what a piece makes of the state that enters it
+  float* seg_through;             // [N * H][n_seg] what a piece makes of the state that enters it, dk x dk by tiles (backwards: and its transpose)
   int* seg_begin;                 // [N * H][n_seg] an episode begins in the piece
   int T, N, H, chunks, back;
   int blocks_v, blocks;           // workgroups of a (row, head): for v's columns; and for the identity's besides
