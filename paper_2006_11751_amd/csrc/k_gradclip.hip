@@ -8,6 +8,10 @@
 //
 // Tensors are described in the launches' arguments, up to kTensors of them in one; no table has to be copied to the device, and a
 // recorded graph holds its own.
+//
+// Bound by memory.  54 tensors, 856 MB: 184 us for the squares (4.7 TB/s), 319 to read again and write (5.4); half the chunks 203 and 339, four
+// pieces ahead in place of eight 187 and 318.  Few numbers: 16 tensors of 11.5 MB 4.6 and 6.0 us, 300 tensors of all sizes, 67 MB, in three
+// launches a pass 24 and 37 us.
 #include <math.h>
 
 #include <algorithm>
@@ -24,9 +28,9 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kTensors = 120;      // of one launch: its arguments stay under 4 KB
-constexpr int kChunks = 1024;      // of the whole list, and one more for each tensor's rest
+constexpr int kChunks = 2048;      // of the whole list, and one more for each tensor's rest
 constexpr int64_t kLeast = 16384;  // numbers of a chunk, and what it is a multiple of
-constexpr int kAhead = 4;          // pieces of 16 bytes that a thread has on their way
+constexpr int kAhead = 8;          // pieces of 16 bytes that a thread has on their way
 
 struct ClipTensor {
   const void* in;
@@ -110,7 +114,10 @@ __device__ inline double squares(const unsigned char* p, int64_t n) {
     const double a = BF16 ? bf16_lo(((const uint16_t*)p)[e]) : ((const float*)p)[e];
     sum[1] = fma(a, a, sum[1]);
   }
-  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  double all = 0.0;
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a) all += sum[a];
+  return all;
 }
 
 __global__ __launch_bounds__(kThreads) void clip_squares_kernel(ClipArgs g) {

@@ -17,6 +17,7 @@ by the shapes, strides, types and devices of its arguments, and the checks are m
 They are not part of autograd's graph: results carry no history, whether or not an argument requires a gradient, and the
 gradients are what the *_backward functions return.
 """
+import array
 import ctypes as C
 import operator
 
@@ -632,7 +633,7 @@ def _list_key(name, tensors):
 
 
 class _ListPlan(_Plan):
-    __slots__ = ("sizes", "types", "kinds")
+    __slots__ = ("sizes", "types")
 
 
 def clip_gradients(grads, max_norm, eps=1e-6, in_place=True, out=None, stream=None):
@@ -650,7 +651,7 @@ def clip_gradients(grads, max_norm, eps=1e-6, in_place=True, out=None, stream=No
     torch = binding._torch()
     data_ptr = torch.Tensor.data_ptr
     norm, = _results(out, plan)
-    pointers = plan.kinds(*map(data_ptr, grads))
+    pointers = array.array("Q", map(data_ptr, grads))
     results = pointers
     if not in_place:
         to = out.get("grads")
@@ -658,9 +659,10 @@ def clip_gradients(grads, max_norm, eps=1e-6, in_place=True, out=None, stream=No
             to = out["grads"] = [torch.empty_like(g) for g in grads]
         elif len(to) != len(grads) or _list_key("out['grads']", to) != key:
             _refuse("out['grads'] does not fit: %d tensors of the same sizes, types and strides as the gradients are wanted" % len(grads))
-        results = plan.kinds(*map(data_ptr, to))
+        results = array.array("Q", map(data_ptr, to))
     config = SfGradclipConfig(C.sizeof(SfGradclipConfig), len(grads), max_norm, eps)
-    _check(_lib.sf_gradclip(C.addressof(config), pointers, plan.sizes, plan.types, results, norm, _workspace(out, plan), _stream(plan.index)))
+    _check(_lib.sf_gradclip(C.addressof(config), pointers.buffer_info()[0], plan.sizes, plan.types, results.buffer_info()[0], norm,
+                            _workspace(out, plan), _stream(plan.index)))
     return out
 
 
@@ -674,5 +676,5 @@ def _clip_plan(grads, key):
     n = len(grads)
     sizes = (C.c_int64 * n)(*key[1])
     plan = _ListPlan(SfGradclipConfig(), (("norm", (1,), binding._torch().float32),), _lib.sf_gradclip_workspace_bytes(n, sizes), grads[0].device)
-    plan.key, plan.sizes, plan.types, plan.kinds = key, sizes, (C.c_int32 * n)(*types), C.c_void_p * n
+    plan.key, plan.sizes, plan.types = key, sizes, (C.c_int32 * n)(*types)
     return plan

@@ -57,8 +57,8 @@ def test_workspace_bytes():
     size = lambda *s: lib.sf_gradclip_workspace_bytes(len(s), (C.c_int64 * len(s))(*s))
     assert size() == 0 and size(0, 0) == 0 and size(1) == 256 and size(*[1] * 40) == 512
     assert size(-1) == -1 and lib.sf_gradclip_workspace_bytes(1, None) == -1
-    # a number for each chunk, at most 1024 and one more for each tensor's rest
-    assert size(1 << 40) <= 8 * 1025 + 256 and size(1 << 30, 1, 1 << 31) <= 8 * 1027 + 256
+    # a number for each chunk, at most 2048 and one more for each tensor's rest
+    assert size(1 << 40) <= 8 * 2049 + 256 and size(1 << 30, 1, 1 << 31) <= 8 * 2051 + 256
 
 
 def test_the_binding_refuses():

@@ -41,6 +41,30 @@ def test_head_sizes(torch_cuda, dk, dv, T, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 128), (40, 72), (100, 24), (13, 7), (127, 65), (72, 128), (16, 96)])
+def test_pieces(torch_cuda, dk, dv, dtype):
+    """Few heads and a long axis: T is cut; the last chunk is not whole."""
+    x, do, ds = ref.make(1100, 2, 3, 1, dk, dv, dtype, seed=dk, p_done=0.01)
+    both(torch_cuda, x, do, ds, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dk,dv", [(64, 128), (128, 128), (40, 72), (16, 96), (100, 120)])
+def test_many_heads_with_wide_values(torch_cuda, dk, dv, dtype):
+    """(128 columns of v for each workgroup.)"""
+    x, do, ds = ref.make(70, 64, 8, 8, dk, dv, dtype, seed=dv)
+    both(torch_cuda, x, do, ds, dtype)
+
+
+def test_many_pieces_with_wide_values(torch_cuda):
+    torch = torch_cuda
+    x, _, _ = ref.make(16390, 1, 8, 4, 24, 72, "bf16", seed=7, p_done=0.0005, memory=300.0)
+    got = call(x)
+    want, size = ref.oracle(x)
+    ref.check(got, want, size, 24, 72, 301.0, True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("T", [30, 90])
 @pytest.mark.parametrize("H,Hk", [(4, 1), (6, 2), (3, 3), (1, 1), (24, 8)])
 def test_shared_heads(torch_cuda, H, Hk, T, dtype):
@@ -50,7 +74,7 @@ def test_shared_heads(torch_cuda, H, Hk, T, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("marks", ["none", "null", "first", "all", "last", "edges"])
-@pytest.mark.parametrize("T", [32, 333])
+@pytest.mark.parametrize("T", [32, 333, 900])
 def test_episode_ends(torch_cuda, T, marks, dtype):
     torch = torch_cuda
     x, do, ds = ref.make(T, 2, 2, 2, 32, 64, dtype, seed=5, memory=100.0)
@@ -71,7 +95,7 @@ def test_episode_ends(torch_cuda, T, marks, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("T", [30, 300])
+@pytest.mark.parametrize("T", [30, 300, 900])
 def test_decays_of_zero_and_one_and_no_state(torch_cuda, T, dtype):
     torch = torch_cuda
     x, do, _ = ref.make(T, 2, 4, 2, 64, 64, dtype, p_done=0.01, seed=9)
@@ -140,7 +164,7 @@ def test_results_at_odd_addresses_and_nothing_behind_them(torch_cuda):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("T,dk,dv", [(32, 64, 64), (100, 64, 64), (100, 40, 128)])
+@pytest.mark.parametrize("T,dk,dv", [(32, 64, 64), (100, 64, 64), (100, 40, 128), (700, 64, 64), (700, 128, 72)])
 def test_not_finite_values_stay_where_they_are(torch_cuda, T, dk, dv, dtype):
     """An episode with NaN and infinities in it: the ones before and behind it are as if it were not there, and so are the
     results and query gradients of its own steps before the first of them."""
