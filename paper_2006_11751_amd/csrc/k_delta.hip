@@ -85,7 +85,7 @@ enum Sweep { kResults = 0, kStates = 1, kBack = 2 };
 //   kResults: o and the last state;  kStates: the states that enter the chunks, or the last one of a piece;  kBack: R, from the last chunk to the first
 // ALONE: of one chunk, whose matrices the first wave makes (else they are read).
 template <int DTYPE, int D, int NT, int SWEEP, bool ALONE, int KNOWN>
-__global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : D == 64 ? 4 : 3) void delta_sweep_kernel(DeltaArgs g) {
+__global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : (D == 64 ? 4 : 3) - ALONE) void delta_sweep_kernel(DeltaArgs g) {
   typedef Num<DTYPE> M;
   typedef SweepLds<DTYPE, D, NT> L;
   constexpr int W = M::kPieceWords, NP = C * D / 8 / kThreads, ND = D / 16, kRow = D / 8, kRowV = DV * NT / 8;
@@ -112,10 +112,8 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : D == 64 ? 
   int* const flag = (int*)(lds + L::kFlag);
 
   if (tid < 2) flag[tid] = 0;
-  if constexpr (ALONE) {
-    __syncthreads();
-    if (wave == 0) make_chunk<DTYPE, D, SWEEP == kBack, VEC>(g, n, h, hk, 0, g.T, lane, steps, (float*)(lds + L::kA), mP, mT);
-  }
+  StepIn in = {};
+  if constexpr (ALONE) in = read_step(g, n, h, 0, g.T, lane);
 
   const int v0 = v_block + 16 * NT * wave;  // this wave's columns of v, by tiles of 16; this lane's are v0 + 16 c + li
   const bool has_v = WHOLE || v0 < dv;
@@ -217,10 +215,10 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : D == 64 ? 
 
   if (t_begin < t_end) request(begin_c);
   bool any_begin = false;
-  for (int c = kUp ? first : last, turn = 0; t_begin < t_end && (kUp ? c <= last : c >= first); c += kUp ? 1 : -1, turn ^= 1) {
+  for (int c = kUp ? first : last, turn = 0; t_begin < t_end && (ALONE ? turn == 0 : kUp ? c <= last : c >= first); c += kUp ? 1 : -1, turn ^= 1) {
     const int t0 = c * C, valid = min(C, g.T - t0);
     if (SWEEP != kResults && g.kept && has_v) store_state(g.kept + ((size_t)bh * g.chunks + c) * ((size_t)dk * dv));
-    if constexpr (!ALONE) __syncthreads();  // the chunk before has been read
+    __syncthreads();  // the chunk before has been read
     float test = 0.0f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -239,10 +237,36 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : D == 64 ? 
       *(f32x4*)(mT + to) = n_t;
       if constexpr (kQ) *(f32x4*)(mP + to) = n_p;
       if (tid < kStepWords / 4) *(f32x4*)((float*)&steps + 4 * tid) = n_steps;
+    } else if (wave == 0) {
+      put_steps(steps, in, (unsigned)__ballot(begins(in)), valid, lane);
     }
     if (test != 0.0f) flag[turn] = 1;
     __syncthreads();
-    if (c != (kUp ? last : first)) request(kUp ? c + 1 : c - 1);
+    if constexpr (ALONE) {
+      // A^T and P, a tile of 16 x 16 of each a wave
+      const int I = wave >> 1, J = wave & 1;
+      float* const mA = (float*)(lds + L::kA);
+      f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, p = a;
+      if (J <= I) {
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+          if (!has_k(s)) continue;
+          const int at = (32 * s + 8 * lg) * M::kBytes;
+          const auto ki = M::row(tk + (16 * I + li) * L::kPitch + at), kj = M::row(tk + (16 * J + li) * L::kPitch + at);
+          a = M::mma(ki, kj, a);                                                 // [i][j]
+          p = M::mma(kj, M::row(tq + (16 * I + li) * L::kPitch + at), p);  // [j][i]
+        }
+        a = decayed(steps, a, I, J, true, true, 1.0f, li, lg);
+        p = decayed(steps, p, J, I, false, false, g.scale, li, lg);
+      }
+      *(f32x4*)(mA + (16 * J + li) * kMat + 16 * I + 4 * lg) = a;
+      *(f32x4*)(mP + (16 * I + li) * kMat + 16 * J + 4 * lg) = p;
+      __syncthreads();
+      if (wave == 3) invert(mA, steps.beta, mT, lane);
+    }
+    if constexpr (!ALONE) {
+      if (c != (kUp ? last : first)) request(kUp ? c + 1 : c - 1);
+    }
     // (marks of begins are where the episode's number grows)
     const int my_ep = steps.ep[lane & (C - 1)];
     const float my_steps = fmaf(steps.gh[lane & (C - 1)], 0.0f, steps.beta[lane & (C - 1)] * 0.0f);
@@ -251,7 +275,10 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : D == 64 ? 
     any_begin = any_begin || marked;
     const bool odd = flag[turn] != 0 || __any(my_steps != 0.0f);
     if (tid == 0) flag[turn ^ 1] = 0;  // (read by all before the barrier above)
-    if (!has_v) continue;
+    if (!has_v) {
+      if constexpr (ALONE) __syncthreads();
+      continue;
+    }
 
     // what the state gives the steps: k S, and q S
     f32x4 ks[NT][2] = {}, qs[NT][2] = {};
@@ -282,6 +309,7 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : D == 64 ? 
         }
       }
     }
+    if constexpr (ALONE) __syncthreads();  // T is there
     // (of a state with something not finite every product is not finite: that an episode begins in the chunk does not stop it)
     float state_test = 0.0f;
 #pragma unroll
@@ -562,7 +590,9 @@ __global__ __launch_bounds__(512) void delta_join_kernel(DeltaArgs g) {
 
 // Sums of the gradients of shared heads: in [rows][H][d] fp32, out [rows][H / share][d].
 template <int DTYPE>
-__global__ __launch_bounds__(kThreads) void delta_share_kernel(const float* in, void* out, int64_t n_out, int d, int share) {
+__global__ __launch_bounds__(kThreads) void delta_share_kernel(const float* in_q, const float* in_k, void* out_q, void* out_k, int64_t n_out, int d, int share) {
+  const float* const in = blockIdx.y ? in_k : in_q;
+  void* const out = blockIdx.y ? out_k : out_q;
   for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < n_out; e += (int64_t)gridDim.x * kThreads) {
     const float* x = in + e / d * share * d + e % d;
     float sum = 0.0f;
@@ -995,8 +1025,7 @@ extern "C" int sf_deltarule_backward(const sf_deltarule_config* cfg, const void*
     const int64_t count = (int64_t)cfg->T * cfg->N * cfg->Hk * cfg->dk;
     const unsigned grid = (unsigned)std::min<int64_t>((count + kThreads - 1) / kThreads, 1 << 20);
     const auto kern = cfg->dtype == SF_DTYPE_BF16 ? delta_share_kernel<SF_DTYPE_BF16> : delta_share_kernel<SF_DTYPE_FP32>;
-    kern<<<grid, kThreads, 0, st>>>(part_q, dq, count, cfg->dk, share);
-    kern<<<grid, kThreads, 0, st>>>(part_k, dk, count, cfg->dk, share);
+    kern<<<dim3(grid, 2), kThreads, 0, st>>>(part_q, part_k, dq, dk, count, cfg->dk, share);
     err = hipGetLastError();
   }
   return launched(fn, err);

@@ -142,8 +142,7 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
           const int at = (32 * s + 8 * lg) * M::kBytes;
           if (32 * s < dk) acc = M::mma(M::row(rows + (16 * I + li) * L::kPitch + at), M::row(tk + (16 * J + li) * L::kPitch + at), acc);
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[r] = decays[r] != 0.0f && (!strict || 16 * I + 4 * lg + r > 16 * J + li) ? acc[r] * decays[r] : 0.0f;
+        acc = decayed(steps, acc, I, J, true, strict, 1.0f, li, lg);
       }
       *(f32x4*)(to_matrix + (16 * J + li) * kMat + 16 * I + 4 * lg) = acc;  // [j][i]
     };

@@ -288,6 +288,22 @@ __device__ inline void invert(const float* at, const float* beta, float* T, int 
   for (int r = 0; r < 4; ++r) T[(16 + 4 * lg + r) * kMat + li] = -t21[r];
 }
 
+// A tile of products of steps with D and the mask: its rows are steps 16 rows + 4 lg + r, its columns 16 columns + li; rows_later: a row is
+// the later step of the two; strict: not the step with itself.
+__device__ inline f32x4 decayed(const Steps& steps, f32x4 x, int rows, int columns, bool rows_later, bool strict, float scale, int li, int lg) {
+  const int c = 16 * columns + li, ec = steps.ep[c];
+  const float hc = steps.gh[c], lc = steps.gl[c];
+  const f32x4 h4 = *(const f32x4*)(steps.gh + 16 * rows + 4 * lg), l4 = *(const f32x4*)(steps.gl + 16 * rows + 4 * lg);
+  const i32x4 e4 = *(const i32x4*)(steps.ep + 16 * rows + 4 * lg);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int later = rows_later ? 16 * rows + 4 * lg + r - c : c - (16 * rows + 4 * lg + r);
+    const float d = rows_later ? decay_of(h4[r], l4[r], hc, lc) : decay_of(hc, lc, h4[r], l4[r]);
+    x[r] = later >= (strict ? 1 : 0) && e4[r] == ec ? x[r] * (scale * d) : 0.0f;
+  }
+  return x;
+}
+
 // One wave: a chunk's Steps, A^T and P (backwards P^T, without the scale) into LDS (pitch kMat).  Keys and queries are read as operands.
 template <int DTYPE, int D, bool BACK, bool VEC>
 __device__ inline void make_products(const DeltaArgs& g, int n, int h, int hk, int t0, int valid, int lane, Steps& steps, float* mA, float* mP) {
@@ -334,34 +350,13 @@ __device__ inline void make_products(const DeltaArgs& g, int n, int h, int hk, i
           a = M::mma(k[I][s], k[J][s], a);                                           // [i][j]
           p = BACK ? M::mma(q[I][s], k[J][s], p) : M::mma(k[J][s], q[I][s], p);  // [i][j], forwards [j][i]
         }
-        // rows are steps 16 R + 4 lg + r of tile R, columns are steps of the other one
-        auto decayed = [&](f32x4 x, int rows, int columns, bool rows_later, bool strict, float scale) {
-          const int c = 16 * columns + li, ec = steps.ep[c];
-          const float hc = steps.gh[c], lc = steps.gl[c];
-          const f32x4 h4 = *(const f32x4*)(steps.gh + 16 * rows + 4 * lg), l4 = *(const f32x4*)(steps.gl + 16 * rows + 4 * lg);
-          const i32x4 e4 = *(const i32x4*)(steps.ep + 16 * rows + 4 * lg);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int later = rows_later ? 16 * rows + 4 * lg + r - c : c - (16 * rows + 4 * lg + r);
-            const float d = rows_later ? decay_of(h4[r], l4[r], hc, lc) : decay_of(hc, lc, h4[r], l4[r]);
-            x[r] = later >= (strict ? 1 : 0) && e4[r] == ec ? x[r] * (scale * d) : 0.0f;
-          }
-          return x;
-        };
-        a = decayed(a, I, J, true, true, 1.0f);
-        p = BACK ? decayed(p, I, J, true, false, 1.0f) : decayed(p, J, I, false, false, g.scale);
+        a = decayed(steps, a, I, J, true, true, 1.0f, li, lg);
+        p = BACK ? decayed(steps, p, I, J, true, false, 1.0f, li, lg) : decayed(steps, p, J, I, false, false, g.scale, li, lg);
       }
       *(f32x4*)(mA + (16 * J + li) * kMat + 16 * I + 4 * lg) = a;                // A^T [j][i]
       if (BACK) *(f32x4*)(mP + (16 * J + li) * kMat + 16 * I + 4 * lg) = p;      // P^T [j][i]
       else *(f32x4*)(mP + (16 * I + li) * kMat + 16 * J + 4 * lg) = p;           // P [i][j]
     }
-  wave_order();
-}
-// And T.
-template <int DTYPE, int D, bool BACK, bool VEC>
-__device__ inline void make_chunk(const DeltaArgs& g, int n, int h, int hk, int t0, int valid, int lane, Steps& steps, float* mA, float* mP, float* mT) {
-  make_products<DTYPE, D, BACK, VEC>(g, n, h, hk, t0, valid, lane, steps, mA, mP);
-  invert(mA, steps.beta, mT, lane);
   wave_order();
 }
 
