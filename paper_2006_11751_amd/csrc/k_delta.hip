@@ -588,16 +588,33 @@ __global__ __launch_bounds__(512) void delta_join_kernel(DeltaArgs g) {
   }
 }
 
-// Sums of the gradients of shared heads: in [rows][H][d] fp32, out [rows][H / share][d].
-template <int DTYPE>
-__global__ __launch_bounds__(kThreads) void delta_share_kernel(const float* in_q, const float* in_k, void* out_q, void* out_k, int64_t n_out, int d, int share) {
+// Sums of the gradients of shared heads, of dq and of dk: in [rows][H][d] fp32, out [rows][H / share][d], each in one order.  A thread has
+// PER neighbours of a row of d; 2^lanes_log2 threads have a row.
+template <int DTYPE, int PER>
+__global__ __launch_bounds__(kThreads) void delta_share_kernel(const float* in_q, const float* in_k, void* out_q, void* out_k, int64_t rows, int d, int share,
+                                                               int lanes_log2) {
+  typedef Num<DTYPE> M;
   const float* const in = blockIdx.y ? in_k : in_q;
-  void* const out = blockIdx.y ? out_k : out_q;
-  for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < n_out; e += (int64_t)gridDim.x * kThreads) {
-    const float* x = in + e / d * share * d + e % d;
-    float sum = 0.0f;
-    for (int i = 0; i < share; ++i) sum += x[(int64_t)i * d];
-    Num<DTYPE>::store((unsigned char*)out + e * Num<DTYPE>::kBytes, sum);
+  unsigned char* const out = (unsigned char*)(blockIdx.y ? out_k : out_q);
+  const int64_t row = (int64_t)blockIdx.x * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2);
+  const int col = (threadIdx.x & ((1 << lanes_log2) - 1)) * PER;
+  if (row >= rows || col >= d) return;
+  const float* const x = in + row * share * d + col;
+  float sum[PER] = {};
+  for (int i = 0; i < share; ++i) {
+    float y[PER];
+    __builtin_memcpy(y, x + (int64_t)i * d, sizeof y);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) sum[j] += y[j];
+  }
+  unsigned char* const to = out + (row * d + col) * M::kBytes;
+  if constexpr (DTYPE == SF_DTYPE_BF16 && PER == 4) {
+    const u32x2 two = {pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+    __builtin_memcpy(to, &two, 8);
+  } else if constexpr (PER == 4) {
+    __builtin_memcpy(to, sum, 16);
+  } else {
+    M::store(to, sum[0]);
   }
 }
 
@@ -1022,10 +1039,14 @@ extern "C" int sf_deltarule_backward(const sf_deltarule_config* cfg, const void*
   g.f32 = share > 1;
   err = delta_gradients(cfg, g, st);
   if (err == hipSuccess && share > 1) {
-    const int64_t count = (int64_t)cfg->T * cfg->N * cfg->Hk * cfg->dk;
-    const unsigned grid = (unsigned)std::min<int64_t>((count + kThreads - 1) / kThreads, 1 << 20);
-    const auto kern = cfg->dtype == SF_DTYPE_BF16 ? delta_share_kernel<SF_DTYPE_BF16> : delta_share_kernel<SF_DTYPE_FP32>;
-    kern<<<dim3(grid, 2), kThreads, 0, st>>>(part_q, part_k, dq, dk, count, cfg->dk, share);
+    const int64_t rows = (int64_t)cfg->T * cfg->N * cfg->Hk;
+    const int per = cfg->dk % 4 == 0 ? 4 : 1;
+    int lanes_log2 = 0;
+    while (per << lanes_log2 < cfg->dk) ++lanes_log2;
+    const int64_t in_block = kThreads >> lanes_log2, blocks = (rows + in_block - 1) / in_block;
+    const auto kern = cfg->dtype == SF_DTYPE_BF16 ? (per == 4 ? delta_share_kernel<SF_DTYPE_BF16, 4> : delta_share_kernel<SF_DTYPE_BF16, 1>)
+                                                  : (per == 4 ? delta_share_kernel<SF_DTYPE_FP32, 4> : delta_share_kernel<SF_DTYPE_FP32, 1>);
+    kern<<<dim3((unsigned)blocks, 2), kThreads, 0, st>>>(part_q, part_k, dq, dk, rows, cfg->dk, share, lanes_log2);
     err = hipGetLastError();
   }
   return launched(fn, err);

@@ -10,13 +10,15 @@ template <int DTYPE, int D>
 struct GradLds {
   static constexpr int kPitch = Pitch<DTYPE, D>::value, kTile = C * kPitch, kPitchF = (D + 4) * 4, kTileF = C * kPitchF;
   static constexpr int kWaves = D / 16, kThreads = 64 * kWaves;
-  // q, k, v, do; u and z in fp32; A^T, P^T and T, which make room for dP D and its like as operands
-  static constexpr int kU = 4 * kTile, kZ = kU + kTileF, kA = kZ + kTileF, kP = kA + C * kMat * 4, kT = kP + C * kMat * 4,
+  // q, k, do, v; u and z in fp32, before them slabs of the states, and with 128 columns in the place of z first v (two workgroups a CU
+  // then); A^T, P^T and T, which make room for dP D and its like as operands
+  static constexpr bool kShared = D == 128;
+  static constexpr int kU = (kShared ? 3 : 4) * kTile, kZ = kU + kTileF, kV = kShared ? kZ : 3 * kTile, kA = kZ + kTileF, kP = kA + C * kMat * 4, kT = kP + C * kMat * 4,
                        kOperand = 4096, kM = kA;  // [3] of two terms (or halves) of 2 x 64 lanes x 16 bytes
-  static_assert(3 * kOperand <= 3 * C * kMat * 4, "operands");
+  static_assert(3 * kOperand <= 3 * C * kMat * 4 && kTile <= kTileF, "operands in the matrices' place, v in that of z");
   static constexpr int kSteps = kT + C * kMat * 4, kFlag = kSteps + (int)sizeof(Steps);
-  static constexpr int kSums = kFlag + 32;  // float [kWaves + 4][C] of each kind
-  static constexpr int kSumRows = 2 * kWaves + 5;
+  static constexpr int kSums = kFlag + 32;
+  static constexpr int kSumRows = 2 * kWaves + (kWaves == 4 ? 4 : 8) + 1;  // of C numbers
   static constexpr int kBytes = kSums + kSumRows * C * 4;
 };
 
@@ -24,7 +26,7 @@ struct GradLds {
 // columns of v and then for 16 of k.
 // ALONE: the only chunk, whose matrices the first wave makes (else they are read).
 template <int DTYPE, int D, bool ALONE, int KNOWN>
-__global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) void delta_grad_kernel(DeltaArgs g) {
+__global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4) void delta_grad_kernel(DeltaArgs g) {
   typedef Num<DTYPE> M;
   typedef GradLds<DTYPE, D> L;
   constexpr bool VEC = KNOWN != kAny, WHOLE = KNOWN == kWhole;
@@ -39,14 +41,14 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h);
   const int dk = WHOLE ? D : g.k.d, dv = WHOLE ? D : g.v.d, t0 = chunk * C, valid = min(C, g.T - t0);
   auto base = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
-  unsigned char *const tq = lds, *const tk = lds + L::kTile, *const tv = lds + 2 * L::kTile, *const to = lds + 3 * L::kTile;
+  unsigned char *const tq = lds, *const tk = lds + L::kTile, *const to = lds + 2 * L::kTile, *const tv = lds + L::kV;
   float *const mU = (float*)(lds + L::kU), *const mZ = (float*)(lds + L::kZ), *const mA = (float*)(lds + L::kA), *const mP = (float*)(lds + L::kP),
                *const mT = (float*)(lds + L::kT);
   constexpr int kF = D + 4;
   int* const flag = (int*)(lds + L::kFlag);  // by waves
   Steps& steps = *(Steps*)(lds + L::kSteps);
   // by waves: sums over their columns for each step; by tiles: of dP P + dA A along its rows and columns; a number of each wave
-  float *const sum_b = (float*)(lds + L::kSums), *const sum_g = sum_b + L::kWaves * C, *const sum_m = sum_g + L::kWaves * C, *const sum_1 = sum_m + 4 * C;
+  float *const sum_b = (float*)(lds + L::kSums), *const sum_g = sum_b + L::kWaves * C, *const sum_m = sum_g + L::kWaves * C, *const sum_1 = sum_m + (L::kWaves == 4 ? 4 : 8) * C;
 
   const size_t state = (size_t)dk * dv;
   const float* const s0 = g.kept_s ? g.kept_s + ((size_t)bh * g.chunks + chunk) * state : nullptr;
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
   float test = 0.0f;
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
-    put_piece<DTYPE>(lds + a * L::kTile, L::kPitch, w[a], tid, kRow8);
+    put_piece<DTYPE>(a == 0 ? tq : a == 1 ? tk : a == 2 ? tv : to, L::kPitch, w[a], tid, kRow8);
     test = finite_test<DTYPE>(w[a], test);
   }
   if constexpr (!ALONE) {
@@ -150,6 +152,16 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
     if (L::kWaves == 4 || wave >= 4) product(tq, mP, false);
   }
 
+  // this wave's columns of v and do
+  typename M::Raw vt, ot;
+  auto own_columns = [&]() {
+    vt = columns<DTYPE>(tv, L::kPitch, y0, 4, li, lg);
+    ot = columns<DTYPE>(to, L::kPitch, y0, 4, li, lg);
+  };
+  if constexpr (L::kShared) {
+    own_columns();
+    __syncthreads();  // v makes room
+  }
   // what the states give the steps; the slabs go through the places of u and z
   f32x4 ks[2] = {}, qs[2] = {}, kr[2] = {};
   float through = 0.0f;
@@ -225,7 +237,10 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
       else M::store((unsigned char*)out + i * M::kBytes, v);
     };
     auto decay = [&](int i, int j) { return decay_of(steps.gh[i], steps.gl[i], steps.gh[j], steps.gl[j]); };
-    float *const dP = mT, *const dA = (float*)tv;  // [i][j], in the places of T and, when e is made, of v
+    // dP and dA [i][j] lie where A^T and P^T [j][i] have nothing; dP's diagonal behind the rows
+    auto dP = [&](int i, int j) -> float& { return mP[i * kMat + (i == j ? C : j)]; };
+    auto dA = [&](int i, int j) -> float& { return mA[i * kMat + j]; };
+    const unsigned char* const v_at = base(g.v) + (int64_t)t0 * g.v.st * M::kBytes;
     for (int e = tid; e < C * C; e += kT) {
       const int i = e / C, j = e % C;
       float a = 0.0f, p = 0.0f;
@@ -237,6 +252,7 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
           a *= decay(i, j);
         }
       }
+      if (j > i) continue;
       mA[j * kMat + i] = a;
       mP[j * kMat + i] = p;
     }
@@ -262,7 +278,7 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
           }
         ks *= steps.ep[i] == 0 ? steps.enter[i] : 0.0f;
         qs *= steps.ep[i] == 0 ? steps.enter[i] * g.scale : 0.0f;
-        e = at(tv, i, tid) - ks;
+        e = M::element(v_at + (i * g.v.st + tid) * M::kBytes) - ks;
         for (int j = 0; j < i; ++j)
           if (steps.ep[j] == steps.ep[i]) e -= mA[j * kMat + i] * steps.beta[j] * mU[j * kF + tid];
         mU[i * kF + tid] = e;
@@ -314,18 +330,18 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
           a -= steps.beta[i] * mZ[i * kF + c] * (steps.beta[j] * mU[j * kF + c]);
         }
       }
-      dP[i * C + j] = p;  // (without the scale, which is in P)
-      dA[i * C + j] = j < i ? a : 0.0f;
+      if (j <= i) dP(i, j) = p;  // (without the scale, which is in P)
+      if (j < i) dA(i, j) = a;
     }
     __syncthreads();
     if (tid < valid) {
       float s = sum_g[tid];
       for (int j = 0; j <= tid; ++j)
         if (steps.ep[j] == steps.ep[tid])
-          s += dP[tid * C + j] * mP[j * kMat + tid] + (j < tid ? dA[tid * C + j] * mA[j * kMat + tid] : 0.0f);
+          s += dP(tid, j) * mP[j * kMat + tid] + (j < tid ? dA(tid, j) * mA[j * kMat + tid] : 0.0f);
       for (int i = tid; i < valid; ++i)
         if (steps.ep[i] == steps.ep[tid])
-          s -= dP[i * C + tid] * mP[tid * kMat + i] + (i > tid ? dA[i * C + tid] * mA[tid * kMat + i] : 0.0f);
+          s -= dP(i, tid) * mP[tid * kMat + i] + (i > tid ? dA(i, tid) * mA[tid * kMat + i] : 0.0f);
       sum_b[tid] = s + (tid == valid - 1 ? tail : 0.0f);
     } else if (tid < C) {
       sum_b[tid] = 0.0f;
@@ -341,14 +357,14 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
       for (int j = 0; j <= t; ++j)
         if (steps.ep[j] == steps.ep[t]) {
           const float d = decay(t, j);
-          q += g.scale * dP[t * C + j] * d * at(tk, j, x);
-          if (j < t) k += dA[t * C + j] * d * at(tk, j, x);
+          q += g.scale * dP(t, j) * d * at(tk, j, x);
+          if (j < t) k += dA(t, j) * d * at(tk, j, x);
         }
       for (int i = t; i < valid; ++i)
         if (steps.ep[i] == steps.ep[t]) {
           const float d = decay(i, t);
-          k += g.scale * dP[i * C + t] * d * at(tq, i, x);
-          if (i > t) k += dA[i * C + t] * d * at(tk, i, x);
+          k += g.scale * dP(i, t) * d * at(tq, i, x);
+          if (i > t) k += dA(i, t) * d * at(tk, i, x);
         }
       if (s0 && steps.ep[t] == 0) {
         float z = 0.0f;
@@ -381,7 +397,7 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
   f32x4 z[2];
   {
-    const typename M::Raw vt = columns<DTYPE>(tv, L::kPitch, y0, 4, li, lg), ot = columns<DTYPE>(to, L::kPitch, y0, 4, li, lg);
+    if constexpr (!L::kShared) own_columns();
     float v[8], o[8];
     M::values(vt, v);
     M::values(ot, o);
@@ -545,7 +561,7 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
     if (li == 0) *(f32x4*)(tile_sums + J * C + 16 * I + 4 * lg) = row_sums;
     if (lg == 0) tile_sums[2 * C + I * C + 16 * J + li] = col_sum;
   } else {
-    float* const mine = (wave < 4 ? (float*)tv : (float*)tv + 4 * C);  // (v has been read)
+    float* const mine = wave < 4 ? tile_sums : tile_sums + 4 * C;
     if (li == 0) *(f32x4*)(mine + J * C + 16 * I + 4 * lg) = row_sums;
     if (lg == 0) mine[2 * C + I * C + 16 * J + li] = col_sum;
   }
@@ -569,8 +585,8 @@ __global__ __launch_bounds__(4 * D, D == 64 && DTYPE == SF_DTYPE_BF16 ? 3 : 2) v
     if (L::kWaves == 4) {
       add(tile_sums);
     } else {
-      add((float*)tv);
-      add((float*)tv + 4 * C);
+      add(tile_sums);
+      add(tile_sums + 4 * C);
     }
     const float d = decay_gradient(i == valid - 1 ? s + rest : s);
     if (lane < valid) {
