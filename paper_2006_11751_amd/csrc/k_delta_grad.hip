@@ -122,7 +122,8 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
   const int e_last = __builtin_amdgcn_readlane(my_ep, valid - 1);
   const bool marked = e_last != 0;
   // steps that an episode begins with: another one's episode than the step before
-  const unsigned begin = (unsigned)__ballot(lane < valid && my_ep != (lane ? __shfl_up(my_ep, 1) : 0));
+  const int ep_before = __shfl_up(my_ep, 1);  // (by all lanes: one that does not take part gives nothing)
+  const unsigned begin = (unsigned)__ballot(lane < valid && my_ep != (lane ? ep_before : 0));
   const float keep = marked ? 0.0f : steps.enter[valid - 1];
 
   // tiles of the chunk's matrices, [i][j] with i in tile I, j in tile J: the first four waves those of A, the last four those of P

@@ -1,7 +1,7 @@
 """The gated delta rule and its gradients, token by token in 64 bits, and how large what enters each result is.
 
 Sizes, for each row and head, by norms over the head's columns and the largest of them over all steps (Cauchy-Schwarz), with C = 32
-steps of a chunk:
+steps of a chunk, or T if that is less:
   o       scale |q| (|S| + C |u|)                 dq  scale |do| (|S| + C |u|)
   dv      |R|                                     dk  |R| |u| + |S| |z| + C (scale |do| |u| |q| + 2 |z| |u|)
   dbeta   |R| |e|      state  |S|   dstate0  |R|  dlog_decay  |R| |S| + C^2 / 2 (scale |do| |u| |q| + |z| |u|)
@@ -17,7 +17,7 @@ import math
 
 import torch
 
-C = 32
+CHUNK = 32
 
 
 def oracle(x, scale=None, do=None, dstate=None):
@@ -26,6 +26,7 @@ def oracle(x, scale=None, do=None, dstate=None):
     T, N, Hk, dk = q.shape
     H, dv = v.shape[2:]
     f64 = dict(dtype=torch.float64, device=q.device)
+    C = min(CHUNK, T)
     scale = dk ** -0.5 if scale is None else scale
     rep = lambda a: a.double().repeat_interleave(H // Hk, 2)
     q, k, v, beta = rep(x["q"]), rep(x["k"]), v.double(), x["beta"].double()
@@ -85,18 +86,19 @@ def oracle(x, scale=None, do=None, dstate=None):
     return g, size
 
 
-def tolerance(name, y, size, dk, dv, length, bf16):
-    n = 2 * (dk + dv + 2 * C) * (C + length)
+def tolerance(name, y, size, dk, dv, length, bf16, T):
+    C = min(CHUNK, T)
+    n = 2 * (dk + dv + 2 * C) * (C + min(length, T))
     tol = n * 2.0 ** -24 * size
     if bf16 and name in ("o", "dq", "dk", "dv"):
         tol = (tol + 3 * 2.0 ** -16 * size) * (1 + 2.0 ** -8) + 2.0 ** -8 * y.abs()
     return tol + 1e-37
 
 
-def check(got, want, size, dk, dv, length, bf16, part=None):
+def check(got, want, size, dk, dv, length, bf16, T, part=None):
     """part: steps that are looked at (of results that have steps)."""
     for name, y in want.items():
-        x, tol = got[name].double(), tolerance(name, y, size[name], dk, dv, length, bf16)
+        x, tol = got[name].double(), tolerance(name, y, size[name], dk, dv, length, bf16, T)
         assert x.shape == y.shape, name
         tol = tol.expand_as(y)
         if part is not None and "state" not in name:

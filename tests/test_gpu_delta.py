@@ -19,7 +19,7 @@ def both(torch, x, do, ds, dtype, scale=None, length=17.0):
     """length: steps that the memory is long (at most T)."""
     got, back = call(x, scale=scale), call(x, do, ds, scale=scale)
     torch.cuda.synchronize()
-    sizes = x["q"].shape[3], x["v"].shape[3], length, dtype == "bf16"
+    sizes = x["q"].shape[3], x["v"].shape[3], length, dtype == "bf16", x["q"].shape[0]
     ref.check(got, *ref.oracle(x, scale), *sizes)
     ref.check(back, *ref.oracle(x, scale, do, ds), *sizes)
     return got, back
@@ -61,7 +61,7 @@ def test_many_pieces_with_wide_values(torch_cuda):
     x, _, _ = ref.make(16390, 1, 8, 4, 24, 72, "bf16", seed=7, p_done=0.0005, memory=300.0)
     got = call(x)
     want, size = ref.oracle(x)
-    ref.check(got, want, size, 24, 72, 301.0, True)
+    ref.check(got, want, size, 24, 72, 301.0, True, 16390)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
@@ -92,6 +92,34 @@ def test_episode_ends(torch_cuda, T, marks, dtype):
         d[T // 2, 1] = 1
     x["done"] = None if marks == "null" else d
     both(torch, x, do, ds, dtype, length=101.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("behind", [0, 30, 62])
+@pytest.mark.parametrize("T", [1, 2, 3, 5])
+def test_every_order_of_episode_begins(torch_cuda, T, behind, dtype):
+    """A row for each; few steps and columns, so that the tolerance is near the roundings.  With `behind` steps before them the T steps cross
+    the border of a chunk: the steps before are of another episode, and nothing of them is looked at."""
+    torch = torch_cuda
+    N = 2 ** T
+    x, do, ds = ref.make(T, N, 2, 2, 8, 8, dtype, seed=40 + T)
+    x["done"] = (torch.arange(N, device="cuda")[None] >> torch.arange(T, device="cuda")[:, None] & 1).byte()
+    if not behind:
+        _, back = both(torch, x, do, ds, dtype)
+    else:
+        y, ydo, _ = ref.make(behind, N, 2, 2, 8, 8, dtype, seed=50)
+        x["done"][0], x["state0"] = 1, None
+        want, wback = ref.oracle(x), ref.oracle(x, None, do, ds)
+        z = {n: torch.cat([y[n], x[n]]) for n in x if n != "state0"}
+        z["state0"] = y["state0"]
+        got, back = call(z), call(z, torch.cat([ydo, do]), ds)
+        sizes = 8, 8, 17.0, dtype == "bf16", T
+        ref.check(dict(o=got["o"][behind:], state=got["state"]), *want, *sizes)
+        back = {n: a[behind:] for n, a in back.items() if n not in ("dstate0", "workspace")}
+        ref.check(back, {n: a for n, a in wback[0].items() if n != "dstate0"}, wback[1], *sizes)
+    # a decay that was made with has a gradient, another one none
+    if T > 1 or not behind:
+        assert torch.equal(back["dlog_decay"] == 0, (x["done"] != 0)[..., None].expand(T, N, 2))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
@@ -184,7 +212,7 @@ def test_not_finite_values_stay_where_they_are(torch_cuda, T, dk, dv, dtype):
     got, back = call(bad), call(bad, bdo, ds)
     want, size = ref.oracle(clean)
     wback, sback = ref.oracle(clean, None, cdo, ds)
-    sizes = dk, dv, 17.0, dtype == "bf16"
+    sizes = dk, dv, 17.0, dtype == "bf16", T
     for part in (slice(behind, T), slice(first, at)):
         ref.check({"o": got["o"]}, {"o": want["o"]}, size, *sizes, part=part)
         ref.check({"dq": back["dq"]}, {"dq": wback["dq"]}, sback, *sizes, part=part)
@@ -221,7 +249,7 @@ def test_a_state_in_place_and_pieces_of_a_trajectory(torch_cuda, dtype):
         out.pop("o", None)
         call(part, out=out)
         o.append(out["o"])
-    ref.check(dict(o=torch.cat(o), state=out["state"]), want, size, 64, 40, 17.0, dtype == "bf16")
+    ref.check(dict(o=torch.cat(o), state=out["state"]), want, size, 64, 40, 17.0, dtype == "bf16", 70)
 
 
 # ---- single steps ---------------------------------------------------------------------------
@@ -245,7 +273,7 @@ def test_steps_on_a_table(torch_cuda, H, Hk, dk, dv, dtype):
     table[ids.long()] = x["state0"]
     before = table.clone()
     got = dict(o=torch.stack([step(x, t, table, ids) for t in range(T)]), state=table[ids.long()])
-    ref.check(got, want, size, dk, dv, 17.0, dtype == "bf16")
+    ref.check(got, want, size, dk, dv, 17.0, dtype == "bf16", T)
     others = torch.ones(n_env, dtype=torch.bool, device="cuda")
     others[ids.long()] = False
     assert torch.equal(table[others], before[others])
@@ -257,16 +285,16 @@ def test_steps_without_ids_and_with_unknown_ones(torch_cuda):
     table = x["state0"].clone()
     o = step(x, 0, table, None)
     want, size = ref.oracle(x)
-    ref.check(dict(o=o[None], state=table), want, size, 32, 32, 17.0, False)
+    ref.check(dict(o=o[None], state=table), want, size, 32, 32, 17.0, False, 1)
     ids = torch.tensor([2, -1, 4, 0], dtype=torch.int32, device="cuda")  # two are not in the table: from a zero state, dropped
     table = x["state0"].clone()
     before = table.clone()
     o = step(x, 0, table, ids)
     y = dict(x, state0=torch.stack([before[2], 0 * before[0], 0 * before[0], before[0]]))
     want, size = ref.oracle(y)
-    ref.check(dict(o=o[None]), dict(o=want["o"]), size, 32, 32, 17.0, False)
+    ref.check(dict(o=o[None]), dict(o=want["o"]), size, 32, 32, 17.0, False, 1)
     assert torch.equal(table[1], before[1]) and torch.equal(table[3], before[3])
-    ref.check(dict(state=table[[2, 0]]), dict(state=want["state"][[0, 3]]), dict(state=size["state"][[0, 3]]), 32, 32, 17.0, False)
+    ref.check(dict(state=table[[2, 0]]), dict(state=want["state"][[0, 3]]), dict(state=size["state"][[0, 3]]), 32, 32, 17.0, False, 1)
 
 
 def test_a_step_does_not_read_the_state_of_an_episode_that_ended(torch_cuda):
@@ -289,7 +317,7 @@ def test_states_behind_32_bits_of_offset(torch_cuda):
     table[ids.long()] = x["state0"]
     o = step(x, 0, table, ids)
     want, size = ref.oracle(x)
-    ref.check(dict(o=o[None], state=table[ids.long()]), want, size, 128, 128, 17.0, True)
+    ref.check(dict(o=o[None], state=table[ids.long()]), want, size, 128, 128, 17.0, True, 1)
     assert not table[:n_env - 2].any()
 
 
