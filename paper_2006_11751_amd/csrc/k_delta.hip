@@ -620,8 +620,8 @@ __global__ __launch_bounds__(kThreads) void delta_share_kernel(const float* in_q
 
 // One step of one (row, head): the state is read and decayed, multiplied with k and q in one go, corrected and written:
 //   o = scale (S'^T q + (q . k) u).
-// A thread holds four neighbours of every (256 / lanes)-th row, so that all its loads are under way at once.
-template <int DTYPE, bool VEC>
+// A thread holds four neighbours of every (256 / lanes)-th row, MOST of them, so that all its loads are under way at once.
+template <int DTYPE, bool VEC, int MOST>
 __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaArgs g, float* table, int n_env, const int32_t* ids, int share, int lanes_log2) {
   typedef Num<DTYPE> M;
   __shared__ __attribute__((aligned(16))) float sq[128], sk[128], part[2][4][128], su[128];
@@ -633,10 +633,9 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaArgs g, float
   const float keep = exp2f(l2);
   const int rows = kThreads >> lanes_log2, row0 = tid >> lanes_log2, c0 = (tid & ((1 << lanes_log2) - 1)) * 4;
   float* s = table + ((int64_t)(known ? id : 0) * g.H + h) * dk * dv;
-  constexpr int kMost = 16;  // rows of a thread: 128 / (256 / 32)
-  float x[kMost][4];
+  float x[MOST][4];
 #pragma unroll
-  for (int i = 0; i < kMost; ++i) {
+  for (int i = 0; i < MOST; ++i) {
     const int r = row0 + i * rows;
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[i][j] = 0.0f;
@@ -658,7 +657,7 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaArgs g, float
   __syncthreads();
   float a[4] = {}, b[4] = {};  // of S'^T k and S'^T q
 #pragma unroll
-  for (int i = 0; i < kMost; ++i) {
+  for (int i = 0; i < MOST; ++i) {
     const int r = row0 + i * rows;
     if (r >= dk || c0 >= dv) continue;
 #pragma unroll
@@ -694,7 +693,7 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaArgs g, float
   if (!known || c0 >= dv) return;
   const f32x4 u4 = *(const f32x4*)(su + c0);
 #pragma unroll
-  for (int i = 0; i < kMost; ++i) {
+  for (int i = 0; i < MOST; ++i) {
     const int r = row0 + i * rows;
     if (r >= dk) continue;
 #pragma unroll
@@ -1079,11 +1078,20 @@ extern "C" int sf_deltarule_step(const sf_deltarule_config* cfg, const void* q, 
   // a thread has four columns; rows of a multiple of four floats are read 16 bytes at a time
   int lanes_log2 = 0;
   while ((4 << lanes_log2) < cfg->dv) ++lanes_log2;
-  if (lanes_log2 < 4) lanes_log2 = 4;  // (256 threads then have 16 rows each of at most 256)
-  const bool vec = cfg->dv % 4 == 0;
-  const auto kern = cfg->dtype == SF_DTYPE_BF16 ? (vec ? delta_step_kernel<SF_DTYPE_BF16, true> : delta_step_kernel<SF_DTYPE_BF16, false>)
-                                                : (vec ? delta_step_kernel<SF_DTYPE_FP32, true> : delta_step_kernel<SF_DTYPE_FP32, false>);
-  kern<<<(unsigned)(cfg->N * cfg->H), kThreads, 0, reinterpret_cast<hipStream_t>(hip_stream)>>>(g, state_table, n_env, env_ids, cfg->H / cfg->Hk,
-                                                                                            lanes_log2);
+  if (lanes_log2 < 4) lanes_log2 = 4;  // (256 threads then have at most 16 rows each)
+  const int most = (cfg->dk + (kThreads >> lanes_log2) - 1) / (kThreads >> lanes_log2);  // rows of a thread
+  const auto launch = [&](auto dtype, auto vec) {
+    constexpr int kType = decltype(dtype)::value;
+    constexpr bool kVec = decltype(vec)::value;
+    const auto kern = most <= 4 ? delta_step_kernel<kType, kVec, 4> : most <= 8 ? delta_step_kernel<kType, kVec, 8> : delta_step_kernel<kType, kVec, 16>;
+    kern<<<(unsigned)(cfg->N * cfg->H), kThreads, 0, reinterpret_cast<hipStream_t>(hip_stream)>>>(g, state_table, n_env, env_ids, cfg->H / cfg->Hk,
+                                                                                              lanes_log2);
+  };
+  const auto by_type = [&](auto vec) {
+    if (cfg->dtype == SF_DTYPE_BF16) launch(std::integral_constant<int, SF_DTYPE_BF16>(), vec);
+    else launch(std::integral_constant<int, SF_DTYPE_FP32>(), vec);
+  };
+  if (cfg->dv % 4 == 0) by_type(std::true_type());
+  else by_type(std::false_type());
   return launched(fn, hipGetLastError());
 }
