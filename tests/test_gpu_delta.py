@@ -324,9 +324,10 @@ def test_states_behind_32_bits_of_offset(torch_cuda):
 # ---- the binding ----------------------------------------------------------------------------
 
 
-def test_the_same_bits_each_time_in_a_graph_and_on_a_stream(torch_cuda):
+@pytest.mark.parametrize("T,d,dtype", [(100, 64, "bf16"), (20, 128, "bf16"), (40, 128, "fp32"), (700, 128, "bf16")])
+def test_the_same_bits_each_time_in_a_graph_and_on_a_stream(torch_cuda, T, d, dtype):
     torch = torch_cuda
-    x, do, ds = ref.make(100, 3, 4, 2, 64, 64, "bf16", seed=1)
+    x, do, ds = ref.make(T, 3, 4, 2, d, d, dtype, seed=1)
     side = torch.cuda.Stream()
     for extra in ((), (do, ds)):
         want = {n: t.clone() for n, t in call(x, *extra).items() if n != "workspace"}
@@ -390,6 +391,43 @@ def test_tensors_may_be_dropped_right_after_a_call_on_another_stream(torch_cuda)
         for n, t in want.items():
             assert torch.equal(got[n], t), n
         del taken
+
+
+def test_a_call_runs_on_its_tensors_device(torch_cuda, monkeypatch):
+    """With another device current (there is one here: that it is another is pretended until torch is told to change to it)."""
+    torch = torch_cuda
+    from paper_2006_11751_amd import memory
+    x, do, ds = ref.make(40, 3, 4, 2, 32, 32, "bf16", seed=1)
+    calls = (lambda: call(x)["state"], lambda: call(x, do, ds)["dk"], lambda: step(x, 0, x["state0"].clone(), None))
+    want = [c() for c in calls]
+    real, told = torch.cuda.device, []
+
+    class device(real):
+        def __init__(self, d):
+            told.append(d)
+            super().__init__(d)
+
+    other = lambda: 0 if told else 1
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", other)
+    monkeypatch.setattr(memory, "_current_device", other, raising=False)
+    got = []
+    for c in calls:
+        del told[:]
+        got.append(c())
+        assert told == [do.device]
+    monkeypatch.undo()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_number_that_changes_in_place_is_read_at_every_call(torch_cuda):
+    torch = torch_cuda
+    x, do, ds = ref.make(40, 2, 2, 2, 16, 16, "fp32", seed=1)
+    scale = torch.tensor(0.5)
+    calls = (lambda: call(x, scale=scale)["o"], lambda: call(x, do, scale=scale)["dq"], lambda: step(x, 0, x["state0"].clone(), None, scale=scale))
+    before = [c() for c in calls]
+    scale.fill_(1.0)
+    assert all(torch.equal(c(), 2 * was) for c, was in zip(calls, before))
 
 
 def test_what_the_binding_refuses(torch_cuda):
