@@ -47,7 +47,6 @@ constexpr int kMat = 36; // a row of a matrix of the chunk's steps, in fp32: 32 
 // A decay that is zero in 32 bits begins the memory anew, as done does.
 constexpr double kLeastLog2 = -126.0;
 
-
 typedef Num<SF_DTYPE_FP32> F32;
 
 // Memory is read and written through buffers that begin at a uniform address: what differs from lane to lane is an offset, what is not
@@ -264,6 +263,8 @@ __device__ inline void invert(const float* at, const float* beta, float* T, int 
 #pragma unroll
     for (int i = l + 1; i < 16; ++i)
       t[i] = fmaf(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, a[i]), 0x150 + l, 0xF, 0xF, true)), t[l], t[i]);
+#pragma unroll
+    for (int i = l + 1; i < 16; ++i) asm volatile("" : "+v"(a[i]), "+v"(t[i]));  // (else the broadcasts of all steps come first, in 120 registers)
   };
 #define SF_STEP(l) step(std::integral_constant<int, l>())
   SF_STEP(0); SF_STEP(1); SF_STEP(2); SF_STEP(3); SF_STEP(4); SF_STEP(5); SF_STEP(6); SF_STEP(7);
