@@ -87,7 +87,8 @@ int sf_linattn_step(const sf_linattn_config* cfg, const void* q, const void* k, 
  * The passes over trajectories compute this in chunks of 32 steps, whose corrections are solved for by substitution.
  *
  * Arrays are time-major: q, k [T][N][Hk][dk], v [T][N][H][dv] and do, io, with strides as in sf_linattn_config, of any
- * alignment of the elements; a call is fast if rows are of a multiple of eight elements and 16-byte aligned.  o, dq, dk, dv are dense.
+ * alignment of the elements; a call is fast if rows are of a multiple of eight elements, 16-byte aligned,
+ * and a step's rows begin at least a row and at most 2^23 elements behind those of the step before.  o, dq, dk, dv are dense.
  *   log_decay, beta  dev [T][N][H] fp32 dense, their gradients alike.  log_decay is meant to be <= 0.  The gradient of a log_decay that no
  *                    decay was made with (done, or below 2^-126) is 0.
  *   done             dev [T][N] bytes or NULL
@@ -96,7 +97,7 @@ int sf_linattn_step(const sf_linattn_config* cfg, const void* q, const void* k, 
  * rounded from such, with 2^-16 of what enters the last products left out.  Of numbers whose products leave the range of fp32
  * nothing is promised, but that they stay in their row, head and chunk of 32 steps or go on by the state.
  * Results must not overlap inputs, nor one another, but for state as said below.
- * Errors: SF_ERR_ARG, SF_ERR_SHAPE (as sf_linattn; N * H * T / 32 beyond 2^31 - 1), SF_ERR_ALIAS, SF_ERR_DEVICE. */
+ * Errors: SF_ERR_ARG, SF_ERR_SHAPE (as sf_linattn; N * H times chunks of 32 steps beyond 2^26 - 128, for gradients 2^23 - 128), SF_ERR_ALIAS, SF_ERR_DEVICE. */
 typedef struct {
   uint32_t struct_size; /* sizeof(sf_deltarule_config) */
   int32_t dtype;        /* SF_DTYPE_* of q, k, v, o and their gradients */

@@ -22,7 +22,7 @@
 // and kept as two fp32 numbers, so that differences of steps close to each other do not lose to what came before.
 //
 // Zeros of masks are selected, but a product still multiplies them with the other operand's rows, and 0 x NaN is NaN.  So what enters
-// a chunk is tested: one with a NaN or an infinity is taken again as chunks of one step (the gradients': number by number).
+// a chunk is tested: one with a NaN or an infinity is taken step by step, by each wave for its own columns (the gradients': number by number).
 #include <math.h>
 
 #include <algorithm>
@@ -83,7 +83,7 @@ enum Sweep { kResults = 0, kStates = 1, kBack = 2 };
 // product without a shuffle: a 16x16 accumulator holds rows 4 lg .. 4 lg + 3 of one column per lane (lg = lane / 16), two of them are
 // the eight K-slots of an operand of 16x16x32, and the other operand follows the same numbering of the K axis.
 //   kResults: o and the last state;  kStates: the states that enter the chunks, or the last one of a piece;  kBack: R, from the last chunk to the first
-// ALONE: of one chunk, whose matrices the first wave makes (else they are read).
+// ALONE: of one chunk, whose products are made here, a tile by each wave, and T by the last one (else they are read).
 template <int DTYPE, int D, int NT, int SWEEP, bool ALONE, int KNOWN>
 __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : (D == 64 ? 4 : 3) - ALONE) void delta_sweep_kernel(DeltaArgs g) {
   typedef Num<DTYPE> M;
@@ -596,25 +596,26 @@ __global__ __launch_bounds__(kThreads) void delta_share_kernel(const float* in_q
   typedef Num<DTYPE> M;
   const float* const in = blockIdx.y ? in_k : in_q;
   unsigned char* const out = (unsigned char*)(blockIdx.y ? out_k : out_q);
-  const int64_t row = (int64_t)blockIdx.x * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2);
-  const int col = (threadIdx.x & ((1 << lanes_log2) - 1)) * PER;
-  if (row >= rows || col >= d) return;
-  const float* const x = in + row * share * d + col;
-  float sum[PER] = {};
-  for (int i = 0; i < share; ++i) {
-    float y[PER];
-    __builtin_memcpy(y, x + (int64_t)i * d, sizeof y);
+  const int col = (threadIdx.x & ((1 << lanes_log2) - 1)) * PER, in_block = kThreads >> lanes_log2;
+  if (col >= d) return;
+  for (int64_t row = (int64_t)blockIdx.x * in_block + (threadIdx.x >> lanes_log2); row < rows; row += (int64_t)gridDim.x * in_block) {
+    const float* const x = in + row * share * d + col;
+    float sum[PER] = {};
+    for (int i = 0; i < share; ++i) {
+      float y[PER];
+      __builtin_memcpy(y, x + (int64_t)i * d, sizeof y);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) sum[j] += y[j];
-  }
-  unsigned char* const to = out + (row * d + col) * M::kBytes;
-  if constexpr (DTYPE == SF_DTYPE_BF16 && PER == 4) {
-    const u32x2 two = {pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
-    __builtin_memcpy(to, &two, 8);
-  } else if constexpr (PER == 4) {
-    __builtin_memcpy(to, sum, 16);
-  } else {
-    M::store(to, sum[0]);
+      for (int j = 0; j < PER; ++j) sum[j] += y[j];
+    }
+    unsigned char* const to = out + (row * d + col) * M::kBytes;
+    if constexpr (DTYPE == SF_DTYPE_BF16 && PER == 4) {
+      const u32x2 two = {pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+      __builtin_memcpy(to, &two, 8);
+    } else if constexpr (PER == 4) {
+      __builtin_memcpy(to, sum, 16);
+    } else {
+      M::store(to, sum[0]);
+    }
   }
 }
 
@@ -710,7 +711,7 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaArgs g, float
 
 // ---- host side ---------------------------------------------------------------------------------
 
-int check(const sf_deltarule_config* c, const char* fn) {
+int check(const sf_deltarule_config* c, const char* fn, bool backward = false) {
   if (!c || c->struct_size != sizeof(sf_deltarule_config)) {
     set_error("%s: null configuration or struct_size mismatch", fn);
     return SF_ERR_ARG;
@@ -723,8 +724,10 @@ int check(const sf_deltarule_config* c, const char* fn) {
     set_error("%s: T = %d, N = %d, H = %d, Hk = %d, dk = %d, dv = %d out of range", fn, c->T, c->N, c->H, c->Hk, c->dk, c->dv);
     return SF_ERR_SHAPE;
   }
-  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > 1 << 21 || (int64_t)c->N * c->H * ((c->T + (int64_t)C - 1) / C) > INT32_MAX - 128) {
-    set_error("%s: T * N or N * H * T / 32 beyond 2^31 - 1, or N * H beyond 2^21", fn);
+  // (a launch's threads are counted in 32 bits: 64 a chunk forwards, up to 512 backwards, of 128 chunks at a time)
+  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > 1 << 21 ||
+      (int64_t)c->N * c->H * ((c->T + (int64_t)C - 1) / C) > (backward ? 1 << 23 : 1 << 26) - 128) {
+    set_error("%s: T * N beyond 2^31 - 1, N * H beyond 2^21, or N * H times chunks of 32 steps beyond %s - 128", fn, backward ? "2^23" : "2^26");
     return SF_ERR_SHAPE;
   }
   if (!isfinite(c->scale)) {
@@ -924,7 +927,7 @@ int launched(const char* fn, hipError_t e) {
 using namespace sf;
 
 extern "C" int64_t sf_deltarule_workspace_bytes(const sf_deltarule_config* cfg, int backward) {
-  if (check(cfg, "sf_deltarule_workspace_bytes") != SF_OK) return -1;
+  if (check(cfg, "sf_deltarule_workspace_bytes", backward != 0) != SF_OK) return -1;
   return (int64_t)workspace_of(cfg, backward).total;
 }
 
@@ -970,7 +973,7 @@ extern "C" int sf_deltarule_backward(const sf_deltarule_config* cfg, const void*
                                      void* dq, void* dk, void* dv, float* dlog_decay, float* dbeta, float* dstate0, void* workspace,
                                      void* hip_stream) {
   static const char* fn = "sf_deltarule_backward";
-  int rc = check(cfg, fn);
+  int rc = check(cfg, fn, true);
   if (rc != SF_OK) return rc;
   const size_t e = cfg->dtype == SF_DTYPE_BF16 ? 2 : 4;
   const bool none = (int64_t)cfg->T * cfg->N == 0;
@@ -1042,7 +1045,7 @@ extern "C" int sf_deltarule_backward(const sf_deltarule_config* cfg, const void*
     const int per = cfg->dk % 4 == 0 ? 4 : 1;
     int lanes_log2 = 0;
     while (per << lanes_log2 < cfg->dk) ++lanes_log2;
-    const int64_t in_block = kThreads >> lanes_log2, blocks = (rows + in_block - 1) / in_block;
+    const int64_t in_block = kThreads >> lanes_log2, blocks = std::min<int64_t>((rows + in_block - 1) / in_block, 1 << 14);
     const auto kern = cfg->dtype == SF_DTYPE_BF16 ? (per == 4 ? delta_share_kernel<SF_DTYPE_BF16, 4> : delta_share_kernel<SF_DTYPE_BF16, 1>)
                                                   : (per == 4 ? delta_share_kernel<SF_DTYPE_FP32, 4> : delta_share_kernel<SF_DTYPE_FP32, 1>);
     kern<<<dim3((unsigned)blocks, 2), kThreads, 0, st>>>(part_q, part_k, dq, dk, rows, cfg->dk, share, lanes_log2);

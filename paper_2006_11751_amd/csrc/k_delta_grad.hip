@@ -1,4 +1,11 @@
 // The gradients of the gated delta rule, chunk by chunk (k_delta.hip has the formulas and what goes before).
+//
+// A chunk's workgroup keeps everything it makes in LDS and registers: it reads q, k, v, do, both states and the chunk's matrices once and
+// writes its gradients once.  At 2048 rows of 32 steps, 8 heads of 64, that is 1.28 GB (240 us at a copy's rate), and it takes 445 us:
+// bound by the wait of each of its dozen dependent parts for the one before (42 thousand cycles a workgroup, 3 a CU: 18 products of a
+// wave each follow another's result through LDS), not by memory or by the matrix units, both of which are busy less than half the time.
+// What it measured otherwise: one workgroup a CU more or less (bf16, 64 columns) 480 us with 2, spills with 4; compile-time sizes 788
+// (the compiler then hoists all addresses and spills), so that sizes are always arguments here.
 #include "sf_delta.h"
 #include "sf_internal.h"
 
@@ -24,12 +31,12 @@ struct GradLds {
 
 // All gradients of one chunk, given the states S that enters it and R behind it: one workgroup for each (row, head, chunk), a wave for 16
 // columns of v and then for 16 of k.
-// ALONE: the only chunk, whose matrices the first wave makes (else they are read).
-template <int DTYPE, int D, bool ALONE, int KNOWN>
+// ALONE: the only chunk, whose products are made here by the first eight waves (of four: each) and T by the last one (else they are
+// read).  VEC: all arrays are read in 16-byte pieces.
+template <int DTYPE, int D, bool ALONE, bool VEC>
 __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4) void delta_grad_kernel(DeltaArgs g) {
   typedef Num<DTYPE> M;
   typedef GradLds<DTYPE, D> L;
-  constexpr bool VEC = KNOWN != kAny, WHOLE = KNOWN == kWhole;
   constexpr int W = M::kPieceWords, ND = D / 16, kRow8 = D / 8, kT = L::kThreads;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   // (workgroups go round the XCDs: 16 neighbours, whose rows of a step are neighbours too, for each)
@@ -39,7 +46,7 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
   const int n = (int)g.heads.of(bh), h = bh - n * g.H, hk = (int)g.share.of(h);
-  const int dk = WHOLE ? D : g.k.d, dv = WHOLE ? D : g.v.d, t0 = chunk * C, valid = min(C, g.T - t0);
+  const int dk = g.k.d, dv = g.v.d, t0 = chunk * C, valid = min(C, g.T - t0);
   auto base = [&](const Strided& a) { return (const unsigned char*)a.p + (n * a.sn + (a.shared ? hk : h) * a.sh) * M::kBytes; };
   unsigned char *const tq = lds, *const tk = lds + L::kTile, *const to = lds + 2 * L::kTile, *const tv = lds + L::kV;
   float *const mU = (float*)(lds + L::kU), *const mZ = (float*)(lds + L::kZ), *const mA = (float*)(lds + L::kA), *const mP = (float*)(lds + L::kP),
@@ -90,10 +97,10 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const int row = 32 * s + (tid + p * kT) / kPer, c = (tid + p * kT) % kPer * 4;
-      const unsigned at = WHOLE || c < dv ? (unsigned)(row * dv + c) * 4 : kOutside;  // (rows past dk lie past the end)
+      const unsigned at = c < dv ? (unsigned)(row * dv + c) * 4 : kOutside;  // (rows past dk lie past the end)
       ns[p] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from_s, at, 0, 0));
       nr[p] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from_r, at, 0, 0));
-      if (!WHOLE && c + 4 > dv)  // (the next row's numbers)
+      if (c + 4 > dv)  // (the next row's numbers)
 #pragma unroll
         for (int i = 1; i < 4; ++i)
           if (c + i >= dv) ns[p][i] = nr[p][i] = 0.0f;
@@ -466,7 +473,7 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
         }
       const typename M::Sum zt = three_terms<DTYPE>(zs), dt = three_terms<DTYPE>(os);
       const auto to_state = buffer(g.dstate0 + (size_t)bh * state, (unsigned)state * 4);
-      const unsigned y_at = WHOLE || y < dv ? (unsigned)(8 * lg * dv + y) * 4 : kOutside;
+      const unsigned y_at = y < dv ? (unsigned)(8 * lg * dv + y) * 4 : kOutside;
 #pragma unroll
       for (int a = 0; a < ND; ++a) {
         if (32 * (a >> 1) >= dk) continue;
@@ -691,9 +698,9 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
   }
 }
 
-template <int DTYPE, int D, bool ALONE, int KNOWN>
+template <int DTYPE, int D, bool ALONE, bool VEC>
 hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
-  const auto kern = delta_grad_kernel<DTYPE, D, ALONE, KNOWN>;
+  const auto kern = delta_grad_kernel<DTYPE, D, ALONE, VEC>;
   constexpr int bytes = GradLds<DTYPE, D>::kBytes;
   static_assert(bytes <= 160 * 1024, "LDS");
   if (bytes > 64 * 1024) {
@@ -705,8 +712,7 @@ hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
 }
 template <int DTYPE, int D, bool ALONE>
 hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {
-  if (!(g.q.vec && g.k.vec && g.v.vec && g.d_o.vec)) return launch_grad<DTYPE, D, ALONE, kAny>(g, st);
-  return launch_grad<DTYPE, D, ALONE, kPieces>(g, st);
+  return g.q.vec && g.k.vec && g.v.vec && g.d_o.vec ? launch_grad<DTYPE, D, ALONE, true>(g, st) : launch_grad<DTYPE, D, ALONE, false>(g, st);
 }
 template <int DTYPE, int D>
 hipError_t launch_grad(const DeltaArgs& g, hipStream_t st) {

@@ -79,6 +79,20 @@ def test_bad_configurations(kw, code, text):
     assert lib.sf_deltarule(None, *[None] * 11) == -1
 
 
+def test_the_most_chunks_of_a_call():
+    """What a launch can count: 2^26 chunks of 32 steps forwards, 2^23 for gradients, less 128."""
+    memory = _memory()
+    lib = memory.load_library()
+    size = lambda backward, **kw: lib.sf_deltarule_workspace_bytes(_config(memory, Hk=1, dk=1, dv=1, **kw), backward)
+    for backward, T in ((0, 1 << 13), (1, 1 << 10)):
+        assert size(backward, T=32 * T - 32, N=1 << 11, H=4) > 0
+        assert size(backward, T=32 * T, N=1 << 11, H=4) == -1 and "2^2%d" % (3 if backward else 6) in lib.sf_last_error().decode()
+    kw = dict(T=1 << 15, N=1 << 11, H=4, Hk=1, dk=1, dv=1)
+    assert lib.sf_deltarule_backward(_config(memory, **kw), *[None] * 17) == -2 and "2^23" in lib.sf_last_error().decode()
+    assert lib.sf_deltarule(_config(memory, **kw), *[None] * 11) == -1 and "q is null" in lib.sf_last_error().decode()
+    assert lib.sf_deltarule(_config(memory, **dict(kw, T=1 << 18)), *[None] * 11) == -2 and "2^26" in lib.sf_last_error().decode()
+
+
 def test_bad_pointers_and_tables():
     """(Addresses that are never read: the calls come back before they launch anything.)"""
     memory = _memory()

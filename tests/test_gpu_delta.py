@@ -393,6 +393,16 @@ def test_tensors_may_be_dropped_right_after_a_call_on_another_stream(torch_cuda)
         del taken
 
 
+def test_many_rows_of_shared_heads(torch_cuda):
+    """Sums of shared heads' gradients over more rows than the workgroups of a launch have at a time: those of heads of their own, added."""
+    torch = torch_cuda
+    x, do, ds = ref.make(1100, 130, 2, 1, 128, 16, "fp32", seed=1)
+    own = dict(x, q=x["q"].expand(-1, -1, 2, -1).contiguous(), k=x["k"].expand(-1, -1, 2, -1).contiguous())
+    got, want = call(x, do, ds), call(own, do, ds)
+    assert all(torch.equal(got[n], want[n][:, :, :1] + want[n][:, :, 1:]) for n in ("dq", "dk"))
+    assert all(torch.equal(got[n], want[n]) for n in ("dv", "dlog_decay", "dbeta", "dstate0"))
+
+
 def test_a_call_runs_on_its_tensors_device(torch_cuda, monkeypatch):
     """With another device current (there is one here: that it is another is pretended until torch is told to change to it)."""
     torch = torch_cuda
