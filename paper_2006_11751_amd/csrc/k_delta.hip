@@ -41,7 +41,9 @@ struct SweepLds {
                        kFlag = kSteps + (int)sizeof(Steps), kA = kFlag + 16, kBytes = kA, kBytesAlone = kA + C * kMat * 4;
 };
 
-// The matrices of every chunk, for the sweeps and the gradients: a wave makes one chunk's.
+// The matrices of every chunk, for the sweeps and the gradients: a wave makes one chunk's.  They do not depend on a state, so that all
+// are made at once and the sweeps, whose chunks wait for one another, only read them: 9 KB a chunk (backwards 13) in fp32.  bf16, 128 columns of
+// k: 4096 chunks 22 us, 8192 35 us, of which the products are little and a wave's chain (read, decays, substitution, write) most.
 template <int DTYPE, int D, bool BACK, bool VEC>
 __global__ __launch_bounds__(kThreads) void delta_chunks_kernel(DeltaArgs g) {
   constexpr int kWave = 2 * C * kMat * 4 + (int)sizeof(Steps);  // (T takes the place of P when that has left)
@@ -82,6 +84,11 @@ enum Sweep { kResults = 0, kStates = 1, kBack = 2 };
 // part of the state stays in registers as the accumulator of the update.  The products are arranged so that accumulators feed the next
 // product without a shuffle: a 16x16 accumulator holds rows 4 lg .. 4 lg + 3 of one column per lane (lg = lane / 16), two of them are
 // the eight K-slots of an operand of 16x16x32, and the other operand follows the same numbering of the K axis.
+// Bound by the length of a chunk's chain, not by memory or the matrix units: k S (ks), T and its correction, o, the update of S, each of which
+// waits for the one before: 7.2 thousand cycles a chunk with 16 columns a wave, 9.7 with 32 (k S 2.5, o 2.2, S 1.8, the rest staging and
+// steps).  What fills the waits is other workgroups, 3 or 4 a CU, so registers count: 128 of them with 64 columns of k, 168 with 128.
+// 512 steps of 64 rows, 8 heads of 128, bf16: 120 us.  A single chunk is bound by memory instead where rows are many: 32 steps of 2048 rows,
+// 8 heads of 64, bf16 204 us (4.0 TB/s), of 128 569 (4.7); fp32 276 and 898.  With few rows it is the launch and one chain: 64 rows 10.1 us.
 //   kResults: o and the last state;  kStates: the states that enter the chunks, or the last one of a piece;  kBack: R, from the last chunk to the first
 // ALONE: of one chunk, whose products are made here, a tile by each wave, and T by the last one (else they are read).
 template <int DTYPE, int D, int NT, int SWEEP, bool ALONE, int KNOWN>
@@ -530,7 +537,8 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : (D == 64 ?
 
 // What enters each piece of T, from the pieces' own states and what they make of one that enters:  S <- M S + own, backwards R <- M^T R + own;
 // where an episode begins in the piece, own alone.  A workgroup has 16 columns of one (row, head), a wave 16 rows of the state; the state goes
-// round through LDS.
+// round through LDS.  Two pieces' matrices are on their way at a time; on the fp32 matrix instruction, as this is where a state's errors would
+// add up.  32 pieces of 8 heads of 128: 51 us, a piece's 1.6 is what a product of 128 x 128 with 16 columns takes after the one before.
 template <bool BACK>
 __global__ __launch_bounds__(512) void delta_join_kernel(DeltaArgs g) {
   constexpr int kPitch = 132;
@@ -589,7 +597,8 @@ __global__ __launch_bounds__(512) void delta_join_kernel(DeltaArgs g) {
 }
 
 // Sums of the gradients of shared heads, of dq and of dk: in [rows][H][d] fp32, out [rows][H / share][d], each in one order.  A thread has
-// PER neighbours of a row of d; 2^lanes_log2 threads have a row.
+// PER neighbours of a row of d; 2^lanes_log2 threads have a row.  (A gradients kernel that went over the heads of a group would need no sums,
+// but has a group's share fewer workgroups, where they are few already.)  Bound by memory: 1024 steps of 8 rows, 8 heads of 128, two on each key, 14 us.
 template <int DTYPE, int PER>
 __global__ __launch_bounds__(kThreads) void delta_share_kernel(const float* in_q, const float* in_k, void* out_q, void* out_k, int64_t rows, int d, int share,
                                                                int lanes_log2) {
@@ -621,7 +630,10 @@ __global__ __launch_bounds__(kThreads) void delta_share_kernel(const float* in_q
 
 // One step of one (row, head): the state is read and decayed, multiplied with k and q in one go, corrected and written:
 //   o = scale (S'^T q + (q . k) u).
-// A thread holds four neighbours of every (256 / lanes)-th row, MOST of them, so that all its loads are under way at once.
+// A thread holds four neighbours of every (256 / lanes)-th row, MOST of them, so that all its loads are under way at once and the state
+// passes through registers once.  Bound by memory: 2048 rows, 8 heads of 64, 113 us (4.85 TB/s of state read and written; a copy has
+// 5.3).  MOST is the smallest of 4, 8 and 16 that does: with 16 always the registers left half the workgroups a CU, 127 us.  16 rows: 6 us, of
+// which the launch is most.
 template <int DTYPE, bool VEC, int MOST>
 __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaArgs g, float* table, int n_env, const int32_t* ids, int share, int lanes_log2) {
   typedef Num<DTYPE> M;
@@ -884,8 +896,13 @@ void launch_sweep(DeltaArgs& g, hipStream_t st) {
 template <int DTYPE, int D, int SWEEP, bool ALONE>
 void launch_sweep(DeltaArgs& g, bool vec, hipStream_t st) {
   if (!vec) return launch_sweep<DTYPE, D, 1, SWEEP, ALONE, kAny>(g, st);
+  // Two tiles of 16 columns a wave read the chunk's rows and matrices half as often and have two chains of products to fill each other's
+  // waits, but half the workgroups; of w workgroups of 64 columns, us with one | two tiles, 512 steps, heads of 128, forwards:
+  //   bf16 w = 64 51 | 70, 256 59 | 77, 512 89 | 92, 1024 162 | 154, 4096 622 | 591;  fp32 512 229 | 193, 1024 442 | 340, 4096 1710 | 1321
+  // and forwards and gradients, bf16: 512 441 | 447, 1024 893 | 857.
+  // With whole tiles (KNOWN) the bounds of columns fold away: 64 rows, heads of 64 81 us, else 83, of 128 153 and 161.
   if constexpr (!ALONE)
-    if (g.v.d > DV && (int64_t)g.N * g.H * g.n_seg * (g.piece && SWEEP == kStates ? 4 : 2) >= 1024) {
+    if (g.v.d > DV && (int64_t)g.N * g.H * g.n_seg * (g.piece && SWEEP == kStates ? 4 : 2) >= (DTYPE == SF_DTYPE_FP32 ? 512 : 1024)) {
       const bool whole = g.k.d == D && g.v.d == 2 * DV && !(g.piece && SWEEP == kStates && D == 64);  // (the identity has D columns)
       return whole ? launch_sweep<DTYPE, D, 2, SWEEP, ALONE, kWhole>(g, st) : launch_sweep<DTYPE, D, 2, SWEEP, ALONE, kPieces>(g, st);
     }
