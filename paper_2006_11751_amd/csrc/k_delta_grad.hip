@@ -1,11 +1,12 @@
 // The gradients of the gated delta rule, chunk by chunk (k_delta.hip has the formulas and what goes before).
 //
 // A chunk's workgroup keeps all it makes in LDS and registers: q, k, v, do, both states and the chunk's matrices are read once, the
-// gradients written once.  At 2048 rows of 32 steps, 8 heads of 64, bf16, that is 1.28 GB, 240 us at a copy's rate; it takes 441 us (2.9 TB/s).
+// gradients written once.  At 2048 rows of 32 steps, 8 heads of 64, bf16, that is 1.28 GB, 240 us at a copy's rate; it takes 436 us (2.9 TB/s).
 // Bound by its chain: a dozen parts that each wait for the one before through LDS and a barrier, 42 thousand cycles, which only other workgroups
-// of the CU fill.  So LDS counts: 51 KB with 64 columns in bf16 are 3 workgroups a CU, with 2 it takes 536 us; and of 128 columns v
+// of the CU fill.  (The vector units have an instruction half of the time, a third of them splits into bf16 terms, the matrix units a
+// quarter.)  So LDS counts: 51 KB with 64 columns in bf16 are 3 workgroups a CU, with 2 it takes 536 us; and of 128 columns v
 // leaves LDS before z comes, for 2 a CU.  Sizes are arguments: as constants the compiler kept all their offsets at once and spilled, 788 us.
-// fp32, 64 rows: 28 us, 1024 steps of 8 rows, 8 heads of 128, bf16: 140 us of 335 (the others are the sweeps').
+// fp32, 64 rows: 28 us, 1024 steps of 8 rows, 8 heads of 128, bf16: 136 us of 332 (the others are the sweeps').
 #include "sf_delta.h"
 #include "sf_internal.h"
 
@@ -52,6 +53,7 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
   float *const mU = (float*)(lds + L::kU), *const mZ = (float*)(lds + L::kZ), *const mA = (float*)(lds + L::kA), *const mP = (float*)(lds + L::kP),
                *const mT = (float*)(lds + L::kT);
   constexpr int kF = D + 4;
+  constexpr bool kF32 = DTYPE == SF_DTYPE_FP32;
   int* const flag = (int*)(lds + L::kFlag);  // by waves
   Steps& steps = *(Steps*)(lds + L::kSteps);
   // by waves: sums over their columns for each step; by tiles: of dP P + dA A along its rows and columns; a number of each wave
@@ -563,6 +565,45 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
   col_sum += __shfl_xor(col_sum, 16);
   col_sum += __shfl_xor(col_sum, 32);
   __syncthreads();  // T has been read, and the sums of this part have a place of their own
+  auto store = [&](void* out, int64_t at, int d, const unsigned* piece) {
+    if (col8 + 8 <= d) {
+#pragma unroll
+      for (int i = 0; i < W; i += 4) __builtin_memcpy((unsigned char*)out + at * M::kBytes + 4 * i, piece + i, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (col8 + i >= d) continue;
+        if constexpr (kF32) ((unsigned*)out)[at + i] = piece[i];
+        else ((uint16_t*)out)[at + i] = (uint16_t)(piece[i / 2] >> (16 * (i & 1)));
+      }
+    }
+  };
+  auto store_dv = [&](const float* x) {
+    if (row8 >= valid) return;
+    unsigned piece[W];
+    if constexpr (kF32) {
+      __builtin_memcpy(piece, x, 32);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) piece[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+    }
+    store(g.dv, (t0 + row8) * step_v + head_v + col8, dv, piece);
+  };
+  // In bf16 u and z are kept from here as the two terms that they enter the products of dk with, else each wave would split all of them
+  // (32 steps of 2048 rows, 8 heads of 64: 441 us, so 436; 1024 steps of 8 rows, 8 heads of 128, with the sweeps 337 and 332).
+  float* const at_z = mZ + row8 * kF + col8;
+  if constexpr (!kF32) {
+    float* const at_u = mU + row8 * kF + col8;
+    float z8[8], u8[8];
+    __builtin_memcpy(z8, at_z, 32);
+    __builtin_memcpy(u8, at_u, 32);
+    store_dv(z8);
+    const typename M::Out zt = two_terms<DTYPE>(z8), ut = two_terms<DTYPE>(u8);
+    *(u32x4*)at_z = zt.t[0];
+    *(u32x4*)(at_z + 4) = zt.t[1];
+    *(u32x4*)at_u = ut.t[0];
+    *(u32x4*)(at_u + 4) = ut.t[1];
+  }
   // (rows of tile I from tile J, less columns of tile J from tile I: both halves of the waves add up behind the barrier)
   float* const tile_sums = sum_m;
   if (L::kWaves == 4) {
@@ -603,6 +644,14 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
     }
   }
 
+  auto terms8 = [&](const float* tile, int row, int s) {  // of rows8
+    if constexpr (kF32) {
+      return two_terms<DTYPE>(rows8(tile, row, s).x);
+    } else {
+      const u32x4* const at = (const u32x4*)(tile + row * kF + 32 * s + 8 * lg);
+      return typename M::Out{{at[0], at[1]}};
+    }
+  };
   // dq and dk, 16 columns a wave, [k][step]
   f32x4 dq[2] = {}, dkk[2] = {};
   if (y0 < dk) {
@@ -615,8 +664,8 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
       for (int t = 0; t < 2; ++t) {
         const int i = 16 * t + li;
         dq[t] = M::mma(st, M::row(to + i * L::kPitch + (32 * s + 8 * lg) * M::kBytes), dq[t]);
-        zs[t] = mma_oo<DTYPE>(st, two_terms<DTYPE>(rows8(mZ, i, s).x), zs[t]);
-        us[t] = mma_oo<DTYPE>(rt, two_terms<DTYPE>(rows8(mU, i, s).x), us[t]);
+        zs[t] = mma_oo<DTYPE>(st, terms8(mZ, i, s), zs[t]);
+        us[t] = mma_oo<DTYPE>(rt, terms8(mU, i, s), us[t]);
       }
     }
     const typename M::Raw kt = columns<DTYPE>(tk, L::kPitch, y0, 4, li, lg), qt = columns<DTYPE>(tq, L::kPitch, y0, 4, li, lg);
@@ -631,8 +680,7 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
     }
   }
   __syncthreads();
-  // out by whole rows, through the places of q and k; dv from z
-  constexpr bool kF32 = DTYPE == SF_DTYPE_FP32;
+  // out by whole rows, through the places of q and k
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int i = 16 * t + li, c = y0 + 4 * lg;
@@ -663,39 +711,16 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
   }
   __syncthreads();
   if (row8 >= valid) return;
-  auto store = [&](void* out, int64_t at, int d, const unsigned* piece) {
-    if (col8 + 8 <= d) {
-#pragma unroll
-      for (int i = 0; i < W; i += 4) __builtin_memcpy((unsigned char*)out + at * M::kBytes + 4 * i, piece + i, 16);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (col8 + i >= d) continue;
-        if constexpr (kF32) ((unsigned*)out)[at + i] = piece[i];
-        else ((uint16_t*)out)[at + i] = (uint16_t)(piece[i / 2] >> (16 * (i & 1)));
-      }
-    }
-  };
-  unsigned piece[W];
   if (kF32 || !g.f32) {
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
+      unsigned piece[W];
 #pragma unroll
       for (int i = 0; i < W; i += 4) *(u32x4*)(piece + i) = *(const u32x4*)(lds + a * L::kTile + row8 * L::kPitch + col8 * M::kBytes + 4 * i);
       store(a == 0 ? g.dq : g.dk, (t0 + row8) * step_k + head_k + col8, dk, piece);
     }
   }
-  {
-    const float* const x = mZ + row8 * kF + col8;
-    if constexpr (kF32) {
-      *(u32x4*)piece = *(const u32x4*)x;
-      *(u32x4*)(piece + 4) = *(const u32x4*)(x + 4);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) piece[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-    }
-    store(g.dv, (t0 + row8) * step_v + head_v + col8, dv, piece);
-  }
+  if constexpr (kF32) store_dv(at_z);
 }
 
 template <int DTYPE, int D, bool ALONE, bool VEC>
