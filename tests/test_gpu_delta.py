@@ -192,7 +192,7 @@ def test_results_at_odd_addresses_and_nothing_behind_them(torch_cuda):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("T,dk,dv", [(32, 64, 64), (100, 64, 64), (100, 40, 128), (700, 64, 64), (700, 128, 72)])
+@pytest.mark.parametrize("T,dk,dv", [(32, 64, 64), (32, 128, 128), (32, 40, 72), (100, 64, 64), (100, 40, 128), (700, 64, 64), (700, 128, 72)])
 def test_not_finite_values_stay_where_they_are(torch_cuda, T, dk, dv, dtype):
     """An episode with NaN and infinities in it: the ones before and behind it are as if it were not there, and so are the
     results and query gradients of its own steps before the first of them."""
@@ -401,6 +401,23 @@ def test_many_rows_of_shared_heads(torch_cuda):
     got, want = call(x, do, ds), call(own, do, ds)
     assert all(torch.equal(got[n], want[n][:, :, :1] + want[n][:, :, 1:]) for n in ("dq", "dk"))
     assert all(torch.equal(got[n], want[n]) for n in ("dv", "dlog_decay", "dbeta", "dstate0"))
+
+
+def test_calls_at_the_same_time_on_two_streams(torch_cuda):
+    """Each with results and a workspace of its own."""
+    torch = torch_cuda
+    made = [ref.make(700, 2, 4, 2, 64, 128, "bf16", seed=s) for s in (1, 2)]
+    want = [(call(*m), call(m[0])) for m in made]
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in made], [({}, {}) for _ in made]
+    for _ in range(3):
+        for m, st, (back, forth) in zip(made, streams, outs):
+            call(*m, out=back, stream=st)
+            call(m[0], out=forth, stream=st)
+    torch.cuda.synchronize()
+    for pair, got in zip(want, outs):
+        for w, g in zip(pair, got):
+            assert all(torch.equal(w[n], g[n]) for n in w if n != "workspace")
 
 
 def test_a_call_runs_on_its_tensors_device(torch_cuda, monkeypatch):
