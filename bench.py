@@ -16,6 +16,7 @@ import argparse
 import hashlib
 import json
 import os
+import re
 import sys
 import time
 
@@ -72,18 +73,28 @@ PREWARM_SECONDS = 0.3
 TRAFFIC_TABLE = os.path.join(ROOT, "profiles", "hbm_traffic_table.txt")
 
 
+def operator_sources(csrc):
+    """The sources that include sf_memory.h, themselves or through a header that does: operators that no step launches."""
+    text = {name: open(os.path.join(csrc, name), "rb").read() for name in os.listdir(csrc) if name.endswith((".hip", ".h"))}
+    includes = {name: {n.decode() for n in re.findall(rb'^[ \t]*#[ \t]*include[ \t]*"([^"]+)"', t, re.M)} for name, t in text.items()}
+    found = {"sf_memory.h"}
+    while True:
+        more = {name for name, of in includes.items() if of & found} - found
+        if not more:
+            return found
+        found |= more
+
+
 def source_hash():
     """Identifies the kernels that run: sha256 over the library's sources (without the operators of sf_memory.h, which no
     step launches)."""
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2006_11751_amd", "csrc")
+    left_out = operator_sources(csrc)
     for name in sorted(os.listdir(csrc)):
-        if name.endswith((".hip", ".h")):
-            text = open(os.path.join(csrc, name), "rb").read()
-            if b'#include "sf_memory.h"' in text:
-                continue
+        if name.endswith((".hip", ".h")) and name not in left_out:
             h.update(name.encode())
-            h.update(text)
+            h.update(open(os.path.join(csrc, name), "rb").read())
     h.update(open(os.path.join(ROOT, "include", "sf_policy.h"), "rb").read())
     return h.hexdigest()[:16]
 
