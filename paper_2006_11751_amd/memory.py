@@ -601,7 +601,9 @@ def _ffn_back_plan(x, w_gate, w_up, w_down, dy, act):
 
 
 def _dense(t):
-    """Whether a tensor's elements fill its memory, in whatever order of its axes."""
+    """Whether a tensor's elements fill its memory, in whatever order of its axes (those of one without elements do)."""
+    if t.numel() == 0:
+        return True
     size = 1
     for stride, n in sorted((stride, n) for stride, n in zip(t.stride(), t.shape) if n != 1):
         if stride != size:

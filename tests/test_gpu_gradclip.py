@@ -195,3 +195,17 @@ def test_it_runs_on_its_tensors_device(torch_cuda, monkeypatch):
     got = memory.clip_gradients(grads, 1.0, in_place=False)
     monkeypatch.undo()
     assert told == [grads[0].device] and torch.equal(got["norm"], want["norm"])
+
+
+def test_tensors_of_no_numbers_beside_other_orders_of_axes(torch_cuda):
+    torch = torch_cuda
+    from paper_2006_11751_amd import memory
+    a, b = make(torch, [(40, 70), 31], "f")
+    grads = [a.T, torch.zeros(2, 0, device="cuda"), b, torch.zeros(4, 6, device="cuda")[:, 3:3]]
+    out = {}
+    for _ in range(2):
+        memory.clip_gradients(grads, 1.0, in_place=False, out=out)
+        check(torch, grads, out["grads"], 1.0, out["norm"])
+    kept = [g.clone() for g in grads]
+    norm = memory.clip_gradients(grads, 1.0)["norm"]
+    check(torch, kept, grads, 1.0, norm)
