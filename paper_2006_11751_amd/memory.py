@@ -616,22 +616,22 @@ _tensor_facts = None  # of a list's tensors, by functions that map() calls (a li
 
 
 def _list_key(name, tensors):
-    """What a list of gradients is: the device's index, sizes and types; their strides where a tensor is not contiguous."""
+    """What a list of gradients is: the device's index, shapes and types; their strides where tensors are not contiguous."""
     global _tensor_facts
     if _tensor_facts is None:
         T = binding._torch().Tensor
-        _tensor_facts = T.get_device, T.numel, operator.attrgetter("dtype"), T.is_contiguous
-    device, numel, dtype, contiguous = _tensor_facts
+        _tensor_facts = T.get_device, operator.attrgetter("shape"), operator.attrgetter("dtype"), T.is_contiguous
+    device, shape, dtype, contiguous = _tensor_facts
     try:
         where = set(map(device, tensors))
-        sizes, types = list(map(numel, tensors)), list(map(dtype, tensors))
-        strides = None if all(map(contiguous, tensors)) else [(t.shape, t.stride()) for t in tensors]
+        shapes, types = list(map(shape, tensors)), list(map(dtype, tensors))
+        strides = None if all(map(contiguous, tensors)) else [None if contiguous(t) else t.stride() for t in tensors]
     except TypeError:
         _refuse("%s: a list of tensors is wanted" % name)
     if len(where) != 1 or min(where) < 0:
         _refuse("%s: %s, tensors on one GPU are wanted" % (name, "an empty list" if not where else "on %s" % ", ".join(
             "the CPU" if i < 0 else "cuda:%d" % i for i in sorted(where))))
-    return [where, sizes, types, strides]
+    return [where, shapes, types, strides]
 
 
 class _ListPlan(_Plan):
@@ -660,7 +660,7 @@ def clip_gradients(grads, max_norm, eps=1e-6, in_place=True, out=None, stream=No
         if to is None:
             to = out["grads"] = [torch.empty_like(g) for g in grads]
         elif len(to) != len(grads) or _list_key("out['grads']", to) != key:
-            _refuse("out['grads'] does not fit: %d tensors of the same sizes, types and strides as the gradients are wanted" % len(grads))
+            _refuse("out['grads'] does not fit: %d tensors of the same shapes, types and strides as the gradients are wanted" % len(grads))
         results = array.array("Q", map(data_ptr, to))
     config = SfGradclipConfig(C.sizeof(SfGradclipConfig), len(grads), max_norm, eps)
     _check(_lib.sf_gradclip(C.addressof(config), pointers.buffer_info()[0], plan.sizes, plan.types, results.buffer_info()[0], norm,
@@ -676,7 +676,7 @@ def _clip_plan(grads, key):
             if not _dense(g):
                 _refuse("grads[%d] is not dense: %s, strides %s" % (i, tuple(g.shape), g.stride()))
     n = len(grads)
-    sizes = (C.c_int64 * n)(*key[1])
+    sizes = (C.c_int64 * n)(*(shape.numel() for shape in key[1]))
     plan = _ListPlan(SfGradclipConfig(), (("norm", (1,), binding._torch().float32),), _lib.sf_gradclip_workspace_bytes(n, sizes), grads[0].device)
     plan.key, plan.sizes, plan.types = key, sizes, (C.c_int32 * n)(*types)
     return plan

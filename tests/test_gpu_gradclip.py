@@ -209,3 +209,16 @@ def test_tensors_of_no_numbers_beside_other_orders_of_axes(torch_cuda):
     kept = [g.clone() for g in grads]
     norm = memory.clip_gradients(grads, 1.0)["norm"]
     check(torch, kept, grads, 1.0, norm)
+
+
+def test_results_of_another_shape_are_refused(torch_cuda):
+    """Also where they have as many numbers, and are contiguous like the gradients."""
+    torch = torch_cuda
+    from paper_2006_11751_amd import memory
+    grads = make(torch, [(6, 4), 5], "f")
+    for shape in ((4, 6), (24,), (6, 4, 1), (6, 5)):
+        with pytest.raises(ValueError, match="does not fit"):
+            memory.clip_gradients(grads, 1.0, in_place=False, out=dict(grads=make(torch, [shape, 5], "f")))
+    out = dict(grads=make(torch, [(6, 4), 5], "f", seed=1))
+    memory.clip_gradients(grads, 1.0, in_place=False, out=out)
+    check(torch, grads, out["grads"], 1.0, out["norm"])

@@ -11,3 +11,23 @@ def test_a_tensor_of_no_numbers_is_dense():
         assert memory._dense(t), shape
         assert memory._dense(t.T if t.dim() == 2 else t), shape
     assert memory._dense(torch.zeros(4, 6)[:, :0]) and memory._dense(torch.zeros(4, 6)[:, 3:3].T)
+
+
+def key(monkeypatch, *tensors):
+    monkeypatch.setattr(memory, "_tensor_facts", None)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    return memory._list_key("grads", list(tensors))
+
+
+def test_lists_that_are_the_same_and_that_are_not(monkeypatch):
+    """By shapes, types and, of tensors that are not contiguous, strides."""
+    z = torch.zeros
+    base = key(monkeypatch, z(6, 4), z(5))
+    assert base == key(monkeypatch, z(6, 4), z(5))
+    for other in ((z(4, 6), z(5)), (z(24), z(5)), (z(6, 4), z(5, 1)), (z(6, 4), z(6)), (z(6, 4, dtype=torch.bfloat16), z(5)), (z(4, 6).T, z(5)), (z(6, 4),),
+                  (z(6, 4), z(5), z(0))):
+        assert base != key(monkeypatch, *other), [t.shape for t in other]
+    assert key(monkeypatch, z(4, 6).T, z(5)) == key(monkeypatch, z(4, 6).T, z(5))
+    # strides of an axis of one element, in a tensor that is contiguous: any
+    one = z(7, 4)[::2][:1]
+    assert one.stride() == (8, 1) and key(monkeypatch, one, z(4, 6).T) == key(monkeypatch, z(1, 4), z(4, 6).T)
