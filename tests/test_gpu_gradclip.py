@@ -222,3 +222,30 @@ def test_results_of_another_shape_are_refused(torch_cuda):
     out = dict(grads=make(torch, [(6, 4), 5], "f", seed=1))
     memory.clip_gradients(grads, 1.0, in_place=False, out=out)
     check(torch, grads, out["grads"], 1.0, out["norm"])
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("n", [119, 120, 121, 4100, 20000])
+def test_thousands_of_tensors(torch_cuda, n, in_place):
+    """On both sides of what one launch takes, and so many that the chunks' sums are far more than a workgroup adds up in one round; the same bits
+    each time and in a graph."""
+    torch = torch_cuda
+    from paper_2006_11751_amd import memory
+    sizes = [1 + 37 * i % 53 for i in range(n)]
+    whole, = make(torch, [sum(sizes)], "f", seed=n)
+    grads = list(whole.split(sizes))
+    kept, out = whole.clone(), {}
+    memory.clip_gradients(grads, 1.0, in_place=in_place, out=out)
+    got = [whole if in_place else torch.cat(out["grads"])]
+    check(torch, [kept], got, 1.0, out["norm"])
+    first = out["norm"].clone(), got[0].clone()
+    whole.copy_(kept)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        memory.clip_gradients(grads, 1.0, in_place=in_place, out=out)
+    for _ in range(3):
+        whole.copy_(kept)
+        out["norm"].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out["norm"], first[0]) and torch.equal(whole if in_place else torch.cat(out["grads"]), first[1])

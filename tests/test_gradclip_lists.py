@@ -31,3 +31,15 @@ def test_lists_that_are_the_same_and_that_are_not(monkeypatch):
     # strides of an axis of one element, in a tensor that is contiguous: any
     one = z(7, 4)[::2][:1]
     assert one.stride() == (8, 1) and key(monkeypatch, one, z(4, 6).T) == key(monkeypatch, z(1, 4), z(4, 6).T)
+
+
+def test_the_workspace_of_lists_that_take_several_launches():
+    """A number for each chunk, and from 121 tensors that have numbers on one more for their sum."""
+    import ctypes as C
+    lib = memory.load_library()
+    size = lambda *s: lib.sf_gradclip_workspace_bytes(len(s), (C.c_int64 * len(s))(*s))
+    up = lambda n: (8 * n + 255) // 256 * 256
+    for n in (1, 32, 33, 96, 120):
+        assert size(*[5] * n) == up(n) and size(*[5] * n, *[0] * 200) == up(n)
+    for n in (127, 128, 4095, 4096, 100000):
+        assert size(*[5] * n) == up(n + 1)
