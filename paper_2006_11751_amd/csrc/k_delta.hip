@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : (D == 64 ?
           x[r] = S[c][2 * s][r];
           x[4 + r] = S[c][2 * s + 1][r];
         }
-        st[c] = three_terms<DTYPE>(x);
+        st[c] = three_terms<DTYPE, SWEEP == kResults>(x);
       }
 #pragma unroll
       for (int J = 0; J < 2; ++J) {
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : (D == 64 ?
       if constexpr (SWEEP == kResults) {
         typename M::Out uo[NT];
 #pragma unroll
-        for (int c = 0; c < NT; ++c) uo[c] = two_terms<DTYPE>(us[c]);
+        for (int c = 0; c < NT; ++c) uo[c] = M::out_terms(us[c]);
         const auto to = buffer((unsigned char*)g.o + (((int64_t)t0 * g.N + n) * g.H + h) * dv * M::kBytes, kWholeBuffer);
 #pragma unroll
         for (int I = 0; I < 2; ++I) {
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : (D == 64 ?
             ps[r] = p.a[r];
             ps[4 + r] = p.b[r];
           }
-          const typename M::Out pt = two_terms<DTYPE>(ps);
+          const typename M::Out pt = M::out_terms(ps);
 #pragma unroll
           for (int c = 0; c < NT; ++c) {
             const f32x4 own = mma_oo<DTYPE>(uo[c], pt, from_state * qs[c][I]);  // [y][i]

@@ -598,7 +598,7 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
     __builtin_memcpy(z8, at_z, 32);
     __builtin_memcpy(u8, at_u, 32);
     store_dv(z8);
-    const typename M::Out zt = two_terms<DTYPE>(z8), ut = two_terms<DTYPE>(u8);
+    const typename M::Out zt = M::out_terms(z8), ut = M::out_terms(u8);
     *(u32x4*)at_z = zt.t[0];
     *(u32x4*)(at_z + 4) = zt.t[1];
     *(u32x4*)at_u = ut.t[0];
@@ -646,7 +646,7 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
 
   auto terms8 = [&](const float* tile, int row, int s) {  // of rows8
     if constexpr (kF32) {
-      return two_terms<DTYPE>(rows8(tile, row, s).x);
+      return M::out_terms(rows8(tile, row, s).x);
     } else {
       const u32x4* const at = (const u32x4*)(tile + row * kF + 32 * s + 8 * lg);
       return typename M::Out{{at[0], at[1]}};
@@ -659,7 +659,7 @@ __global__ __launch_bounds__(4 * D, DTYPE == SF_DTYPE_FP32 ? 2 : D == 64 ? 3 : 4
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
       if (32 * s >= dv) continue;
-      const typename M::Out st = two_terms<DTYPE>(row_s[s]), rt = two_terms<DTYPE>(row_r[s]);
+      const typename M::Out st = M::out_terms(row_s[s]), rt = M::out_terms(row_r[s]);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int i = 16 * t + li;
