@@ -737,7 +737,7 @@ int check(const sf_deltarule_config* c, const char* fn, bool backward = false) {
     return SF_ERR_SHAPE;
   }
   // (a launch's threads are counted in 32 bits: 64 a chunk forwards, up to 512 backwards, of 128 chunks at a time)
-  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > 1 << 21 ||
+  if ((int64_t)c->T * c->N > INT32_MAX || (int64_t)c->N * c->H > kMostHeads ||
       (int64_t)c->N * c->H * ((c->T + (int64_t)C - 1) / C) > (backward ? 1 << 23 : 1 << 26) - 128) {
     set_error("%s: T * N beyond 2^31 - 1, N * H beyond 2^21, or N * H times chunks of 32 steps beyond %s - 128", fn, backward ? "2^23" : "2^26");
     return SF_ERR_SHAPE;

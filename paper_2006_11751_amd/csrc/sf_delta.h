@@ -42,6 +42,7 @@ hipError_t delta_gradients(const sf_deltarule_config* c, const DeltaArgs& g, hip
 namespace {
 
 constexpr int C = 32;    // steps of a chunk
+constexpr int kMostHeads = 1 << 21;  // (row, head)s of a call
 constexpr int DV = 64;   // columns of v of a workgroup that goes over the chunks: 16 a wave
 constexpr int kMat = 36; // a row of a matrix of the chunk's steps, in fp32: 32 and 4, so that 16 rows' pieces lie in different banks
 // A decay that is zero in 32 bits begins the memory anew, as done does.
@@ -161,22 +162,15 @@ struct StepIn {
 };
 // Lane i < 32 reads step t0 + i.
 __device__ inline StepIn read_step(const DeltaArgs& g, int n, int h, int t0, int valid, int lane) {
+  static_assert((int64_t)(C - 1) * kMostHeads * 4 < kWholeBuffer, "a chunk's steps are in reach of one buffer");
   const int64_t row = (int64_t)t0 * g.N + n;
-  const int64_t last = (int64_t)(valid - 1) * g.N;  // (rows may lie far apart)
+  const unsigned at = (unsigned)(lane * g.N);
+  const auto ld = buffer(g.log_decay + row * g.H + h, kWholeBuffer), be = buffer(g.beta + row * g.H + h, kWholeBuffer);
+  const auto dn = buffer(g.done + (g.done ? row : 0), g.done ? kWholeBuffer : 0);
   StepIn s;
-  if (last * g.H < (int64_t)1 << 28) {
-    const unsigned at = (unsigned)(lane * g.N);
-    const auto ld = buffer(g.log_decay + row * g.H + h, kWholeBuffer), be = buffer(g.beta + row * g.H + h, kWholeBuffer);
-    const auto dn = buffer(g.done + (g.done ? row : 0), g.done ? kWholeBuffer : 0);
-    s.ld = load_float(ld, lane < valid ? at * g.H * 4 : kOutside, 0);
-    s.beta = load_float(be, lane < valid ? at * g.H * 4 : kOutside, 0);
-    s.done = __builtin_amdgcn_raw_buffer_load_b8(dn, lane < valid ? at : kOutside, 0, 0) != 0;
-  } else {
-    const int64_t r = row + (int64_t)(lane < valid ? lane : 0) * g.N, at = r * g.H + h;
-    s.ld = lane < valid ? g.log_decay[at] : 0.0f;
-    s.beta = lane < valid ? g.beta[at] : 0.0f;
-    s.done = lane < valid && g.done && g.done[r] != 0;
-  }
+  s.ld = load_float(ld, lane < valid ? at * g.H * 4 : kOutside, 0);
+  s.beta = load_float(be, lane < valid ? at * g.H * 4 : kOutside, 0);
+  s.done = __builtin_amdgcn_raw_buffer_load_b8(dn, lane < valid ? at : kOutside, 0, 0) != 0;
   return s;
 }
 __device__ inline bool begins(const StepIn& s) { return s.done || s.ld * 1.44269504f < (float)kLeastLog2; }

@@ -481,3 +481,23 @@ def test_what_the_binding_refuses(torch_cuda):
         memory.delta_rule_step(*(a[0] for a in good), x["state0"], env_ids=torch.zeros(2, dtype=torch.int64, device="cuda"))
     with pytest.raises(memory.SfError, match="H = 4"):
         memory.delta_rule(*(torch.zeros(3, 2, 3, 8, device="cuda") for _ in range(2)), x["v"], x["log_decay"], x["beta"])
+
+
+@pytest.mark.parametrize("T", [2, 34])
+def test_many_rows_of_one_head(torch_cuda, T):
+    """Steps of the decays 8 MB apart, near the most rows of a call; the first and last rows."""
+    torch = torch_cuda
+    N, rows = (1 << 21) - 1, [0, 1, (1 << 20) + 3, (1 << 21) - 2]
+    x, do, ds = ref.make(T, len(rows), 1, 1, 1, 2, "bf16", seed=T)
+    y = {n: torch.zeros((a.shape[0], N) + a.shape[2:] if n != "state0" else (N,) + a.shape[1:], dtype=a.dtype, device="cuda") for n, a in x.items()}
+    ydo, yds = torch.zeros(T, N, 1, 2, dtype=do.dtype, device="cuda"), torch.zeros(N, 1, 1, 2, device="cuda")
+    for n, a in x.items():
+        if n == "state0":
+            y[n][rows] = a
+        else:
+            y[n][:, rows] = a
+    ydo[:, rows], yds[rows] = do, ds
+    pick = lambda r: {n: a[rows] if "state" in n else a[:, rows] for n, a in r.items() if n != "workspace"}
+    sizes = 1, 2, 17.0, True, T
+    ref.check(pick(call(y)), *ref.oracle(x), *sizes)
+    ref.check(pick(call(y, ydo, yds)), *ref.oracle(x, None, do, ds), *sizes)
