@@ -501,3 +501,41 @@ def test_many_rows_of_one_head(torch_cuda, T):
     sizes = 1, 2, 17.0, True, T
     ref.check(pick(call(y)), *ref.oracle(x), *sizes)
     ref.check(pick(call(y, ydo, yds)), *ref.oracle(x, None, do, ds), *sizes)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("which", ["q", "k", "v", "do", "all"])
+@pytest.mark.parametrize("T", [3, 35])
+def test_steps_far_apart(torch_cuda, T, which, dtype):
+    """More than 2^23 elements from step to step, as a packed projection of many rows has them: in 35 steps 640 MB (fp32 1.3 GB) and more."""
+    torch = torch_cuda
+    apart = (1 << 23) + (1 << 20) + 8
+    x, do, ds = ref.make(T, 3, 2, 2, 64, 72, dtype, seed=T)
+    want, back = call(x), call(x, do, ds)
+    arrays = dict(q=x["q"], k=x["k"], v=x["v"], do=do)
+    for n in arrays if which == "all" else (which,):
+        a = arrays[n]
+        whole = torch.full((T * apart,), float("nan"), dtype=a.dtype, device="cuda")
+        far = whole.as_strided(a.shape, (apart,) + a.stride()[1:])
+        far.copy_(a)
+        arrays[n] = far
+    y = dict(x, **{n: a for n, a in arrays.items() if n != "do"})
+    sizes = 64, 72, 17.0, dtype == "bf16", T
+    got, gback = call(y), call(y, arrays["do"], ds)
+    ref.check(got, *ref.oracle(x), *sizes)
+    ref.check(gback, *ref.oracle(x, None, do, ds), *sizes)
+    assert all(torch.equal(a, got[n]) for n, a in want.items() if n != "workspace")
+    assert all(torch.equal(a, gback[n]) for n, a in back.items() if n != "workspace")
+
+
+@pytest.mark.parametrize("dtype,N", [("bf16", 1 << 14), ("fp32", 1 << 14), ("bf16", 1 << 15)])
+@pytest.mark.parametrize("T", [2, 34])
+def test_results_whose_steps_are_far_apart(torch_cuda, T, N, dtype):
+    """2^24 numbers of o and more in a step: a chunk of results is beyond 2^31 bytes, counted in fp32; some rows, the first and last ones among them."""
+    torch = torch_cuda
+    rows = [0, 1, N // 2 + 5, N - 1]
+    x, do, ds = ref.make(T, N, 8, 8, 8, 128, dtype, seed=T)
+    pick = lambda r: {n: a[rows] if "state" in n else a[:, rows] for n, a in r.items() if n != "workspace"}
+    few, sizes = pick(x), (8, 128, 17.0, dtype == "bf16", T)
+    ref.check(pick(call(x)), *ref.oracle(few), *sizes)
+    ref.check(pick(call(x, do, ds)), *ref.oracle(few, None, do[:, rows], ds[rows]), *sizes)
