@@ -531,7 +531,7 @@ def test_steps_far_apart(torch_cuda, T, which, dtype):
 @pytest.mark.parametrize("dtype,N", [("bf16", 1 << 14), ("fp32", 1 << 14), ("bf16", 1 << 15)])
 @pytest.mark.parametrize("T", [2, 34])
 def test_results_whose_steps_are_far_apart(torch_cuda, T, N, dtype):
-    """2^24 numbers of o and more in a step: a chunk of results is beyond 2^31 bytes, counted in fp32; some rows, the first and last ones among them."""
+    """2^24 or 2^25 numbers of o in a step: a chunk of results is 2^31 bytes, or in bf16 half of that; some rows, the first and last ones among them."""
     torch = torch_cuda
     rows = [0, 1, N // 2 + 5, N - 1]
     x, do, ds = ref.make(T, N, 8, 8, 8, 128, dtype, seed=T)
