@@ -86,13 +86,17 @@ enum Sweep { kResults = 0, kStates = 1, kBack = 2 };
 // the eight K-slots of an operand of 16x16x32, and the other operand follows the same numbering of the K axis.
 // Bound by the length of a chunk's chain, not by memory or the matrix units: k S (ks), T and its correction, o, the update of S, each of which
 // waits for the one before: 7.2 thousand cycles a chunk with 16 columns a wave, 9.7 with 32 (k S 2.5, o 2.2, S 1.8, the rest staging and
-// steps).  What fills the waits is other workgroups, 3 or 4 a CU, so registers count: 128 of them with 64 columns of k, 168 with 128.
-// 512 steps of 64 rows, 8 heads of 128, bf16: 120 us, the vector units busy 0.46 of it, the matrix units 0.36.  A single chunk is bound by memory instead where rows are many: 32 steps of 2048 rows,
-// 8 heads of 64, bf16 204 us (4.0 TB/s), of 128 569 (4.7); fp32 276 and 898.  With few rows it is the launch and one chain: 64 rows 10.1 us.
+// steps).  What fills the waits is other workgroups, so registers count, but a spill lies in the chain: bounds of 3 workgroups a CU with 64 columns of k and
+// 2 with 128 spill nothing with one tile; of 4 and 3 they spilled up to 39 registers, forwards, gradients, us so | before: fp32, 512 steps of 8 heads, 16 rows
+// of 64 columns 67 | 77, 190 | 203, 8 rows of 128 95 | 117, 289 | 302; bf16 the same within 2 %.  With two tiles and 128 columns of k, at 256 registers, fp32 spills 8 to 38 of
+// them, bf16 with columns that are no whole tiles 15 to 28; a bound of one workgroup, which spills none, is slower (fp32, 64 rows 377 us, so 334).
+// 512 steps of 64 rows, 8 heads of 128, bf16: 120 us, the vector units busy 0.46 of it, the matrix units 0.36.  A single chunk is bound by memory instead
+// where rows are many: 32 steps of 2048 rows, 8 heads of 64, bf16 204 us (4.0 TB/s), of 128 569 (4.7); fp32 276 and 898.  With few rows it is the
+// launch and one chain: 64 rows 10.1 us.
 //   kResults: o and the last state;  kStates: the states that enter the chunks, or the last one of a piece;  kBack: R, from the last chunk to the first
 // ALONE: of one chunk, whose products are made here, a tile by each wave, and T by the last one (else they are read).
 template <int DTYPE, int D, int NT, int SWEEP, bool ALONE, int KNOWN>
-__global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 ? 2 : (D == 64 ? 4 : 3) - ALONE) void delta_sweep_kernel(DeltaArgs g) {
+__global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 || D == 128 ? 2 : 3) void delta_sweep_kernel(DeltaArgs g) {
   typedef Num<DTYPE> M;
   typedef SweepLds<DTYPE, D, NT> L;
   constexpr int W = M::kPieceWords, NP = C * D / 8 / kThreads, ND = D / 16, kRow = D / 8, kRowV = DV * NT / 8;
@@ -897,12 +901,14 @@ template <int DTYPE, int D, int SWEEP, bool ALONE>
 void launch_sweep(DeltaArgs& g, bool vec, hipStream_t st) {
   if (!vec) return launch_sweep<DTYPE, D, 1, SWEEP, ALONE, kAny>(g, st);
   // Two tiles of 16 columns a wave read the chunk's rows and matrices half as often and have two chains of products to fill each other's
-  // waits, but half the workgroups; of w workgroups of 64 columns, us with one | two tiles, 512 steps, heads of 128, forwards:
-  //   bf16 w = 64 51 | 70, 256 59 | 77, 512 89 | 92, 1024 162 | 154, 4096 622 | 591;  fp32 512 229 | 193, 1024 442 | 340, 4096 1710 | 1321
-  // and forwards and gradients, bf16: 512 441 | 447, 1024 893 | 857.
-  // With whole tiles (KNOWN) the bounds of columns fold away: 64 rows, heads of 64 81 us, else 83, of 128 153 and 161.
+  // waits, but half the workgroups; of w workgroups of 64 columns, us with one | two tiles, 512 steps, heads of 128, forwards, gradients:
+  //   bf16 w = 256 63 | 82, 262 | 303;  512 87 | 87, 444 | 453;  768 133 | 129, 650 | 657;  1024 165 | 147, 853 | 829;  4096 640 | 584, 3289 | 3262
+  //   fp32 w = 256 113 | 167, 436 | 538;  512 174 | 184, 768 | 814;  768 267 | 306, 1142 | 1238;  1024 344 | 334, 1478 | 1496;  4096 1324 | 1261, 5948 | 5892
+  // With whole tiles (KNOWN) the bounds of columns fold away.  512 steps of 8 heads, us with | without, forwards, gradients:
+  //   bf16 16 rows of 64 44 | 48, 127 | 136;  8 rows of 128 52 | 63, 166 | 185;  64 rows of 128 148 | 152, 833 | 865
+  //   fp32 16 rows of 64 67 | 75, 190 | 204;  8 rows of 128 95 | 110, 289 | 323;  64 rows of 128 332 | 354, 1484 | 1492
   if constexpr (!ALONE)
-    if (g.v.d > DV && (int64_t)g.N * g.H * g.n_seg * (g.piece && SWEEP == kStates ? 4 : 2) >= (DTYPE == SF_DTYPE_FP32 ? 512 : 1024)) {
+    if (g.v.d > DV && (int64_t)g.N * g.H * g.n_seg * (g.piece && SWEEP == kStates ? 4 : 2) >= 1024) {
       const bool whole = g.k.d == D && g.v.d == 2 * DV && !(g.piece && SWEEP == kStates && D == 64);  // (the identity has D columns)
       return whole ? launch_sweep<DTYPE, D, 2, SWEEP, ALONE, kWhole>(g, st) : launch_sweep<DTYPE, D, 2, SWEEP, ALONE, kPieces>(g, st);
     }
