@@ -43,7 +43,7 @@ struct SweepLds {
 
 // The matrices of every chunk, for the sweeps and the gradients: a wave makes one chunk's.  They do not depend on a state, so that all
 // are made at once and the sweeps, whose chunks wait for one another, only read them: 9 KB a chunk (backwards 13) in fp32.  bf16, 128 columns of
-// k: 4096 chunks 22 us, 8192 35 us, of which the products are little and a wave's chain (read, decays, substitution, write) most.
+// k: 4096 chunks 21 us, 8192 30 to 35 us, of which the products are little and a wave's chain (read, decays, substitution, write) most.
 template <int DTYPE, int D, bool BACK, bool VEC>
 __global__ __launch_bounds__(kThreads) void delta_chunks_kernel(DeltaArgs g) {
   constexpr int kWave = 2 * C * kMat * 4 + (int)sizeof(Steps);  // (T takes the place of P when that has left)
@@ -90,7 +90,7 @@ enum Sweep { kResults = 0, kStates = 1, kBack = 2 };
 // 2 with 128 spill nothing with one tile; of 4 and 3 they spilled up to 39 registers, forwards, gradients, us so | before: fp32, 512 steps of 8 heads, 16 rows
 // of 64 columns 67 | 77, 190 | 203, 8 rows of 128 95 | 117, 289 | 302; bf16 the same within 2 %.  With two tiles and 128 columns of k, at 256 registers, fp32 spills 8 to 38 of
 // them, bf16 with columns that are no whole tiles 15 to 28; a bound of one workgroup, which spills none, is slower (fp32, 64 rows 377 us, so 334).
-// 512 steps of 64 rows, 8 heads of 128, bf16: 120 us, the vector units busy 0.46 of it, the matrix units 0.36.  A single chunk is bound by memory instead
+// 512 steps of 64 rows, 8 heads of 128, bf16: 120 us, the vector units busy 0.51 of it, the matrix units 0.40.  A single chunk is bound by memory instead
 // where rows are many: 32 steps of 2048 rows, 8 heads of 64, bf16 204 us (4.0 TB/s), of 128 569 (4.7); fp32 276 and 898.  With few rows it is the
 // launch and one chain: 64 rows 10.1 us.
 //   kResults: o and the last state;  kStates: the states that enter the chunks, or the last one of a piece;  kBack: R, from the last chunk to the first
@@ -542,7 +542,7 @@ __global__ __launch_bounds__(kThreads, KNOWN == kAny || NT == 2 || D == 128 ? 2 
 // What enters each piece of T, from the pieces' own states and what they make of one that enters:  S <- M S + own, backwards R <- M^T R + own;
 // where an episode begins in the piece, own alone.  A workgroup has 16 columns of one (row, head), a wave 16 rows of the state; the state goes
 // round through LDS.  Two pieces' matrices are on their way at a time; on the fp32 matrix instruction, as this is where a state's errors would
-// add up.  32 pieces of 8 heads of 128: 51 us, a piece's 1.6 is what a product of 128 x 128 with 16 columns takes after the one before.
+// add up.  32 pieces of 8 heads of 128: 49 us, a piece's 1.5 is what a product of 128 x 128 with 16 columns takes after the one before.
 template <bool BACK>
 __global__ __launch_bounds__(512) void delta_join_kernel(DeltaArgs g) {
   constexpr int kPitch = 132;
@@ -636,8 +636,8 @@ __global__ __launch_bounds__(kThreads) void delta_share_kernel(const float* in_q
 //   o = scale (S'^T q + (q . k) u).
 // A thread holds four neighbours of every (256 / lanes)-th row, MOST of them, so that all its loads are under way at once and the state
 // passes through registers once.  Bound by memory: 2048 rows, 8 heads of 64, 113 us (4.85 TB/s of state read and written; a copy has
-// 5.3).  MOST is the smallest of 4, 8 and 16 that does: with 16 always the registers left half the workgroups a CU, 127 us.  16 rows: 6 us, of
-// which the launch is most.
+// 5.3; 90 us where the same rows come call after call and part of them is still in the last-level cache).  MOST is the smallest of 4, 8 and 16
+// that does: with 16 always the registers left half the workgroups a CU, 127 us.  16 rows: 6 us, of which the launch is most.
 template <int DTYPE, bool VEC, int MOST>
 __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaArgs g, float* table, int n_env, const int32_t* ids, int share, int lanes_log2) {
   typedef Num<DTYPE> M;
@@ -772,7 +772,8 @@ int chunks_of(const sf_deltarule_config* c) { return (c->T + C - 1) / C; }
 
 // Pieces of T where heads are few: a pass over the pieces with the identity's columns besides, and as many steps in a row to join them as there
 // are pieces, for chunks in a row that are fewer by that factor.  Both grow together least at a number of pieces near the root of
-// twice the chunks, while the workgroups (w, one for each 64 columns of a head) find CUs that are idle; from w = 128 on no number pays.
+// twice the chunks, while the workgroups (w, one for each 64 columns of a head) find CUs that are idle; at w = 128 no number pays for 1024 or 2048 steps (for
+// 4096, four pieces save 4 % in bf16, 9 % in fp32).
 // us with 1, 4, 8, 16, 32 pieces, bf16, forwards | backwards (H heads over all rows):
 //   H x columns, T      w
 //    8 x  64, 1024      8    67  45  36  39    -  | 146  103   83   87    -
@@ -786,6 +787,11 @@ int chunks_of(const sf_deltarule_config* c) { return (c->T + C - 1) / C; }
 //   32 x 128, 4096     64   336 206 182 190  230  | 1020 747  713  733  855
 //  128 x  64, 1024    128    76  82  90 117    -  | 237  246  267  315    -
 //   64 x 128, 2048    128   182 184 190 224  335  | 694  716  731  847 1059
+// fp32, with 1, 4, 8, 16:
+//    8 x  64, 1024      8   109  63  47  46 | 212  144  111  108
+//    8 x 128, 4096     16   643 293 173 142 | 1269 721  467  382
+//   64 x  64, 2048     64   223 143 133 143 | 542  411  392  419
+//   32 x 128, 1024     64   175 120 120 142 | 431  347  344  410
 struct Split {
   int n_seg, seg_len;
 };

@@ -6,7 +6,7 @@
 // of the CU fill.  (The vector units have an instruction half of the time, a third of them splits into bf16 terms, the matrix units a
 // quarter.)  So LDS counts: 51 KB with 64 columns in bf16 are 3 workgroups a CU, with 2 it takes 536 us; and of 128 columns v
 // leaves LDS before z comes, for 2 a CU.  Sizes are arguments: as constants the compiler kept all their offsets at once and spilled, 788 us.
-// fp32, 64 rows: 28 us, 1024 steps of 8 rows, 8 heads of 128, bf16: 136 us of 332 (the others are the sweeps').
+// fp32, 64 rows: 29 us, 1024 steps of 8 rows, 8 heads of 128, bf16: 129 us of 330 (the others are the sweeps').
 #include "sf_delta.h"
 #include "sf_internal.h"
 

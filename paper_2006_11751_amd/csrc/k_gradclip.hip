@@ -12,8 +12,8 @@
 // recorded graph holds its own.
 //
 // Bound by memory.  54 tensors, 856 MB: 184 us for the squares (4.7 TB/s), 319 to read again and write (5.4); half the chunks 203 and 339, four
-// pieces ahead in place of eight 187 and 318.  Few numbers: 16 tensors of 11.5 MB 4.6 and 6.0 us, 300 tensors of all sizes, 67 MB, in three
-// launches a pass 24 and 37 us.
+// pieces ahead in place of eight 187 and 318.  Few numbers: 16 tensors of 11.5 MB 4.2 and 6.1 us, 300 tensors of all sizes, 67 MB, in three
+// launches a pass 24 and 33 us, and 3 for the sums in between.
 #include <math.h>
 
 #include <algorithm>

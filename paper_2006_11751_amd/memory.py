@@ -639,7 +639,7 @@ class _ListPlan(_Plan):
 
 
 def clip_gradients(grads, max_norm, eps=1e-6, in_place=True, out=None, stream=None):
-    """The global norm of a list of gradients (bf16 or fp32 or both, dense in any order of their axes), and the gradients times
+    """The global norm of a list of gradients (at least one; bf16 or fp32 or both, dense in any order of their axes), and the gradients times
     min(1, max_norm / (norm + eps)): in place, or in_place=False as results.  Results: norm, fp32 [1], before clipping, and unless
     in place grads, a list of tensors like the ones given."""
     out, max_norm, eps = {} if out is None else out, _number(max_norm), _number(eps)
